@@ -2,7 +2,8 @@
  * libss - sequence-scheduled batched greedy decoding on one MI355X (gfx950).
  *
  * C ABI.  Every pointer argument says "host" or "device" below; nothing in a
- * signature is a framework type.  All functions are synchronous on return.
+ * signature is a framework type.  All functions are synchronous on return, except
+ * the operators on device tensors at the end, which only enqueue.
  * Every function that returns int returns SS_OK (0) or a negative ss_status;
  * ss_last_error() then gives a thread-local message.  No exception or abort
  * crosses this boundary; outputs are untouched when an error is returned
@@ -18,6 +19,7 @@
 #ifndef SS_H
 #define SS_H
 
+#include <stddef.h>
 #include <stdint.h>
 
 #ifdef __cplusplus
@@ -383,6 +385,102 @@ int ss_bench_weight_stream(ss_weights* w, int32_t B, int32_t iters, double* ms_o
  *   bytes_out  host, nullable: bytes read per iteration (each matrix rounded down to whole 64 KiB chunks)
  */
 int ss_bench_read_stream(ss_weights* w, int32_t iters, double* ms_out, int64_t* bytes_out, void* hip_stream);
+
+/* ------------------------------------------------------------------ operators on device tensors */
+
+/*
+ * The operators below work on tensors that the caller holds on the GPU.  They enqueue on `hip_stream` (NULL: the default
+ * stream) of the current device and return; they allocate nothing, keep nothing between calls and wait for nothing, so they may be
+ * captured into a graph.  Nothing in their results depends on what else runs or on the order of workgroups: the same call gives
+ * the same bits.  Calls on different streams are independent as long as their outputs, caches that are written, and workspaces
+ * are their own; graphs that may replay at the same time need workspaces of their own.  All pointers in the structures and all
+ * tables are device pointers of the current device; tables are read when the work runs, not when it is enqueued, and entries
+ * that lead outside the tensors are passed over, not followed.
+ * Errors: SS_EINVAL (NULL, bad counts, types, strides or alignment; nothing was enqueued), SS_EDEVICE (launch failed).
+ */
+#define SS_F16 2 /* IEEE half                                                        */
+#define SS_I8  3 /* caches only: 8-bit codes with one scale per vector (below)        */
+
+/* Rows of heads: element e of head h of row r at p + (r * row_stride + h * head_stride + e) elements.  p is 16-byte aligned, the
+ * strides are multiples of 8. */
+typedef struct {
+    void*   p;
+    int64_t row_stride, head_stride; /* in elements */
+    int64_t rows;
+    int32_t dtype;                   /* SS_F16 or SS_BF16 */
+} ss_rows;
+
+/*
+ * The key/value cache of one layer, in the layout that this library's own generation uses: every sequence owns a slab of slots, and
+ * element e of the vector of head h in slot s of sequence i is at (start[i] * n_kv_heads + h * slots[i] + s) * head_dim + e of k and v.
+ * Slabs must not overlap; start[i] + slots[i] <= total_slots.
+ * SS_I8: a vector x is held as codes round(x / scale) and scale = max|x| / 127 (float32, at start[i] * n_kv_heads + h * slots[i] + s of
+ * k_scale and v_scale); quotient and division rounded to nearest.  A vector with an infinity or NaN is read back as NaN.
+ */
+typedef struct {
+    void *k, *v;              /* device, 16-byte aligned, total_slots * n_kv_heads * head_dim elements */
+    float *k_scale, *v_scale; /* device, total_slots * n_kv_heads, SS_I8 only                          */
+    const int64_t* start;     /* device, int64[n_seq]                                                  */
+    const int32_t* slots;     /* device, int32[n_seq]                                                  */
+    int64_t total_slots;
+    int32_t n_seq, n_kv_heads, head_dim; /* head_dim 64 or 128     */
+    int32_t dtype;                       /* SS_F16, SS_BF16, SS_I8 */
+} ss_cache;
+
+/*
+ * Keys and values of n tokens into the cache: token t goes to slot[t] of sequence seq[t] (device, int32[n]); tokens whose
+ * sequence or slot does not exist (-1, say, for padding) are passed over.  A pair (seq, slot) may occur once per call.
+ *   k, v   [n][n_kv_heads][head_dim], both of one type.  A 16-bit cache of that type holds them as they are; half holds bf16 values
+ *          beyond its range as +-65504.
+ */
+int ss_cache_write(const ss_cache* cache, const ss_rows* k, const ss_rows* v, const int32_t* seq, const int32_t* slot, int32_t n,
+                   void* hip_stream);
+
+/* The way back: row t of k and v is what slot[t] of sequence seq[t] stands for, rounded to the rows' type.  Rows of tokens that
+ * do not exist stay as they are.  A slot may be read any number of times. */
+int ss_cache_read(const ss_cache* cache, const int32_t* seq, const int32_t* slot, int32_t n, const ss_rows* k, const ss_rows* v,
+                  void* hip_stream);
+
+#define SS_TREE_MAX_NODES 1024
+
+/*
+ * Attention of drafted trees, or of single tokens, over a cache (decoding and its verification of drafts).  The j-th sequence of
+ * the call has context[j] slots of history and behind them, in slots context[j], context[j] + 1, ..., the keys and values of its
+ * nodes (ss_cache_write has put them there).  Node t attends to the whole history and to those nodes that its mask names:
+ *   out[t][head] = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale * <q[t][head], k_s>)
+ * A row that sees nothing gets zeros.  Slots that a row does not see have no influence on it, whatever they hold.
+ *   q, out       [rows][n_heads][head_dim], of one type, that of the cache if it has 16 bits; head h uses key/value head
+ *                h / (n_heads / n_kv_heads)
+ *   seq          device, int32[n_seq], nullable: the sequence of the cache; NULL = the j-th is j.  A sequence that does not
+ *                exist gets zeros; a context beyond its slab ends there
+ *   context      device, int32[n_seq]
+ *   max_context  the largest context (host; it only chooses how the work is shared out: a larger one is attended all the same)
+ *   nodes        device, int32[n_seq + 1], nullable: rows nodes[j] .. nodes[j+1] - 1 are the nodes of the j-th sequence (none, or up
+ *                to max_nodes; what lies beyond is passed over).  NULL = one node each, row j (max_nodes 1).  Rows of no sequence
+ *                stay as they are
+ *   mask         device, uint64[rows][(max_nodes + 63) / 64], nullable: bit u of a node's words = it sees node u of its sequence.
+ *                NULL = itself and the nodes before it (a chain)
+ *   workspace    device, 16-byte aligned, at least the bytes that ss_attention_tree_workspace gives for the same counts on the same
+ *                device (0: may be NULL); its contents need not be kept and do not matter
+ */
+int ss_attention_tree(const ss_cache* cache, const ss_rows* q, const ss_rows* out, int32_t n_heads, int32_t n_seq, const int32_t* seq,
+                      const int32_t* context, int32_t max_context, const int32_t* nodes, int32_t max_nodes, const uint64_t* mask, float scale,
+                      void* workspace, size_t workspace_bytes, void* hip_stream);
+int ss_attention_tree_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seq, int32_t max_context,
+                                int32_t max_nodes, size_t* bytes);
+
+/* Host only.  The mask of a tree whose node t hangs below node parents[t] < t (-1: below the history): a node sees itself and the nodes
+ * above it.  parents: host, int32[n]; mask: host, uint64[n][(max_nodes + 63) / 64]. */
+int ss_tree_mask(const int32_t* parents, int32_t n, int32_t max_nodes, uint64_t* mask);
+
+/*
+ * Causal attention of whole prompts that lie behind each other: rows offsets[i] .. offsets[i+1] - 1 (device, int32[n_seq + 1]) are the
+ * tokens of sequence i, none or up to max_len (what lies beyond is passed over); each attends to itself and the tokens of
+ * its sequence before it.  Rows of no sequence stay as they are.
+ *   q, out [rows][n_heads][head_dim], k, v [rows][n_kv_heads][head_dim], one type; head h uses key/value head h / (n_heads / n_kv_heads)
+ */
+int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_rows* v, const ss_rows* out, int32_t n_heads, int32_t n_kv_heads,
+                        int32_t head_dim, const int32_t* offsets, int32_t n_seq, int32_t max_len, float scale, void* hip_stream);
 
 #ifdef __cplusplus
 }

@@ -20,12 +20,14 @@ SS_SORT, SS_BIN, SS_FCR, SS_VBS, SS_COMPACT = 1, 2, 4, 8, 16
 SS_VBS_CLAMP_FLOOR, SS_VBS_PAPER_POW2 = 0, 1
 SS_OPT_IN_FLIGHT, SS_IN_FLIGHT_MAX, SS_IN_FLIGHT_DEFAULT = 2, 4, 4
 SS_OPT_WEIGHT_COPIES = 3
-SS_BF16, SS_F32 = 0, 1
+SS_BF16, SS_F32, SS_F16, SS_I8 = 0, 1, 2, 3
+SS_TREE_MAX_NODES = 1024
 FLAG_BITS = dict(SORT=SS_SORT, BIN=SS_BIN, FCR=SS_FCR, VBS=SS_VBS, COMPACT=SS_COMPACT)
 
 EXPORTS = ["ss_last_error", "ss_set_verbose", "ss_set_gemm_mode", "ss_schedule", "ss_schedule_failures", "ss_plan_free", "ss_weights_create",
            "ss_weights_destroy", "ss_set_option", "ss_decode_microbatch", "ss_decode_microbatch_static", "ss_forward_logits", "ss_run_group", "ss_generate_microbatch",
-           "ss_run_group_generate", "ss_bench_decode_step", "ss_bench_decode_steps_in_flight", "ss_bench_weight_stream", "ss_bench_read_stream"]
+           "ss_run_group_generate", "ss_bench_decode_step", "ss_bench_decode_steps_in_flight", "ss_bench_weight_stream", "ss_bench_read_stream",
+           "ss_cache_write", "ss_cache_read", "ss_attention_tree", "ss_attention_tree_workspace", "ss_tree_mask", "ss_attention_packed"]
 
 
 class SsError(RuntimeError):
@@ -67,6 +69,16 @@ class ss_gen_opts(C.Structure):
     _fields_ = [("eos_id", C.c_int32), ("temperature", C.c_float), ("draws", C.c_void_p),
                 ("draws_stride", C.c_int32), ("seed", C.c_uint64), ("draw_ids", C.c_void_p),
                 ("target_lens", C.c_void_p), ("sync_every", C.c_int32)]
+
+
+class ss_rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("rows", C.c_int64), ("dtype", C.c_int32)]
+
+
+class ss_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("start", C.c_void_p),
+                ("slots", C.c_void_p), ("total_slots", C.c_int64), ("n_seq", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("dtype", C.c_int32)]
 
 
 def _struct_dict(s: C.Structure) -> dict:
@@ -112,6 +124,15 @@ def lib():
         L.ss_bench_decode_steps_in_flight.argtypes = [vp, i32p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, vp]
         L.ss_bench_weight_stream.argtypes = [vp, C.c_int32, C.c_int32, vp, vp, vp]
         L.ss_bench_read_stream.argtypes = [vp, C.c_int32, vp, vp, vp]
+        rows, cache = C.POINTER(ss_rows), C.POINTER(ss_cache)
+        L.ss_cache_write.argtypes = [cache, rows, rows, vp, vp, C.c_int32, vp]
+        L.ss_cache_read.argtypes = [cache, vp, vp, C.c_int32, rows, rows, vp]
+        L.ss_attention_tree.argtypes = [cache, rows, rows, C.c_int32, C.c_int32, vp, vp, C.c_int32, vp, C.c_int32, vp, C.c_float,
+                                        vp, C.c_size_t, vp]
+        L.ss_attention_tree_workspace.argtypes = [C.c_int32] * 6 + [C.POINTER(C.c_size_t)]
+        L.ss_tree_mask.argtypes = [vp, C.c_int32, C.c_int32, vp]
+        L.ss_attention_packed.argtypes = [rows, rows, rows, rows, C.c_int32, C.c_int32, C.c_int32, vp, C.c_int32, C.c_int32,
+                                          C.c_float, vp]
         for name in EXPORTS:
             if name not in ("ss_last_error", "ss_set_verbose", "ss_set_gemm_mode", "ss_plan_free", "ss_weights_destroy"):
                 getattr(L, name).restype = C.c_int
@@ -327,3 +348,195 @@ def ss_bench_read_stream(w: Weights, iters: int, stream: Optional[int] = None):
     nbytes = C.c_int64(0)
     _check(lib().ss_bench_read_stream(w.h, iters, _ptr(ms), C.byref(nbytes), stream))
     return ms, int(nbytes.value)
+
+
+# ---------------------------------------------------------------------------------------------------- operators on device tensors
+# Tensors are torch's, used where they lie: nothing is copied.  The calls go to torch's current stream of the tensors' device (or to
+# `stream`, a HIP stream handle) and return once enqueued.
+
+_torch = None
+
+
+def _with_torch():
+    """torch, with the library on the same HIP runtime: pointers and streams of another one mean nothing to it."""
+    global _torch
+    if _torch is None:
+        import torch
+
+        lib()
+        with open("/proc/self/maps") as f:
+            runtimes = {line.split()[-1] for line in f if "libamdhip64" in line}
+        if len(runtimes) > 1:
+            raise RuntimeError("torch and this library have loaded a HIP runtime each (" + ", ".join(sorted(runtimes)) +
+                               "): import torch before the library is first used")
+        _torch = torch
+    return _torch
+
+
+def _element_type(dtype) -> int:
+    t = _torch
+    code = {t.float16: SS_F16, t.bfloat16: SS_BF16, t.int8: SS_I8}.get(dtype)
+    if code is None:
+        raise TypeError(f"tensors of {dtype} are not supported: float16, bfloat16, and int8 for caches")
+    return code
+
+
+def _on_gpu(t, name: str, device):
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be on a GPU: it is on {t.device}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} must be on {device}: it is on {t.device}")
+
+
+def _rows(t, name: str, device, heads: Optional[int], head_dim: int) -> ss_rows:
+    """[rows, heads, head_dim] with any strides but the last."""
+    _on_gpu(t, name, device)
+    if t.dim() != 3 or t.shape[2] != head_dim or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [rows, {'heads' if heads is None else heads}, {head_dim}]: it is {list(t.shape)}")
+    r, h, e = t.stride()
+    if e != 1:
+        raise ValueError(f"{name}: the elements of a head must be neighbours")
+    return ss_rows(t.data_ptr(), r, h, t.shape[0], _element_type(t.dtype))
+
+
+def _table(t, name: str, device, count: int, dtype=None):
+    if t is None:
+        return None
+    _on_gpu(t, name, device)
+    dtype = dtype or _torch.int32
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() != count:
+        raise ValueError(f"{name} must be {count} contiguous values of {dtype}: it is {list(t.shape)} of {t.dtype}")
+    return t.data_ptr()
+
+
+class _Enqueue:
+    """The device of a call and its stream, for its launches and for what it allocates."""
+
+    def __init__(self, device, stream: Optional[int]):
+        t = _torch
+        self.contexts = []
+        if device.index != t.cuda.current_device():
+            self.contexts.append(t.cuda.device(device))
+        if stream is not None:
+            self.contexts.append(t.cuda.stream(t.cuda.ExternalStream(stream, device=device)))
+        self.device, self.stream = device, stream
+
+    def __enter__(self):
+        for c in self.contexts:
+            c.__enter__()
+        return self.stream if self.stream is not None else _torch.cuda.current_stream(self.device).cuda_stream
+
+    def __exit__(self, *exc):
+        for c in reversed(self.contexts):
+            c.__exit__(*exc)
+
+
+class Cache:
+    """The key/value cache of one layer (ss_cache): a view of tensors that the caller owns.
+
+    k, v              flat, total slots * n_kv_heads * head_dim elements of float16, bfloat16 or int8
+    start, slots      int64 and int32 [sequences]: first slot and number of slots of each sequence's slab
+    k_scale, v_scale  flat float32, total slots * n_kv_heads, with int8
+    """
+
+    def __init__(self, k, v, start, slots, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None):
+        t = _with_torch()
+        dev, n = k.device, start.numel()
+        if n_kv_heads < 1 or head_dim not in (64, 128):
+            raise ValueError("n_kv_heads must be positive, head_dim 64 or 128")
+        if k.numel() % (n_kv_heads * head_dim):
+            raise ValueError("k does not hold whole slots")
+        total = k.numel() // (n_kv_heads * head_dim)
+        dtype = _element_type(k.dtype)
+        ptr = [_table(x, name, dev, k.numel(), k.dtype) for x, name in ((k, "k"), (v, "v"))]
+        if (dtype == SS_I8) != (k_scale is not None) or (dtype == SS_I8) != (v_scale is not None):
+            raise ValueError("k_scale and v_scale belong to int8 caches, and only to them")
+        ptr += [_table(x, name, dev, total * n_kv_heads, t.float32) for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+        ptr += [_table(start, "start", dev, n, t.int64), _table(slots, "slots", dev, n)]
+        self.k, self.v, self.k_scale, self.v_scale, self.start, self.slots = k, v, k_scale, v_scale, start, slots
+        self.n_seq, self.n_kv_heads, self.head_dim, self.total_slots, self.device = n, n_kv_heads, head_dim, total, dev
+        self.struct = ss_cache(*ptr, total, n, n_kv_heads, head_dim, dtype)
+
+    @classmethod
+    def allocate(cls, slots: Sequence[int], n_kv_heads: int, head_dim: int, dtype, device="cuda") -> "Cache":
+        """An empty cache of torch.float16, bfloat16 or int8 with a slab of slots[i] slots for sequence i, one behind the other."""
+        t = _with_torch()
+        n = np.asarray(slots, dtype=np.int64)
+        if n.ndim != 1 or (n < 0).any():
+            raise ValueError("slots must be a list of numbers >= 0")
+        total = int(n.sum())
+        k, v = (t.zeros(total * n_kv_heads * head_dim, dtype=dtype, device=device) for _ in range(2))
+        scales = [t.zeros(total * n_kv_heads, device=device) if dtype == t.int8 else None for _ in range(2)]
+        start = t.from_numpy(np.cumsum(n) - n).to(device)
+        return cls(k, v, start, t.from_numpy(n.astype(np.int32)).to(device), n_kv_heads, head_dim, *scales)
+
+
+def ss_cache_write(cache: Cache, k, v, seq, slot, stream: Optional[int] = None) -> None:
+    """Keys and values [n, n_kv_heads, head_dim] of n tokens to slot[t] of sequence seq[t] (int32 [n]; -1: passed over)."""
+    dev, n = cache.device, k.shape[0]
+    kr, vr = (_rows(x, name, dev, cache.n_kv_heads, cache.head_dim) for x, name in ((k, "k"), (v, "v")))
+    sq, sl = _table(seq, "seq", dev, n), _table(slot, "slot", dev, n)
+    with _Enqueue(dev, stream) as s:
+        _check(lib().ss_cache_write(cache.struct, kr, vr, sq, sl, n, s))
+
+
+def ss_cache_read(cache: Cache, seq, slot, dtype=None, k=None, v=None, stream: Optional[int] = None):
+    """(k, v) [n, n_kv_heads, head_dim]: what slot[t] of sequence seq[t] stands for.  Into k and v if they are given, whose rows of
+    tokens that do not exist stay as they are; into new tensors of `dtype` otherwise, where those rows are undefined."""
+    t = _with_torch()
+    dev, n = cache.device, seq.numel()
+    with _Enqueue(dev, stream) as s:
+        shape = (n, cache.n_kv_heads, cache.head_dim)
+        k = t.empty(shape, dtype=dtype or t.float16, device=dev) if k is None else k
+        v = t.empty(shape, dtype=k.dtype, device=dev) if v is None else v
+        kr, vr = (_rows(x, name, dev, cache.n_kv_heads, cache.head_dim) for x, name in ((k, "k"), (v, "v")))
+        _check(lib().ss_cache_read(cache.struct, _table(seq, "seq", dev, n), _table(slot, "slot", dev, n), n, kr, vr, s))
+    return k, v
+
+
+def ss_tree_mask(parents, max_nodes: int) -> np.ndarray:
+    """int64 [n, (max_nodes + 63) // 64] on the host: the bits of the nodes that each node of a tree sees (itself and those above it);
+    parents[t] < t, -1 for a node below the history."""
+    p = _i32(parents)
+    mask = np.zeros((len(p), (max(max_nodes, 1) + 63) // 64), np.int64)
+    _check(lib().ss_tree_mask(_ptr(p), len(p), max_nodes, _ptr(mask)))
+    return mask
+
+
+def ss_attention_tree(q, cache: Cache, context, max_context: int, nodes=None, max_nodes: int = 1, mask=None, seq=None,
+                      scale: Optional[float] = None, out=None, stream: Optional[int] = None):
+    """Attention of single tokens, or of the nodes of drafted trees, over a cache that holds their own keys and values behind context[j]
+    slots of history.  q [rows, heads, head_dim]; context int32 [n]; nodes int32 [n + 1] (None: a row each); mask int64
+    [rows, words] as of ss_tree_mask (None: a chain); seq int32 [n] (None: sequence j).  scale: head_dim ** -0.5 if not given.
+    Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
+    t = _with_torch()
+    dev, hd, n = cache.device, cache.head_dim, context.numel()
+    qr = _rows(q, "q", dev, None, hd)
+    heads, rows = q.shape[1], q.shape[0]
+    words = (max(max_nodes, 1) + 63) // 64
+    tables = (_table(seq, "seq", dev, n), _table(context, "context", dev, n), max_context, _table(nodes, "nodes", dev, n + 1),
+              max_nodes, _table(mask, "mask", dev, rows * words, t.int64))
+    L = lib()
+    need = C.c_size_t(0)
+    with _Enqueue(dev, stream) as s:
+        out = t.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
+        outr = _rows(out, "out", dev, heads, hd)
+        _check(L.ss_attention_tree_workspace(heads, cache.n_kv_heads, hd, n, max_context, max_nodes, need))
+        work = t.empty(need.value, dtype=t.uint8, device=dev) if need.value else None
+        _check(L.ss_attention_tree(cache.struct, qr, outr, heads, n, *tables, hd ** -0.5 if scale is None else scale,
+                                   work.data_ptr() if work is not None else None, need.value, s))
+    return out
+
+
+def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] = None, out=None, stream: Optional[int] = None):
+    """Causal attention of packed prompts: rows offsets[i] .. offsets[i+1] - 1 (int32) are sequence i's tokens, at most max_len.  q [rows,
+    heads, head_dim]; k, v [rows, kv_heads, head_dim].  Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
+    t = _with_torch()
+    dev, (rows, heads, hd), n = q.device, q.shape, offsets.numel() - 1
+    qr, kr, vr = _rows(q, "q", None, None, hd), _rows(k, "k", dev, None, hd), _rows(v, "v", dev, k.shape[1], hd)
+    at = _table(offsets, "offsets", dev, n + 1)
+    with _Enqueue(dev, stream) as s:
+        out = t.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
+        _check(lib().ss_attention_packed(qr, kr, vr, _rows(out, "out", dev, heads, hd), heads, k.shape[1], hd, at, n, max_len,
+                                         hd ** -0.5 if scale is None else scale, s))
+    return out

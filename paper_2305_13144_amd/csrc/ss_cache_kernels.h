@@ -1,0 +1,947 @@
+// Kernels of the operators on device tensors: a key/value cache in 8 or 16 bits, the attention of single tokens or of drafted
+// trees over it, and the causal attention of packed prompts.  Included by ss_kernels.hip.
+#ifndef SS_CACHE_KERNELS_H
+#define SS_CACHE_KERNELS_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "ss_device.h"
+
+namespace ss {
+
+// ------------------------------------------------------------------------------------------ element types
+// T: _Float16 or __bf16.  Operands of the matrix instructions are 8 of them per lane.
+template <typename T>
+struct Half;
+template <>
+struct Half<_Float16> {
+    typedef f16x8 x8;
+    static __device__ __forceinline__ f32x4 mma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+template <>
+struct Half<__bf16> {
+    typedef bf16x8 x8;
+    static __device__ __forceinline__ f32x4 mma(x8 a, x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+
+constexpr float kLowest = -3.0e38f;   // running maximum of no score: finite, so that exp2(-inf - kLowest) is 0
+
+// Eight values of 16 bits as floats, and back (half saturates at its largest finite value, NaN stays NaN).
+template <typename T>
+__device__ __forceinline__ void to_floats(const u32x4& r, float (&f)[8])
+{
+    const typename Half<T>::x8 h = __builtin_bit_cast(typename Half<T>::x8, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)h[i];
+}
+template <typename T>
+__device__ __forceinline__ u32x4 from_floats(const float (&f)[8])
+{
+    typename Half<T>::x8 h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (std::is_same<T, _Float16>::value) h[i] = __builtin_bit_cast(_Float16, f2h(f[i]));
+        else h[i] = (__bf16)f[i];
+    }
+    return __builtin_bit_cast(u32x4, h);
+}
+
+// First slot's vector of head h of sequence i in a cache, or -1 if the tables do not describe a slab inside it.
+__device__ __forceinline__ int64_t slab_of(const CacheView& c, int i, int* slots)
+{
+    const int64_t at = c.start[i];
+    const int n = c.slots[i];
+    *slots = n;
+    return at >= 0 && n >= 0 && at + n <= c.total ? at * c.n_kv : -1;
+}
+
+// ------------------------------------------------------------------------------------------ cache: write and read
+// A vector of HD elements is HD / 8 neighbouring lanes', 16 bytes each.  A workgroup has kCacheVecs passes over 2048 / HD
+// vectors; vectors are numbered token by token, head by head, keys in one half of the grid and values in the other.
+constexpr int kCachePasses = 4;
+
+// Largest magnitude in a vector as the bits of a float: those are ordered as the numbers, with infinities and NaN on top.
+template <int HD>
+__device__ __forceinline__ uint32_t vector_top(uint32_t m)
+{
+    auto top = [&](float o) { const uint32_t u = __float_as_uint(o); m = m > u ? m : u; };
+    top(dpp<kDppXor1>(__uint_as_float(m)));
+    top(dpp<kDppXor2>(__uint_as_float(m)));
+    top(dpp<kDppHalfMirror>(__uint_as_float(m)));
+    if (HD == 128) top(dpp<kDppMirror>(__uint_as_float(m)));
+    return m;
+}
+
+// A vector in 8 bits: scale = max|x| / 127 and code = x / scale, both divisions and the step to a whole number rounded to
+// nearest (even), as written.  x times the reciprocal is within 127 * 2^-23 of that quotient, so only quotients that near to
+// the middle of two codes are divided.  A vector with an infinity or NaN gets the scale NaN (it is read back as NaN
+// throughout, by those who read it), one of zeros the scale 0.
+template <int HD>
+__device__ __forceinline__ float quantise(const float (&x)[8], uint2* codes)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t u = __float_as_uint(x[i]) & 0x7fffffffu;
+        m = m > u ? m : u;
+    }
+    m = vector_top<HD>(m);
+    const bool whole = m < 0x7f800000u;
+    const float scale = whole ? __uint_as_float(m) / 127.f : __uint_as_float(0x7fc00000u);
+    const bool plain = scale > 0x1p-100f;   // the reciprocal of a smaller one may not be a normal number
+    const float inv = plain ? 1.f / scale : 0.f;
+    int code[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float y = x[i] * inv;
+        float r = rintf(y);
+        if (!plain || fabsf(y - r) > 0.4999f) r = scale > 0.f ? rintf(x[i] / scale) : 0.f;
+        code[i] = whole ? (int)fminf(fmaxf(r, -127.f), 127.f) : 0;
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = (code[4 * i] & 255) | (code[4 * i + 1] & 255) << 8 | (code[4 * i + 2] & 255) << 16 | (uint32_t)(code[4 * i + 3] & 255) << 24;
+    *codes = make_uint2(w[0], w[1]);
+    return scale;
+}
+
+__device__ __forceinline__ void codes_to_floats(const uint2& c, float scale, float (&f)[8])
+{
+    const uint32_t w[2] = {c.x, c.y};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (float)((int)(w[i >> 2] << (24 - 8 * (i & 3))) >> 24) * scale;
+}
+
+// TOKEN: type of the tokens' rows; CACHE: int8_t, _Float16 or __bf16.
+// Bound by the bytes: 2 in and 1 out per element.  All loads of a workgroup's passes are issued before the first is used.
+template <int HD, typename TOKEN, typename CACHE>
+__global__ __launch_bounds__(256) void k_cache_write(CacheView c, RowsView k, RowsView v, const int32_t* __restrict__ seq,
+                                                     const int32_t* __restrict__ slot, int n)
+{
+    constexpr int LPV = HD / 8, VPP = 256 / LPV;
+    const bool values = blockIdx.y;
+    const RowsView src = values ? v : k;
+    const int part = threadIdx.x % LPV;
+    const int64_t first = (int64_t)blockIdx.x * (VPP * kCachePasses) + threadIdx.x / LPV, count = (int64_t)n * c.n_kv;
+    u32x4 in[kCachePasses];
+    int64_t to[kCachePasses];
+#pragma unroll
+    for (int p = 0; p < kCachePasses; ++p) {
+        const int64_t i = min(first + p * VPP, count - 1);
+        const int t = (int)(i / c.n_kv), h = (int)(i - (int64_t)t * c.n_kv), s = seq[t], at = slot[t];
+        in[p] = *(const u32x4*)((const TOKEN*)src.p + (int64_t)t * src.row + (int64_t)h * src.head + part * 8);
+        to[p] = -1;
+        if (s >= 0 && s < c.n_seq && first + p * VPP < count) {
+            int slots;
+            const int64_t base = slab_of(c, s, &slots);
+            if (base >= 0 && at >= 0 && at < slots) to[p] = base + (int64_t)h * slots + at;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < kCachePasses; ++p) {
+        if constexpr (std::is_same<CACHE, TOKEN>::value) {
+            if (to[p] >= 0) *(u32x4*)((CACHE*)(values ? c.v : c.k) + to[p] * HD + part * 8) = in[p];
+        } else {
+            float x[8];
+            to_floats<TOKEN>(in[p], x);
+            if constexpr (std::is_same<CACHE, int8_t>::value) {
+                uint2 codes;
+                const float scale = quantise<HD>(x, &codes);
+                if (to[p] < 0) continue;
+                *(uint2*)((int8_t*)(values ? c.v : c.k) + to[p] * HD + part * 8) = codes;
+                if (part == 0) (values ? c.v_scale : c.k_scale)[to[p]] = scale;
+            } else {
+                if (to[p] >= 0) *(u32x4*)((CACHE*)(values ? c.v : c.k) + to[p] * HD + part * 8) = from_floats<CACHE>(x);
+            }
+        }
+    }
+}
+
+template <int HD, typename TOKEN, typename CACHE>
+__global__ __launch_bounds__(256) void k_cache_read(CacheView c, RowsView k, RowsView v, const int32_t* __restrict__ seq,
+                                                    const int32_t* __restrict__ slot, int n)
+{
+    constexpr int LPV = HD / 8, VPP = 256 / LPV;
+    const bool values = blockIdx.y;
+    const RowsView dst = values ? v : k;
+    const int part = threadIdx.x % LPV;
+    const int64_t first = (int64_t)blockIdx.x * (VPP * kCachePasses) + threadIdx.x / LPV, count = (int64_t)n * c.n_kv;
+    u32x4 in[kCachePasses];
+    float scale[kCachePasses];
+    TOKEN* to[kCachePasses];
+#pragma unroll
+    for (int p = 0; p < kCachePasses; ++p) {
+        const int64_t i = min(first + p * VPP, count - 1);
+        const int t = (int)(i / c.n_kv), h = (int)(i - (int64_t)t * c.n_kv), s = seq[t], at = slot[t];
+        to[p] = nullptr;
+        if (s < 0 || s >= c.n_seq || first + p * VPP >= count) continue;
+        int slots;
+        const int64_t base = slab_of(c, s, &slots);
+        if (base < 0 || at < 0 || at >= slots) continue;
+        const int64_t from = base + (int64_t)h * slots + at;
+        to[p] = (TOKEN*)dst.p + (int64_t)t * dst.row + (int64_t)h * dst.head + part * 8;
+        const CACHE* src = (const CACHE*)(values ? c.v : c.k) + from * HD + part * 8;
+        if constexpr (std::is_same<CACHE, int8_t>::value) {
+            const uint2 w = *(const uint2*)src;
+            in[p] = u32x4{w.x, w.y, 0u, 0u};
+            scale[p] = (values ? c.v_scale : c.k_scale)[from];
+        } else {
+            in[p] = *(const u32x4*)src;
+        }
+    }
+#pragma unroll
+    for (int p = 0; p < kCachePasses; ++p) {
+        if (!to[p]) continue;
+        if constexpr (std::is_same<CACHE, TOKEN>::value) {
+            *(u32x4*)to[p] = in[p];
+        } else {
+            float x[8];
+            if constexpr (std::is_same<CACHE, int8_t>::value) codes_to_floats(make_uint2(in[p][0], in[p][1]), scale[p], x);
+            else to_floats<CACHE>(in[p], x);
+            *(u32x4*)to[p] = from_floats<TOKEN>(x);
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ attention over a cache
+// Rows of a unit: the (node, query head) pairs of one sequence and one key/value head, row r = node * G + (head within its
+// group), G = query heads per key/value head; a decode step is the tree of one node.  A wave takes 16 * QT rows through steps of
+// 32 slots with an online softmax in powers of two:
+//   scores      S^T[slot][row] = K Q^T        K the A operand (16 slots x 32 elements), Q^T the B operand
+//   weights     lane (row = lane % 16, g = lane / 16) holds slots 4g..4g+3 of both 16-slot tiles: the very B operand of
+//   values      O^T[element][row] += V^T P^T  with its slots taken in that order; V^T's A operand holds, for element
+//               ET * (lane % 16) + t of tile t, the same 8 slots, so a lane loads ET neighbouring elements of 8 slots (whole
+//               cache lines per 16 lanes) and exchanges them in registers.
+// Nothing is staged in LDS: a decode step uses each byte of the cache once, a tree of up to 32 rows too, and the rows beyond
+// come back to it through L2 (their workgroups are neighbours on one die).  The four waves of a workgroup take turns
+// over a unit's steps and join their sums through LDS at the end; a unit's slots are cut into chunks for as many workgroups as
+// fill the chip (tree_plan), whose sums k_tree_join adds up.
+// 8-bit caches: codes become halves exactly (1152 + code as a half's bits, less 1152), the key's scale multiplies the score
+// and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R < 1 with R a power
+// of two above the scales that the row has met so far.  A row of bf16 queries is brought into half's range by a power of two.
+// Slots that a row must not see weigh 0 whatever they hold: scores by selection, values through value_sums where one is
+// infinite or NaN.
+template <typename C, typename T>
+struct MathType { typedef T type; };           // 16-bit cache: its own type
+template <typename T>
+struct MathType<int8_t, T> { typedef _Float16 type; };
+
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+// First row and number of rows (nodes) of the j-th sequence of a call; none where the table leaves the rows that there are.
+__device__ __forceinline__ int tree_nodes(const TreeArgs& a, int j, int* n)
+{
+    const int first = a.nodes ? a.nodes[j] : j, count = a.nodes ? min(a.nodes[j + 1] - first, a.max_nodes) : 1;
+    *n = first >= 0 && count > 0 && first + (int64_t)count <= a.q.rows ? count : 0;
+    return first;
+}
+
+// N neighbouring results of a row's head, e0 on: to its row, or (the engine's projections) to the packed layout.
+template <typename T, int N>
+__device__ __forceinline__ void tree_store(const TreeArgs& a, int row, int head, int e0, const float (&x)[N])
+{
+    T r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (std::is_same<T, _Float16>::value) r[i] = __builtin_bit_cast(_Float16, f2h(x[i]));
+        else r[i] = (T)x[i];
+    }
+    T* to;
+    if (a.packed_d) to = (T*)a.out.p + pk_index(row, head * a.c.hd + e0, a.packed_d);
+    else to = (T*)a.out.p + (int64_t)row * a.out.row + (int64_t)head * a.out.head + e0;
+    typedef uint32_t words __attribute__((ext_vector_type(N * 2 / 4 > 0 ? N * 2 / 4 : 1)));
+    if constexpr (N >= 2) *(words*)to = __builtin_bit_cast(words, r);
+    else *to = r[0];
+}
+
+// Four bytes' codes as halves: two pairs chosen by sel_lo and sel_hi (byte numbers of b:a, zeros between them).
+__device__ __forceinline__ uint32_t code_pair(uint32_t a, uint32_t b, uint32_t sel)
+{
+    const uint32_t u = __builtin_amdgcn_perm(b, a, sel) ^ 0x64806480u;   // 1024 + (code + 128) as halves
+    const f16x2 h = __builtin_bit_cast(f16x2, u) - f16x2{(_Float16)1152.f, (_Float16)1152.f};
+    return __builtin_bit_cast(uint32_t, h);
+}
+
+// A step's operands as they come from memory.
+template <int HD, typename C>
+struct TreeStep {
+    static constexpr bool I8 = std::is_same<C, int8_t>::value;
+    static constexpr int KL = I8 ? HD / 64 : HD / 32;   // 16-byte loads per key tile and lane
+    static constexpr int VW = I8 ? HD / 64 : HD / 32;   // words per slot and lane: ET elements
+    u32x4 k[2][KL];
+    uint32_t v[8][VW];
+    f32x4u ks[2], vs[2];
+};
+
+template <int HD, typename C>
+__device__ __forceinline__ void tree_load(TreeStep<HD, C>& st, const C* __restrict__ K, const C* __restrict__ V,
+                                          const float* __restrict__ kscale, const float* __restrict__ vscale, int base, int last,
+                                          int ql, int g)
+{
+    constexpr bool I8 = TreeStep<HD, C>::I8;
+    constexpr int ET = HD / 16, VW = TreeStep<HD, C>::VW;
+    const bool inside = base + 31 <= last;   // uniform
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+        const int s = min(base + kt * 16 + ql, last);
+        const C* p = K + (size_t)s * HD;
+#pragma unroll
+        for (int i = 0; i < TreeStep<HD, C>::KL; ++i)
+            st.k[kt][i] = *(const u32x4*)(I8 ? p + 64 * i + 16 * g : p + 32 * i + 8 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int sv = min(base + kt * 16 + 4 * g + i, last);
+            const uint32_t* q = (const uint32_t*)(V + (size_t)sv * HD + ET * ql);
+            if constexpr (VW == 4) {
+                const u32x4 w = *(const u32x4*)q;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) st.v[kt * 4 + i][j] = w[j];
+            } else if constexpr (VW == 2) {
+                const uint2 w = *(const uint2*)q;
+                st.v[kt * 4 + i][0] = w.x;
+                st.v[kt * 4 + i][1] = w.y;
+            } else {
+                st.v[kt * 4 + i][0] = *q;
+            }
+        }
+        if constexpr (I8) {
+            const int s4 = base + kt * 16 + 4 * g;
+            if (inside) {
+                st.ks[kt] = *(const f32x4u*)(kscale + s4);
+                st.vs[kt] = *(const f32x4u*)(vscale + s4);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    st.ks[kt][i] = kscale[min(s4 + i, last)];
+                    st.vs[kt][i] = vscale[min(s4 + i, last)];
+                }
+            }
+        }
+    }
+}
+
+template <int HD, typename T, typename C, int QT>
+__global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
+{
+    typedef typename MathType<C, T>::type M;
+    typedef typename Half<M>::x8 m8;
+    typedef TreeStep<HD, C> Step;
+    constexpr bool I8 = Step::I8;
+    constexpr int KS = HD / 32, ET = HD / 16, NW = 4, ROWS = 16 * QT;
+    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+    __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
+    const CacheView& c = a.c;
+
+    // blocks of rows of one unit are 8 apart: on one die, whose L2 hands the unit's slots on
+    const int id = blockIdx.x, G = a.heads / c.n_kv;
+    const int rb = (id >> 3) % a.row_blocks;
+    const int unit = (id >> 3) / a.row_blocks * 8 + (id & 7);
+    const int h = unit % c.n_kv, chunk = unit / c.n_kv % a.chunks, j = unit / c.n_kv / a.chunks;
+    const int n_seq = a.d_n ? *a.d_n : a.n_seq;
+    if (j >= min(n_seq, a.n_seq)) return;
+    const int seq = a.seq ? a.seq[j] : j;
+    int n_nodes;
+    const int node0 = tree_nodes(a, j, &n_nodes);
+    const int n_rows = n_nodes * G, r0 = rb * ROWS;
+    if (r0 >= n_rows) return;
+    int slots = 0, len = 0;
+    int64_t base = -1;
+    const int ctx = max(a.context[j], 0);
+    if (seq >= 0 && seq < c.n_seq) base = slab_of(c, seq, &slots);
+    if (base >= 0) len = (int)min((int64_t)ctx + n_nodes, (int64_t)slots);
+    const int n_chunks = tree_chunks(len, a.chunk, a.chunks);
+    if (chunk >= n_chunks) return;
+    const int s_begin = chunk * a.chunk, s_end = chunk + 1 == n_chunks ? len : s_begin + a.chunk, last = len - 1;
+
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ql = lane & 15, g = lane >> 4;
+    const int64_t head_base = base + (int64_t)h * slots;
+    const C* K = (const C*)c.k + head_base * HD;
+    const C* V = (const C*)c.v + head_base * HD;
+    const float *kscale = I8 ? c.k_scale + head_base : nullptr, *vscale = I8 ? c.v_scale + head_base : nullptr;
+    const int first = s_begin + 32 * wave;
+    Step now, next;
+    if (first < s_end) tree_load<HD, C>(now, K, V, kscale, vscale, first, last, ql, g);
+
+    m8 qf[QT][KS];
+    float qscale[QT];   // of a row's scores, in units of log2
+    int node[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const int r = min(r0 + u * 16 + ql, n_rows - 1);
+        node[u] = r / G;
+        const T* qp = (const T*)a.q.p + (int64_t)(node0 + node[u]) * a.q.row + (int64_t)(h * G + r - node[u] * G) * a.q.head;
+        u32x4 w[KS];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) w[ks] = *(const u32x4*)(I8 ? qp + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1) : qp + 32 * ks + 8 * g);
+        qscale[u] = a.scale * 1.44269504088896341f;
+        if constexpr (std::is_same<M, T>::value) {
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) qf[u][ks] = __builtin_bit_cast(m8, w[ks]);
+        } else {   // bf16 queries, half arithmetic: the row's largest magnitude becomes 2^14 to 2^15
+            float x[KS][8], top = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                to_floats<T>(w[ks], x[ks]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[ks][e]));
+            }
+            top = across<32>(across<16>(top, Max()), Max());
+            const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);   // the largest is below 2^(ex + 1)
+            const float down = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+            qscale[u] *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qf[u][ks][e] = (_Float16)(x[ks][e] * down);
+        }
+    }
+    f32x4 o[QT][ET];
+    float m_run[QT], l_run[QT], R[QT], R_inv[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+#pragma unroll
+        for (int t = 0; t < ET; ++t) o[u][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        m_run[u] = kLowest;
+        l_run[u] = R[u] = R_inv[u] = 0.f;
+    }
+
+    for (int s0 = first; s0 < s_end; s0 += 32 * NW) {
+        if (s0 + 32 * NW < s_end) tree_load<HD, C>(next, K, V, kscale, vscale, s0 + 32 * NW, last, ql, g);
+        f32x4 s[QT][2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+            m8 kf[KS];
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                if constexpr (I8) {
+                    const uint32_t lo = now.k[kt][ks >> 1][2 * (ks & 1)], hi = now.k[kt][ks >> 1][2 * (ks & 1) + 1];
+                    const u32x4 w = {code_pair(lo, lo, 0x0c010c00u), code_pair(lo, lo, 0x0c030c02u), code_pair(hi, hi, 0x0c010c00u),
+                                     code_pair(hi, hi, 0x0c030c02u)};
+                    kf[ks] = __builtin_bit_cast(m8, w);
+                } else {
+                    kf[ks] = __builtin_bit_cast(m8, now.k[kt][ks]);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                s[u][kt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) s[u][kt] = Half<M>::mma(kf[ks], qf[u][ks], s[u][kt]);
+            }
+        }
+        const bool tail = s0 + 31 >= min(ctx, len);   // some slot is a node's, or beyond all
+        m8 pb[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float mt = kLowest;
+            uint32_t seen[2] = {15u, 15u};   // of this lane's slots, by its row
+            if (tail) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    seen[kt] = 0;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int at = s0 + kt * 16 + 4 * g + i, n = at - ctx;
+                        bool yes = n < 0;
+                        if (n >= 0 && n < n_nodes)
+                            yes = a.mask ? (a.mask[(int64_t)(node0 + node[u]) * a.words + (n >> 6)] >> (n & 63)) & 1 : n <= node[u];
+                        if (yes && at < s_end) seen[kt] |= 1u << i;
+                    }
+                }
+            }
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float x = s[u][kt][i] * qscale[u];
+                    if constexpr (I8) x *= now.ks[kt][i];
+                    if (tail && !(seen[kt] >> i & 1)) x = -__builtin_inff();
+                    s[u][kt][i] = x;
+                    mt = fmaxf(mt, x);
+                }
+            mt = across<32>(across<16>(mt, Max()), Max());
+            if (__any(mt > m_run[u])) {
+                const float m_new = fmaxf(m_run[u], mt), alpha = __builtin_amdgcn_exp2f(m_run[u] - m_new);
+                m_run[u] = m_new;
+                l_run[u] *= alpha;
+#pragma unroll
+                for (int t = 0; t < ET; ++t) o[u][t] *= alpha;
+            }
+            if constexpr (I8) {   // a power of two above the scales that the row has met
+                float top = 0.f;
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, tail && !(seen[kt] >> i & 1) ? 0.f : now.vs[kt][i]);
+                if (__any(top > R[u])) {
+                    top = across<32>(across<16>(top, Max()), Max());
+                    const uint32_t two = min(__float_as_uint(top) + 0x01000000u, 0x7f000000u) & 0x7f800000u;
+                    const float R_new = top > R[u] ? __uint_as_float(two) : R[u];
+                    const float down = R[u] * __uint_as_float(0x7f000000u - __float_as_uint(R_new));
+                    R[u] = R_new;
+                    R_inv[u] = R_new > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(R_new)) : 0.f;
+#pragma unroll
+                    for (int t = 0; t < ET; ++t) o[u][t] *= down;
+                }
+            }
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(s[u][kt][i] - m_run[u]);
+                    l_run[u] += p;
+                    float w = p;
+                    if constexpr (I8) w = tail && !(seen[kt] >> i & 1) ? 0.f : p * (now.vs[kt][i] * R_inv[u]);
+                    pb[u][kt * 4 + i] = (M)w;
+                }
+        }
+        bool odd = false;   // some value of a tail's slots is infinite or NaN
+        if constexpr (!I8) {
+            if (tail) {
+                constexpr uint32_t EXP = std::is_same<M, _Float16>::value ? 0x7c00u : 0x7f80u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int w = 0; w < Step::VW; ++w) {
+                        const uint32_t x = now.v[i][w];
+                        odd = odd || (x & EXP) == EXP || (x >> 16 & EXP) == EXP;
+                    }
+                odd = __any(odd);
+            }
+        }
+        if (odd) {   // slot by slot, so that those a row does not see stay out of its sums
+            for (int n = 0; n < 32; ++n) {
+                const int sv = min(s0 + (n & 16) + (n & 15), last), from = ql + 16 * ((n & 15) >> 2);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    float p = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i == (n >> 4) * 4 + (n & 3)) p = __shfl((float)pb[u][i], from);
+#pragma unroll
+                    for (int t = 0; t < ET; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float x = I8 ? 0.f : (float)((const M*)V)[(size_t)sv * HD + ET * (4 * g + i) + t];
+                            if (p != 0.f) o[u][t][i] = fmaf(p, x, o[u][t][i]);
+                        }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < ET; ++t) {
+                u32x4 w;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (I8) w[i] = code_pair(now.v[2 * i][t >> 2], now.v[2 * i + 1][t >> 2], 0x0c040c00u + (t & 3) * 0x00010001u);
+                    else w[i] = __builtin_amdgcn_perm(now.v[2 * i + 1][t >> 1], now.v[2 * i][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+                }
+                const m8 vf = __builtin_bit_cast(m8, w);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) o[u][t] = Half<M>::mma(vf, pb[u], o[u][t]);
+            }
+        }
+        now = next;
+    }
+
+    // the waves' sums together: each brings its own to the common maximum
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        l_run[u] = across<32>(across<16>(l_run[u], Add()), Add());
+        if (g == 0) {
+            s_m[wave][u * 16 + ql] = m_run[u];
+            s_l[wave][u * 16 + ql] = l_run[u];
+        }
+    }
+    __syncthreads();
+    float m_all[QT], l_all[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        m_all[u] = kLowest;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) m_all[u] = fmaxf(m_all[u], s_m[w][u * 16 + ql]);
+        l_all[u] = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f(s_m[w][u * 16 + ql] - m_all[u]);
+        const float f = __builtin_amdgcn_exp2f(m_run[u] - m_all[u]) * (I8 ? R[u] : 1.f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < ET; t += 4) {
+                const float4 x = make_float4(o[u][t][i] * f, o[u][t + 1][i] * f, o[u][t + 2][i] * f, o[u][t + 3][i] * f);
+                *(float4*)&s_o[wave][u][i][lane][t] = x;
+            }
+    }
+    __syncthreads();
+    // wave i takes elements ET * (4g + i) .. of every row: ET neighbours per lane
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const int r = r0 + u * 16 + ql;
+        float x[ET];
+#pragma unroll
+        for (int t = 0; t < ET; ++t) {
+            x[t] = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) x[t] += s_o[w][u][wave][lane][t];
+        }
+        if (r >= n_rows) continue;
+        const int e0 = ET * (4 * g + wave);
+        if (n_chunks > 1) {
+            const size_t at = ((size_t)unit * a.max_nodes * G + r) * (HD + 2);
+            float* to = a.part + at;
+#pragma unroll
+            for (int t = 0; t < ET; ++t) to[e0 + t] = x[t];
+            if (wave == 0 && g == 0) {
+                to[HD] = m_all[u];
+                to[HD + 1] = l_all[u];
+            }
+        } else {
+            const float inv = l_all[u] != 0.f ? 1.f / l_all[u] : 0.f;   // a row that sees nothing gets zeros
+#pragma unroll
+            for (int t = 0; t < ET; ++t) x[t] *= inv;
+            tree_store<T, ET>(a, node0 + r / G, h * G + r % G, e0, x);
+        }
+    }
+}
+
+// Adds up the chunks of rows whose slots were shared out: a wave per row.
+template <int HD, typename T>
+__global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
+{
+    constexpr int E = HD / 64;
+    const CacheView& c = a.c;
+    const int G = a.heads / c.n_kv, per = a.max_nodes * G, lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int r = (int)(id % per), h = (int)(id / per % c.n_kv), j = (int)(id / per / c.n_kv);
+    const int n_seq = a.d_n ? *a.d_n : a.n_seq;
+    if (j >= min(n_seq, a.n_seq)) return;
+    const int seq = a.seq ? a.seq[j] : j;
+    int n_nodes;
+    const int node0 = tree_nodes(a, j, &n_nodes);
+    if (r >= n_nodes * G || seq < 0 || seq >= c.n_seq) return;
+    int slots = 0;
+    if (slab_of(c, seq, &slots) < 0) return;
+    const int len = (int)min((int64_t)max(a.context[j], 0) + n_nodes, (int64_t)slots);
+    const int n = tree_chunks(len, a.chunk, a.chunks);
+    if (n < 2) return;
+    const size_t step = (size_t)c.n_kv * per * (HD + 2);
+    const float* p = a.part + (((size_t)j * a.chunks * c.n_kv + h) * per + r) * (HD + 2);
+    float m = kLowest, l = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int k = 0; k < n; ++k) m = fmaxf(m, p[k * step + HD]);
+    for (int k = 0; k < n; ++k) {
+        const float f = __builtin_amdgcn_exp2f(p[k * step + HD] - m);
+        l += p[k * step + HD + 1] * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += p[k * step + E * lane + e] * f;
+    }
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] *= inv;
+    tree_store<T, E>(a, node0 + r / G, h * G + r % G, E * lane, o);
+}
+
+// ------------------------------------------------------------------------------------------ attention of packed prompts
+// Causal attention of sequences that lie behind each other: rows offsets[i] .. offsets[i+1] - 1 are sequence i's tokens.  A
+// workgroup takes 64 * QT queries of one head (a wave 16 * QT of them) through tiles of 64 keys: the scores are formed as
+// S^T = K Q^T, so that a query's numbers stay in its lanes and the weights are already the operand that O^T += V^T P^T takes.
+// Keys of one tile lie in LDS as they come, values transposed.
+constexpr int kPackTile = 64;
+
+template <int HD, typename T, int QT, int NBUF>
+__global__ __launch_bounds__(256, QT == 2 ? 2 : 3) void k_attention_packed(PackedArgs a)
+{
+    typedef typename Half<T>::x8 t8;
+    typedef T t4 __attribute__((ext_vector_type(4)));
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    constexpr int KT = kPackTile;
+    constexpr int KS = HD / 32, ET = HD / 16, OCT = HD / 8;
+    constexpr int KROW = HD + 8, VROW = KT + 8;
+    constexpr int PPT = KT * OCT / 256, NKG = KT / PPT;
+    __shared__ __attribute__((aligned(16))) T k_lds[NBUF][KT * KROW];
+    __shared__ __attribute__((aligned(16))) T v_lds[NBUF][HD * VROW];
+    __shared__ int odd_lds[NBUF];
+    const int h = blockIdx.x, i_seq = blockIdx.y, qt = gridDim.z - 1 - blockIdx.z;
+    const int first = a.offsets[i_seq], end = a.offsets[i_seq + 1];
+    if (first < 0 || end > a.q.rows) return;
+    const int p = min(end - first, a.max_len);
+    const int q0 = qt * 64 * QT;
+    if (q0 >= p) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int ql = lane & 15, g = lane >> 4;
+    const int hk = h / (a.heads / a.n_kv);
+    const T* Kg = (const T*)a.k.p + (int64_t)first * a.k.row + (int64_t)hk * a.k.head;
+    const T* Vg = (const T*)a.v.p + (int64_t)first * a.v.row + (int64_t)hk * a.v.head;
+    const int wave_first = q0 + wave * 16 * QT;
+    const int wave_last = wave_first < p ? min(wave_first + 16 * QT - 1, p - 1) : -1;
+    const int n_keys = min(p, q0 + 64 * QT);
+    const int n_tiles = (n_keys + KT - 1) / KT;
+    const float scale = a.scale * 1.44269504088896341f;
+
+    u32x4 kreg[PPT], vreg[PPT];
+    const u32x4 zero4 = {0u, 0u, 0u, 0u};
+    auto load_tile = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+            const int c = tid + i * 256, key = t * KT + c / OCT;
+            const u32x4 kv = *(const u32x4*)(Kg + (int64_t)min(key, n_keys - 1) * a.k.row + c % OCT * 8);
+            kreg[i] = key < n_keys ? kv : zero4;
+        }
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+            const int key = t * KT + (tid % NKG) * PPT + i;
+            const u32x4 vv = *(const u32x4*)(Vg + (int64_t)min(key, n_keys - 1) * a.v.row + tid / NKG * 8);
+            vreg[i] = key < n_keys ? vv : zero4;
+        }
+    };
+    auto stage_tile = [&](int b, int t) {
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) {
+            const int c = tid + i * 256;
+            *(u32x4*)&k_lds[b][(c / OCT) * KROW + (c % OCT) * 8] = kreg[i];
+        }
+        T* vt = &v_lds[b][(tid / NKG) * 8 * VROW + vt_pos((tid % NKG) * PPT)];
+        t8 v[PPT];
+#pragma unroll
+        for (int i = 0; i < PPT; ++i) v[i] = __builtin_bit_cast(t8, vreg[i]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (PPT == 4) {
+                const t4 o = {v[0][e], v[1][e], v[PPT - 2][e], v[PPT - 1][e]};
+                *(t4*)(vt + e * VROW) = o;
+            } else {
+                const t2 o = {v[0][e], v[1][e]};
+                *(t2*)(vt + e * VROW) = o;
+            }
+        }
+        if (t * KT + KT - 1 > q0) {   // some query does not see all of the tile
+            constexpr uint32_t EXP = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < PPT; ++i)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) odd = odd || (vreg[i][w] & EXP) == EXP || (vreg[i][w] >> 16 & EXP) == EXP;
+            if (odd) odd_lds[b] = t + 1;
+        }
+    };
+    if (tid < NBUF) odd_lds[tid] = 0;
+    load_tile(0);
+    __syncthreads();
+
+    t8 qf[QT][KS];
+    int qpos[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        qpos[u] = min(wave_first + u * 16 + ql, p - 1);
+        const T* qp = (const T*)a.q.p + (int64_t)(first + qpos[u]) * a.q.row + (int64_t)h * a.q.head + 8 * g;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) qf[u][ks] = *(const t8*)(qp + 32 * ks);
+    }
+    f32x4 o[QT][ET];
+    float m_run[QT], l_run[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+#pragma unroll
+        for (int t = 0; t < ET; ++t) o[u][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        m_run[u] = kLowest;
+        l_run[u] = 0.f;
+    }
+
+    auto use_tile = [&](int b, int k0, auto masked) {
+        constexpr bool MASKED = decltype(masked)::value;
+        f32x4 s[QT][4];
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u) s[u][kt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            if (MASKED && k0 + kt * 16 > wave_last) continue;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const t8 kf = *(const t8*)&k_lds[b][(kt * 16 + ql) * KROW + ks * 32 + 8 * g];
+#pragma unroll
+                for (int u = 0; u < QT; ++u) s[u][kt] = Half<T>::mma(kf, qf[u][ks], s[u][kt]);
+            }
+        }
+        t8 pb[QT][2];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float mt = kLowest;
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[u][kt][i] *= scale;
+                    if (MASKED && k0 + kt * 16 + 4 * g + i > qpos[u]) s[u][kt][i] = -__builtin_inff();
+                    mt = fmaxf(mt, s[u][kt][i]);
+                }
+            mt = across<32>(across<16>(mt, Max()), Max());
+            if (__any(mt > m_run[u])) {
+                const float m_new = fmaxf(m_run[u], mt);
+                const float alpha = __builtin_amdgcn_exp2f(m_run[u] - m_new);
+                m_run[u] = m_new;
+                l_run[u] *= alpha;
+#pragma unroll
+                for (int tt = 0; tt < ET; ++tt) o[u][tt] *= alpha;
+            }
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float pv = __builtin_amdgcn_exp2f(s[u][kt][i] - m_run[u]);
+                    l_run[u] += pv;
+                    pb[u][kt >> 1][(kt & 1) * 4 + i] = (T)pv;
+                }
+        }
+        if (MASKED && odd_lds[b] == k0 / KT + 1) {   // an infinite or NaN value: slot by slot, so that only those who see it meet it
+            for (int n = 0; n < KT; ++n) {
+                const int from = ql + 16 * ((n & 15) >> 2);
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    float w = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (i == (n >> 4) * 4 + (n & 3)) w = __shfl((float)pb[u][i >> 3][i & 7], from);
+                    if (w == 0.f || k0 + n > qpos[u]) continue;
+#pragma unroll
+                    for (int tt = 0; tt < ET; ++tt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            o[u][tt][i] = fmaf(w, (float)v_lds[b][(tt * 16 + 4 * g + i) * VROW + vt_pos(n)], o[u][tt][i]);
+                }
+            }
+            return;
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if (MASKED && k0 + c * 32 > wave_last) continue;
+#pragma unroll
+            for (int tt = 0; tt < ET; ++tt) {
+                const t8 vf = *(const t8*)&v_lds[b][(tt * 16 + ql) * VROW + c * 32 + 8 * g];
+#pragma unroll
+                for (int u = 0; u < QT; ++u) o[u][tt] = Half<T>::mma(vf, pb[u][c], o[u][tt]);
+            }
+        }
+    };
+    stage_tile(0, 0);
+    for (int t = 0; t < n_tiles; ++t) {
+        const int b = NBUF == 2 ? t & 1 : 0;
+        __syncthreads();
+        if (t + 1 < n_tiles) load_tile(t + 1);
+        const int k0 = t * KT;
+        if (k0 <= wave_last) {
+            if (k0 + KT - 1 <= wave_first) use_tile(b, k0, std::false_type{});
+            else use_tile(b, k0, std::true_type{});
+        }
+        if (NBUF == 1) __syncthreads();
+        if (t + 1 < n_tiles) stage_tile(NBUF == 2 ? b ^ 1 : 0, t + 1);
+    }
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        float l = l_run[u];
+        l = across<32>(across<16>(l, Add()), Add());
+        if (wave_first + u * 16 + ql >= p) continue;
+        const float inv = 1.f / l;
+#pragma unroll
+        for (int tt = 0; tt < ET; ++tt) {
+            t4 r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float x = o[u][tt][e] * inv;
+                if constexpr (std::is_same<T, _Float16>::value) r[e] = __builtin_bit_cast(_Float16, f2h(x));
+                else r[e] = (T)x;
+            }
+            T* to = a.packed_d ? (T*)a.out.p + pk_index(first + qpos[u], h * HD + tt * 16 + 4 * g, a.packed_d)
+                               : (T*)a.out.p + (int64_t)(first + qpos[u]) * a.out.row + (int64_t)h * a.out.head + tt * 16 + 4 * g;
+            *(t4*)to = r;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ launches
+template <int HD, typename TOKEN, typename CACHE>
+static void cache_write(const CacheView& c, const RowsView& k, const RowsView& v, const int32_t* seq, const int32_t* slot, int n, hipStream_t s)
+{
+    const int64_t per = 2048 / HD * kCachePasses, vecs = (int64_t)n * c.n_kv;
+    k_cache_write<HD, TOKEN, CACHE><<<dim3((unsigned)((vecs + per - 1) / per), 2), 256, 0, s>>>(c, k, v, seq, slot, n);
+}
+template <int HD, typename TOKEN, typename CACHE>
+static void cache_read(const CacheView& c, const RowsView& k, const RowsView& v, const int32_t* seq, const int32_t* slot, int n, hipStream_t s)
+{
+    const int64_t per = 2048 / HD * kCachePasses, vecs = (int64_t)n * c.n_kv;
+    k_cache_read<HD, TOKEN, CACHE><<<dim3((unsigned)((vecs + per - 1) / per), 2), 256, 0, s>>>(c, k, v, seq, slot, n);
+}
+// f(head dim, tokens' type, cache's type) with values of those types and dims.
+template <class F>
+static void with_types(int hd, int token, int cache, F f)
+{
+    auto by_cache = [&](auto dim, auto t) {
+        if (cache == kI8) f(dim, t, int8_t{});
+        else if (cache == kF16) f(dim, t, _Float16{});
+        else f(dim, t, __bf16{});
+    };
+    auto by_token = [&](auto dim) {
+        if (token == kF16) by_cache(dim, _Float16{});
+        else by_cache(dim, __bf16{});
+    };
+    if (hd == 128) by_token(std::integral_constant<int, 128>{});
+    else by_token(std::integral_constant<int, 64>{});
+}
+
+void launch_cache_write(const CacheView& c, const RowsView& k, const RowsView& v, int token, const int32_t* seq, const int32_t* slot, int n,
+                        hipStream_t s)
+{
+    with_types(c.hd, token, c.dtype, [&](auto dim, auto t, auto e) { cache_write<decltype(dim)::value, decltype(t), decltype(e)>(c, k, v, seq, slot, n, s); });
+}
+
+void launch_cache_read(const CacheView& c, const RowsView& k, const RowsView& v, int token, const int32_t* seq, const int32_t* slot, int n,
+                       hipStream_t s)
+{
+    with_types(c.hd, token, c.dtype, [&](auto dim, auto t, auto e) { cache_read<decltype(dim)::value, decltype(t), decltype(e)>(c, k, v, seq, slot, n, s); });
+}
+
+template <int HD, typename T, typename C, int QT>
+static void attention_tree(TreeArgs a, hipStream_t s)
+{
+    const int units = round_up(a.n_seq * a.c.n_kv * a.chunks, 8);
+    k_attention_tree<HD, T, C, QT><<<dim3((unsigned)units * a.row_blocks), 256, 0, s>>>(a);
+    if (a.chunks > 1) {
+        const int64_t rows = (int64_t)a.n_seq * a.max_nodes * a.heads;
+        k_tree_join<HD, T><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(a);
+    }
+}
+
+void launch_attention_tree(const TreeArgs& a, int token, int tiles, hipStream_t s)
+{
+    with_types(a.c.hd, token, a.c.dtype, [&](auto dim, auto t, auto e) {
+        typedef decltype(t) T;
+        typedef decltype(e) C;
+        if constexpr (std::is_same<C, int8_t>::value || std::is_same<C, T>::value) {
+            if (tiles == 1) attention_tree<decltype(dim)::value, T, C, 1>(a, s);
+            else attention_tree<decltype(dim)::value, T, C, 2>(a, s);
+        }
+    });
+}
+
+template <int HD, typename T>
+static void attention_packed(const PackedArgs& a, int n_seq, hipStream_t s)
+{
+    if (a.max_len >= 256) k_attention_packed<HD, T, 2, 2><<<dim3(a.heads, n_seq, (a.max_len + 127) / 128), 256, 0, s>>>(a);
+    else k_attention_packed<HD, T, 1, 1><<<dim3(a.heads, n_seq, (a.max_len + 63) / 64), 256, 0, s>>>(a);
+}
+
+void launch_attention_packed(const PackedArgs& a, int hd, int token, int n_seq, hipStream_t s)
+{
+    if (hd == 128) token == kF16 ? attention_packed<128, _Float16>(a, n_seq, s) : attention_packed<128, __bf16>(a, n_seq, s);
+    else token == kF16 ? attention_packed<64, _Float16>(a, n_seq, s) : attention_packed<64, __bf16>(a, n_seq, s);
+}
+
+}  // namespace ss
+
+#endif

@@ -145,6 +145,52 @@ void launch_step_update(const MbState& st, int compact, int eos_id, hipStream_t 
 void launch_read_stream(const f16_t* p, size_t bytes, uint32_t* sink, hipStream_t s);
 void launch_fill_i32(int32_t* p, int32_t v, size_t n, hipStream_t s);
 
+// ---- operators on device tensors (ss_cache_kernels.h)
+constexpr int kBF16 = 0, kF16 = 2, kI8 = 3;   // element types: SS_BF16, SS_F16, SS_I8
+
+// A layer's key/value cache: element e of head h in slot s of sequence i at (start[i] * n_kv + h * slots[i] + s) * hd + e.
+struct CacheView {
+    void *k, *v;
+    float *k_scale, *v_scale;   // kI8: one per vector
+    const int64_t* start;
+    const int32_t* slots;
+    int64_t total;              // slots of all slabs
+    int n_seq, n_kv, hd, dtype;
+};
+// Rows of heads: element e of head h of row r at r * row + h * head + e.
+struct RowsView {
+    void* p;
+    int64_t row, head, rows;
+};
+// Tokens t < n to or from slot[t] of sequence seq[t]; those outside the tables are passed over.
+void launch_cache_write(const CacheView& c, const RowsView& k, const RowsView& v, int token, const int32_t* seq, const int32_t* slot, int n,
+                        hipStream_t s);
+void launch_cache_read(const CacheView& c, const RowsView& k, const RowsView& v, int token, const int32_t* seq, const int32_t* slot, int n,
+                       hipStream_t s);
+struct TreeArgs {
+    CacheView c;
+    RowsView q, out;
+    int packed_d;              // > 0: out is a packed [rows, packed_d] operand of a projection
+    const int32_t* seq;        // [n_seq] sequence of the cache, or null: the j-th is j
+    const int32_t* context;    // [n_seq] slots before the nodes' own
+    const int32_t* nodes;      // [n_seq + 1] first row of each sequence's nodes, or null: one node each
+    const uint64_t* mask;      // [rows][words] nodes that a node sees, or null: itself and those before it
+    const int32_t* d_n;        // null, or how many of the n_seq there are
+    float* part;               // chunks > 1: [n_seq][chunks][n_kv][max_nodes * G][hd + 2]
+    float scale;
+    int n_seq, heads, max_nodes, words;
+    int chunk, chunks, row_blocks;   // tree_plan
+};
+void launch_attention_tree(const TreeArgs& a, int token, int tiles, hipStream_t s);
+struct PackedArgs {
+    RowsView q, k, v, out;
+    int packed_d;              // as TreeArgs
+    const int32_t* offsets;    // [n_seq + 1]
+    float scale;
+    int heads, n_kv, max_len;
+};
+void launch_attention_packed(const PackedArgs& a, int hd, int token, int n_seq, hipStream_t s);
+
 }  // namespace ss
 
 #endif

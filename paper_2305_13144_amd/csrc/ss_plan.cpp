@@ -386,4 +386,16 @@ size_t gemm_partial_rows_bound(int n_max)
     return need;
 }
 
+TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu)
+{
+    TreePlan p;
+    p.tiles = rows <= 16 ? 1 : 2;
+    p.row_blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
+    const long long units = (long long)n_seq * n_kv * p.row_blocks;
+    const long long want = std::max(1LL, std::min(2LL * n_cu / std::max(units, 1LL), (max_len + 255LL) / 256));
+    p.chunk = (int)((max_len + want - 1) / want + 127) / 128 * 128;
+    p.chunks = std::max(1, (max_len + p.chunk - 1) / p.chunk);
+    return p;
+}
+
 }  // namespace ss

@@ -180,6 +180,18 @@ PassUnits pass_units(const std::vector<int>& order, const std::vector<int>& rows
 void set_gemm_mode(int mode);
 int gemm_mode();
 
+// Attention over a cache (k_attention_tree): rows of a sequence and key/value head (its nodes times the query heads that
+// share the head) go to workgroups in blocks of 16 * tiles, and its slots in chunks, so many that the chip is full.
+struct TreePlan {
+    int tiles, row_blocks, chunk, chunks;
+};
+TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu);
+// Chunks of a sequence of `len` slots: those it fills, at most `most` of them, at least one.
+constexpr int tree_chunks(int len, int chunk, int most)
+{
+    return len <= chunk ? 1 : len > (most - 1) * (long long)chunk ? most : (len + chunk - 1) / chunk;
+}
+
 }  // namespace ss
 
 #endif
