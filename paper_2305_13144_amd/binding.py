@@ -355,6 +355,7 @@ def ss_bench_read_stream(w: Weights, iters: int, stream: Optional[int] = None):
 # `stream`, a HIP stream handle) and return once enqueued.
 
 _torch = None
+_ELEMENT = {}   # torch dtype -> element type
 
 
 def _with_torch():
@@ -369,66 +370,62 @@ def _with_torch():
         if len(runtimes) > 1:
             raise RuntimeError("torch and this library have loaded a HIP runtime each (" + ", ".join(sorted(runtimes)) +
                                "): import torch before the library is first used")
+        _ELEMENT.update({torch.float16: SS_F16, torch.bfloat16: SS_BF16, torch.int8: SS_I8})
         _torch = torch
     return _torch
 
 
-def _element_type(dtype) -> int:
-    t = _torch
-    code = {t.float16: SS_F16, t.bfloat16: SS_BF16, t.int8: SS_I8}.get(dtype)
-    if code is None:
-        raise TypeError(f"tensors of {dtype} are not supported: float16, bfloat16, and int8 for caches")
-    return code
-
-
-def _on_gpu(t, name: str, device):
+def _refuse(t, name: str, index: int, what: str):
     if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU: it is on {t.device}")
-    if device is not None and t.device != device:
-        raise ValueError(f"{name} must be on {device}: it is on {t.device}")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must be on cuda:{index}: it is on {t.device}")
+    raise ValueError(f"{name} must be {what}: it is {list(t.shape)} of {t.dtype} with strides {list(t.stride())}")
 
 
-def _rows(t, name: str, device, heads: Optional[int], head_dim: int) -> ss_rows:
-    """[rows, heads, head_dim] with any strides but the last."""
-    _on_gpu(t, name, device)
-    if t.dim() != 3 or t.shape[2] != head_dim or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be [rows, {'heads' if heads is None else heads}, {head_dim}]: it is {list(t.shape)}")
+def _rows(t, name: str, index: int, heads: Optional[int], head_dim: int) -> ss_rows:
+    """[rows, heads, head_dim] of float16 or bfloat16 with any strides but the last; on device `index`."""
+    shape, dtype = t.shape, _ELEMENT.get(t.dtype, SS_I8)
+    if t.get_device() != index or len(shape) != 3 or shape[2] != head_dim or (heads is not None and shape[1] != heads) or dtype == SS_I8:
+        _refuse(t, name, index, f"[rows, {'heads' if heads is None else heads}, {head_dim}] of float16 or bfloat16")
     r, h, e = t.stride()
     if e != 1:
-        raise ValueError(f"{name}: the elements of a head must be neighbours")
-    return ss_rows(t.data_ptr(), r, h, t.shape[0], _element_type(t.dtype))
+        _refuse(t, name, index, "a tensor whose last dimension is contiguous")
+    return ss_rows(t.data_ptr(), r, h, shape[0], dtype)
 
 
-def _table(t, name: str, device, count: int, dtype=None):
+def _table(t, name: str, index: int, count: int, dtype):
     if t is None:
         return None
-    _on_gpu(t, name, device)
-    dtype = dtype or _torch.int32
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() != count:
-        raise ValueError(f"{name} must be {count} contiguous values of {dtype}: it is {list(t.shape)} of {t.dtype}")
+    if t.get_device() != index or t.dtype is not dtype or t.numel() != count or not t.is_contiguous():
+        _refuse(t, name, index, f"{count} contiguous values of {dtype}")
     return t.data_ptr()
 
 
-class _Enqueue:
-    """The device of a call and its stream, for its launches and for what it allocates."""
+class _Elsewhere:
+    """Launches and allocations on a device that is not the current one, or on a given stream."""
 
-    def __init__(self, device, stream: Optional[int]):
+    def __init__(self, index: int, stream: Optional[int]):
         t = _torch
-        self.contexts = []
-        if device.index != t.cuda.current_device():
-            self.contexts.append(t.cuda.device(device))
+        self.contexts = [t.cuda.device(index)]
         if stream is not None:
-            self.contexts.append(t.cuda.stream(t.cuda.ExternalStream(stream, device=device)))
-        self.device, self.stream = device, stream
+            self.contexts.append(t.cuda.stream(t.cuda.ExternalStream(stream, device=index)))
 
     def __enter__(self):
         for c in self.contexts:
             c.__enter__()
-        return self.stream if self.stream is not None else _torch.cuda.current_stream(self.device).cuda_stream
 
     def __exit__(self, *exc):
         for c in reversed(self.contexts):
             c.__exit__(*exc)
+
+
+def _enqueue(index: int, stream: Optional[int], call):
+    """call(stream handle) with `index` the current device and the stream current, the default one included."""
+    if stream is None and index == _torch.cuda.current_device():
+        return call(_torch.cuda.current_stream(index).cuda_stream)
+    with _Elsewhere(index, stream):
+        return call(_torch.cuda.current_stream(index).cuda_stream)
 
 
 class Cache:
@@ -441,20 +438,20 @@ class Cache:
 
     def __init__(self, k, v, start, slots, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None):
         t = _with_torch()
-        dev, n = k.device, start.numel()
         if n_kv_heads < 1 or head_dim not in (64, 128):
             raise ValueError("n_kv_heads must be positive, head_dim 64 or 128")
-        if k.numel() % (n_kv_heads * head_dim):
-            raise ValueError("k does not hold whole slots")
+        if k.dtype not in _ELEMENT or not k.is_cuda or k.numel() % (n_kv_heads * head_dim):
+            _refuse(k, "k", k.get_device(), "whole slots of float16, bfloat16 or int8")
+        index, n, dtype = k.get_device(), start.numel(), _ELEMENT[k.dtype]
         total = k.numel() // (n_kv_heads * head_dim)
-        dtype = _element_type(k.dtype)
-        ptr = [_table(x, name, dev, k.numel(), k.dtype) for x, name in ((k, "k"), (v, "v"))]
         if (dtype == SS_I8) != (k_scale is not None) or (dtype == SS_I8) != (v_scale is not None):
             raise ValueError("k_scale and v_scale belong to int8 caches, and only to them")
-        ptr += [_table(x, name, dev, total * n_kv_heads, t.float32) for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
-        ptr += [_table(start, "start", dev, n, t.int64), _table(slots, "slots", dev, n)]
+        ptr = [_table(x, name, index, k.numel(), k.dtype) for x, name in ((k, "k"), (v, "v"))]
+        ptr += [_table(x, name, index, total * n_kv_heads, t.float32) for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+        ptr += [_table(start, "start", index, n, t.int64), _table(slots, "slots", index, n, t.int32)]
         self.k, self.v, self.k_scale, self.v_scale, self.start, self.slots = k, v, k_scale, v_scale, start, slots
-        self.n_seq, self.n_kv_heads, self.head_dim, self.total_slots, self.device = n, n_kv_heads, head_dim, total, dev
+        self.n_seq, self.n_kv_heads, self.head_dim, self.total_slots = n, n_kv_heads, head_dim, total
+        self.device, self.index = k.device, index
         self.struct = ss_cache(*ptr, total, n, n_kv_heads, head_dim, dtype)
 
     @classmethod
@@ -473,25 +470,25 @@ class Cache:
 
 def ss_cache_write(cache: Cache, k, v, seq, slot, stream: Optional[int] = None) -> None:
     """Keys and values [n, n_kv_heads, head_dim] of n tokens to slot[t] of sequence seq[t] (int32 [n]; -1: passed over)."""
-    dev, n = cache.device, k.shape[0]
-    kr, vr = (_rows(x, name, dev, cache.n_kv_heads, cache.head_dim) for x, name in ((k, "k"), (v, "v")))
-    sq, sl = _table(seq, "seq", dev, n), _table(slot, "slot", dev, n)
-    with _Enqueue(dev, stream) as s:
-        _check(lib().ss_cache_write(cache.struct, kr, vr, sq, sl, n, s))
+    index, n, kv, hd, i32 = cache.index, k.shape[0], cache.n_kv_heads, cache.head_dim, _torch.int32
+    kr, vr = _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd)
+    sq, sl = _table(seq, "seq", index, n, i32), _table(slot, "slot", index, n, i32)
+    _check(_enqueue(index, stream, lambda s: _lib.ss_cache_write(cache.struct, kr, vr, sq, sl, n, s)))
 
 
 def ss_cache_read(cache: Cache, seq, slot, dtype=None, k=None, v=None, stream: Optional[int] = None):
     """(k, v) [n, n_kv_heads, head_dim]: what slot[t] of sequence seq[t] stands for.  Into k and v if they are given, whose rows of
-    tokens that do not exist stay as they are; into new tensors of `dtype` otherwise, where those rows are undefined."""
-    t = _with_torch()
-    dev, n = cache.device, seq.numel()
-    with _Enqueue(dev, stream) as s:
-        shape = (n, cache.n_kv_heads, cache.head_dim)
-        k = t.empty(shape, dtype=dtype or t.float16, device=dev) if k is None else k
-        v = t.empty(shape, dtype=k.dtype, device=dev) if v is None else v
-        kr, vr = (_rows(x, name, dev, cache.n_kv_heads, cache.head_dim) for x, name in ((k, "k"), (v, "v")))
-        _check(lib().ss_cache_read(cache.struct, _table(seq, "seq", dev, n), _table(slot, "slot", dev, n), n, kr, vr, s))
-    return k, v
+    tokens that do not exist stay as they are; into new tensors of `dtype` (float16) otherwise, where those rows are undefined."""
+    t, index, n, kv, hd = _torch, cache.index, seq.numel(), cache.n_kv_heads, cache.head_dim
+    sq, sl = _table(seq, "seq", index, n, t.int32), _table(slot, "slot", index, n, t.int32)
+
+    def call(s):
+        ko = t.empty((n, kv, hd), dtype=dtype or t.float16, device=cache.device) if k is None else k
+        vo = t.empty((n, kv, hd), dtype=ko.dtype, device=cache.device) if v is None else v
+        _check(_lib.ss_cache_read(cache.struct, sq, sl, n, _rows(ko, "k", index, kv, hd), _rows(vo, "v", index, kv, hd), s))
+        return ko, vo
+
+    return _enqueue(index, stream, call)
 
 
 def ss_tree_mask(parents, max_nodes: int) -> np.ndarray:
@@ -503,40 +500,53 @@ def ss_tree_mask(parents, max_nodes: int) -> np.ndarray:
     return mask
 
 
+def ss_attention_tree_workspace(n_heads: int, n_kv_heads: int, head_dim: int, n_seq: int, max_context: int, max_nodes: int = 1) -> int:
+    """Bytes of workspace that ss_attention_tree takes for these counts on the current device."""
+    need = C.c_size_t(0)
+    _check(lib().ss_attention_tree_workspace(n_heads, n_kv_heads, head_dim, n_seq, max_context, max_nodes, need))
+    return need.value
+
+
 def ss_attention_tree(q, cache: Cache, context, max_context: int, nodes=None, max_nodes: int = 1, mask=None, seq=None,
-                      scale: Optional[float] = None, out=None, stream: Optional[int] = None):
+                      scale: Optional[float] = None, out=None, workspace=None, stream: Optional[int] = None):
     """Attention of single tokens, or of the nodes of drafted trees, over a cache that holds their own keys and values behind context[j]
     slots of history.  q [rows, heads, head_dim]; context int32 [n]; nodes int32 [n + 1] (None: a row each); mask int64
     [rows, words] as of ss_tree_mask (None: a chain); seq int32 [n] (None: sequence j).  scale: head_dim ** -0.5 if not given.
-    Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
-    t = _with_torch()
-    dev, hd, n = cache.device, cache.head_dim, context.numel()
-    qr = _rows(q, "q", dev, None, hd)
-    heads, rows = q.shape[1], q.shape[0]
-    words = (max(max_nodes, 1) + 63) // 64
-    tables = (_table(seq, "seq", dev, n), _table(context, "context", dev, n), max_context, _table(nodes, "nodes", dev, n + 1),
-              max_nodes, _table(mask, "mask", dev, rows * words, t.int64))
-    L = lib()
-    need = C.c_size_t(0)
-    with _Enqueue(dev, stream) as s:
-        out = t.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
-        outr = _rows(out, "out", dev, heads, hd)
-        _check(L.ss_attention_tree_workspace(heads, cache.n_kv_heads, hd, n, max_context, max_nodes, need))
-        work = t.empty(need.value, dtype=t.uint8, device=dev) if need.value else None
-        _check(L.ss_attention_tree(cache.struct, qr, outr, heads, n, *tables, hd ** -0.5 if scale is None else scale,
-                                   work.data_ptr() if work is not None else None, need.value, s))
-    return out
+    workspace: a uint8 tensor (a new one if not given).  Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
+    t, index, hd, n = _torch, cache.index, cache.head_dim, context.numel()
+    qr, i32 = _rows(q, "q", index, None, hd), t.int32
+    rows, heads = q.shape[0], q.shape[1]
+    tables = (_table(seq, "seq", index, n, i32), _table(context, "context", index, n, i32), max_context,
+              _table(nodes, "nodes", index, n + 1, i32), max_nodes, _table(mask, "mask", index, rows * ((max(max_nodes, 1) + 63) // 64), t.int64),
+              hd ** -0.5 if scale is None else scale)
+
+    def call(s):
+        o = t.empty((rows, heads, hd), dtype=q.dtype, device=cache.device) if out is None else out
+        w = workspace
+        if w is None:
+            need = ss_attention_tree_workspace(heads, cache.n_kv_heads, hd, n, max_context, max_nodes)
+            w = t.empty(need, dtype=t.uint8, device=cache.device) if need else None
+        _check(_lib.ss_attention_tree(cache.struct, qr, _rows(o, "out", index, heads, hd), heads, n, *tables,
+                                      _table(w, "workspace", index, 0 if w is None else w.numel(), t.uint8), 0 if w is None else w.numel(), s))
+        return o
+
+    return _enqueue(index, stream, call)
 
 
 def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] = None, out=None, stream: Optional[int] = None):
     """Causal attention of packed prompts: rows offsets[i] .. offsets[i+1] - 1 (int32) are sequence i's tokens, at most max_len.  q [rows,
     heads, head_dim]; k, v [rows, kv_heads, head_dim].  Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
     t = _with_torch()
-    dev, (rows, heads, hd), n = q.device, q.shape, offsets.numel() - 1
-    qr, kr, vr = _rows(q, "q", None, None, hd), _rows(k, "k", dev, None, hd), _rows(v, "v", dev, k.shape[1], hd)
-    at = _table(offsets, "offsets", dev, n + 1)
-    with _Enqueue(dev, stream) as s:
-        out = t.empty((rows, heads, hd), dtype=q.dtype, device=dev) if out is None else out
-        _check(lib().ss_attention_packed(qr, kr, vr, _rows(out, "out", dev, heads, hd), heads, k.shape[1], hd, at, n, max_len,
-                                         hd ** -0.5 if scale is None else scale, s))
-    return out
+    index, (rows, heads, hd), kv, n = q.get_device(), q.shape, k.shape[1], offsets.numel() - 1
+    if index < 0:
+        _refuse(q, "q", index, "")
+    parts = _rows(q, "q", index, heads, hd), _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd)
+    at = _table(offsets, "offsets", index, n + 1, t.int32)
+
+    def call(s):
+        o = t.empty((rows, heads, hd), dtype=q.dtype, device=q.device) if out is None else out
+        _check(_lib.ss_attention_packed(*parts, _rows(o, "out", index, heads, hd), heads, kv, hd, at, n, max_len,
+                                        hd ** -0.5 if scale is None else scale, s))
+        return o
+
+    return _enqueue(index, stream, call)

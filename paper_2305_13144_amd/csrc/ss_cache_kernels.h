@@ -649,219 +649,235 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 }
 
 // ------------------------------------------------------------------------------------------ attention of packed prompts
-// Causal attention of sequences that lie behind each other: rows offsets[i] .. offsets[i+1] - 1 are sequence i's tokens.  A
-// workgroup takes 64 * QT queries of one head (a wave 16 * QT of them) through tiles of 64 keys: the scores are formed as
-// S^T = K Q^T, so that a query's numbers stay in its lanes and the weights are already the operand that O^T += V^T P^T takes.
-// Keys of one tile lie in LDS as they come, values transposed.
-constexpr int kPackTile = 64;
+// Causal attention of sequences that lie behind each other: rows offsets[i] .. offsets[i+1] - 1 are sequence i's tokens.  A wave
+// takes 32 queries of one head through tiles of 64 keys.  As above the scores are formed as S^T = K Q^T, now in blocks of 32 keys x 32
+// queries, so that a query's numbers are in two lanes and the weights are already the operand that O^T += V^T P^T takes:
+//   weights  lane (query = lane % 32, hi = lane / 32) holds keys 8b + 4hi + (0..3), b = 0..3, of a block; two b's are an operand
+//   values   the same keys of element lane % 32: four neighbouring keys of one element, what the transposed LDS read returns
+// Keys and values are copied into LDS as they lie in memory (two tiles, one on its way while the other is used), pieces of 16 bytes
+// changing places within a row so that neither the 16 bytes of 8 or more keys nor the 4 x 16 values of a transposed read meet
+// in a bank.
+constexpr int kPackTile = 64, kPackQueries = 32;
 
-template <int HD, typename T, int QT, int NBUF>
-__global__ __launch_bounds__(256, QT == 2 ? 2 : 3) void k_attention_packed(PackedArgs a)
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+template <typename T>
+__device__ __forceinline__ f32x16 mma32(typename Half<T>::x8 a, typename Half<T>::x8 b, f32x16 c)
+{
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef s16x4 __attribute__((address_space(3)))* lds_s16x4;
+// 16 lanes: 4 rows x 16 elements; lane i gives the place of elements 4 (i % 4) .. of row i / 4 and gets element i of the rows.
+__device__ __forceinline__ uint2 lds_read_transposed(const void* p)
+{
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)p));
+}
+
+template <int HD, typename T, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
 {
     typedef typename Half<T>::x8 t8;
-    typedef T t4 __attribute__((ext_vector_type(4)));
-    typedef T t2 __attribute__((ext_vector_type(2)));
-    constexpr int KT = kPackTile;
-    constexpr int KS = HD / 32, ET = HD / 16, OCT = HD / 8;
-    constexpr int KROW = HD + 8, VROW = KT + 8;
-    constexpr int PPT = KT * OCT / 256, NKG = KT / PPT;
-    __shared__ __attribute__((aligned(16))) T k_lds[NBUF][KT * KROW];
-    __shared__ __attribute__((aligned(16))) T v_lds[NBUF][HD * VROW];
-    __shared__ int odd_lds[NBUF];
-    const int h = blockIdx.x, i_seq = blockIdx.y, qt = gridDim.z - 1 - blockIdx.z;
+    constexpr int KT = kPackTile, QW = kPackQueries;
+    constexpr int ROW = HD * 2, PIECES = ROW / 16;      // bytes and 16-byte pieces of a row
+    constexpr int RPC = 64 / PIECES;                    // rows of a copy of 1 KiB
+    constexpr int COPIES = KT / RPC / NW;               // copies of a tile per wave
+    constexpr int KS = HD / 16, ET = HD / 32;
+    constexpr int TILE = KT * ROW;
+    static_assert(COPIES * RPC * NW == KT, "whole copies");
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][TILE];
+    __shared__ int odd_lds;
+
+    // query heads that share a head of keys and values are on one die
+    const int G = a.heads / a.n_kv, hk = blockIdx.x % a.n_kv, h = hk * G + blockIdx.x / a.n_kv;
+    const int i_seq = blockIdx.y, qt = gridDim.z - 1 - blockIdx.z;
     const int first = a.offsets[i_seq], end = a.offsets[i_seq + 1];
     if (first < 0 || end > a.q.rows) return;
     const int p = min(end - first, a.max_len);
-    const int q0 = qt * 64 * QT;
+    const int q0 = qt * QW * NW;
     if (q0 >= p) return;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int ql = lane & 15, g = lane >> 4;
-    const int hk = h / (a.heads / a.n_kv);
-    const T* Kg = (const T*)a.k.p + (int64_t)first * a.k.row + (int64_t)hk * a.k.head;
-    const T* Vg = (const T*)a.v.p + (int64_t)first * a.v.row + (int64_t)hk * a.v.head;
-    const int wave_first = q0 + wave * 16 * QT;
-    const int wave_last = wave_first < p ? min(wave_first + 16 * QT - 1, p - 1) : -1;
-    const int n_keys = min(p, q0 + 64 * QT);
-    const int n_tiles = (n_keys + KT - 1) / KT;
-    const float scale = a.scale * 1.44269504088896341f;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int ql = lane & 31, hi = lane >> 5;
+    const int wave_first = q0 + wave * QW, wave_last = wave_first < p ? min(wave_first + QW, p) - 1 : -1;   // -1: no query
+    const int n_keys = min(p, q0 + QW * NW), n_tiles = (n_keys + KT - 1) / KT;
+    const float sc = fmaxf(fabsf(a.scale) * 1.44269504088896341f, 1e-37f);   // of the scores, in units of log2
 
-    u32x4 kreg[PPT], vreg[PPT];
-    const u32x4 zero4 = {0u, 0u, 0u, 0u};
-    auto load_tile = [&](int t) {
+    const char* Kg = (const char*)((const T*)a.k.p + (int64_t)first * a.k.row + (int64_t)hk * a.k.head);
+    const char* Vg = (const char*)((const T*)a.v.p + (int64_t)first * a.v.row + (int64_t)hk * a.v.head);
+    const unsigned k_row = (unsigned)a.k.row * 2, v_row = (unsigned)a.v.row * 2;   // bytes; the host refuses longer rows
+    // copy c of a wave: rows (c * NW + wave) * RPC + lane / PIECES of the tile; the lane's piece depends on the row's last bits only
+    const int c_row = wave * RPC + lane / PIECES;
+    const unsigned k_piece = ((lane % PIECES) ^ (c_row % PIECES)) * 16, v_piece = ((lane % PIECES) ^ 2 * (c_row % (PIECES / 2))) * 16;
+    const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0]);
+    const unsigned k_off = c_row * k_row + k_piece, v_off = c_row * v_row + v_piece;
+    auto copy_tile = [&](int t, int b, bool whole) {
+        const char *kp = Kg + (int64_t)t * KT * k_row, *vp = Vg + (int64_t)t * KT * v_row;
+        const int left = n_keys - 1 - t * KT;   // last row of the tile that there is; later ones repeat it
 #pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-            const int c = tid + i * 256, key = t * KT + c / OCT;
-            const u32x4 kv = *(const u32x4*)(Kg + (int64_t)min(key, n_keys - 1) * a.k.row + c % OCT * 8);
-            kreg[i] = key < n_keys ? kv : zero4;
-        }
-#pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-            const int key = t * KT + (tid % NKG) * PPT + i;
-            const u32x4 vv = *(const u32x4*)(Vg + (int64_t)min(key, n_keys - 1) * a.v.row + tid / NKG * 8);
-            vreg[i] = key < n_keys ? vv : zero4;
-        }
-    };
-    auto stage_tile = [&](int b, int t) {
-#pragma unroll
-        for (int i = 0; i < PPT; ++i) {
-            const int c = tid + i * 256;
-            *(u32x4*)&k_lds[b][(c / OCT) * KROW + (c % OCT) * 8] = kreg[i];
-        }
-        T* vt = &v_lds[b][(tid / NKG) * 8 * VROW + vt_pos((tid % NKG) * PPT)];
-        t8 v[PPT];
-#pragma unroll
-        for (int i = 0; i < PPT; ++i) v[i] = __builtin_bit_cast(t8, vreg[i]);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            if constexpr (PPT == 4) {
-                const t4 o = {v[0][e], v[1][e], v[PPT - 2][e], v[PPT - 1][e]};
-                *(t4*)(vt + e * VROW) = o;
+        for (int c = 0; c < COPIES; ++c) {
+            const unsigned place = b * 2 * TILE + (c * NW + wave) * 1024;
+            if (whole) {
+                lds_copy_1k(lds_at, place, kp + c * NW * RPC * k_row, k_off);
+                lds_copy_1k(lds_at, place + TILE, vp + c * NW * RPC * v_row, v_off);
             } else {
-                const t2 o = {v[0][e], v[1][e]};
-                *(t2*)(vt + e * VROW) = o;
+                const unsigned r = min(c_row + c * NW * RPC, left);
+                lds_copy_1k(lds_at, place, kp, r * k_row + k_piece);
+                lds_copy_1k(lds_at, place + TILE, vp, r * v_row + v_piece);
             }
-        }
-        if (t * KT + KT - 1 > q0) {   // some query does not see all of the tile
-            constexpr uint32_t EXP = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < PPT; ++i)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) odd = odd || (vreg[i][w] & EXP) == EXP || (vreg[i][w] >> 16 & EXP) == EXP;
-            if (odd) odd_lds[b] = t + 1;
         }
     };
-    if (tid < NBUF) odd_lds[tid] = 0;
-    load_tile(0);
-    __syncthreads();
+    copy_tile(0, 0, false);
+    if (threadIdx.x == 0) odd_lds = 0;
 
-    t8 qf[QT][KS];
-    int qpos[QT];
+    t8 qf[KS];
+    const int qpos = min(wave_first + ql, p - 1);
+    {
+        const T* qp = (const T*)a.q.p + (int64_t)(first + qpos) * a.q.row + (int64_t)h * a.q.head + 8 * hi;
+        const uint32_t flip = a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-        qpos[u] = min(wave_first + u * 16 + ql, p - 1);
-        const T* qp = (const T*)a.q.p + (int64_t)(first + qpos[u]) * a.q.row + (int64_t)h * a.q.head + 8 * g;
+        for (int ks = 0; ks < KS; ++ks) {
+            u32x4 w = *(const u32x4*)(qp + 16 * ks);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) qf[u][ks] = *(const t8*)(qp + 32 * ks);
+            for (int i = 0; i < 4; ++i) w[i] ^= flip;
+            qf[ks] = __builtin_bit_cast(t8, w);
+        }
     }
-    f32x4 o[QT][ET];
-    float m_run[QT], l_run[QT];
+    f32x16 o[ET];
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
+    for (int t = 0; t < ET; ++t)
 #pragma unroll
-        for (int t = 0; t < ET; ++t) o[u][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
-        m_run[u] = kLowest;
-        l_run[u] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m_run = kLowest, l_run = 0.f;
 
-    auto use_tile = [&](int b, int k0, auto masked) {
+    // places of this lane's pieces: keys' rows are ql (+ 32), values' rows 4hi + (0..3) (+ 8 ...)
+    const unsigned k_at = ql * ROW + (hi ^ (ql % PIECES)) * 16;   // piece 2 * ks + hi: this with bits of ks turned over
+    const int v_r = 4 * hi + ((lane & 15) >> 2);
+    unsigned v_at[ET];
+#pragma unroll
+    for (int t = 0; t < ET; ++t)
+        v_at[t] = TILE + v_r * ROW + ((t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ 2 * (v_r % (PIECES / 2))) * 16 + (lane & 1) * 8;
+
+    auto use_tile = [&](auto buffer, int k0, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
-        f32x4 s[QT][4];
+        const char* tile = &lds[decltype(buffer)::value][0][0];
+        f32x16 s[2];
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) {
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int u = 0; u < QT; ++u) s[u][kt] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            if (MASKED && k0 + kt * 16 > wave_last) continue;
+            for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                const t8 kf = *(const t8*)&k_lds[b][(kt * 16 + ql) * KROW + ks * 32 + 8 * g];
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                for (int u = 0; u < QT; ++u) s[u][kt] = Half<T>::mma(kf, qf[u][ks], s[u][kt]);
+            for (int kt = 0; kt < 2; ++kt) {
+                if (MASKED && k0 + kt * 32 > wave_last) continue;
+                s[kt] = mma32<T>(*(const t8*)(tile + (k_at ^ ks * 32) + kt * 32 * ROW), qf[ks], s[kt]);
             }
-        }
-        t8 pb[QT][2];
+        float mt = kLowest;
 #pragma unroll
-        for (int u = 0; u < QT; ++u) {
-            float mt = kLowest;
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    s[u][kt][i] *= scale;
-                    if (MASKED && k0 + kt * 16 + 4 * g + i > qpos[u]) s[u][kt][i] = -__builtin_inff();
-                    mt = fmaxf(mt, s[u][kt][i]);
-                }
-            mt = across<32>(across<16>(mt, Max()), Max());
-            if (__any(mt > m_run[u])) {
-                const float m_new = fmaxf(m_run[u], mt);
-                const float alpha = __builtin_amdgcn_exp2f(m_run[u] - m_new);
-                m_run[u] = m_new;
-                l_run[u] *= alpha;
-#pragma unroll
-                for (int tt = 0; tt < ET; ++tt) o[u][tt] *= alpha;
+            for (int i = 0; i < 16; ++i) {
+                if (MASKED && k0 + kt * 32 + 8 * (i >> 2) + 4 * hi + (i & 3) > qpos) s[kt][i] = -__builtin_inff();
+                mt = fmaxf(mt, s[kt][i]);
             }
+        mt = across<32>(mt, Max());
+        // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1
+        if (__any((mt - m_run) * sc > 8.f)) {
+            const float m_new = fmaxf(m_run, mt), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
+            m_run = m_new;
+            l_run *= alpha;
 #pragma unroll
-            for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float pv = __builtin_amdgcn_exp2f(s[u][kt][i] - m_run[u]);
-                    l_run[u] += pv;
-                    pb[u][kt >> 1][(kt & 1) * 4 + i] = (T)pv;
-                }
+            for (int t = 0; t < ET; ++t) o[t] *= alpha;
         }
-        if (MASKED && odd_lds[b] == k0 / KT + 1) {   // an infinite or NaN value: slot by slot, so that only those who see it meet it
+        const float m_sc = fmaxf(m_run * sc, kLowest);   // its rounding is a factor common to all of a query's keys
+        t8 pb[4];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float pv = __builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, -m_sc));
+                l_run += pv;
+                pb[kt * 2 + (i >> 3)][i & 7] = (T)pv;
+            }
+        if (MASKED && odd_lds == k0 + 1) {   // an infinite or NaN value: key by key, so that only those who see it meet it
             for (int n = 0; n < KT; ++n) {
-                const int from = ql + 16 * ((n & 15) >> 2);
+                float w = 0.f;
 #pragma unroll
-                for (int u = 0; u < QT; ++u) {
-                    float w = 0.f;
+                for (int i = 0; i < 32; ++i)
+                    if (i == (n >> 5) * 16 + ((n & 31) >> 3) * 4 + (n & 3)) w = __shfl((float)pb[i >> 3][i & 7], ql + 32 * ((n >> 2) & 1));
+                if (w == 0.f || k0 + n > qpos) continue;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (i == (n >> 4) * 4 + (n & 3)) w = __shfl((float)pb[u][i >> 3][i & 7], from);
-                    if (w == 0.f || k0 + n > qpos[u]) continue;
+                for (int t = 0; t < ET; ++t)
 #pragma unroll
-                    for (int tt = 0; tt < ET; ++tt)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            o[u][tt][i] = fmaf(w, (float)v_lds[b][(tt * 16 + 4 * g + i) * VROW + vt_pos(n)], o[u][tt][i]);
-                }
+                    for (int i = 0; i < 16; ++i) {
+                        const int e = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3), piece = (e >> 3) ^ 2 * (n % (PIECES / 2));
+                        o[t][i] = fmaf(w, (float)*(const T*)(tile + TILE + n * ROW + piece * 16 + (e & 7) * 2), o[t][i]);
+                    }
             }
             return;
         }
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            if (MASKED && k0 + c * 32 > wave_last) continue;
+        for (int c = 0; c < 4; ++c) {
+            if (MASKED && k0 + c * 16 > wave_last) continue;
 #pragma unroll
-            for (int tt = 0; tt < ET; ++tt) {
-                const t8 vf = *(const t8*)&v_lds[b][(tt * 16 + ql) * VROW + c * 32 + 8 * g];
-#pragma unroll
-                for (int u = 0; u < QT; ++u) o[u][tt] = Half<T>::mma(vf, pb[u][c], o[u][tt]);
+            for (int t = 0; t < ET; ++t) {
+                const uint2 lo = lds_read_transposed(tile + v_at[t] + c * 16 * ROW), up = lds_read_transposed(tile + v_at[t] + (c * 16 + 8) * ROW);
+                o[t] = mma32<T>(__builtin_bit_cast(t8, u32x4{lo.x, lo.y, up.x, up.y}), pb[c], o[t]);
             }
         }
     };
-    stage_tile(0, 0);
-    for (int t = 0; t < n_tiles; ++t) {
-        const int b = NBUF == 2 ? t & 1 : 0;
-        __syncthreads();
-        if (t + 1 < n_tiles) load_tile(t + 1);
-        const int k0 = t * KT;
-        if (k0 <= wave_last) {
-            if (k0 + KT - 1 <= wave_first) use_tile(b, k0, std::false_type{});
-            else use_tile(b, k0, std::true_type{});
-        }
-        if (NBUF == 1) __syncthreads();
-        if (t + 1 < n_tiles) stage_tile(NBUF == 2 ? b ^ 1 : 0, t + 1);
+    const std::integral_constant<int, 0> even{};
+    const std::integral_constant<int, 1> odd{};
+    // tiles that every query of the workgroup sees whole, an even number of them
+    const int n_whole = q0 / KT;
+    for (int t = 0; t < n_whole; t += 2) {
+        wait_copies_and_meet<0>();   // this tile is there, and nobody reads the other one any more
+        copy_tile(t + 1, 1, true);
+        use_tile(even, t * KT, std::false_type{});
+        wait_copies_and_meet<0>();
+        copy_tile(t + 2, 0, t + 2 < n_whole);
+        use_tile(odd, t * KT + KT, std::false_type{});
     }
+    // tiles up to the workgroup's own queries
+    auto last_tile = [&](int t, auto buffer) {
+        wait_copies_and_meet<0>();
+        if (t + 1 < n_tiles) copy_tile(t + 1, (t + 1) & 1, false);
+        constexpr uint32_t EXP = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
+        bool found = false;
 #pragma unroll
-    for (int u = 0; u < QT; ++u) {
-        float l = l_run[u];
-        l = across<32>(across<16>(l, Add()), Add());
-        if (wave_first + u * 16 + ql >= p) continue;
-        const float inv = 1.f / l;
+        for (int i = 0; i < TILE / 16 / (64 * NW); ++i) {
+            const u32x4 w = *(const u32x4*)(&lds[decltype(buffer)::value][1][0] + (i * 64 * NW + threadIdx.x) * 16);
 #pragma unroll
-        for (int tt = 0; tt < ET; ++tt) {
-            t4 r;
+            for (int j = 0; j < 4; ++j) found = found || (w[j] & EXP) == EXP || (w[j] >> 16 & EXP) == EXP;
+        }
+        if (found) odd_lds = t * KT + 1;
+        __syncthreads();
+        if (t * KT <= wave_last) use_tile(buffer, t * KT, std::true_type{});
+    };
+    for (int t = n_whole; t < n_tiles; t += 2) {
+        last_tile(t, even);
+        if (t + 1 < n_tiles) last_tile(t + 1, odd);
+    }
+    const float l = across<32>(l_run, Add());
+    if (wave_first + ql >= p) return;
+    const float inv = 1.f / l;
+#pragma unroll
+    for (int t = 0; t < ET; ++t)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            T r[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float x = o[u][tt][e] * inv;
+                const float x = o[t][4 * b + e] * inv;
                 if constexpr (std::is_same<T, _Float16>::value) r[e] = __builtin_bit_cast(_Float16, f2h(x));
                 else r[e] = (T)x;
             }
-            T* to = a.packed_d ? (T*)a.out.p + pk_index(first + qpos[u], h * HD + tt * 16 + 4 * g, a.packed_d)
-                               : (T*)a.out.p + (int64_t)(first + qpos[u]) * a.out.row + (int64_t)h * a.out.head + tt * 16 + 4 * g;
-            *(t4*)to = r;
+            const int e0 = 32 * t + 8 * b + 4 * hi;
+            T* to = a.packed_d ? (T*)a.out.p + pk_index(first + qpos, h * HD + e0, a.packed_d)
+                               : (T*)a.out.p + (int64_t)(first + qpos) * a.out.row + (int64_t)h * a.out.head + e0;
+            *(uint2*)to = __builtin_bit_cast(uint2, r);
         }
-    }
 }
 
 // ------------------------------------------------------------------------------------------ launches
@@ -932,8 +948,8 @@ void launch_attention_tree(const TreeArgs& a, int token, int tiles, hipStream_t 
 template <int HD, typename T>
 static void attention_packed(const PackedArgs& a, int n_seq, hipStream_t s)
 {
-    if (a.max_len >= 256) k_attention_packed<HD, T, 2, 2><<<dim3(a.heads, n_seq, (a.max_len + 127) / 128), 256, 0, s>>>(a);
-    else k_attention_packed<HD, T, 1, 1><<<dim3(a.heads, n_seq, (a.max_len + 63) / 64), 256, 0, s>>>(a);
+    constexpr int NW = 4, QUERIES = kPackQueries * NW;
+    k_attention_packed<HD, T, NW><<<dim3(a.heads, n_seq, (a.max_len + QUERIES - 1) / QUERIES), 64 * NW, 0, s>>>(a);
 }
 
 void launch_attention_packed(const PackedArgs& a, int hd, int token, int n_seq, hipStream_t s)

@@ -122,6 +122,31 @@ __device__ __forceinline__ float group_sum(float v)
 // Place of a slot of a tile of 64 in its staged V^T rows: a lane's 8 slots of two 16-slot score tiles are neighbours.
 __device__ __forceinline__ int vt_pos(int k) { return (k & 32) + ((k >> 2) & 3) * 8 + ((k >> 4) & 1) * 4 + (k & 3); }
 
+// 16 bytes per lane straight into LDS: the wave's 64 pieces land behind each other at slot + place, from base + lane_off.
+// The copies are written in assembly because the compiler would wait for all of them before every LDS read: it counts
+// only its own loads, and the waits here are written out.  They name no output register; waits that the compiler adds
+// for loads of its own can only be too strict.
+__device__ __forceinline__ void lds_copy_1k(unsigned slot, unsigned place, const void* base, unsigned lane_off)
+{
+    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(slot), "s"(place), "v"(lane_off), "s"(base)
+                 : "memory", "scc");
+}
+
+// At most N copies of this wave are still on their way, its LDS reads are done, and then so are every other wave's.  The
+// builtin tells the compiler that the operands read before are in their registers (after a wait in assembly it would wait
+// for each of them once more).
+template <int N>
+__device__ __forceinline__ void wait_copies_and_meet()
+{
+    static_assert(N < 64, "the counter has 6 bits");
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));   // vmcnt(N) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+}
+
 }  // namespace ss
 
 #endif

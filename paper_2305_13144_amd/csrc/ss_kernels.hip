@@ -879,30 +879,6 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_gemm_few(FewArgs a)
 // 1692 us instead of 1748 (1.31 PFLOP/s; launched alone, 1603).  Measured against the kernel it replaced (weights straight
 // from L2 to registers, 64 or 128 rows per tile) before that, gate|up: 256 rows 73.7 -> 56.3 us, 494 123 -> 81, 995 216 ->
 // 166, 3146 544 -> 488, 12311 1989 -> 1743; down 494 67 -> 49, 995 98 -> 87, 4200 504 -> 351.
-// The copies are written in assembly because the compiler would wait for all of them before every LDS read: it counts
-// only its own loads, and the waits here are written out.  They name no output register; waits that the compiler adds
-// for loads of its own can only be too strict.
-__device__ __forceinline__ void lds_copy_1k(unsigned slot, unsigned place, const void* base, unsigned lane_off)
-{
-    asm volatile("s_add_u32 m0, %0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3" ::"s"(slot), "s"(place), "v"(lane_off), "s"(base)
-                 : "memory", "scc");
-}
-
-// At most N copies of this wave are still on their way, its LDS reads are done, and then so are every other wave's.  The
-// builtin tells the compiler that the operands read before are in their registers (after a wait in assembly it would wait
-// for each of them once more).
-template <int N>
-__device__ __forceinline__ void wait_copies_and_meet()
-{
-    static_assert(N < 64, "the counter has 6 bits");
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));   // vmcnt(N) lgkmcnt(0)
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-}
-
 // Unsliced launches finish their results themselves.  EPI_RESIDUAL adds the sums to the residual stream in place, EPI_QKV
 // rotates q and k and puts q, k and v where the attention reads them, instead of writing fp32 sums for the next launch to
 // read.  12311 token-rows, 7B, per layer: the rotation launch (184 us) is gone, the norms take 108 us instead of 167, o
