@@ -655,11 +655,20 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 //   weights  lane (query = lane % 32, hi = lane / 32) holds keys 8b + 4hi + (0..3), b = 0..3, of a block; two b's are an operand
 //   values   the same keys of element lane % 32: four neighbouring keys of one element, what the transposed LDS read returns
 // Keys and values are copied into LDS as they lie in memory (two tiles, one on its way while the other is used), pieces of 16 bytes
-// changing places within a row so that neither the 16 bytes of 8 or more keys nor the 4 x 16 values of a transposed read meet
-// in a bank.
+// changing places within a row so that what is read at once lies in different banks.
 constexpr int kPackTile = 64, kPackQueries = 32;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+// sum + a's two values, in fp32.
+template <typename T>
+__device__ __forceinline__ float add_pair(uint32_t a, float sum)
+{
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    const t2 one = {(T)1.f, (T)1.f};
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_amdgcn_fdot2(__builtin_bit_cast(t2, a), one, sum, false);
+    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(t2, a), one, sum, false);
+}
+
 template <typename T>
 __device__ __forceinline__ f32x16 mma32(typename Half<T>::x8 a, typename Half<T>::x8 b, f32x16 c)
 {
@@ -706,9 +715,13 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     const char* Kg = (const char*)((const T*)a.k.p + (int64_t)first * a.k.row + (int64_t)hk * a.k.head);
     const char* Vg = (const char*)((const T*)a.v.p + (int64_t)first * a.v.row + (int64_t)hk * a.v.head);
     const unsigned k_row = (unsigned)a.k.row * 2, v_row = (unsigned)a.v.row * 2;   // bytes; the host refuses longer rows
+    // In 256 bytes, the banks' width, lie the 16-byte pieces of 16 keys' rows that 16 lanes read at once, and the 32 bytes of 4 rows at
+    // two places that 32 lanes read transposed.
+    auto key_turn = [](int r) { return HD == 128 ? r & 15 : r >> 1 & 7; };
+    auto value_turn = [](int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; };
     // copy c of a wave: rows (c * NW + wave) * RPC + lane / PIECES of the tile; the lane's piece depends on the row's last bits only
     const int c_row = wave * RPC + lane / PIECES;
-    const unsigned k_piece = ((lane % PIECES) ^ (c_row % PIECES)) * 16, v_piece = ((lane % PIECES) ^ 2 * (c_row % (PIECES / 2))) * 16;
+    const unsigned k_piece = ((lane % PIECES) ^ key_turn(c_row)) * 16, v_piece = ((lane % PIECES) ^ value_turn(c_row)) * 16;
     const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0]);
     const unsigned k_off = c_row * k_row + k_piece, v_off = c_row * v_row + v_piece;
     auto copy_tile = [&](int t, int b, bool whole) {
@@ -751,12 +764,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     float m_run = kLowest, l_run = 0.f;
 
     // places of this lane's pieces: keys' rows are ql (+ 32), values' rows 4hi + (0..3) (+ 8 ...)
-    const unsigned k_at = ql * ROW + (hi ^ (ql % PIECES)) * 16;   // piece 2 * ks + hi: this with bits of ks turned over
+    const unsigned k_at = ql * ROW + (hi ^ key_turn(ql)) * 16;   // piece 2 * ks + hi: this with bits of ks turned over
     const int v_r = 4 * hi + ((lane & 15) >> 2);
     unsigned v_at[ET];
 #pragma unroll
     for (int t = 0; t < ET; ++t)
-        v_at[t] = TILE + v_r * ROW + ((t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ 2 * (v_r % (PIECES / 2))) * 16 + (lane & 1) * 8;
+        v_at[t] = TILE + v_r * ROW + ((t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ value_turn(v_r)) * 16 + (lane & 1) * 8;
 
     auto use_tile = [&](auto buffer, int k0, auto masked) {
         constexpr bool MASKED = decltype(masked)::value;
@@ -796,10 +809,12 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const float pv = __builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, -m_sc));
-                l_run += pv;
-                pb[kt * 2 + (i >> 3)][i & 7] = (T)pv;
+                pb[kt * 2 + (i >> 3)][i & 7] = (T)__builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, -m_sc));
             }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l_run = add_pair<T>(__builtin_bit_cast(u32x4, pb[c])[i], l_run);
         if (MASKED && odd_lds == k0 + 1) {   // an infinite or NaN value: key by key, so that only those who see it meet it
             for (int n = 0; n < KT; ++n) {
                 float w = 0.f;
@@ -811,7 +826,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
                 for (int t = 0; t < ET; ++t)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        const int e = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3), piece = (e >> 3) ^ 2 * (n % (PIECES / 2));
+                        const int e = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3), piece = (e >> 3) ^ value_turn(n);
                         o[t][i] = fmaf(w, (float)*(const T*)(tile + TILE + n * ROW + piece * 16 + (e & 7) * 2), o[t][i]);
                     }
             }
