@@ -741,6 +741,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
         }
     };
     copy_tile(0, 0, false);
+    if (n_tiles > 1) copy_tile(1, 1, false);
     if (threadIdx.x == 0) odd_lds = 0;
 
     t8 qf[KS];
@@ -848,7 +849,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     const int n_whole = q0 / KT;
     for (int t = 0; t < n_whole; t += 2) {
         wait_copies_and_meet<0>();   // this tile is there, and nobody reads the other one any more
-        copy_tile(t + 1, 1, true);
+        if (t) copy_tile(t + 1, 1, true);
         use_tile(even, t * KT, std::false_type{});
         wait_copies_and_meet<0>();
         copy_tile(t + 2, 0, t + 2 < n_whole);
@@ -857,7 +858,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     // tiles up to the workgroup's own queries
     auto last_tile = [&](int t, auto buffer) {
         wait_copies_and_meet<0>();
-        if (t + 1 < n_tiles) copy_tile(t + 1, (t + 1) & 1, false);
+        if (t && t + 1 < n_tiles) copy_tile(t + 1, (t + 1) & 1, false);
         constexpr uint32_t EXP = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
         bool found = false;
 #pragma unroll
@@ -874,9 +875,10 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
         last_tile(t, even);
         if (t + 1 < n_tiles) last_tile(t + 1, odd);
     }
-    const float l = across<32>(l_run, Add());
-    if (wave_first + ql >= p) return;
-    const float inv = 1.f / l;
+    // results go through LDS, so that 16 (8) lanes write a head's 256 (128) bytes: a wave has 32 rows of its own there
+    const float l = across<32>(l_run, Add()), inv = 1.f / l;
+    wait_copies_and_meet<0>();
+    char* rows = &lds[0][0][0] + wave * QW * ROW;
 #pragma unroll
     for (int t = 0; t < ET; ++t)
 #pragma unroll
@@ -888,11 +890,19 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
                 if constexpr (std::is_same<T, _Float16>::value) r[e] = __builtin_bit_cast(_Float16, f2h(x));
                 else r[e] = (T)x;
             }
-            const int e0 = 32 * t + 8 * b + 4 * hi;
-            T* to = a.packed_d ? (T*)a.out.p + pk_index(first + qpos, h * HD + e0, a.packed_d)
-                               : (T*)a.out.p + (int64_t)(first + qpos) * a.out.row + (int64_t)h * a.out.head + e0;
-            *(uint2*)to = __builtin_bit_cast(uint2, r);
+            *(uint2*)(rows + ql * ROW + (((4 * t + b) ^ key_turn(ql)) * 16 + (hi ^ (ql >> 4)) * 8)) = __builtin_bit_cast(uint2, r);
         }
+#pragma unroll
+    for (int i = 0; i < QW / RPC; ++i) {
+        const int r = i * RPC + lane / PIECES, piece = (lane % PIECES) ^ key_turn(r);
+        u32x4 w = *(const u32x4*)(rows + r * ROW + (lane % PIECES) * 16);
+        if (r >> 4) w = u32x4{w[2], w[3], w[0], w[1]};
+        if (wave_first + r >= p) continue;
+        const int row = first + wave_first + r;
+        T* to = a.packed_d ? (T*)a.out.p + pk_index(row, h * HD + piece * 8, a.packed_d)
+                           : (T*)a.out.p + (int64_t)row * a.out.row + (int64_t)h * a.out.head + piece * 8;
+        *(u32x4*)to = w;
+    }
 }
 
 // ------------------------------------------------------------------------------------------ launches
