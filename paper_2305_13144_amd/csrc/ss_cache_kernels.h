@@ -772,27 +772,26 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     for (int t = 0; t < ET; ++t)
         v_at[t] = TILE + v_r * ROW + ((t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ value_turn(v_r)) * 16 + (lane & 1) * 8;
 
-    auto use_tile = [&](auto buffer, int k0, auto masked) {
-        constexpr bool MASKED = decltype(masked)::value;
-        const char* tile = &lds[decltype(buffer)::value][0][0];
-        f32x16 s[2];
+    // BLOCKS of 32 keys of the tile; DIAGONAL: the last of them is the wave's own, whose key n only queries from n on see
+    auto use_tile = [&](auto buffer, int k0, auto blocks, auto diagonal) {
+        constexpr int NB = decltype(blocks)::value;
+        constexpr bool DIAGONAL = decltype(diagonal)::value;
+        const char* tile = &lds[buffer][0][0];
+        f32x16 s[NB];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < NB; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                if (MASKED && k0 + kt * 32 > wave_last) continue;
-                s[kt] = mma32<T>(*(const t8*)(tile + (k_at ^ ks * 32) + kt * 32 * ROW), qf[ks], s[kt]);
-            }
+            for (int kt = 0; kt < NB; ++kt) s[kt] = mma32<T>(*(const t8*)(tile + (k_at ^ ks * 32) + kt * 32 * ROW), qf[ks], s[kt]);
         float mt = kLowest;
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < NB; ++kt)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                if (MASKED && k0 + kt * 32 + 8 * (i >> 2) + 4 * hi + (i & 3) > qpos) s[kt][i] = -__builtin_inff();
+                if (DIAGONAL && kt == NB - 1 && 8 * (i >> 2) + (i & 3) > ql - 4 * hi) s[kt][i] = -__builtin_inff();
                 mt = fmaxf(mt, s[kt][i]);
             }
         mt = across<32>(mt, Max());
@@ -805,75 +804,65 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
             for (int t = 0; t < ET; ++t) o[t] *= alpha;
         }
         const float m_sc = fmaxf(m_run * sc, kLowest);   // its rounding is a factor common to all of a query's keys
-        t8 pb[4];
+        t8 pb[2 * NB];
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
+        for (int kt = 0; kt < NB; ++kt)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                pb[kt * 2 + (i >> 3)][i & 7] = (T)__builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, -m_sc));
-            }
+            for (int i = 0; i < 16; ++i) pb[kt * 2 + (i >> 3)][i & 7] = (T)__builtin_amdgcn_exp2f(fmaf(s[kt][i], sc, -m_sc));
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+        for (int c = 0; c < 2 * NB; ++c)
 #pragma unroll
             for (int i = 0; i < 4; ++i) l_run = add_pair<T>(__builtin_bit_cast(u32x4, pb[c])[i], l_run);
-        if (MASKED && odd_lds == k0 + 1) {   // an infinite or NaN value: key by key, so that only those who see it meet it
-            for (int n = 0; n < KT; ++n) {
-                float w = 0.f;
 #pragma unroll
-                for (int i = 0; i < 32; ++i)
-                    if (i == (n >> 5) * 16 + ((n & 31) >> 3) * 4 + (n & 3)) w = __shfl((float)pb[i >> 3][i & 7], ql + 32 * ((n >> 2) & 1));
-                if (w == 0.f || k0 + n > qpos) continue;
-#pragma unroll
-                for (int t = 0; t < ET; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int e = 32 * t + 8 * (i >> 2) + 4 * hi + (i & 3), piece = (e >> 3) ^ value_turn(n);
-                        o[t][i] = fmaf(w, (float)*(const T*)(tile + TILE + n * ROW + piece * 16 + (e & 7) * 2), o[t][i]);
-                    }
-            }
-            return;
-        }
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            if (MASKED && k0 + c * 16 > wave_last) continue;
+        for (int c = 0; c < 2 * NB; ++c)
 #pragma unroll
             for (int t = 0; t < ET; ++t) {
                 const uint2 lo = lds_read_transposed(tile + v_at[t] + c * 16 * ROW), up = lds_read_transposed(tile + v_at[t] + (c * 16 + 8) * ROW);
                 o[t] = mma32<T>(__builtin_bit_cast(t8, u32x4{lo.x, lo.y, up.x, up.y}), pb[c], o[t]);
             }
-        }
     };
     const std::integral_constant<int, 0> even{};
-    const std::integral_constant<int, 1> odd{};
+    const std::integral_constant<int, 1> odd{}, one{};
+    const std::integral_constant<int, 2> two{};
     // tiles that every query of the workgroup sees whole, an even number of them
     const int n_whole = q0 / KT;
     for (int t = 0; t < n_whole; t += 2) {
         wait_copies_and_meet<0>();   // this tile is there, and nobody reads the other one any more
         if (t) copy_tile(t + 1, 1, true);
-        use_tile(even, t * KT, std::false_type{});
+        use_tile(even, t * KT, two, std::false_type{});
         wait_copies_and_meet<0>();
         copy_tile(t + 2, 0, t + 2 < n_whole);
-        use_tile(odd, t * KT + KT, std::false_type{});
+        use_tile(odd, t * KT + KT, two, std::false_type{});
     }
     // tiles up to the workgroup's own queries
-    auto last_tile = [&](int t, auto buffer) {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    constexpr unsigned short kInf = std::is_same<T, _Float16>::value ? 0x7c00 : 0x7f80;
+    for (int t = n_whole; t < n_tiles; ++t) {
+        const int k0 = t * KT, buffer = t & 1;
         wait_copies_and_meet<0>();
         if (t && t + 1 < n_tiles) copy_tile(t + 1, (t + 1) & 1, false);
-        constexpr uint32_t EXP = std::is_same<T, _Float16>::value ? 0x7c00u : 0x7f80u;
-        bool found = false;
+        // infinite and NaN values count as 0 here, so that queries before them do not meet them as 0 * x: see below
+        u16x2 top = {0, 0};
+        u32x4 w[TILE / 16 / (64 * NW)];
+        char* values = &lds[buffer][1][0] + threadIdx.x * 16;
 #pragma unroll
         for (int i = 0; i < TILE / 16 / (64 * NW); ++i) {
-            const u32x4 w = *(const u32x4*)(&lds[decltype(buffer)::value][1][0] + (i * 64 * NW + threadIdx.x) * 16);
+            w[i] = *(const u32x4*)(values + i * 1024 * NW);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) found = found || (w[j] & EXP) == EXP || (w[j] >> 16 & EXP) == EXP;
+            for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[i][j] & 0x7fff7fffu));
         }
-        if (found) odd_lds = t * KT + 1;
+        if (top[0] >= kInf || top[1] >= kInf) {
+            for (int i = 0; i < TILE / 16 / (64 * NW) * 8; ++i) {
+                uint16_t* x = (uint16_t*)(values + (i >> 3) * 1024 * NW) + (i & 7);
+                if ((*x & 0x7fff) >= kInf) *x = 0;
+            }
+            odd_lds = 1;
+        }
         __syncthreads();
-        if (t * KT <= wave_last) use_tile(buffer, t * KT, std::true_type{});
-    };
-    for (int t = n_whole; t < n_tiles; t += 2) {
-        last_tile(t, even);
-        if (t + 1 < n_tiles) last_tile(t + 1, odd);
+        if (k0 > wave_last) continue;
+        if (k0 + KT <= wave_first) use_tile(buffer, k0, two, std::false_type{});
+        else if (k0 < wave_first) use_tile(buffer, k0, two, std::true_type{});
+        else use_tile(buffer, k0, one, std::true_type{});
     }
     // results go through LDS, so that 16 (8) lanes write a head's 256 (128) bytes: a wave has 32 rows of its own there
     const float l = across<32>(l_run, Add()), inv = 1.f / l;
@@ -892,6 +881,17 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
             }
             *(uint2*)(rows + ql * ROW + (((4 * t + b) ^ key_turn(ql)) * 16 + (hi ^ (ql >> 4)) * 8)) = __builtin_bit_cast(uint2, r);
         }
+    if (odd_lds) {   // rare: the values that counted as 0, to the queries that see them (a positive weight times infinity or NaN)
+        for (int n = q0; n <= wave_last; ++n)
+            for (int e = lane; e < HD; e += 64) {
+                const float x = (float)((const T*)(Vg + (int64_t)n * v_row))[e];
+                if (fabsf(x) <= 3.4e38f) continue;
+                for (int r = max(n - wave_first, 0); r < QW; ++r) {
+                    T* to = (T*)(rows + r * ROW + (((e >> 3) ^ key_turn(r)) * 16 + ((e >> 2 & 1) ^ (r >> 4)) * 8)) + (e & 3);
+                    *to = (T)((float)*to + x);
+                }
+            }
+    }
 #pragma unroll
     for (int i = 0; i < QW / RPC; ++i) {
         const int r = i * RPC + lane / PIECES, piece = (lane % PIECES) ^ key_turn(r);
