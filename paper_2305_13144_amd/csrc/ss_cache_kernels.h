@@ -231,7 +231,6 @@ struct MathType { typedef T type; };           // 16-bit cache: its own type
 template <typename T>
 struct MathType<int8_t, T> { typedef _Float16 type; };
 
-typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(4)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
 // First row and number of rows (nodes) of the j-th sequence of a call; none where the table leaves the rows that there are.
@@ -268,73 +267,28 @@ __device__ __forceinline__ uint32_t code_pair(uint32_t a, uint32_t b, uint32_t s
     return __builtin_bit_cast(uint32_t, h);
 }
 
-// A step's operands as they come from memory.
-template <int HD, typename C>
-struct TreeStep {
-    static constexpr bool I8 = std::is_same<C, int8_t>::value;
-    static constexpr int KL = I8 ? HD / 64 : HD / 32;   // 16-byte loads per key tile and lane
-    static constexpr int VW = I8 ? HD / 64 : HD / 32;   // words per slot and lane: ET elements
-    u32x4 k[2][KL];
-    uint32_t v[8][VW];
-    f32x4u ks[2], vs[2];
-};
-
-template <int HD, typename C>
-__device__ __forceinline__ void tree_load(TreeStep<HD, C>& st, const C* __restrict__ K, const C* __restrict__ V,
-                                          const float* __restrict__ kscale, const float* __restrict__ vscale, int base, int last,
-                                          int ql, int g)
+// sum + a's two values, in fp32.
+template <typename T>
+__device__ __forceinline__ float add_pair(uint32_t a, float sum)
 {
-    constexpr bool I8 = TreeStep<HD, C>::I8;
-    constexpr int ET = HD / 16, VW = TreeStep<HD, C>::VW;
-    const bool inside = base + 31 <= last;   // uniform
-#pragma unroll
-    for (int kt = 0; kt < 2; ++kt) {
-        const int s = min(base + kt * 16 + ql, last);
-        const C* p = K + (size_t)s * HD;
-#pragma unroll
-        for (int i = 0; i < TreeStep<HD, C>::KL; ++i)
-            st.k[kt][i] = *(const u32x4*)(I8 ? p + 64 * i + 16 * g : p + 32 * i + 8 * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int sv = min(base + kt * 16 + 4 * g + i, last);
-            const uint32_t* q = (const uint32_t*)(V + (size_t)sv * HD + ET * ql);
-            if constexpr (VW == 4) {
-                const u32x4 w = *(const u32x4*)q;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) st.v[kt * 4 + i][j] = w[j];
-            } else if constexpr (VW == 2) {
-                const uint2 w = *(const uint2*)q;
-                st.v[kt * 4 + i][0] = w.x;
-                st.v[kt * 4 + i][1] = w.y;
-            } else {
-                st.v[kt * 4 + i][0] = *q;
-            }
-        }
-        if constexpr (I8) {
-            const int s4 = base + kt * 16 + 4 * g;
-            if (inside) {
-                st.ks[kt] = *(const f32x4u*)(kscale + s4);
-                st.vs[kt] = *(const f32x4u*)(vscale + s4);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    st.ks[kt][i] = kscale[min(s4 + i, last)];
-                    st.vs[kt][i] = vscale[min(s4 + i, last)];
-                }
-            }
-        }
-    }
+    typedef T t2 __attribute__((ext_vector_type(2)));
+    const t2 one = {(T)1.f, (T)1.f};
+    if constexpr (std::is_same<T, _Float16>::value) return __builtin_amdgcn_fdot2(__builtin_bit_cast(t2, a), one, sum, false);
+    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(t2, a), one, sum, false);
 }
 
 template <int HD, typename T, typename C, int QT>
-__global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
+__global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArgs a)
 {
     typedef typename MathType<C, T>::type M;
     typedef typename Half<M>::x8 m8;
-    typedef TreeStep<HD, C> Step;
-    constexpr bool I8 = Step::I8;
+    constexpr bool I8 = std::is_same<C, int8_t>::value;
     constexpr int KS = HD / 32, ET = HD / 16, NW = 4, ROWS = 16 * QT;
+    constexpr int ROW = HD * sizeof(C);      // bytes of a vector
+    constexpr int KL = ROW / 64;             // 16-byte loads per 16 slots and lane
+    constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+    __shared__ int s_odd;
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
     const CacheView& c = a.c;
 
@@ -358,48 +312,120 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
     const int n_chunks = tree_chunks(len, a.chunk, a.chunks);
     if (chunk >= n_chunks) return;
     const int s_begin = chunk * a.chunk, s_end = chunk + 1 == n_chunks ? len : s_begin + a.chunk, last = len - 1;
+    const int shared_end = min(ctx, len);   // slots before this are seen by every row
 
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, ql = lane & 15, g = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ql = lane & 15, g = lane >> 4;
     const int64_t head_base = base + (int64_t)h * slots;
-    const C* K = (const C*)c.k + head_base * HD;
-    const C* V = (const C*)c.v + head_base * HD;
+    const char *K = (const char*)c.k + head_base * ROW, *V = (const char*)c.v + head_base * ROW;
     const float *kscale = I8 ? c.k_scale + head_base : nullptr, *vscale = I8 ? c.v_scale + head_base : nullptr;
     const int first = s_begin + 32 * wave;
-    Step now, next;
-    if (first < s_end) tree_load<HD, C>(now, K, V, kscale, vscale, first, last, ql, g);
+    if (threadIdx.x == 0) s_odd = 0;
 
+    // A step's operands as they come from memory; those of the next step are requested as soon as the registers are free.
+    u32x4 kreg[2][KL];
+    uint32_t vreg[8][VW];
+    f32x4u ks[2], vs[2];
+    const unsigned k_off = ql * ROW + 16 * g, v_off = 4 * g * ROW + ET * ql * (int)sizeof(C);
+    auto load_v = [](uint32_t (&v)[VW], const char* p) {
+        if constexpr (VW == 4) {
+            const u32x4 w = *(const u32x4*)p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = w[i];
+        } else if constexpr (VW == 2) {
+            const uint2 w = *(const uint2*)p;
+            v[0] = w.x;
+            v[1] = w.y;
+        } else {
+            v[0] = *(const uint32_t*)p;
+        }
+    };
+    auto load_keys = [&](int s0) {
+        if (s0 + 31 <= last) {
+            const char* p = K + (int64_t)s0 * ROW;
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < KL; ++i) kreg[kt][i] = *(const u32x4*)(p + k_off + kt * 16 * ROW + 64 * i);
+            if constexpr (I8)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) ks[kt] = *(const f32x4u*)(kscale + s0 + 4 * g + kt * 16);
+        } else {   // slots beyond the last repeat it
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const char* p = K + (int64_t)min(s0 + kt * 16 + ql, last) * ROW + 16 * g;
+#pragma unroll
+                for (int i = 0; i < KL; ++i) kreg[kt][i] = *(const u32x4*)(p + 64 * i);
+                if constexpr (I8)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) ks[kt][i] = kscale[min(s0 + kt * 16 + 4 * g + i, last)];
+            }
+        }
+    };
+    auto load_values = [&](int s0) {
+        if (s0 + 31 <= last) {
+            const char* p = V + (int64_t)s0 * ROW;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) load_v(vreg[i], p + v_off + ((i >> 2) * 16 + (i & 3)) * ROW);
+            if constexpr (I8)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) vs[kt] = *(const f32x4u*)(vscale + s0 + 4 * g + kt * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int s = min(s0 + (i >> 2) * 16 + 4 * g + (i & 3), last);
+                load_v(vreg[i], V + (int64_t)s * ROW + ET * ql * (int)sizeof(C));
+                if constexpr (I8) vs[i >> 2][i & 3] = vscale[s];
+            }
+        }
+    };
+    if (first < s_end) {
+        load_keys(first);
+        load_values(first);
+    }
+
+    // queries, and what brings their scores to units of log2: for 16-bit caches a factor sc > 0 (a negative one turns the
+    // queries over), else the key's scale times qscale
+    const float log2_scale = a.scale * 1.44269504088896341f, sc = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
+    float qscale = log2_scale;
     m8 qf[QT][KS];
-    float qscale[QT];   // of a row's scores, in units of log2
     int node[QT];
+    u32x4 qreg[QT][KS];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const int r = min(r0 + u * 16 + ql, n_rows - 1);
         node[u] = r / G;
         const T* qp = (const T*)a.q.p + (int64_t)(node0 + node[u]) * a.q.row + (int64_t)(h * G + r - node[u] * G) * a.q.head;
-        u32x4 w[KS];
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) w[ks] = *(const u32x4*)(I8 ? qp + 64 * (ks >> 1) + 16 * g + 8 * (ks & 1) : qp + 32 * ks + 8 * g);
-        qscale[u] = a.scale * 1.44269504088896341f;
-        if constexpr (std::is_same<M, T>::value) {
+        for (int i = 0; i < KS; ++i) qreg[u][i] = *(const u32x4*)(I8 ? qp + 64 * (i >> 1) + 16 * g + 8 * (i & 1) : qp + 32 * i + 8 * g);
+    }
+    if constexpr (std::is_same<M, T>::value) {
+        const uint32_t flip = !I8 && a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) qf[u][ks] = __builtin_bit_cast(m8, w[ks]);
-        } else {   // bf16 queries, half arithmetic: the row's largest magnitude becomes 2^14 to 2^15
-            float x[KS][8], top = 0.f;
+        for (int u = 0; u < QT; ++u)
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
-                to_floats<T>(w[ks], x[ks]);
+            for (int i = 0; i < KS; ++i) qf[u][i] = __builtin_bit_cast(m8, qreg[u][i] ^ u32x4{flip, flip, flip, flip});
+    } else {   // bf16 queries, half arithmetic: the largest magnitude of the rows becomes 2^14 to 2^15
+        float top = 0.f, x[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[ks][e]));
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                to_floats<T>(qreg[u][i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
             }
-            top = across<32>(across<16>(top, Max()), Max());
-            const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);   // the largest is below 2^(ex + 1)
-            const float down = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-            qscale[u] *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+        top = wave_max(top);
+        const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);   // the largest is below 2^(ex + 1)
+        const float down = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+        qscale *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
+        for (int u = 0; u < QT; ++u)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) qf[u][ks][e] = (_Float16)(x[ks][e] * down);
-        }
+            for (int i = 0; i < KS; ++i) {
+                to_floats<T>(qreg[u][i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qf[u][i][e] = (_Float16)(x[e] * down);
+            }
     }
     f32x4 o[QT][ET];
     float m_run[QT], l_run[QT], R[QT], R_inv[QT];
@@ -410,64 +436,71 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
         m_run[u] = kLowest;
         l_run[u] = R[u] = R_inv[u] = 0.f;
     }
+    auto sees = [&](int nd, int slot) {   // slot < len
+        const int n = slot - ctx;
+        if (n < 0) return true;
+        return a.mask ? (bool)(a.mask[(int64_t)(node0 + nd) * a.words + (n >> 6)] >> (n & 63) & 1) : n <= nd;
+    };
 
-    for (int s0 = first; s0 < s_end; s0 += 32 * NW) {
-        if (s0 + 32 * NW < s_end) tree_load<HD, C>(next, K, V, kscale, vscale, s0 + 32 * NW, last, ql, g);
+    auto step = [&](int s0, auto tail_step) {
+        constexpr bool TAIL = decltype(tail_step)::value;   // some slot is a node's, or there is none
+        const int s_next = s0 + 32 * NW;
         f32x4 s[QT][2];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt) {
             m8 kf[KS];
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks) {
+            for (int i = 0; i < KS; ++i) {
                 if constexpr (I8) {
-                    const uint32_t lo = now.k[kt][ks >> 1][2 * (ks & 1)], hi = now.k[kt][ks >> 1][2 * (ks & 1) + 1];
-                    const u32x4 w = {code_pair(lo, lo, 0x0c010c00u), code_pair(lo, lo, 0x0c030c02u), code_pair(hi, hi, 0x0c010c00u),
-                                     code_pair(hi, hi, 0x0c030c02u)};
-                    kf[ks] = __builtin_bit_cast(m8, w);
+                    const uint32_t lo = kreg[kt][i >> 1][2 * (i & 1)], up = kreg[kt][i >> 1][2 * (i & 1) + 1];
+                    const u32x4 w = {code_pair(lo, lo, 0x0c010c00u), code_pair(lo, lo, 0x0c030c02u), code_pair(up, up, 0x0c010c00u),
+                                     code_pair(up, up, 0x0c030c02u)};
+                    kf[i] = __builtin_bit_cast(m8, w);
                 } else {
-                    kf[ks] = __builtin_bit_cast(m8, now.k[kt][ks]);
+                    kf[i] = __builtin_bit_cast(m8, kreg[kt][i]);
                 }
             }
 #pragma unroll
             for (int u = 0; u < QT; ++u) {
                 s[u][kt] = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) s[u][kt] = Half<M>::mma(kf[ks], qf[u][ks], s[u][kt]);
+                for (int i = 0; i < KS; ++i) s[u][kt] = Half<M>::mma(kf[i], qf[u][i], s[u][kt]);
             }
         }
-        const bool tail = s0 + 31 >= min(ctx, len);   // some slot is a node's, or beyond all
+        f32x4 kq[2];
+        if constexpr (I8)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) kq[kt][i] = ks[kt][i] * qscale;
+        if (s_next < s_end) load_keys(s_next);
         m8 pb[QT];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             float mt = kLowest;
             uint32_t seen[2] = {15u, 15u};   // of this lane's slots, by its row
-            if (tail) {
+            if constexpr (TAIL)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
                     seen[kt] = 0;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int at = s0 + kt * 16 + 4 * g + i, n = at - ctx;
-                        bool yes = n < 0;
-                        if (n >= 0 && n < n_nodes)
-                            yes = a.mask ? (a.mask[(int64_t)(node0 + node[u]) * a.words + (n >> 6)] >> (n & 63)) & 1 : n <= node[u];
-                        if (yes && at < s_end) seen[kt] |= 1u << i;
+                        const int at = s0 + kt * 16 + 4 * g + i;
+                        if (at < s_end && sees(node[u], at)) seen[kt] |= 1u << i;
                     }
                 }
-            }
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float x = s[u][kt][i] * qscale[u];
-                    if constexpr (I8) x *= now.ks[kt][i];
-                    if (tail && !(seen[kt] >> i & 1)) x = -__builtin_inff();
-                    s[u][kt][i] = x;
-                    mt = fmaxf(mt, x);
+                    if constexpr (I8) s[u][kt][i] *= kq[kt][i];
+                    if (TAIL && !(seen[kt] >> i & 1)) s[u][kt][i] = -__builtin_inff();
+                    mt = fmaxf(mt, s[u][kt][i]);
                 }
             mt = across<32>(across<16>(mt, Max()), Max());
-            if (__any(mt > m_run[u])) {
-                const float m_new = fmaxf(m_run[u], mt), alpha = __builtin_amdgcn_exp2f(m_run[u] - m_new);
+            // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1
+            if (__any((mt - m_run[u]) * sc > 8.f)) {
+                const float m_new = fmaxf(m_run[u], mt), alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc);
                 m_run[u] = m_new;
                 l_run[u] *= alpha;
 #pragma unroll
@@ -478,7 +511,7 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, tail && !(seen[kt] >> i & 1) ? 0.f : now.vs[kt][i]);
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, TAIL && !(seen[kt] >> i & 1) ? 0.f : vs[kt][i]);
                 if (__any(top > R[u])) {
                     top = across<32>(across<16>(top, Max()), Max());
                     const uint32_t two = min(__float_as_uint(top) + 0x01000000u, 0x7f000000u) & 0x7f800000u;
@@ -490,65 +523,53 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
                     for (int t = 0; t < ET; ++t) o[u][t] *= down;
                 }
             }
+            const float m_sc = fmaxf(m_run[u] * sc, kLowest);   // its rounding is a factor common to all of a row's slots
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(s[u][kt][i] - m_run[u]);
-                    l_run[u] += p;
-                    float w = p;
-                    if constexpr (I8) w = tail && !(seen[kt] >> i & 1) ? 0.f : p * (now.vs[kt][i] * R_inv[u]);
-                    pb[u][kt * 4 + i] = (M)w;
-                }
-        }
-        bool odd = false;   // some value of a tail's slots is infinite or NaN
-        if constexpr (!I8) {
-            if (tail) {
-                constexpr uint32_t EXP = std::is_same<M, _Float16>::value ? 0x7c00u : 0x7f80u;
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int w = 0; w < Step::VW; ++w) {
-                        const uint32_t x = now.v[i][w];
-                        odd = odd || (x & EXP) == EXP || (x >> 16 & EXP) == EXP;
+                    const float p = __builtin_amdgcn_exp2f(I8 ? s[u][kt][i] - m_sc : fmaf(s[u][kt][i], sc, -m_sc));
+                    if constexpr (I8) {
+                        l_run[u] += p;
+                        pb[u][kt * 4 + i] = (M)(TAIL && !(seen[kt] >> i & 1) ? 0.f : p * (vs[kt][i] * R_inv[u]));
+                    } else {
+                        pb[u][kt * 4 + i] = (M)p;
                     }
-                odd = __any(odd);
-            }
-        }
-        if (odd) {   // slot by slot, so that those a row does not see stay out of its sums
-            for (int n = 0; n < 32; ++n) {
-                const int sv = min(s0 + (n & 16) + (n & 15), last), from = ql + 16 * ((n & 15) >> 2);
-#pragma unroll
-                for (int u = 0; u < QT; ++u) {
-                    float p = 0.f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i == (n >> 4) * 4 + (n & 3)) p = __shfl((float)pb[u][i], from);
-#pragma unroll
-                    for (int t = 0; t < ET; ++t)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float x = I8 ? 0.f : (float)((const M*)V)[(size_t)sv * HD + ET * (4 * g + i) + t];
-                            if (p != 0.f) o[u][t][i] = fmaf(p, x, o[u][t][i]);
-                        }
                 }
-            }
-        } else {
+            if constexpr (!I8)
 #pragma unroll
-            for (int t = 0; t < ET; ++t) {
-                u32x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (I8) w[i] = code_pair(now.v[2 * i][t >> 2], now.v[2 * i + 1][t >> 2], 0x0c040c00u + (t & 3) * 0x00010001u);
-                    else w[i] = __builtin_amdgcn_perm(now.v[2 * i + 1][t >> 1], now.v[2 * i][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
-                }
-                const m8 vf = __builtin_bit_cast(m8, w);
-#pragma unroll
-                for (int u = 0; u < QT; ++u) o[u][t] = Half<M>::mma(vf, pb[u], o[u][t]);
-            }
+                for (int i = 0; i < 4; ++i) l_run[u] = add_pair<M>(__builtin_bit_cast(u32x4, pb[u])[i], l_run[u]);
         }
-        now = next;
-    }
+        if constexpr (TAIL && !I8) {   // infinite and NaN values count as 0 here, so that no row meets them as 0 * x: see below
+            constexpr uint32_t INF = std::is_same<M, _Float16>::value ? 0x7c00u : 0x7f80u;
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int w = 0; w < VW; ++w) {
+                    const uint32_t x = vreg[i][w], lo = (x & INF) == INF ? 0xffffu : 0u, up = (x >> 16 & INF) == INF ? 0xffff0000u : 0u;
+                    odd = odd || (lo | up);
+                    vreg[i][w] = x & ~(lo | up);
+                }
+            if (odd) s_odd = 1;
+        }
+#pragma unroll
+        for (int t = 0; t < ET; ++t) {
+            u32x4 w;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (I8) w[i] = code_pair(vreg[2 * i][t >> 2], vreg[2 * i + 1][t >> 2], 0x0c040c00u + (t & 3) * 0x00010001u);
+                else w[i] = __builtin_amdgcn_perm(vreg[2 * i + 1][t >> 1], vreg[2 * i][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+            }
+            const m8 vf = __builtin_bit_cast(m8, w);
+#pragma unroll
+            for (int u = 0; u < QT; ++u) o[u][t] = Half<M>::mma(vf, pb[u], o[u][t]);
+        }
+        if (s_next < s_end) load_values(s_next);
+    };
+    int s0 = first;
+    for (; s0 < s_end && s0 + 31 < shared_end; s0 += 32 * NW) step(s0, std::false_type{});
+    for (; s0 < s_end; s0 += 32 * NW) step(s0, std::true_type{});
 
     // the waves' sums together: each brings its own to the common maximum
 #pragma unroll
@@ -568,8 +589,8 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
         for (int w = 0; w < NW; ++w) m_all[u] = fmaxf(m_all[u], s_m[w][u * 16 + ql]);
         l_all[u] = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f(s_m[w][u * 16 + ql] - m_all[u]);
-        const float f = __builtin_amdgcn_exp2f(m_run[u] - m_all[u]) * (I8 ? R[u] : 1.f);
+        for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f((s_m[w][u * 16 + ql] - m_all[u]) * sc);
+        const float f = __builtin_amdgcn_exp2f((m_run[u] - m_all[u]) * sc) * (I8 ? R[u] : 1.f);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -580,6 +601,7 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
     }
     __syncthreads();
     // wave i takes elements ET * (4g + i) .. of every row: ET neighbours per lane
+    const int e0 = ET * (4 * g + wave);
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const int r = r0 + u * 16 + ql;
@@ -591,16 +613,20 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
             for (int w = 0; w < NW; ++w) x[t] += s_o[w][u][wave][lane][t];
         }
         if (r >= n_rows) continue;
-        const int e0 = ET * (4 * g + wave);
-        if (n_chunks > 1) {
-            const size_t at = ((size_t)unit * a.max_nodes * G + r) * (HD + 2);
-            float* to = a.part + at;
+        if constexpr (!I8)
+            if (s_odd)   // rare: the values that counted as 0, to the rows that see them (a positive weight times infinity or NaN)
+                for (int slot = s_begin + max(shared_end - s_begin, 0) / 32 * 32; slot < s_end; ++slot) {
+                    if (!sees(node[u], slot)) continue;
+                    const C* v = (const C*)(V + (int64_t)slot * ROW) + e0;
 #pragma unroll
-            for (int t = 0; t < ET; ++t) to[e0 + t] = x[t];
-            if (wave == 0 && g == 0) {
-                to[HD] = m_all[u];
-                to[HD + 1] = l_all[u];
-            }
+                    for (int t = 0; t < ET; ++t)
+                        if (!(fabsf((float)v[t]) <= 3.4e38f)) x[t] += (float)v[t];
+                }
+        if (n_chunks > 1) {
+            float* to = a.part + ((size_t)unit * a.max_nodes * G + r) * (HD + 4);
+#pragma unroll
+            for (int t = 0; t < ET; t += 4) *(float4*)(to + e0 + t) = make_float4(x[t], x[t + 1], x[t + 2], x[t + 3]);
+            if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(fmaxf(m_all[u] * sc, kLowest), l_all[u]);
         } else {
             const float inv = l_all[u] != 0.f ? 1.f / l_all[u] : 0.f;   // a row that sees nothing gets zeros
 #pragma unroll
@@ -610,15 +636,17 @@ __global__ __launch_bounds__(256) void k_attention_tree(TreeArgs a)
     }
 }
 
-// Adds up the chunks of rows whose slots were shared out: a wave per row.
+// Adds up the chunks of rows whose slots were shared out: a workgroup per row, whose groups of HD / 4 lanes take the chunks in turn
+// and join like the waves above.
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 {
-    constexpr int E = HD / 64;
+    constexpr int LPG = HD / 4, GROUPS = 256 / LPG;
+    __shared__ float s_m[GROUPS], s_l[GROUPS];
+    __shared__ float4 s_o[GROUPS][LPG];
     const CacheView& c = a.c;
-    const int G = a.heads / c.n_kv, per = a.max_nodes * G, lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int r = (int)(id % per), h = (int)(id / per % c.n_kv), j = (int)(id / per / c.n_kv);
+    const int G = a.heads / c.n_kv, per = a.max_nodes * G, id = blockIdx.x;
+    const int r = id % per, h = id / per % c.n_kv, j = id / per / c.n_kv;
     const int n_seq = a.d_n ? *a.d_n : a.n_seq;
     if (j >= min(n_seq, a.n_seq)) return;
     const int seq = a.seq ? a.seq[j] : j;
@@ -627,25 +655,44 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
     if (r >= n_nodes * G || seq < 0 || seq >= c.n_seq) return;
     int slots = 0;
     if (slab_of(c, seq, &slots) < 0) return;
-    const int len = (int)min((int64_t)max(a.context[j], 0) + n_nodes, (int64_t)slots);
-    const int n = tree_chunks(len, a.chunk, a.chunks);
+    const int n = tree_chunks((int)min((int64_t)max(a.context[j], 0) + n_nodes, (int64_t)slots), a.chunk, a.chunks);
     if (n < 2) return;
-    const size_t step = (size_t)c.n_kv * per * (HD + 2);
-    const float* p = a.part + (((size_t)j * a.chunks * c.n_kv + h) * per + r) * (HD + 2);
-    float m = kLowest, l = 0.f, o[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int k = 0; k < n; ++k) m = fmaxf(m, p[k * step + HD]);
-    for (int k = 0; k < n; ++k) {
-        const float f = __builtin_amdgcn_exp2f(p[k * step + HD] - m);
-        l += p[k * step + HD + 1] * f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += p[k * step + E * lane + e] * f;
+    const int group = threadIdx.x / LPG, e = threadIdx.x % LPG;
+    const size_t step = (size_t)c.n_kv * per * (HD + 4);
+    const float* p = a.part + (((size_t)j * a.chunks * c.n_kv + h) * per + r) * (HD + 4);
+    float m = kLowest, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int k = group; k < n; k += GROUPS) {
+        const float4 x = *(const float4*)(p + k * step + 4 * e);
+        const float2 ml = *(const float2*)(p + k * step + HD);
+        const float m_new = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - m_new), fx = __builtin_amdgcn_exp2f(ml.x - m_new);
+        m = m_new;
+        l = l * f + ml.y * fx;
+        o = make_float4(o.x * f + x.x * fx, o.y * f + x.y * fx, o.z * f + x.z * fx, o.w * f + x.w * fx);
+    }
+    s_o[group][e] = o;
+    if (e == 0) {
+        s_m[group] = m;
+        s_l[group] = l;
+    }
+    __syncthreads();
+    if (group > 0) return;
+    for (int k = 0; k < GROUPS; ++k) m = fmaxf(m, s_m[k]);
+    float x[4] = {0.f, 0.f, 0.f, 0.f};
+    l = 0.f;
+    for (int k = 0; k < GROUPS; ++k) {
+        const float f = __builtin_amdgcn_exp2f(s_m[k] - m);
+        const float4 y = s_o[k][e];
+        l += s_l[k] * f;
+        x[0] += y.x * f;
+        x[1] += y.y * f;
+        x[2] += y.z * f;
+        x[3] += y.w * f;
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[e] *= inv;
-    tree_store<T, E>(a, node0 + r / G, h * G + r % G, E * lane, o);
+    for (int i = 0; i < 4; ++i) x[i] *= inv;
+    tree_store<T, 4>(a, node0 + r / G, h * G + r % G, 4 * e, x);
 }
 
 // ------------------------------------------------------------------------------------------ attention of packed prompts
@@ -659,16 +706,6 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 constexpr int kPackTile = 64, kPackQueries = 32;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-// sum + a's two values, in fp32.
-template <typename T>
-__device__ __forceinline__ float add_pair(uint32_t a, float sum)
-{
-    typedef T t2 __attribute__((ext_vector_type(2)));
-    const t2 one = {(T)1.f, (T)1.f};
-    if constexpr (std::is_same<T, _Float16>::value) return __builtin_amdgcn_fdot2(__builtin_bit_cast(t2, a), one, sum, false);
-    else return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(t2, a), one, sum, false);
-}
-
 template <typename T>
 __device__ __forceinline__ f32x16 mma32(typename Half<T>::x8 a, typename Half<T>::x8 b, f32x16 c)
 {
@@ -953,8 +990,7 @@ static void attention_tree(TreeArgs a, hipStream_t s)
     const int units = round_up(a.n_seq * a.c.n_kv * a.chunks, 8);
     k_attention_tree<HD, T, C, QT><<<dim3((unsigned)units * a.row_blocks), 256, 0, s>>>(a);
     if (a.chunks > 1) {
-        const int64_t rows = (int64_t)a.n_seq * a.max_nodes * a.heads;
-        k_tree_join<HD, T><<<dim3((unsigned)((rows + 3) / 4)), 256, 0, s>>>(a);
+        k_tree_join<HD, T><<<dim3((unsigned)a.n_seq * a.max_nodes * a.heads), 256, 0, s>>>(a);
     }
 }
 

@@ -176,7 +176,7 @@ struct TreeArgs {
     const int32_t* nodes;      // [n_seq + 1] first row of each sequence's nodes, or null: one node each
     const uint64_t* mask;      // [rows][words] nodes that a node sees, or null: itself and those before it
     const int32_t* d_n;        // null, or how many of the n_seq there are
-    float* part;               // chunks > 1: [n_seq][chunks][n_kv][max_nodes * G][hd + 2]
+    float* part;               // chunks > 1: [n_seq][chunks][n_kv][max_nodes * G][hd + 4]: sums, their maximum, their weight
     float scale;
     int n_seq, heads, max_nodes, words;
     int chunk, chunks, row_blocks;   // tree_plan

@@ -102,7 +102,7 @@ ss::TreePlan plan_of(int32_t n_heads, int32_t n_kv_heads, int32_t n_seq, int32_t
 
 size_t part_bytes(const ss::TreePlan& p, int32_t n_heads, int32_t head_dim, int32_t n_seq, int32_t max_nodes)
 {
-    return p.chunks > 1 ? (size_t)n_seq * p.chunks * max_nodes * n_heads * (head_dim + 2) * 4 : 0;
+    return p.chunks > 1 ? (size_t)n_seq * p.chunks * max_nodes * n_heads * (head_dim + 4) * 4 : 0;
 }
 
 }  // namespace

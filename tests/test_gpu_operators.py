@@ -266,6 +266,32 @@ def test_a_long_context_is_shared_out_and_joined(dtype, held):
     check_tree(7, [20000, 11, 4097], [3, 1, 20], 1, 4, 128, dtype, held)
 
 
+@pytest.mark.parametrize("dtype,held", HELD)
+def test_many_small_weights_count_beside_a_large_one(dtype, held):
+    """One slot of score 0 and thousands whose weights, 2^-15 each, are below half's normal range: together a quarter."""
+    n, dim = 8192, 128
+    k = torch.zeros(n, 1, dim, device="cuda")
+    k[:, 0, 0] = -1
+    k[77, 0, 0] = 0
+    v = randn(gen(70), n, 1, dim) + 1
+    H = Held(71, [n], 1, dim, held)
+    H.raw["k"].copy_(k[:, 0])
+    if held == I8:
+        H.raw["k_scale"].fill_(1)
+    else:
+        H.raw["v"].copy_(v[:, 0])
+    q = torch.zeros(1, 1, dim, dtype=dtype, device="cuda")
+    q[0, 0, 0] = 15
+    out = ss.ss_attention_tree(q, H.cache, i32([n - 1]), n, scale=math.log(2))
+    kk, vv = H.rows("k", 0, 0, n), H.rows("v", 0, 0, n)
+    assert_attention(out[:, 0], q[:, 0], kk, vv, torch.ones(1, n, dtype=torch.bool, device="cuda"), math.log(2), F16 if held == I8 else held)
+    if held != I8:
+        qs = torch.zeros(n, 1, dim, dtype=dtype, device="cuda")
+        qs[-1] = q[0]
+        out = ss.ss_attention_packed(qs, k.to(dtype), v.to(dtype), i32([0, n]), n, scale=math.log(2))
+        assert_attention(out[-1:, 0], q[:, 0], kk, vv, torch.ones(1, n, dtype=torch.bool, device="cuda"), math.log(2), dtype)
+
+
 def test_the_same_call_gives_the_same_bits():
     H, q, out = check_tree(8, [5000, 40], [7, 30], 2, 4, 128, BF16, I8)
     ctx, nodes = i32([5000, 40]), i32([0, 7, 37])
