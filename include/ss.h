@@ -402,7 +402,7 @@ int ss_bench_read_stream(ss_weights* w, int32_t iters, double* ms_out, int64_t* 
 #define SS_I8  3 /* caches only: 8-bit codes with one scale per vector (below)        */
 
 /* Rows of heads: element e of head h of row r at p + (r * row_stride + h * head_stride + e) elements.  p is 16-byte aligned, the
- * strides are multiples of 8. */
+ * strides are multiples of 8 from 0 (a row or head that all share, of inputs) to 2^24. */
 typedef struct {
     void*   p;
     int64_t row_stride, head_stride; /* in elements */

@@ -231,14 +231,59 @@ struct MathType { typedef T type; };           // 16-bit cache: its own type
 template <typename T>
 struct MathType<int8_t, T> { typedef _Float16 type; };
 
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
-// First row and number of rows (nodes) of the j-th sequence of a call; none where the table leaves the rows that there are.
-__device__ __forceinline__ int tree_nodes(const TreeArgs& a, int j, int* n)
+// The j-th sequence of a call: its rows (nodes), its history, its slots (history and nodes, as far as the slab goes) and the first
+// vector of its slab.  No rows where the tables leave the rows that there are, no slots where they leave the cache.
+struct TreeSeq {
+    int node0, n_nodes, ctx, len, slots;
+    int64_t base;
+};
+__device__ __forceinline__ TreeSeq tree_sequence(const TreeArgs& a, int j)
 {
-    const int first = a.nodes ? a.nodes[j] : j, count = a.nodes ? min(a.nodes[j + 1] - first, a.max_nodes) : 1;
-    *n = first >= 0 && count > 0 && first + (int64_t)count <= a.q.rows ? count : 0;
-    return first;
+    const CacheView& c = a.c;
+    TreeSeq s{j, 0, 0, 0, 0, 0};
+    // what does not depend on other tables is read at once
+    int seq = j, count = 1;
+    const int live = a.d_n ? *a.d_n : a.n_seq, own = min(j, c.n_seq - 1);
+    int64_t at = c.start[own];
+    s.slots = c.slots[own];
+    s.ctx = max(a.context[j], 0);
+    if (a.nodes) {
+        s.node0 = a.nodes[j];
+        count = min(a.nodes[j + 1] - s.node0, a.max_nodes);
+    }
+    if (a.seq) {
+        seq = a.seq[j];
+        const int there = min(max(seq, 0), c.n_seq - 1);
+        at = c.start[there];
+        s.slots = c.slots[there];
+    }
+    if (j < live && s.node0 >= 0 && count > 0 && s.node0 + (int64_t)count <= a.q.rows) s.n_nodes = count;
+    if (seq >= 0 && seq < c.n_seq && at >= 0 && s.slots >= 0 && at + s.slots <= c.total) {
+        s.base = at * c.n_kv;
+        s.len = (int)min((int64_t)s.ctx + s.n_nodes, (int64_t)s.slots);
+    }
+    return s;
+}
+
+// Bits of 64 neighbouring slots that a node sees, the first of them the slot of node n (n < 0: in the history) and `there` of them
+// there.
+__device__ __forceinline__ uint64_t tree_seen(const TreeArgs& a, int row, int node, int n, int there)
+{
+    uint64_t bits;
+    n = max(n, -64);
+    if (a.mask) {
+        const uint64_t* m = a.mask + (int64_t)row * a.words;
+        const int w = n >> 6, sh = n & 63;
+        if (n == -64) bits = ~0ull;
+        else if (n < 0) bits = m[0] << -n | ((1ull << -n) - 1);
+        else bits = (w < a.words ? m[w] >> sh : 0) | (sh && w + 1 < a.words ? m[w + 1] << (64 - sh) : 0);
+    } else {   // those up to itself
+        bits = node - n >= 63 ? ~0ull : node < n ? 0 : (2ull << (node - n)) - 1;
+    }
+    return there >= 64 ? bits : there > 0 ? bits & ((1ull << there) - 1) : 0;
 }
 
 // N neighbouring results of a row's head, e0 on: to its row, or (the engine's projections) to the packed layout.
@@ -292,30 +337,18 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
     const CacheView& c = a.c;
 
-    // blocks of rows of one unit are 8 apart: on one die, whose L2 hands the unit's slots on
-    const int id = blockIdx.x, G = a.heads / c.n_kv;
-    const int rb = (id >> 3) % a.row_blocks;
-    const int unit = (id >> 3) / a.row_blocks * 8 + (id & 7);
-    const int h = unit % c.n_kv, chunk = unit / c.n_kv % a.chunks, j = unit / c.n_kv / a.chunks;
-    const int n_seq = a.d_n ? *a.d_n : a.n_seq;
-    if (j >= min(n_seq, a.n_seq)) return;
-    const int seq = a.seq ? a.seq[j] : j;
-    int n_nodes;
-    const int node0 = tree_nodes(a, j, &n_nodes);
+    // blocks of rows that share their slots are n_kv apart: with 8 heads or a multiple on one die, whose L2 hands the slots on
+    const int G = a.heads / c.n_kv, rb = blockIdx.x / c.n_kv, h = blockIdx.x - rb * c.n_kv, chunk = blockIdx.y, j = blockIdx.z;
+    const TreeSeq sq = tree_sequence(a, j);
+    const int node0 = sq.node0, n_nodes = sq.n_nodes, ctx = sq.ctx, len = sq.len, slots = sq.slots;
     const int n_rows = n_nodes * G, r0 = rb * ROWS;
-    if (r0 >= n_rows) return;
-    int slots = 0, len = 0;
-    int64_t base = -1;
-    const int ctx = max(a.context[j], 0);
-    if (seq >= 0 && seq < c.n_seq) base = slab_of(c, seq, &slots);
-    if (base >= 0) len = (int)min((int64_t)ctx + n_nodes, (int64_t)slots);
     const int n_chunks = tree_chunks(len, a.chunk, a.chunks);
-    if (chunk >= n_chunks) return;
+    if (r0 >= n_rows || chunk >= n_chunks) return;
     const int s_begin = chunk * a.chunk, s_end = chunk + 1 == n_chunks ? len : s_begin + a.chunk, last = len - 1;
     const int shared_end = min(ctx, len);   // slots before this are seen by every row
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), ql = lane & 15, g = lane >> 4;
-    const int64_t head_base = base + (int64_t)h * slots;
+    const int64_t head_base = sq.base + (int64_t)h * slots;
     const char *K = (const char*)c.k + head_base * ROW, *V = (const char*)c.v + head_base * ROW;
     const float *kscale = I8 ? c.k_scale + head_base : nullptr, *vscale = I8 ? c.v_scale + head_base : nullptr;
     const int first = s_begin + 32 * wave;
@@ -326,17 +359,19 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     uint32_t vreg[8][VW];
     f32x4u ks[2], vs[2];
     const unsigned k_off = ql * ROW + 16 * g, v_off = 4 * g * ROW + ET * ql * (int)sizeof(C);
-    auto load_v = [](uint32_t (&v)[VW], const char* p) {
+    // rows of one block use the cache's bytes once
+    auto load16 = [](const char* p) { return QT == 1 ? __builtin_nontemporal_load((const u32x4*)p) : *(const u32x4*)p; };
+    auto load_v = [&](uint32_t (&v)[VW], const char* p) {
         if constexpr (VW == 4) {
-            const u32x4 w = *(const u32x4*)p;
+            const u32x4 w = load16(p);
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = w[i];
         } else if constexpr (VW == 2) {
-            const uint2 w = *(const uint2*)p;
-            v[0] = w.x;
-            v[1] = w.y;
+            const u32x2 w = QT == 1 ? __builtin_nontemporal_load((const u32x2*)p) : *(const u32x2*)p;
+            v[0] = w[0];
+            v[1] = w[1];
         } else {
-            v[0] = *(const uint32_t*)p;
+            v[0] = QT == 1 ? __builtin_nontemporal_load((const uint32_t*)p) : *(const uint32_t*)p;
         }
     };
     auto load_keys = [&](int s0) {
@@ -345,7 +380,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int i = 0; i < KL; ++i) kreg[kt][i] = *(const u32x4*)(p + k_off + kt * 16 * ROW + 64 * i);
+                for (int i = 0; i < KL; ++i) kreg[kt][i] = load16(p + k_off + kt * 16 * ROW + 64 * i);
             if constexpr (I8)
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) ks[kt] = *(const f32x4u*)(kscale + s0 + 4 * g + kt * 16);
@@ -354,7 +389,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
             for (int kt = 0; kt < 2; ++kt) {
                 const char* p = K + (int64_t)min(s0 + kt * 16 + ql, last) * ROW + 16 * g;
 #pragma unroll
-                for (int i = 0; i < KL; ++i) kreg[kt][i] = *(const u32x4*)(p + 64 * i);
+                for (int i = 0; i < KL; ++i) kreg[kt][i] = load16(p + 64 * i);
                 if constexpr (I8)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) ks[kt][i] = kscale[min(s0 + kt * 16 + 4 * g + i, last)];
@@ -436,12 +471,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         m_run[u] = kLowest;
         l_run[u] = R[u] = R_inv[u] = 0.f;
     }
-    auto sees = [&](int nd, int slot) {   // slot < len
-        const int n = slot - ctx;
-        if (n < 0) return true;
-        return a.mask ? (bool)(a.mask[(int64_t)(node0 + nd) * a.words + (n >> 6)] >> (n & 63) & 1) : n <= nd;
-    };
-
     auto step = [&](int s0, auto tail_step) {
         constexpr bool TAIL = decltype(tail_step)::value;   // some slot is a node's, or there is none
         const int s_next = s0 + 32 * NW;
@@ -479,16 +508,11 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         for (int u = 0; u < QT; ++u) {
             float mt = kLowest;
             uint32_t seen[2] = {15u, 15u};   // of this lane's slots, by its row
-            if constexpr (TAIL)
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt) {
-                    seen[kt] = 0;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int at = s0 + kt * 16 + 4 * g + i;
-                        if (at < s_end && sees(node[u], at)) seen[kt] |= 1u << i;
-                    }
-                }
+            if constexpr (TAIL) {
+                const uint64_t bits = tree_seen(a, node0 + node[u], node[u], s0 - ctx, s_end - s0) >> (4 * g);
+                seen[0] = bits & 15;
+                seen[1] = bits >> 16 & 15;
+            }
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -616,14 +640,14 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         if constexpr (!I8)
             if (s_odd)   // rare: the values that counted as 0, to the rows that see them (a positive weight times infinity or NaN)
                 for (int slot = s_begin + max(shared_end - s_begin, 0) / 32 * 32; slot < s_end; ++slot) {
-                    if (!sees(node[u], slot)) continue;
+                    if (!tree_seen(a, node0 + node[u], node[u], slot - ctx, 1)) continue;
                     const C* v = (const C*)(V + (int64_t)slot * ROW) + e0;
 #pragma unroll
                     for (int t = 0; t < ET; ++t)
                         if (!(fabsf((float)v[t]) <= 3.4e38f)) x[t] += (float)v[t];
                 }
         if (n_chunks > 1) {
-            float* to = a.part + ((size_t)unit * a.max_nodes * G + r) * (HD + 4);
+            float* to = a.part + ((((size_t)j * a.chunks + chunk) * c.n_kv + h) * a.max_nodes * G + r) * (HD + 4);
 #pragma unroll
             for (int t = 0; t < ET; t += 4) *(float4*)(to + e0 + t) = make_float4(x[t], x[t + 1], x[t + 2], x[t + 3]);
             if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(fmaxf(m_all[u] * sc, kLowest), l_all[u]);
@@ -636,63 +660,62 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     }
 }
 
-// Adds up the chunks of rows whose slots were shared out: a workgroup per row, whose groups of HD / 4 lanes take the chunks in turn
-// and join like the waves above.
-template <int HD, typename T>
+// Adds up the chunks of rows whose slots were shared out.  A group of HD / 4 lanes adds up chunks like the waves above; WIDE: the groups of
+// a workgroup take the chunks of one row in turn (few rows, many chunks: the time is that of the loads one after another), else a
+// row each.
+template <int HD, typename T, bool WIDE>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 {
     constexpr int LPG = HD / 4, GROUPS = 256 / LPG;
     __shared__ float s_m[GROUPS], s_l[GROUPS];
     __shared__ float4 s_o[GROUPS][LPG];
     const CacheView& c = a.c;
-    const int G = a.heads / c.n_kv, per = a.max_nodes * G, id = blockIdx.x;
-    const int r = id % per, h = id / per % c.n_kv, j = id / per / c.n_kv;
-    const int n_seq = a.d_n ? *a.d_n : a.n_seq;
-    if (j >= min(n_seq, a.n_seq)) return;
-    const int seq = a.seq ? a.seq[j] : j;
-    int n_nodes;
-    const int node0 = tree_nodes(a, j, &n_nodes);
-    if (r >= n_nodes * G || seq < 0 || seq >= c.n_seq) return;
-    int slots = 0;
-    if (slab_of(c, seq, &slots) < 0) return;
-    const int n = tree_chunks((int)min((int64_t)max(a.context[j], 0) + n_nodes, (int64_t)slots), a.chunk, a.chunks);
-    if (n < 2) return;
     const int group = threadIdx.x / LPG, e = threadIdx.x % LPG;
+    const int G = a.heads / c.n_kv, per = a.max_nodes * G, h = blockIdx.y, j = blockIdx.z;
+    const int r = WIDE ? blockIdx.x : blockIdx.x * GROUPS + group;
+    const TreeSeq sq = tree_sequence(a, j);
+    const int n = tree_chunks(sq.len, a.chunk, a.chunks);
+    if (n < 2 || r >= sq.n_nodes * G) return;
     const size_t step = (size_t)c.n_kv * per * (HD + 4);
     const float* p = a.part + (((size_t)j * a.chunks * c.n_kv + h) * per + r) * (HD + 4);
-    float m = kLowest, l = 0.f;
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = group; k < n; k += GROUPS) {
-        const float4 x = *(const float4*)(p + k * step + 4 * e);
-        const float2 ml = *(const float2*)(p + k * step + HD);
-        const float m_new = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - m_new), fx = __builtin_amdgcn_exp2f(ml.x - m_new);
+    float m = kLowest, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m_k, float l_k, const float4& y) {
+        const float m_new = fmaxf(m, m_k), f = __builtin_amdgcn_exp2f(m - m_new), f_k = __builtin_amdgcn_exp2f(m_k - m_new);
         m = m_new;
-        l = l * f + ml.y * fx;
-        o = make_float4(o.x * f + x.x * fx, o.y * f + x.y * fx, o.z * f + x.z * fx, o.w * f + x.w * fx);
+        l = l * f + l_k * f_k;
+        x[0] = x[0] * f + y.x * f_k;
+        x[1] = x[1] * f + y.y * f_k;
+        x[2] = x[2] * f + y.z * f_k;
+        x[3] = x[3] * f + y.w * f_k;
+    };
+    constexpr int STEP = WIDE ? GROUPS : 1;
+    for (int k = WIDE ? group : 0; k < n; k += 4 * STEP) {   // four chunks' loads at a time
+        float4 y[4];
+        float2 ml[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float* q = p + min(k + i * STEP, n - 1) * step;
+            y[i] = *(const float4*)(q + 4 * e);
+            ml[i] = *(const float2*)(q + HD);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i * STEP < n) add(ml[i].x, ml[i].y, y[i]);
     }
-    s_o[group][e] = o;
-    if (e == 0) {
-        s_m[group] = m;
-        s_l[group] = l;
-    }
-    __syncthreads();
-    if (group > 0) return;
-    for (int k = 0; k < GROUPS; ++k) m = fmaxf(m, s_m[k]);
-    float x[4] = {0.f, 0.f, 0.f, 0.f};
-    l = 0.f;
-    for (int k = 0; k < GROUPS; ++k) {
-        const float f = __builtin_amdgcn_exp2f(s_m[k] - m);
-        const float4 y = s_o[k][e];
-        l += s_l[k] * f;
-        x[0] += y.x * f;
-        x[1] += y.y * f;
-        x[2] += y.z * f;
-        x[3] += y.w * f;
+    if constexpr (WIDE) {
+        s_o[group][e] = make_float4(x[0], x[1], x[2], x[3]);
+        if (e == 0) {
+            s_m[group] = m;
+            s_l[group] = l;
+        }
+        __syncthreads();
+        if (group > 0) return;
+        for (int k = 1; k < GROUPS; ++k) add(s_m[k], s_l[k], s_o[k][e]);
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] *= inv;
-    tree_store<T, 4>(a, node0 + r / G, h * G + r % G, 4 * e, x);
+    tree_store<T, 4>(a, sq.node0 + r / G, h * G + r % G, 4 * e, x);
 }
 
 // ------------------------------------------------------------------------------------------ attention of packed prompts
@@ -942,6 +965,290 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     }
 }
 
+// ------------------------------------------------------------------------------------------ trees of many rows over a cache
+// What k_attention_tree computes, for units of more rows than a wave or two can hold: a wave takes 32 rows as the packed kernel takes 32
+// queries, the four waves of a workgroup share tiles of 64 slots in LDS, and slots of 8-bit caches become halves once on their way
+// there, not once per wave.  Copies of 16-bit slots go straight into LDS; codes pass through registers, requested a tile ahead.
+template <int HD, typename T, typename C>
+__global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
+{
+    typedef typename MathType<C, T>::type M;
+    typedef typename Half<M>::x8 m8;
+    constexpr bool I8 = std::is_same<C, int8_t>::value;
+    constexpr int NW = 4, KT = 64, QW = 32, ROWS = NW * QW;
+    constexpr int ROW = HD * 2, PIECES = ROW / 16, RPC = 64 / PIECES, COPIES = KT / RPC / NW;
+    constexpr int KS = HD / 16, ET = HD / 32, TILE = KT * ROW;
+    constexpr int PT = HD / 64;   // 16-byte pieces of codes per thread
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][TILE];
+    __shared__ __attribute__((aligned(16))) float s_ks[2][KT], s_vs[2][KT];
+    __shared__ float s_top[2], s_q[NW];
+    __shared__ int s_odd;
+    const CacheView& c = a.c;
+    const int G = a.heads / c.n_kv, rb = blockIdx.x / c.n_kv, h = blockIdx.x - rb * c.n_kv, chunk = blockIdx.y, j = blockIdx.z;
+    const TreeSeq sq = tree_sequence(a, j);
+    const int node0 = sq.node0, n_nodes = sq.n_nodes, ctx = sq.ctx, len = sq.len;
+    const int n_rows = n_nodes * G, r0 = rb * ROWS;
+    const int n_chunks = tree_chunks(len, a.chunk, a.chunks);
+    if (r0 >= n_rows || chunk >= n_chunks) return;
+    const int s_begin = chunk * a.chunk, s_end = chunk + 1 == n_chunks ? len : s_begin + a.chunk, last = len - 1;
+    const int shared_end = min(ctx, len);   // slots before this are seen by every row
+    const int n_tiles = (s_end - s_begin + KT - 1) / KT;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), ql = lane & 31, hi = lane >> 5;
+    const int64_t head_base = sq.base + (int64_t)h * sq.slots + s_begin;
+    const char *K = (const char*)c.k + head_base * HD * (int)sizeof(C), *V = (const char*)c.v + head_base * HD * (int)sizeof(C);
+    const float *kscale = I8 ? c.k_scale + head_base : nullptr, *vscale = I8 ? c.v_scale + head_base : nullptr;
+    const int left = last - s_begin;   // last slot there is, from the chunk's first; later ones repeat it
+
+    // banks: see k_attention_packed
+    auto key_turn = [](int r) { return HD == 128 ? r & 15 : r >> 1 & 7; };
+    auto value_turn = [](int r) { return HD == 128 ? (r & 3) << 2 : (r & 2) << 1; };
+    const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0]);
+    const int c_row = wave * RPC + lane / PIECES;   // 16-bit: row of copy 0
+    const unsigned k_piece = ((lane % PIECES) ^ key_turn(c_row)) * 16, v_piece = ((lane % PIECES) ^ value_turn(c_row)) * 16;
+    u32x4 kreg[PT], vreg[PT];
+    float sreg = 0.f;
+    auto request = [&](int t, int b) {
+        if constexpr (I8) {
+            const int64_t r = min(t * KT + (tid >> 2), left);
+#pragma unroll
+            for (int i = 0; i < PT; ++i) {
+                kreg[i] = *(const u32x4*)(K + r * HD + (i * 4 + (tid & 3)) * 16);
+                vreg[i] = *(const u32x4*)(V + r * HD + (i * 4 + (tid & 3)) * 16);
+            }
+            if (tid < 2 * KT) sreg = (tid < KT ? kscale : vscale)[min(t * KT + (tid & 63), left)];
+        } else {
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const unsigned place = b * 2 * TILE + (i * NW + wave) * 1024, r = min(c_row + i * NW * RPC, left - t * KT);
+                lds_copy_1k(lds_at, place, K + (int64_t)t * TILE, r * ROW + k_piece);
+                lds_copy_1k(lds_at, place + TILE, V + (int64_t)t * TILE, r * ROW + v_piece);
+            }
+        }
+    };
+    float qscale = a.scale * 1.44269504088896341f;
+    auto stage = [&](int b) {   // codes to halves
+        if constexpr (I8) {
+            const int r = tid >> 2;
+            auto halves = [](uint32_t lo, uint32_t up) {
+                return u32x4{code_pair(lo, lo, 0x0c010c00u), code_pair(lo, lo, 0x0c030c02u), code_pair(up, up, 0x0c010c00u),
+                             code_pair(up, up, 0x0c030c02u)};
+            };
+            // piece 8i + 2 * (tid % 4) + k, turned by its row
+            const unsigned to_k = r * ROW + ((2 * (tid & 3)) ^ key_turn(r)) * 16, to_v = r * ROW + ((2 * (tid & 3)) ^ value_turn(r)) * 16;
+            char* to = &lds[b][0][0];
+#pragma unroll
+            for (int i = 0; i < PT; ++i)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    *(u32x4*)(to + (to_k ^ (i * 128 + k * 16))) = halves(kreg[i][2 * k], kreg[i][2 * k + 1]);
+                    *(u32x4*)(to + TILE + (to_v ^ (i * 128 + k * 16))) = halves(vreg[i][2 * k], vreg[i][2 * k + 1]);
+                }
+            if (tid < KT) {
+                s_ks[b][tid] = sreg * qscale;
+            } else if (tid < 2 * KT) {
+                s_vs[b][tid - KT] = sreg;
+                const float top = wave_max(sreg);
+                if (tid == KT) s_top[b] = top;
+            }
+        }
+    };
+    if (n_tiles > 0) request(0, 0);
+    if (tid == 0) s_odd = 0;
+
+    // queries: as in k_attention_tree, one power of two for the workgroup
+    const int row = min(r0 + wave * QW + ql, n_rows - 1), node = row / G;
+    const bool busy = r0 + wave * QW < n_rows;
+    const float sc = I8 ? 1.f : fmaxf(fabsf(qscale), 1e-37f);
+    m8 qf[KS];
+    {
+        const T* qp = (const T*)a.q.p + (int64_t)(node0 + node) * a.q.row + (int64_t)(h * G + row - node * G) * a.q.head + 8 * hi;
+        u32x4 w[KS];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) w[i] = *(const u32x4*)(qp + 16 * i);
+        if constexpr (std::is_same<M, T>::value) {
+            const uint32_t flip = !I8 && a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) qf[i] = __builtin_bit_cast(m8, w[i] ^ u32x4{flip, flip, flip, flip});
+        } else {
+            float top = 0.f, x[8];
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                to_floats<T>(w[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+            }
+            top = wave_max(top);
+            if (lane == 0) s_q[wave] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(s_q[0], s_q[1]), fmaxf(s_q[2], s_q[3]));
+            const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);
+            const float down = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+            qscale *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                to_floats<T>(w[i], x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) qf[i][e] = (_Float16)(x[e] * down);
+            }
+        }
+    }
+    f32x16 o[ET];
+#pragma unroll
+    for (int t = 0; t < ET; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m_run = kLowest, l_run = 0.f, R = 0.f, R_inv = 0.f;
+    const unsigned k_at = ql * ROW + (hi ^ key_turn(ql)) * 16;
+    const int v_r = 4 * hi + ((lane & 15) >> 2);
+    unsigned v_at[ET];
+#pragma unroll
+    for (int t = 0; t < ET; ++t)
+        v_at[t] = TILE + v_r * ROW + ((t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) ^ value_turn(v_r)) * 16 + (lane & 1) * 8;
+
+    auto use_tile = [&](int b, int k0, auto tail_tile) {
+        constexpr bool TAIL = decltype(tail_tile)::value;
+        const char* tile = &lds[b][0][0];
+        f32x16 s[2];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[kt][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) s[kt] = mma32<M>(*(const m8*)(tile + (k_at ^ ks * 32) + kt * 32 * ROW), qf[ks], s[kt]);
+        if constexpr (I8) __builtin_amdgcn_sched_barrier(0);   // the scales' reads stay behind: their registers are the keys'
+        uint64_t seen = ~0ull;
+        if constexpr (TAIL) seen = tree_seen(a, node0 + node, node, k0 - ctx, s_end - k0) >> (4 * hi);
+        float mt = kLowest, top = 0.f;
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 kq, vq;
+                if constexpr (I8) kq = *(const f32x4*)&s_ks[b][kt * 32 + 8 * g + 4 * hi];
+                if constexpr (I8 && TAIL) vq = *(const f32x4*)&s_vs[b][kt * 32 + 8 * g + 4 * hi];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const bool sees = !TAIL || (seen >> (kt * 32 + 8 * g + e) & 1);
+                    float x = s[kt][4 * g + e];
+                    if constexpr (I8) x *= kq[e];
+                    if (!sees) x = -__builtin_inff();
+                    if constexpr (I8 && TAIL) top = fmaxf(top, sees ? vq[e] : 0.f);
+                    s[kt][4 * g + e] = x;
+                    mt = fmaxf(mt, x);
+                }
+            }
+        mt = across<32>(mt, Max());
+        if (__any((mt - m_run) * sc > 8.f)) {   // see k_attention_tree
+            const float m_new = fmaxf(m_run, mt), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
+            m_run = m_new;
+            l_run *= alpha;
+#pragma unroll
+            for (int t = 0; t < ET; ++t) o[t] *= alpha;
+        }
+        if constexpr (I8) {
+            top = TAIL ? across<32>(top, Max()) : s_top[b];
+            if (__any(top > R)) {
+                const uint32_t two = min(__float_as_uint(top) + 0x01000000u, 0x7f000000u) & 0x7f800000u;
+                const float R_new = top > R ? __uint_as_float(two) : R;
+                const float down = R * __uint_as_float(0x7f000000u - __float_as_uint(R_new));
+                R = R_new;
+                R_inv = R_new > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(R_new)) : 0.f;
+#pragma unroll
+                for (int t = 0; t < ET; ++t) o[t] *= down;
+            }
+        }
+        if constexpr (I8) __builtin_amdgcn_sched_barrier(0);
+        const float m_sc = fmaxf(m_run * sc, kLowest);
+        m8 pb[4];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4 vq;
+                if constexpr (I8) vq = *(const f32x4*)&s_vs[b][kt * 32 + 8 * g + 4 * hi];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(I8 ? s[kt][4 * g + e] - m_sc : fmaf(s[kt][4 * g + e], sc, -m_sc));
+                    float w = p;
+                    if constexpr (I8) {
+                        l_run += p;
+                        w = TAIL && !(seen >> (kt * 32 + 8 * g + e) & 1) ? 0.f : p * (vq[e] * R_inv);
+                    }
+                    pb[kt * 2 + (g >> 1)][(g & 1) * 4 + e] = (M)w;
+                }
+            }
+        if constexpr (!I8)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) l_run = add_pair<M>(__builtin_bit_cast(u32x4, pb[i])[e], l_run);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int t = 0; t < ET; ++t) {
+                const uint2 lo = lds_read_transposed(tile + v_at[t] + i * 16 * ROW), up = lds_read_transposed(tile + v_at[t] + (i * 16 + 8) * ROW);
+                o[t] = mma32<M>(__builtin_bit_cast(m8, u32x4{lo.x, lo.y, up.x, up.y}), pb[i], o[t]);
+            }
+    };
+    // a trip: its tile is in LDS; the next one is requested, codes put into the other half of LDS at its end
+    if (n_tiles > 0) stage(0);
+    auto trip = [&](int t, auto tail_tile) {
+        const int b = t & 1, k0 = s_begin + t * KT;
+        wait_copies_and_meet<0>();
+        if (t + 1 < n_tiles) request(t + 1, b ^ 1);
+        if constexpr (!I8 && decltype(tail_tile)::value) {   // infinite and NaN values count as 0 here, so that no row meets them as 0 * x: see below
+            constexpr unsigned short INF = std::is_same<M, _Float16>::value ? 0x7c00 : 0x7f80;
+            typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 top = {0, 0};
+            char* values = &lds[b][1][0] + tid * 16;
+#pragma unroll
+            for (int i = 0; i < TILE / 4096; ++i) {
+                const u32x4 w = *(const u32x4*)(values + i * 4096);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, w[e] & 0x7fff7fffu));
+            }
+            if (top[0] >= INF || top[1] >= INF) {
+                for (int i = 0; i < TILE / 4096 * 8; ++i) {
+                    uint16_t* x = (uint16_t*)(values + (i >> 3) * 4096) + (i & 7);
+                    if ((*x & 0x7fff) >= INF) *x = 0;
+                }
+                s_odd = 1;
+            }
+            __syncthreads();
+        }
+        if (busy) use_tile(b, k0, tail_tile);
+        if (I8 && t + 1 < n_tiles) stage(b ^ 1);   // last read before this trip's barrier
+    };
+    const int n_shared = min(n_tiles, max(shared_end - s_begin, 0) / KT);   // tiles that every row sees whole
+    for (int t = 0; t < n_shared; ++t) trip(t, std::false_type{});
+    for (int t = n_shared; t < n_tiles; ++t) trip(t, std::true_type{});
+    const float l = across<32>(l_run, Add());
+    wait_copies_and_meet<0>();
+    if (r0 + wave * QW + ql >= n_rows) return;
+    const float f = (I8 ? R : 1.f) * (n_chunks > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f);   // a row that sees nothing gets zeros
+    float* const part = a.part + ((((size_t)j * a.chunks + chunk) * c.n_kv + h) * a.max_nodes * G + row) * (HD + 4);
+    if (n_chunks > 1 && hi == 0) *(float2*)(part + HD) = make_float2(fmaxf(m_run * sc, kLowest), l);
+#pragma unroll
+    for (int t = 0; t < ET; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int e0 = 32 * t + 8 * i + 4 * hi;
+            float x[4] = {o[t][4 * i] * f, o[t][4 * i + 1] * f, o[t][4 * i + 2] * f, o[t][4 * i + 3] * f};
+            if constexpr (!I8)
+                if (s_odd)   // rare: the values that counted as 0, to the rows that see them (a positive weight times infinity or NaN)
+                    for (int slot = s_begin + max(shared_end - s_begin, 0) / KT * KT; slot < s_end; ++slot)
+                        if (tree_seen(a, node0 + node, node, slot - ctx, 1))
+                            for (int e = 0; e < 4; ++e) {
+                                const float y = (float)((const C*)V)[(int64_t)(slot - s_begin) * HD + e0 + e];
+                                if (!(fabsf(y) <= 3.4e38f)) x[e] += y;
+                            }
+            if (n_chunks > 1) *(float4*)(part + e0) = make_float4(x[0], x[1], x[2], x[3]);
+            else tree_store<T, 4>(a, node0 + node, h * G + row - node * G, e0, x);
+        }
+}
+
 // ------------------------------------------------------------------------------------------ launches
 template <int HD, typename TOKEN, typename CACHE>
 static void cache_write(const CacheView& c, const RowsView& k, const RowsView& v, const int32_t* seq, const int32_t* slot, int n, hipStream_t s)
@@ -984,14 +1291,18 @@ void launch_cache_read(const CacheView& c, const RowsView& k, const RowsView& v,
     with_types(c.hd, token, c.dtype, [&](auto dim, auto t, auto e) { cache_read<decltype(dim)::value, decltype(t), decltype(e)>(c, k, v, seq, slot, n, s); });
 }
 
-template <int HD, typename T, typename C, int QT>
-static void attention_tree(TreeArgs a, hipStream_t s)
+template <int HD, typename T, typename C>
+static void attention_tree(const TreeArgs& a, int tiles, hipStream_t s)
 {
-    const int units = round_up(a.n_seq * a.c.n_kv * a.chunks, 8);
-    k_attention_tree<HD, T, C, QT><<<dim3((unsigned)units * a.row_blocks), 256, 0, s>>>(a);
-    if (a.chunks > 1) {
-        k_tree_join<HD, T><<<dim3((unsigned)a.n_seq * a.max_nodes * a.heads), 256, 0, s>>>(a);
-    }
+    const dim3 grid(a.c.n_kv * a.row_blocks, a.chunks, a.n_seq);
+    if (tiles == 1) k_attention_tree<HD, T, C, 1><<<grid, 256, 0, s>>>(a);
+    else if (tiles == 2) k_attention_tree<HD, T, C, 2><<<grid, 256, 0, s>>>(a);
+    else k_attention_tree_tall<HD, T, C><<<grid, 256, 0, s>>>(a);
+    if (a.chunks < 2) return;
+    // a row's chunks one after another are slower than a workgroup's start where there are more than a few and the rows leave units idle
+    const int rows = a.max_nodes * (a.heads / a.c.n_kv), groups = 1024 / HD;
+    if (a.chunks > 8 && (int64_t)rows * a.c.n_kv * a.n_seq <= 4096) k_tree_join<HD, T, true><<<dim3(rows, a.c.n_kv, a.n_seq), 256, 0, s>>>(a);
+    else k_tree_join<HD, T, false><<<dim3((rows + groups - 1) / groups, a.c.n_kv, a.n_seq), 256, 0, s>>>(a);
 }
 
 void launch_attention_tree(const TreeArgs& a, int token, int tiles, hipStream_t s)
@@ -1000,8 +1311,7 @@ void launch_attention_tree(const TreeArgs& a, int token, int tiles, hipStream_t 
         typedef decltype(t) T;
         typedef decltype(e) C;
         if constexpr (std::is_same<C, int8_t>::value || std::is_same<C, T>::value) {
-            if (tiles == 1) attention_tree<decltype(dim)::value, T, C, 1>(a, s);
-            else attention_tree<decltype(dim)::value, T, C, 2>(a, s);
+            attention_tree<decltype(dim)::value, T, C>(a, tiles, s);
         }
     });
 }

@@ -22,6 +22,7 @@ int check_cache(const ss_cache* c)
     if (!c) return fail(SS_EINVAL, "cache is NULL");
     if (c->head_dim != 64 && c->head_dim != 128) return fail(SS_EINVAL, "cache: head_dim must be 64 or 128");
     if (!is_half(c->dtype) && c->dtype != SS_I8) return fail(SS_EINVAL, "cache: dtype must be SS_F16, SS_BF16 or SS_I8");
+    if (c->n_kv_heads > 65535) return fail(SS_EINVAL, "cache: more than 65535 heads");
     if (c->n_seq < 0 || c->n_kv_heads < 1 || c->total_slots < 0) return fail(SS_EINVAL, "cache: bad number of sequences, heads or slots");
     if (c->total_slots > 0 && (!c->k || !c->v)) return fail(SS_EINVAL, "cache: k or v is NULL");
     if (!aligned(c->k) || !aligned(c->v)) return fail(SS_EINVAL, "cache: k and v must be 16-byte aligned");
@@ -36,6 +37,7 @@ int check_rows(const ss_rows* r, const char* name)
     if (!is_half(r->dtype)) return fail(SS_EINVAL, "%s: dtype must be SS_F16 or SS_BF16", name);
     if (r->rows < 0) return fail(SS_EINVAL, "%s: negative number of rows", name);
     if (r->rows > 0 && !r->p) return fail(SS_EINVAL, "%s: NULL pointer", name);
+    if (r->row_stride < 0 || r->head_stride < 0 || r->row_stride > (1 << 24)) return fail(SS_EINVAL, "%s: strides must be 0 to 2^24", name);
     if (!aligned(r->p) || r->row_stride % 8 || r->head_stride % 8)
         return fail(SS_EINVAL, "%s must be 16-byte aligned, its strides multiples of 8 elements", name);
     return SS_OK;
@@ -88,7 +90,9 @@ int check_token_list(const ss_cache* c, const ss_rows* k, const ss_rows* v, cons
 int check_tree_counts(int32_t n_heads, int32_t n_kv_heads, int32_t n_seq, int32_t max_context, int32_t max_nodes)
 {
     if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return fail(SS_EINVAL, "n_heads must be a multiple of the key/value heads");
+    if (n_heads > 65535) return fail(SS_EINVAL, "more than 65535 heads");
     if (n_seq < 0 || max_context < 0) return fail(SS_EINVAL, "negative number of sequences or context");
+    if (n_seq > 65535) return fail(SS_EINVAL, "more than 65535 sequences");
     if (max_nodes < 1 || max_nodes > SS_TREE_MAX_NODES) return fail(SS_EINVAL, "max_nodes must be 1 to %d", SS_TREE_MAX_NODES);
     if (max_context > INT_MAX - SS_TREE_MAX_NODES - 256) return fail(SS_EINVAL, "max_context is too large");
     if ((int64_t)n_seq * n_heads * max_nodes > INT_MAX / 4) return fail(SS_EINVAL, "too many rows");
@@ -155,6 +159,7 @@ extern "C" int ss_attention_tree(const ss_cache* cache, const ss_rows* q, const 
     if (!seq && n_seq > cache->n_seq) return fail(SS_EINVAL, "the cache has fewer than %d sequences", n_seq);
     if (n_seq > 0 && !context) return fail(SS_EINVAL, "context is NULL");
     if (n_seq == 0 || q->rows == 0) return SS_OK;
+    if (cache->n_seq == 0) return fail(SS_EINVAL, "the cache has no sequences");
     const ss::TreePlan p = plan_of(n_heads, cache->n_kv_heads, n_seq, max_context, max_nodes);
     const size_t need = part_bytes(p, n_heads, cache->head_dim, n_seq, max_nodes);
     if (need > workspace_bytes || (need > 0 && !workspace))
@@ -211,6 +216,7 @@ extern "C" int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_
     if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return fail(SS_EINVAL, "n_heads must be a multiple of the key/value heads");
     if (q->dtype != k->dtype || q->dtype != v->dtype || q->dtype != out->dtype) return fail(SS_EINVAL, "q, k, v and out differ in type");
     if (k->rows < q->rows || v->rows < q->rows || out->rows < q->rows) return fail(SS_EINVAL, "k, v or out has fewer rows than q");
+    if (n_heads > 65535) return fail(SS_EINVAL, "more than 65535 heads");
     if (n_seq < 0 || max_len < 0) return fail(SS_EINVAL, "negative number of sequences or length");
     if (n_seq > 65535) return fail(SS_EINVAL, "more than 65535 sequences");
     if (max_len > 64 * 65535) return fail(SS_EINVAL, "max_len is too large");

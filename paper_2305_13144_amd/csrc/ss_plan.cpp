@@ -389,12 +389,14 @@ size_t gemm_partial_rows_bound(int n_max)
 TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu)
 {
     TreePlan p;
-    p.tiles = rows <= 16 ? 1 : 2;
+    p.tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 8;
     p.row_blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
-    const long long units = (long long)n_seq * n_kv * p.row_blocks;
-    const long long want = std::max(1LL, std::min(2LL * n_cu / std::max(units, 1LL), (max_len + 255LL) / 256));
-    p.chunk = (int)((max_len + want - 1) / want + 127) / 128 * 128;
-    p.chunks = std::max(1, (max_len + p.chunk - 1) / p.chunk);
+    const long long units = std::max(1LL, (long long)n_seq * n_kv * p.row_blocks), at_once = (p.tiles == 1 ? 3LL : 2LL) * n_cu;
+    long long chunk = (max_len * units + at_once - 1) / at_once;
+    if (n_seq > 1) chunk = std::min(chunk, 768LL);
+    chunk = std::max(chunk, (max_len + kTreeMaxChunks - 1LL) / kTreeMaxChunks);
+    p.chunk = (int)std::min<long long>((std::max(chunk, 256LL) + 127) / 128 * 128, 1 << 30);
+    p.chunks = std::max(1, (int)((max_len + (long long)p.chunk - 1) / p.chunk));
     return p;
 }
 
