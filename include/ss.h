@@ -168,10 +168,17 @@ void ss_weights_destroy(ss_weights* w);
  *   Other users of the GPU cannot take them: a program that needs that memory itself sets 0.  With or without them the
  *   weights are the same values; logits agree to the rounding differences between launch shapes, as the two forms share
  *   out a sum differently.
+ *   option SS_OPT_CACHE_BITS, value = 16 (a new handle) or 8: how the calls that follow hold keys and values.  8: as ss_cache does with
+ *   SS_I8 below, one byte per element and one float per vector of head_dim: half the memory per slot (plus 4 bytes in 64 or
+ *   128), half the bytes that a decode step reads.  A value is off by at most max|x| / 254 of its vector; a prompt's own attention
+ *   reads its keys, values and queries as halves before they are coded.  Every entry point works with either; the statistics do
+ *   not change.  Decode steps of few rows with short contexts are slower, as the rotation and the attention are launches of their own,
+ *   and small models take no row's step in one workgroup.
  * Errors: SS_EINVAL (NULL handle, unknown option, value out of range), SS_ESTATE (a call is in flight).
  */
 #define SS_OPT_IN_FLIGHT 2
 #define SS_OPT_WEIGHT_COPIES 3
+#define SS_OPT_CACHE_BITS 4
 #define SS_IN_FLIGHT_MAX 4
 #define SS_IN_FLIGHT_DEFAULT 4
 int ss_set_option(ss_weights* w, int32_t option, int32_t value);
@@ -251,6 +258,19 @@ int ss_decode_microbatch_static(ss_weights* w, const int32_t* prompt_tokens, con
  */
 int ss_forward_logits(ss_weights* w, const int32_t* tokens, const int32_t* offsets, int32_t B,
                       const int32_t* n_prompt, int32_t all_prompt_logits, float* logits_out, void* hip_stream);
+
+/*
+ * Logits of drafted trees: what a program that drafts several continuations of every row checks them with, in one forward.
+ * Each of the B prompts is processed as in ss_forward_logits; then all nodes of all trees are fed in one forward: node t of a row stands
+ * at the position behind its parent's (parents[t] = -1: behind the prompt) and sees the prompt, the nodes above it and itself.
+ *   node_tokens   host, int32[node_offsets[B]], ids in [0, vocab), row after row
+ *   node_offsets  host, int32[B+1] from 0, not decreasing; a row may have no nodes, at most SS_TREE_MAX_NODES (below)
+ *   parents       host, int32[node_offsets[B]]: an earlier node of the same row, counted from the row's first, or -1
+ *   logits_out    host, float32, [vocab] rows: for each row that of its prompt's last position, then those of its nodes
+ * Errors: SS_EINVAL (as ss_forward_logits; bad nodes; a node beyond 4096 positions), SS_ENOMEM, SS_EDEVICE, SS_ESTATE.
+ */
+int ss_tree_logits(ss_weights* w, const int32_t* prompt_tokens, const int32_t* prompt_offsets, int32_t B, const int32_t* node_tokens,
+                   const int32_t* node_offsets, const int32_t* parents, float* logits_out, void* hip_stream);
 
 typedef struct {
     int32_t n_mb_first, n_mb_failure; /* micro-batches in the first pass and in the recomputation pass */

@@ -19,13 +19,13 @@ SS_OK, SS_EINVAL, SS_ENOMEM, SS_EDEVICE, SS_ESTATE = 0, -1, -2, -3, -4
 SS_SORT, SS_BIN, SS_FCR, SS_VBS, SS_COMPACT = 1, 2, 4, 8, 16
 SS_VBS_CLAMP_FLOOR, SS_VBS_PAPER_POW2 = 0, 1
 SS_OPT_IN_FLIGHT, SS_IN_FLIGHT_MAX, SS_IN_FLIGHT_DEFAULT = 2, 4, 4
-SS_OPT_WEIGHT_COPIES = 3
+SS_OPT_WEIGHT_COPIES, SS_OPT_CACHE_BITS = 3, 4
 SS_BF16, SS_F32, SS_F16, SS_I8 = 0, 1, 2, 3
 SS_TREE_MAX_NODES = 1024
 FLAG_BITS = dict(SORT=SS_SORT, BIN=SS_BIN, FCR=SS_FCR, VBS=SS_VBS, COMPACT=SS_COMPACT)
 
 EXPORTS = ["ss_last_error", "ss_set_verbose", "ss_set_gemm_mode", "ss_schedule", "ss_schedule_failures", "ss_plan_free", "ss_weights_create",
-           "ss_weights_destroy", "ss_set_option", "ss_decode_microbatch", "ss_decode_microbatch_static", "ss_forward_logits", "ss_run_group", "ss_generate_microbatch",
+           "ss_weights_destroy", "ss_set_option", "ss_decode_microbatch", "ss_decode_microbatch_static", "ss_forward_logits", "ss_tree_logits", "ss_run_group", "ss_generate_microbatch",
            "ss_run_group_generate", "ss_bench_decode_step", "ss_bench_decode_steps_in_flight", "ss_bench_weight_stream", "ss_bench_read_stream",
            "ss_cache_write", "ss_cache_read", "ss_attention_tree", "ss_attention_tree_workspace", "ss_tree_mask", "ss_attention_packed"]
 
@@ -114,6 +114,7 @@ def lib():
                                            C.POINTER(ss_stats), vp]
         L.ss_decode_microbatch_static.argtypes = L.ss_decode_microbatch.argtypes
         L.ss_forward_logits.argtypes = [vp, i32p, i32p, C.c_int32, i32p, C.c_int32, vp, vp]
+        L.ss_tree_logits.argtypes = [vp, i32p, i32p, C.c_int32, i32p, i32p, i32p, vp, vp]
         L.ss_run_group.argtypes = [vp, i32p, i32p, C.c_int32, i32p, i32p, C.c_int32, C.POINTER(ss_policy), i32p, i32p,
                                    C.POINTER(ss_group_stats), vp]
         L.ss_generate_microbatch.argtypes = [vp, i32p, i32p, C.c_int32, C.c_int32, C.POINTER(ss_gen_opts), C.c_uint32,
@@ -255,6 +256,15 @@ def ss_forward_logits(w: Weights, tokens, offsets, n_prompt, all_prompt_logits: 
     rows = int(lens.sum()) if all_prompt_logits else int((lens - npz + 1).sum())
     out = np.empty((rows, w.shape.vocab), np.float32)
     _check(lib().ss_forward_logits(w.h, _ptr(tk), _ptr(of), B, _ptr(npz), int(all_prompt_logits), _ptr(out), stream))
+    return out
+
+
+def ss_tree_logits(w: Weights, prompt_tokens, prompt_offsets, node_tokens, node_offsets, parents, stream: Optional[int] = None) -> np.ndarray:
+    """[B + nodes, vocab]: for each row the logits of its prompt's last position, then those of its drafted nodes."""
+    pt, po, nt, no, pa = (_i32(a) for a in (prompt_tokens, prompt_offsets, node_tokens, node_offsets, parents))
+    B = len(po) - 1
+    out = np.empty((B + int(no[-1]), w.shape.vocab), np.float32)
+    _check(lib().ss_tree_logits(w.h, _ptr(pt), _ptr(po), B, _ptr(nt), _ptr(no), _ptr(pa), _ptr(out), stream))
     return out
 
 

@@ -208,6 +208,66 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheView c, RowsView k, Row
     }
 }
 
+// The engine's way into the cache.  As k_rope_append: row j's sums of q|k|v, whose columns are in the order of qkv_col, rotated at its
+// position; here a vector is HD / 8 lanes', 4 elements of each half per lane.  Keys and values are coded from their fp32 values.
+template <int HD, typename CACHE>
+__global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* __restrict__ part, int ksplit, size_t part_stride,
+                                                      const float* __restrict__ rcos, const float* __restrict__ rsin, f16_t* __restrict__ rows,
+                                                      int dense_kv, CacheView c, const int32_t* __restrict__ slot, int d)
+{
+    constexpr int LPV = HD / 8, VPP = 256 / LPV, MAX_SPLIT = 8;
+    const int j = blockIdx.x, vec = blockIdx.y * VPP + threadIdx.x / LPV, e = threadIdx.x % LPV * 4;
+    const int count = *st.d_n, seq = st.tr_row[j], pos = st.tr_pos[j], at = slot[j];
+    if (j >= count || vec >= 3 * c.n_kv) return;
+    const int which = vec / c.n_kv, h = vec - which * c.n_kv;   // 0 q, 1 k, 2 v
+    const float* p = part + (size_t)j * 3 * d + which * d + h * HD + qkv_col(e);
+    float4 a[MAX_SPLIT], b[MAX_SPLIT];   // every slice's loads before the first sum
+#pragma unroll
+    for (int s = 0; s < MAX_SPLIT; ++s)
+        if (s < ksplit) {
+            a[s] = *(const float4*)(p + s * part_stride);
+            b[s] = *(const float4*)(p + s * part_stride + 16);
+        }
+    const float4 cs = *(const float4*)(rcos + (size_t)pos * (HD / 2) + e), sn = *(const float4*)(rsin + (size_t)pos * (HD / 2) + e);
+#pragma unroll
+    for (int s = 1; s < MAX_SPLIT; ++s)
+        if (s < ksplit) {
+            a[0] = make_float4(a[0].x + a[s].x, a[0].y + a[s].y, a[0].z + a[s].z, a[0].w + a[s].w);
+            b[0] = make_float4(b[0].x + b[s].x, b[0].y + b[s].y, b[0].z + b[s].z, b[0].w + b[s].w);
+        }
+    float x[8] = {a[0].x, a[0].y, a[0].z, a[0].w, b[0].x, b[0].y, b[0].z, b[0].w};
+    if (which < 2) {
+        const float cc[4] = {cs.x, cs.y, cs.z, cs.w}, ss[4] = {sn.x, sn.y, sn.z, sn.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 r = rotated(x[i], x[i + 4], cc[i], ss[i]);
+            x[i] = r.x;
+            x[i + 4] = r.y;
+        }
+    }
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = f2kv(x[2 * i]) | (uint32_t)f2kv(x[2 * i + 1]) << 16;
+    if (which == 0 || dense_kv) {
+        f16_t* to = rows + (size_t)j * 3 * d + which * d + h * HD + e;
+        *(uint2*)to = make_uint2(w[0], w[1]);
+        *(uint2*)(to + HD / 2) = make_uint2(w[2], w[3]);
+    }
+    if (which == 0) return;
+    const int64_t to = c.start[seq] * c.n_kv + (int64_t)h * c.slots[seq] + at;
+    CACHE* const vector = (CACHE*)(which == 1 ? c.k : c.v) + to * HD + e;
+    if constexpr (std::is_same<CACHE, int8_t>::value) {
+        uint2 codes;
+        const float scale = quantise<HD>(x, &codes);
+        *(uint32_t*)vector = codes.x;
+        *(uint32_t*)(vector + HD / 2) = codes.y;
+        if (e == 0) (which == 1 ? c.k_scale : c.v_scale)[to] = scale;
+    } else {
+        *(uint2*)vector = make_uint2(w[0], w[1]);
+        *(uint2*)(vector + HD / 2) = make_uint2(w[2], w[3]);
+    }
+}
+
 // ------------------------------------------------------------------------------------------ attention over a cache
 // Rows of a unit: the (node, query head) pairs of one sequence and one key/value head, row r = node * G + (head within its
 // group), G = query heads per key/value head; a decode step is the tree of one node.  A wave takes 16 * QT rows through steps of
@@ -761,9 +821,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     // query heads that share a head of keys and values are on one die
     const int G = a.heads / a.n_kv, hk = blockIdx.x % a.n_kv, h = hk * G + blockIdx.x / a.n_kv;
     const int i_seq = blockIdx.y, qt = gridDim.z - 1 - blockIdx.z;
-    const int first = a.offsets[i_seq], end = a.offsets[i_seq + 1];
-    if (first < 0 || end > a.q.rows) return;
-    const int p = min(end - first, a.max_len);
+    const int first = a.offsets[i_seq], count = a.lengths ? a.lengths[i_seq] : a.offsets[i_seq + 1] - first;
+    if (first < 0 || first + (int64_t)count > a.q.rows) return;
+    const int p = min(count, a.max_len);
     const int q0 = qt * QW * NW;
     if (q0 >= p) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1289,6 +1349,22 @@ void launch_cache_read(const CacheView& c, const RowsView& k, const RowsView& v,
                        hipStream_t s)
 {
     with_types(c.hd, token, c.dtype, [&](auto dim, auto t, auto e) { cache_read<decltype(dim)::value, decltype(t), decltype(e)>(c, k, v, seq, slot, n, s); });
+}
+
+void launch_rotate_store(const MbState& st, const float* qkv_part, int ksplit, size_t part_stride, const float* rope_cos, const float* rope_sin,
+                         f16_t* rows, int dense_kv, const CacheView& c, const int32_t* slot, int d, int n_max, hipStream_t s)
+{
+    auto go = [&](auto dim, auto t) {
+        constexpr int HD = decltype(dim)::value;
+        const dim3 grid(n_max, (3 * c.n_kv * HD + 2047) / 2048);
+        k_rotate_store<HD, decltype(t)><<<grid, 256, 0, s>>>(st, qkv_part, ksplit, part_stride, rope_cos, rope_sin, rows, dense_kv, c, slot, d);
+    };
+    auto by_cache = [&](auto dim) {
+        if (c.dtype == kI8) go(dim, int8_t{});
+        else go(dim, _Float16{});
+    };
+    if (c.hd == 128) by_cache(std::integral_constant<int, 128>{});
+    else by_cache(std::integral_constant<int, 64>{});
 }
 
 template <int HD, typename T, typename C>

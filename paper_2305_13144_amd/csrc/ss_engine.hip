@@ -122,12 +122,13 @@ struct Buf {
 struct Workspace {
     Buf x, h, ao, act, qrot, pqkv, pd, hsel, logits, kv, ints, i64s, draws;
     Buf logits2, steps;   // ss_forward_logits: the other logits buffer, the tables of every decode step
+    Buf rows16, shares;   // attention over 8-bit caches or of trees: q|k|v as halves, chunks of long contexts
     // Non-null: every buffer is carved out of [arena, arena + arena_bytes) instead of being allocated.
     char* arena = nullptr;
     size_t arena_bytes = 0;
     void release()
     {
-        for (Buf* b : {&x, &h, &ao, &act, &qrot, &pqkv, &pd, &hsel, &logits, &kv, &ints, &i64s, &draws, &logits2, &steps})
+        for (Buf* b : {&x, &h, &ao, &act, &qrot, &pqkv, &pd, &hsel, &logits, &kv, &ints, &i64s, &draws, &logits2, &steps, &rows16, &shares})
             b->release();
     }
 };
@@ -177,6 +178,14 @@ struct LogitPipe {
     }
 };
 
+// A forward over the nodes of drafted trees (ss_tree_logits): tables of its token-rows on the device.
+struct TreeForward {
+    const int32_t *slot, *nodes, *context;   // slot of each node; first node of each row, and their number; slots before a row's nodes
+    const uint64_t* mask;
+    int rows, max_nodes, max_context;
+    ss::TreePlan plan;
+};
+
 struct Lane {
     hipStream_t stream = nullptr;
     LogitPipe pipe;
@@ -185,7 +194,10 @@ struct Lane {
     Workspace ws;
     int32_t* d_sel = nullptr;  // carved from ws.ints
     MbState st{};
-    size_t kv_layer_stride = 0;  // elements between a layer's K and V, and 2x that between layers
+    size_t kv_layer_stride = 0;  // elements between a layer's K and V, and 2x that between layers (8-bit caches: see cache_view)
+    size_t kv_slots = 0;         // slots of the micro-batch
+    int batch_rows = 0;          // rows of the micro-batch, or of those that share forwards
+    const TreeForward* tree = nullptr;   // the forward in flight is one over trees
     // token choice of the forward in flight: cur_inv_temp == 0 selects the argmax; otherwise sampling with the
     // draws in cur_draws, or (cur_draws == nullptr) generated from (cur_seed, cur_ids[row], token number)
     const float* cur_draws = nullptr;
@@ -215,6 +227,7 @@ struct ss_weights {
     std::atomic<int> busy{0};
     void* scratch_ptr = nullptr;   // device address of this device's static scratch array
     int in_flight = SS_IN_FLIGHT_DEFAULT;       // micro-batches a group pass keeps in flight (1 to kLanes)
+    bool cache8 = false;                        // keys and values are held in 8 bits (SS_OPT_CACHE_BITS)
     // The 12-bit weight copies are read and changed under copies_mu: a call holds it while its body runs, a call on another
     // handle that is short of memory takes it to have them.
     std::mutex copies_mu;
@@ -463,8 +476,9 @@ int check_cfg(const ss_model_cfg* c)
 
 // ---------------------------------------------------------------------------------------- workspace
 // n_max token-rows in a forward, B micro-batch rows, n_sel rows whose logits are wanted,
-// slots = total key/value slots of the micro-batch.
-int ensure_workspace(const ss_weights* w, Lane& ln, int n_max, int B, int n_sel, size_t slots, int max_new, hipStream_t s)
+// slots = total key/value slots of the micro-batch; tree_shares: bytes of chunks of a forward over trees (0: there is none).
+int ensure_workspace(const ss_weights* w, Lane& ln, int n_max, int B, int n_sel, size_t slots, int max_new, hipStream_t s, bool trees = false,
+                     size_t tree_shares = 0)
 {
     const ss_model_cfg& c = w->cfg;
     const int d = c.d_model, F = c.d_ffn, V = c.vocab;
@@ -473,6 +487,10 @@ int ensure_workspace(const ss_weights* w, Lane& ln, int n_max, int B, int n_sel,
     const size_t Bp = ss::round_up(B, 4), np = ss::round_up(n_max, 4), sp = ss::round_up(n_sel, 4);
     const size_t n_i32 = 4 + 3 * np + 5 * Bp + 2 * sp + (size_t)B * max_new;
     ln.kv_layer_stride = slots * d;
+    ln.kv_slots = slots;
+    ln.batch_rows = B;
+    const size_t chunks = (std::min<size_t>(slots, ss::kMaxPos) + ss::kTreeDecodeChunk - 1) / ss::kTreeDecodeChunk;
+    const size_t decode_shares = w->cache8 && chunks > 1 ? (size_t)B * chunks * c.n_heads * (c.head_dim + 4) * 4 : 0;
     // Partial-sum buffers hold [ksplit][rows][N] for whatever plan a forward over 1..n_max rows gets.
     // gate|up has none: its SwiGLU epilogue needs whole sums, so it is never cut in slices.
     struct Item { Buf* b; size_t bytes; bool zero; };
@@ -486,7 +504,9 @@ int ensure_workspace(const ss_weights* w, Lane& ln, int n_max, int B, int n_sel,
         {&ws.pd, ss::gemm_partial_rows_bound(n_max) * d * 4, false},
         {&ws.hsel, (size_t)ss::round_up(n_sel, 128) * d * 2, true},
         {&ws.logits, (size_t)ss::round_up(n_sel, 16) * V * 4, false},
-        {&ws.kv, (size_t)c.n_layers * 2 * slots * d * 2, false},
+        {&ws.kv, (size_t)c.n_layers * 2 * slots * (w->cache8 ? d + c.n_heads * 4 : d * 2), false},
+        {&ws.rows16, w->cache8 || trees ? nr * 3 * d * 2 : 0, false},
+        {&ws.shares, std::max(decode_shares, tree_shares), false},
         {&ws.ints, n_i32 * 4, false},
         {&ws.i64s, Bp * 8, false},
     };
@@ -529,6 +549,95 @@ int ensure_workspace(const ss_weights* w, Lane& ln, int n_max, int B, int n_sel,
     st.row_stay = nullptr;
     st.row_so = ws.i64s.as<int64_t>();
     return SS_OK;
+}
+
+// A layer's keys and values for the operators that read them as a cache.  Held in 8 bits a layer is the codes of keys and of values, then
+// the scales of both.
+ss::CacheView cache_view(const ss_weights* w, const Lane& ln, int layer)
+{
+    const ss_model_cfg& c = w->cfg;
+    const size_t slots = ln.kv_slots, d = c.d_model;
+    ss::CacheView v{};
+    v.start = ln.st.row_so;
+    v.slots = ln.st.row_cap;
+    v.total = (int64_t)slots;
+    v.n_seq = ln.batch_rows;
+    v.n_kv = c.n_heads;
+    v.hd = c.head_dim;
+    if (w->cache8) {
+        char* at = ln.ws.kv.as<char>() + (size_t)layer * 2 * slots * (d + c.n_heads * 4);
+        v.dtype = ss::kI8;
+        v.k = at;
+        v.v = at + slots * d;
+        v.k_scale = (float*)(at + 2 * slots * d);
+        v.v_scale = v.k_scale + slots * c.n_heads;
+    } else {
+        v.dtype = ss::kF16;
+        v.k = ln.ws.kv.as<ss::kv_t>() + (size_t)layer * 2 * ln.kv_layer_stride;
+        v.v = (ss::kv_t*)v.k + ln.kv_layer_stride;
+    }
+    return v;
+}
+
+// Attention of one layer through the cache operators, q|k|v's sums being in ws.pqkv: forwards with an 8-bit cache, and those over trees.
+void cache_attention(const ss_weights* w, Lane& ln, int layer, int n, int ksplit, size_t part_stride, bool decode, hipStream_t s)
+{
+    const ss_model_cfg& c = w->cfg;
+    const MbState& st = ln.st;
+    const ss::CacheView cache = cache_view(w, ln, layer);
+    const int64_t d = c.d_model;
+    f16_t* rows = ln.ws.rows16.as<f16_t>();
+    const bool prompt = !decode && !ln.tree;
+    ss::launch_rotate_store(st, ln.ws.pqkv.as<float>(), ksplit, part_stride, w->rope_cos, w->rope_sin, rows, prompt, cache,
+                            ln.tree ? ln.tree->slot : st.tr_pos, c.d_model, n, s);
+    const ss::RowsView q{rows, 3 * d, c.head_dim, n}, out{ln.ws.ao.as<f16_t>(), 0, 0, n};
+    const float scale = 1.f / std::sqrt((float)c.head_dim);
+    if (prompt) {
+        ss::PackedArgs a{};
+        a.q = q;
+        a.k = {rows + d, 3 * d, c.head_dim, n};
+        a.v = {rows + 2 * d, 3 * d, c.head_dim, n};
+        a.out = out;
+        a.packed_d = c.d_model;
+        a.offsets = st.row_j0;
+        a.lengths = st.row_plen;
+        a.scale = scale;
+        a.heads = a.n_kv = c.n_heads;
+        a.max_len = ln.prompt_max_len;
+        ss::launch_attention_packed(a, c.head_dim, ss::kF16, ln.prompt_rows, s);
+        return;
+    }
+    ss::TreeArgs a{};
+    a.c = cache;
+    a.q = q;
+    a.out = out;
+    a.packed_d = c.d_model;
+    a.part = ln.ws.shares.as<float>();
+    a.scale = scale;
+    a.heads = c.n_heads;
+    if (const TreeForward* t = ln.tree) {
+        a.context = t->context;
+        a.nodes = t->nodes;
+        a.mask = t->mask;
+        a.n_seq = t->rows;
+        a.max_nodes = t->max_nodes;
+        a.words = (t->max_nodes + 63) / 64;
+        a.chunk = t->plan.chunk;
+        a.chunks = t->plan.chunks;
+        a.row_blocks = t->plan.row_blocks;
+        ss::launch_attention_tree(a, ss::kF16, t->plan.tiles, s);
+        return;
+    }
+    a.seq = st.tr_row;
+    a.context = st.tr_pos;
+    a.d_n = st.d_n;
+    a.n_seq = n;
+    a.max_nodes = 1;
+    a.words = 1;
+    a.chunk = ss::kTreeDecodeChunk;
+    a.chunks = std::max(1, (std::min(ln.max_ctx, ss::kMaxPos) + ss::kTreeDecodeChunk - 1) / ss::kTreeDecodeChunk);
+    a.row_blocks = 1;
+    ss::launch_attention_tree(a, ss::kF16, 1, s);
 }
 
 // Launch plans of the five projections of a forward over n token-rows with n_sel logit rows; rotate: q|k|v of whole launches are finished there.
@@ -650,7 +759,10 @@ bool few_forward(const ss_weights* w, Lane& ln, int n, hipStream_t s)
         const Layer& L = w->layers[l];
         ss::kv_t* kc = ws.kv.as<ss::kv_t>() + (size_t)l * 2 * ln.kv_layer_stride;
         few.qkv(L, s);
-        ss::launch_attention_decode(st, pqkv, 1, (size_t)n * 3 * d, kc, kc + ln.kv_layer_stride, w->rope_cos, w->rope_sin, ao, d, c.n_heads,
+        if (w->cache8)
+            cache_attention(w, ln, l, n, 1, (size_t)n * 3 * d, true, s);
+        else
+            ss::launch_attention_decode(st, pqkv, 1, (size_t)n * 3 * d, kc, kc + ln.kv_layer_stride, w->rope_cos, w->rope_sin, ao, d, c.n_heads,
                                     c.head_dim, n, ln.plan_rows ? ln.plan_rows : n, ln.prompt_rows, ln.max_ctx, ws.qrot.as<float>(), s);
         few.rest(L, s);
     }
@@ -679,7 +791,8 @@ void forward(const ss_weights* w, Lane& ln, int n, int n_sel, const int32_t* d_s
     const int Fp = ss::padded_k(F);
 
     // small models: a row's whole step in one workgroup
-    if (decode && !d_sel && !d_nsel && n_sel == n && ss::row_step_plan(c.n_layers, d, F, V, n, ln.max_ctx, w->n_cu, hd)) {
+    const bool by_cache = w->cache8 || ln.tree;   // attention through the cache operators
+    if (decode && !by_cache && !d_sel && !d_nsel && n_sel == n && ss::row_step_plan(c.n_layers, d, F, V, n, ln.max_ctx, w->n_cu, hd)) {
         const bool sample = ln.cur_inv_temp > 0.f;
         ss::RowStepArgs a = row_step_args(w, ln);
         a.am = ln.cur_choose && !sample ? st.am : nullptr;
@@ -693,7 +806,7 @@ void forward(const ss_weights* w, Lane& ln, int n, int n_sel, const int32_t* d_s
     if (decode && !d_sel && !d_nsel && n_sel == n && n <= ss::kFewRows && few_forward(w, ln, n, s)) return;
 
     const int plan_rows = decode && ln.plan_rows ? ln.plan_rows : n;
-    const Plans pl = make_plans(w, plan_rows, decode ? plan_rows : n_sel, !decode);
+    const Plans pl = make_plans(w, plan_rows, decode ? plan_rows : n_sel, !decode && !by_cache);
     const ss::GemmPlan &p_qkv = pl.qkv, &p_o = pl.o, &p_gu = pl.gu, &p_d = pl.down, &p_lm = pl.lm;
     const int ks_qkv = p_qkv.ksplit, ks_o = p_o.ksplit, ks_d = p_d.ksplit;
     const size_t st_qkv = (size_t)n * 3 * d, st_d = (size_t)n * d;
@@ -703,7 +816,7 @@ void forward(const ss_weights* w, Lane& ln, int n, int n_sel, const int32_t* d_s
 
     // an unsliced launch of the block kernel adds its sums to the residual stream itself, and in a prompt forward rotates
     // and stores q, k and v (every key of a row must be in place before any of its queries attends)
-    const bool whole_qkv = !decode && p_qkv.block >= 0 && ks_qkv == 1;
+    const bool whole_qkv = !decode && !by_cache && p_qkv.block >= 0 && ks_qkv == 1;
     const bool whole_o = p_o.block >= 0 && ks_o == 1, whole_d = p_d.block >= 0 && ks_d == 1;
     float* const add_d = whole_d ? nullptr : pd;   // what the next norm adds to the residual stream
 
@@ -719,7 +832,9 @@ void forward(const ss_weights* w, Lane& ln, int n, int n_sel, const int32_t* d_s
         } else {
             ss::launch_gemm(mk(L.wqkv, h, pqkv, nullptr, n, 0, p_qkv), ss::EPI_PARTIAL, s);
         }
-        if (decode) {   // one token-row per row: rotation and append are fused into the attention kernel
+        if (by_cache) {
+            cache_attention(w, ln, l, n, ks_qkv, st_qkv, decode, s);
+        } else if (decode) {   // one token-row per row: rotation and append are fused into the attention kernel
             ss::launch_attention_decode(st, pqkv, ks_qkv, st_qkv, kc, vc, w->rope_cos, w->rope_sin, ao, d, H, hd, n,
                                         plan_rows, ln.prompt_rows, ln.max_ctx, qrot, s);
         } else {
@@ -928,7 +1043,7 @@ int decode_microbatch_impl(const ss_weights* w, Lane& ln, const int32_t* prompt_
         };
         const int n_first = live(1);
         auto in_rows = [&](int n) {   // at the longest context; shorter ones, and counts of rows in between, then go that way too
-            return ss::row_step_plan(c.n_layers, c.d_model, c.d_ffn, c.vocab, n, ln.prompt_max_len + steps - 1, w->n_cu, c.head_dim);
+            return !w->cache8 && ss::row_step_plan(c.n_layers, c.d_model, c.d_ffn, c.vocab, n, ln.prompt_max_len + steps - 1, w->n_cu, c.head_dim);
         };
         const bool at_once = steps > 1 && in_rows(n_first) && in_rows(live(steps - 1));
         if (at_once) {
@@ -1310,6 +1425,11 @@ extern "C" int ss_set_option(ss_weights* w, int32_t option, int32_t value)
             return SS_OK;
         });
     }
+    if (option == SS_OPT_CACHE_BITS) {
+        if (value != 8 && value != 16) return ss::fail(SS_EINVAL, "SS_OPT_CACHE_BITS takes 8 or 16");
+        w->cache8 = value == 8;
+        return SS_OK;
+    }
     return ss::fail(SS_EINVAL, "unknown option %d", option);
 }
 
@@ -1688,6 +1808,131 @@ extern "C" int ss_forward_logits(ss_weights* w, const int32_t* tokens, const int
     hipStream_t s = hip_stream ? (hipStream_t)hip_stream : ln.stream;
     return with_memory(
         w, [&] { return forward_logits_impl(w, ln, s, tokens, offsets, B, n_prompt, all_prompt_logits, logits_out); });
+}
+
+namespace {
+
+// Two forwards: the prompts, and the nodes of all trees on top of them.
+int tree_logits_impl(const ss_weights* w, Lane& ln, hipStream_t s, const int32_t* prompt_tokens, const int32_t* prompt_offsets, int32_t B,
+                     const int32_t* node_tokens, const int32_t* node_offsets, const int32_t* parents, float* logits_out)
+{
+    const ss_model_cfg& c = w->cfg;
+    const int V = c.vocab, N = node_offsets[B], n_p = prompt_offsets[B];
+    std::vector<int32_t> lens(B), slab(B), limit(B, 1), sel(B), depth(N);
+    size_t slots = 0;
+    TreeForward tree{};
+    tree.rows = B;
+    for (int i = 0; i < B; ++i) {
+        const int n = node_offsets[i + 1] - node_offsets[i];
+        lens[i] = prompt_offsets[i + 1] - prompt_offsets[i];
+        sel[i] = prompt_offsets[i + 1] - 1;
+        slab[i] = lens[i] + n;
+        slots += (size_t)slab[i];
+        tree.max_nodes = std::max(tree.max_nodes, n);
+        tree.max_context = std::max(tree.max_context, lens[i]);
+        if (lens[i] > ss::kMaxPos) return ss::fail(SS_EINVAL, "row %d: more than %d positions", i, ss::kMaxPos);
+        for (int t = 0; t < n; ++t) {
+            const int at = node_offsets[i] + t, up = parents[at];
+            if (up < -1 || up >= t) return ss::fail(SS_EINVAL, "row %d: parents[%d] must be -1 or an earlier node of the row", i, t);
+            depth[at] = up < 0 ? 0 : depth[node_offsets[i] + up] + 1;
+            if (lens[i] + depth[at] >= ss::kMaxPos) return ss::fail(SS_EINVAL, "row %d: node %d is beyond %d positions", i, t, ss::kMaxPos);
+        }
+    }
+    size_t share_bytes = 0;
+    const int words = (tree.max_nodes + 63) / 64;
+    std::vector<uint64_t> mask((size_t)N * words);
+    if (N > 0) {
+        tree.plan = ss::tree_plan(B, c.n_heads, tree.max_nodes, tree.max_context + tree.max_nodes, w->n_cu);
+        if (tree.plan.chunks > 1) share_bytes = (size_t)B * tree.plan.chunks * tree.max_nodes * c.n_heads * (c.head_dim + 4) * 4;
+        for (int i = 0; i < B; ++i)
+            if (int rc = ss_tree_mask(parents + node_offsets[i], node_offsets[i + 1] - node_offsets[i], tree.max_nodes,
+                                      mask.data() + (size_t)node_offsets[i] * words))
+                return rc;
+    }
+    HIPCHK(hipSetDevice(w->device));
+    if (int rc = ensure_workspace(w, ln, std::max({n_p, N, B}), B, std::max(N, B), slots, 1, s, true, share_bytes)) return rc;
+    // tables of the second forward: masks, then counts, tokens, rows, positions and slots of the nodes, first nodes, contexts
+    std::vector<int32_t> tab(mask.size() * 2 + 4 + 4 * (size_t)N + 2 * (size_t)B + 1);
+    int32_t* const t0 = tab.data() + mask.size() * 2;
+    std::copy(mask.begin(), mask.end(), (uint64_t*)tab.data());
+    t0[0] = N;
+    for (int i = 0; i < B; ++i) {
+        for (int at = node_offsets[i]; at < node_offsets[i + 1]; ++at) {
+            t0[4 + at] = node_tokens[at];
+            t0[4 + N + at] = i;
+            t0[4 + 2 * N + at] = lens[i] + depth[at];
+            t0[4 + 3 * N + at] = lens[i] + at - node_offsets[i];
+        }
+        t0[4 + 4 * N + i] = node_offsets[i];
+        t0[4 + 4 * N + B + 1 + i] = lens[i];
+    }
+    t0[4 + 4 * N + B] = N;
+    if (int rc = ln.ws.steps.ensure(tab.size() * 4, false)) return rc;
+    HIPCHK(hipMemcpyAsync(ln.ws.steps.p, tab.data(), tab.size() * 4, hipMemcpyHostToDevice, s));
+    if (int rc = upload_prompt_state(ln, prompt_tokens, prompt_offsets, lens.data(), B, slab.data(), limit.data(), sel, B, s)) return rc;
+    struct Restore {   // the lane is as it was, however the call ends, and nothing of it still runs
+        Lane& ln;
+        hipStream_t s;
+        MbState st;
+        ~Restore()
+        {
+            (void)hipStreamSynchronize(s);
+            ln.st = st;
+            ln.tree = nullptr;
+            ln.cur_choose = true;
+        }
+    } restore{ln, s, ln.st};
+    ln.cur_choose = false;
+    const size_t row_bytes = (size_t)V * 4;
+    const float* logits = ln.ws.logits.as<float>();
+    forward(w, ln, n_p, B, ln.d_sel, ln.st.d_nlive, false, s);
+    for (int i = 0; i < B; ++i)
+        HIPCHK(hipMemcpyAsync(logits_out + ((size_t)i + node_offsets[i]) * V, logits + (size_t)i * V, row_bytes, hipMemcpyDeviceToHost, s));
+    if (N > 0) {
+        const int32_t* d0 = ln.ws.steps.as<int32_t>() + mask.size() * 2;
+        ln.st.d_n = const_cast<int32_t*>(d0);
+        ln.st.tr_tok = ln.st.d_n + 4;
+        ln.st.tr_row = ln.st.d_n + 4 + N;
+        ln.st.tr_pos = ln.st.d_n + 4 + 2 * N;
+        tree.slot = d0 + 4 + 3 * N;
+        tree.nodes = d0 + 4 + 4 * N;
+        tree.context = d0 + 4 + 4 * N + B + 1;
+        tree.mask = ln.ws.steps.as<uint64_t>();
+        ln.tree = &tree;
+        forward(w, ln, N, N, nullptr, nullptr, false, s);
+        for (int i = 0; i < B; ++i)
+            if (node_offsets[i + 1] > node_offsets[i])
+                HIPCHK(hipMemcpyAsync(logits_out + ((size_t)i + 1 + node_offsets[i]) * V, logits + (size_t)node_offsets[i] * V,
+                                      (size_t)(node_offsets[i + 1] - node_offsets[i]) * row_bytes, hipMemcpyDeviceToHost, s));
+    }
+    HIPCHK(hipStreamSynchronize(s));
+    HIPCHK(hipGetLastError());
+    return SS_OK;
+}
+
+}  // namespace
+
+extern "C" int ss_tree_logits(ss_weights* w, const int32_t* prompt_tokens, const int32_t* prompt_offsets, int32_t B, const int32_t* node_tokens,
+                              const int32_t* node_offsets, const int32_t* parents, float* logits_out, void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_prompts(w, prompt_tokens, prompt_offsets, B)) return rc;
+    if (!node_offsets || !logits_out) return ss::fail(SS_EINVAL, "NULL argument");
+    if (node_offsets[0] != 0) return ss::fail(SS_EINVAL, "node_offsets[0] must be 0");
+    for (int i = 0; i < B; ++i) {
+        if (node_offsets[i + 1] < node_offsets[i]) return ss::fail(SS_EINVAL, "non-monotone node_offsets at row %d", i);
+        if (node_offsets[i + 1] - node_offsets[i] > SS_TREE_MAX_NODES) return ss::fail(SS_EINVAL, "row %d: more than %d nodes", i, SS_TREE_MAX_NODES);
+    }
+    if (node_offsets[B] > 0 && (!node_tokens || !parents)) return ss::fail(SS_EINVAL, "NULL argument");
+    for (int t = 0; t < node_offsets[B]; ++t)
+        if (node_tokens[t] < 0 || node_tokens[t] >= w->cfg.vocab) return ss::fail(SS_EINVAL, "token id %d out of range", node_tokens[t]);
+    BusyGuard guard(w);
+    if (!guard.ok) return ss::fail(SS_ESTATE, "another call is in flight on this handle");
+    Lane& ln = w->lane[0];
+    hipStream_t s = hip_stream ? (hipStream_t)hip_stream : ln.stream;
+    return with_memory(w, [&] {
+        return tree_logits_impl(w, ln, s, prompt_tokens, prompt_offsets, B, node_tokens, node_offsets, parents, logits_out);
+    });
 }
 
 namespace {

@@ -185,11 +185,17 @@ void launch_attention_tree(const TreeArgs& a, int token, int tiles, hipStream_t 
 struct PackedArgs {
     RowsView q, k, v, out;
     int packed_d;              // as TreeArgs
-    const int32_t* offsets;    // [n_seq + 1]
+    const int32_t* offsets;    // [n_seq + 1], or with lengths [n_seq]: first row of each sequence
+    const int32_t* lengths;    // [n_seq], or null
     float scale;
     int heads, n_kv, max_len;
 };
 void launch_attention_packed(const PackedArgs& a, int hd, int token, int n_seq, hipStream_t s);
+// Forwards whose attention is one of the two above: sums the k-slices of q|k|v, rotates q and k at the rows' positions, puts keys and values
+// into slot[j] of sequence st.tr_row[j] of the cache (half or 8 bits), and queries, with dense_kv keys and values too, as
+// halves into rows [n][q d | k d | v d].
+void launch_rotate_store(const MbState& st, const float* qkv_part, int ksplit, size_t part_stride, const float* rope_cos, const float* rope_sin,
+                         f16_t* rows, int dense_kv, const CacheView& c, const int32_t* slot, int d, int n_max, hipStream_t s);
 
 }  // namespace ss
 

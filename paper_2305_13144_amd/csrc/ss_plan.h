@@ -191,6 +191,8 @@ struct TreePlan {
     int tiles, row_blocks, chunk, chunks;
 };
 TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu);
+// The engine's decode forwards: chunks that depend on a row's own context alone, so that what else is alive does not change its sums.
+constexpr int kTreeDecodeChunk = 512;
 // Chunks of a sequence of `len` slots: those it fills, at most `most` of them, at least one.
 constexpr int tree_chunks(int len, int chunk, int most)
 {

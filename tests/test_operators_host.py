@@ -98,7 +98,11 @@ def test_calls_whose_parts_do_not_fit_are_refused(lib):
     refused(tree(lib, out=rows(rows=7)), "fewer rows")
     refused(tree(lib, out=rows(dtype=ss.SS_BF16)), "type")
     refused(tree(lib, c=cache(dtype=ss.SS_BF16)), "type")
-    refused(tree(lib, seq=P, n_seq=2**20, q=rows(rows=2**40), out=rows(rows=2**40), nodes=P, max_nodes=1024), "too many")
+    refused(tree(lib, seq=P, n_seq=65535, heads=64, q=rows(rows=2**40), out=rows(rows=2**40), nodes=P, max_nodes=1024), "too many")
+    refused(tree(lib, seq=P, n_seq=65536, q=rows(rows=2**40), out=rows(rows=2**40)), "sequences")
+    refused(tree(lib, c=cache(n_seq=0, start=0, slots=0), seq=P), "no sequences")
+    refused(tree(lib, q=rows(row_stride=-64)), "strides")
+    refused(packed(lib, heads=65536), "heads")
     refused(packed(lib, heads=5), "multiple")
     refused(packed(lib, dim=80), "head_dim")
     refused(packed(lib, k=rows(dtype=ss.SS_BF16)), "type")
