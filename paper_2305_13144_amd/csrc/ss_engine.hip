@@ -1845,9 +1845,7 @@ int tree_logits_impl(const ss_weights* w, Lane& ln, hipStream_t s, const int32_t
         tree.plan = ss::tree_plan(B, c.n_heads, tree.max_nodes, tree.max_context + tree.max_nodes, w->n_cu);
         if (tree.plan.chunks > 1) share_bytes = (size_t)B * tree.plan.chunks * tree.max_nodes * c.n_heads * (c.head_dim + 4) * 4;
         for (int i = 0; i < B; ++i)
-            if (int rc = ss_tree_mask(parents + node_offsets[i], node_offsets[i + 1] - node_offsets[i], tree.max_nodes,
-                                      mask.data() + (size_t)node_offsets[i] * words))
-                return rc;
+            ss::tree_mask(parents + node_offsets[i], node_offsets[i + 1] - node_offsets[i], words, mask.data() + (size_t)node_offsets[i] * words);
     }
     HIPCHK(hipSetDevice(w->device));
     if (int rc = ensure_workspace(w, ln, std::max({n_p, N, B}), B, std::max(N, B), slots, 1, s, true, share_bytes)) return rc;

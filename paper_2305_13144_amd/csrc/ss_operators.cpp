@@ -194,12 +194,7 @@ extern "C" int ss_tree_mask(const int32_t* parents, int32_t n, int32_t max_nodes
     if (n > max_nodes) return fail(SS_EINVAL, "a tree of %d nodes, max_nodes is %d", n, max_nodes);
     for (int32_t t = 0; t < n; ++t)
         if (parents[t] < -1 || parents[t] >= t) return fail(SS_EINVAL, "parents[%d] must be -1 or an earlier node", t);
-    const int32_t words = (max_nodes + 63) / 64;
-    for (int32_t t = 0; t < n; ++t) {
-        uint64_t* row = mask + (size_t)t * words;
-        for (int32_t w = 0; w < words; ++w) row[w] = parents[t] < 0 ? 0 : mask[(size_t)parents[t] * words + w];
-        row[t >> 6] |= (uint64_t)1 << (t & 63);
-    }
+    ss::tree_mask(parents, n, (max_nodes + 63) / 64, mask);
     return SS_OK;
 }
 

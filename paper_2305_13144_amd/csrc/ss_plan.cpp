@@ -400,4 +400,13 @@ TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu)
     return p;
 }
 
+void tree_mask(const int* parents, int n, int words, uint64_t* mask)
+{
+    for (int t = 0; t < n; ++t) {
+        uint64_t* row = mask + (size_t)t * words;
+        for (int w = 0; w < words; ++w) row[w] = parents[t] < 0 ? 0 : mask[(size_t)parents[t] * words + w];
+        row[t >> 6] |= (uint64_t)1 << (t & 63);
+    }
+}
+
 }  // namespace ss

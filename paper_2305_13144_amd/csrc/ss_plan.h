@@ -4,6 +4,7 @@
 #define SS_PLAN_H
 
 #include <cstddef>
+#include <cstdint>
 #include <vector>
 
 namespace ss {
@@ -191,6 +192,8 @@ struct TreePlan {
     int tiles, row_blocks, chunk, chunks;
 };
 TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu);
+// Bits of the nodes that each node of a tree sees: itself and what its parent (an earlier node, or -1) sees.
+void tree_mask(const int* parents, int n, int words, uint64_t* mask);
 // The engine's decode forwards: chunks that depend on a row's own context alone, so that what else is alive does not change its sums.
 constexpr int kTreeDecodeChunk = 512;
 // Chunks of a sequence of `len` slots: those it fills, at most `most` of them, at least one.
