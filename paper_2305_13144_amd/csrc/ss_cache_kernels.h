@@ -60,9 +60,29 @@ __device__ __forceinline__ int64_t slab_of(const CacheView& c, int i, int* slots
 }
 
 // ------------------------------------------------------------------------------------------ cache: write and read
-// A vector of HD elements is HD / 8 neighbouring lanes', 16 bytes each.  A workgroup has kCacheVecs passes over 2048 / HD
-// vectors; vectors are numbered token by token, head by head, keys in one half of the grid and values in the other.
-constexpr int kCachePasses = 4;
+// A vector of HD elements is HD / 8 neighbouring lanes', 16 bytes each.  A workgroup takes 16 tokens through kCachePasses passes over 128 / HD
+// heads, keys and values in different workgroups: tokens of a prompt are neighbours in the cache, so that a head's vectors leave
+// as runs of 16 (with a token's heads side by side instead 8745 tokens of 32 heads of 128 took 64 us to write and 54 to read).
+constexpr int kCachePasses = 4, kCacheTokens = 16;
+
+// Of a lane: its token, that token's first vector in the cache (-1: none) and slots between heads, its first head.
+struct CachePlace {
+    int t, slots, head;
+    int64_t at;
+    static constexpr int step(int hd) { return 128 / hd; }   // heads of a pass
+    __device__ __forceinline__ CachePlace(const CacheView& c, const int32_t* seq, const int32_t* slot, int n, int vector, int hd)
+    {
+        t = blockIdx.x * kCacheTokens + vector % kCacheTokens;
+        head = blockIdx.y * (kCachePasses * step(hd)) + vector / kCacheTokens;
+        at = -1;
+        slots = 0;
+        if (t >= n) return;
+        const int s = seq[t], place = slot[t];
+        if (s < 0 || s >= c.n_seq) return;
+        const int64_t base = slab_of(c, s, &slots);
+        if (base >= 0 && place >= 0 && place < slots) at = base + place;
+    }
+};
 
 // Largest magnitude in a vector as the bits of a float: those are ordered as the numbers, with infinities and NaN on top.
 template <int HD>
@@ -123,24 +143,18 @@ template <int HD, typename TOKEN, typename CACHE>
 __global__ __launch_bounds__(256) void k_cache_write(CacheView c, RowsView k, RowsView v, const int32_t* __restrict__ seq,
                                                      const int32_t* __restrict__ slot, int n)
 {
-    constexpr int LPV = HD / 8, VPP = 256 / LPV;
-    const bool values = blockIdx.y;
+    constexpr int LPV = HD / 8, STEP = CachePlace::step(HD);
+    const bool values = blockIdx.z;
     const RowsView src = values ? v : k;
     const int part = threadIdx.x % LPV;
-    const int64_t first = (int64_t)blockIdx.x * (VPP * kCachePasses) + threadIdx.x / LPV, count = (int64_t)n * c.n_kv;
+    const CachePlace at(c, seq, slot, n, threadIdx.x / LPV, HD);
     u32x4 in[kCachePasses];
     int64_t to[kCachePasses];
 #pragma unroll
-    for (int p = 0; p < kCachePasses; ++p) {
-        const int64_t i = min(first + p * VPP, count - 1);
-        const int t = (int)(i / c.n_kv), h = (int)(i - (int64_t)t * c.n_kv), s = seq[t], at = slot[t];
-        in[p] = *(const u32x4*)((const TOKEN*)src.p + (int64_t)t * src.row + (int64_t)h * src.head + part * 8);
-        to[p] = -1;
-        if (s >= 0 && s < c.n_seq && first + p * VPP < count) {
-            int slots;
-            const int64_t base = slab_of(c, s, &slots);
-            if (base >= 0 && at >= 0 && at < slots) to[p] = base + (int64_t)h * slots + at;
-        }
+    for (int p = 0; p < kCachePasses; ++p) {   // beyond the last token or head: read again, written nowhere
+        const int h = at.head + p * STEP;
+        in[p] = *(const u32x4*)((const TOKEN*)src.p + (int64_t)min(at.t, n - 1) * src.row + (int64_t)min(h, c.n_kv - 1) * src.head + part * 8);
+        to[p] = at.at >= 0 && h < c.n_kv ? at.at + (int64_t)h * at.slots : -1;
     }
 #pragma unroll
     for (int p = 0; p < kCachePasses; ++p) {
@@ -166,25 +180,22 @@ template <int HD, typename TOKEN, typename CACHE>
 __global__ __launch_bounds__(256) void k_cache_read(CacheView c, RowsView k, RowsView v, const int32_t* __restrict__ seq,
                                                     const int32_t* __restrict__ slot, int n)
 {
-    constexpr int LPV = HD / 8, VPP = 256 / LPV;
-    const bool values = blockIdx.y;
+    constexpr int LPV = HD / 8, STEP = CachePlace::step(HD);
+    const bool values = blockIdx.z;
     const RowsView dst = values ? v : k;
     const int part = threadIdx.x % LPV;
-    const int64_t first = (int64_t)blockIdx.x * (VPP * kCachePasses) + threadIdx.x / LPV, count = (int64_t)n * c.n_kv;
+    const CachePlace at(c, seq, slot, n, threadIdx.x / LPV, HD);
+    if (at.at < 0) return;
     u32x4 in[kCachePasses];
     float scale[kCachePasses];
     TOKEN* to[kCachePasses];
 #pragma unroll
     for (int p = 0; p < kCachePasses; ++p) {
-        const int64_t i = min(first + p * VPP, count - 1);
-        const int t = (int)(i / c.n_kv), h = (int)(i - (int64_t)t * c.n_kv), s = seq[t], at = slot[t];
+        const int h = at.head + p * STEP;
         to[p] = nullptr;
-        if (s < 0 || s >= c.n_seq || first + p * VPP >= count) continue;
-        int slots;
-        const int64_t base = slab_of(c, s, &slots);
-        if (base < 0 || at < 0 || at >= slots) continue;
-        const int64_t from = base + (int64_t)h * slots + at;
-        to[p] = (TOKEN*)dst.p + (int64_t)t * dst.row + (int64_t)h * dst.head + part * 8;
+        if (h >= c.n_kv) continue;
+        const int64_t from = at.at + (int64_t)h * at.slots;
+        to[p] = (TOKEN*)dst.p + (int64_t)at.t * dst.row + (int64_t)h * dst.head + part * 8;
         const CACHE* src = (const CACHE*)(values ? c.v : c.k) + from * HD + part * 8;
         if constexpr (std::is_same<CACHE, int8_t>::value) {
             const uint2 w = *(const uint2*)src;
@@ -1313,14 +1324,14 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
 template <int HD, typename TOKEN, typename CACHE>
 static void cache_write(const CacheView& c, const RowsView& k, const RowsView& v, const int32_t* seq, const int32_t* slot, int n, hipStream_t s)
 {
-    const int64_t per = 2048 / HD * kCachePasses, vecs = (int64_t)n * c.n_kv;
-    k_cache_write<HD, TOKEN, CACHE><<<dim3((unsigned)((vecs + per - 1) / per), 2), 256, 0, s>>>(c, k, v, seq, slot, n);
+    constexpr int heads = kCachePasses * CachePlace::step(HD);
+    k_cache_write<HD, TOKEN, CACHE><<<dim3((n + kCacheTokens - 1) / kCacheTokens, (c.n_kv + heads - 1) / heads, 2), 256, 0, s>>>(c, k, v, seq, slot, n);
 }
 template <int HD, typename TOKEN, typename CACHE>
 static void cache_read(const CacheView& c, const RowsView& k, const RowsView& v, const int32_t* seq, const int32_t* slot, int n, hipStream_t s)
 {
-    const int64_t per = 2048 / HD * kCachePasses, vecs = (int64_t)n * c.n_kv;
-    k_cache_read<HD, TOKEN, CACHE><<<dim3((unsigned)((vecs + per - 1) / per), 2), 256, 0, s>>>(c, k, v, seq, slot, n);
+    constexpr int heads = kCachePasses * CachePlace::step(HD);
+    k_cache_read<HD, TOKEN, CACHE><<<dim3((n + kCacheTokens - 1) / kCacheTokens, (c.n_kv + heads - 1) / heads, 2), 256, 0, s>>>(c, k, v, seq, slot, n);
 }
 // f(head dim, tokens' type, cache's type) with values of those types and dims.
 template <class F>
