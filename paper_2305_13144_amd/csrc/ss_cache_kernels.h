@@ -97,8 +97,9 @@ __device__ __forceinline__ uint32_t vector_top(uint32_t m)
 }
 
 // A vector in 8 bits: scale = max|x| / 127 and code = x / scale, both divisions and the step to a whole number rounded to
-// nearest (even), as written.  x times the reciprocal is within 127 * 2^-23 of that quotient, so only quotients that near to
-// the middle of two codes are divided.  A vector with an infinity or NaN gets the scale NaN (it is read back as NaN
+// nearest (even), as written.  x times the reciprocal is within 127 * 2^-23 < 1.6e-5 of that quotient, and the quotient's own rounding
+// moves it by at most 2^-18, so only where a product is that near to the middle of two codes are quotients formed.  The whole
+// number is the low byte of the product plus 3 * 2^22.  A vector with an infinity or NaN gets the scale NaN (it is read back as NaN
 // throughout, by those who read it), one of zeros the scale 0.
 template <int HD>
 __device__ __forceinline__ float quantise(const float (&x)[8], uint2* codes)
@@ -110,22 +111,31 @@ __device__ __forceinline__ float quantise(const float (&x)[8], uint2* codes)
         m = m > u ? m : u;
     }
     m = vector_top<HD>(m);
-    const bool whole = m < 0x7f800000u;
-    const float scale = whole ? __uint_as_float(m) / 127.f : __uint_as_float(0x7fc00000u);
-    const bool plain = scale > 0x1p-100f;   // the reciprocal of a smaller one may not be a normal number
-    const float inv = plain ? 1.f / scale : 0.f;
-    int code[8];
+    const float scale = m < 0x7f800000u ? __uint_as_float(m) / 127.f : __uint_as_float(0x7fc00000u);
+    const bool plain = scale > 0x1p-100f;   // not 0, not NaN, and its reciprocal a normal number
+    const float inv = 1.f / scale;
+    constexpr float kWhole = 12582912.f;
+    uint32_t code[8];
+    float off = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float y = x[i] * inv;
-        float r = rintf(y);
-        if (!plain || fabsf(y - r) > 0.4999f) r = scale > 0.f ? rintf(x[i] / scale) : 0.f;
-        code[i] = whole ? (int)fminf(fmaxf(r, -127.f), 127.f) : 0;
+        const float y = x[i] * inv, r = y + kWhole;
+        off = fmaxf(off, fabsf(y - (r - kWhole)));
+        code[i] = __float_as_uint(r);
+    }
+    if (__any(!plain || off > 0.49998f)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float r = scale > 0.f ? fminf(fmaxf(rintf(x[i] / scale), -127.f), 127.f) : 0.f;
+            code[i] = (uint32_t)(int)r;
+        }
     }
     uint32_t w[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        w[i] = (code[4 * i] & 255) | (code[4 * i + 1] & 255) << 8 | (code[4 * i + 2] & 255) << 16 | (uint32_t)(code[4 * i + 3] & 255) << 24;
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t lo = __builtin_amdgcn_perm(code[4 * i + 1], code[4 * i], 0x0c0c0400u), up = __builtin_amdgcn_perm(code[4 * i + 3], code[4 * i + 2], 0x04000c0cu);
+        w[i] = lo | up;
+    }
     *codes = make_uint2(w[0], w[1]);
     return scale;
 }
