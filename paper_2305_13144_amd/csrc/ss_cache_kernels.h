@@ -345,7 +345,7 @@ __device__ __forceinline__ TreeSeq tree_sequence(const TreeArgs& a, int j)
     if (j < live && s.node0 >= 0 && count > 0 && s.node0 + (int64_t)count <= a.q.rows) s.n_nodes = count;
     if (seq >= 0 && seq < c.n_seq && at >= 0 && s.slots >= 0 && at + s.slots <= c.total) {
         s.base = at * c.n_kv;
-        s.len = (int)min((int64_t)s.ctx + s.n_nodes, (int64_t)s.slots);
+        s.len = (int)min((int64_t)s.ctx + s.n_nodes, (int64_t)min(s.slots, 0x7fffff00));   // a step beyond it is still a number
     }
     return s;
 }

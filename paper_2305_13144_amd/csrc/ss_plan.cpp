@@ -393,9 +393,10 @@ TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu)
     p.row_blocks = (rows + 16 * p.tiles - 1) / (16 * p.tiles);
     const long long units = std::max(1LL, (long long)n_seq * n_kv * p.row_blocks), at_once = (p.tiles == 1 ? 3LL : 2LL) * n_cu;
     long long chunk = (max_len * units + at_once - 1) / at_once;
-    if (n_seq > 1) chunk = std::min(chunk, 768LL);
-    chunk = std::max(chunk, (max_len + kTreeMaxChunks - 1LL) / kTreeMaxChunks);
-    p.chunk = (int)std::min<long long>((std::max(chunk, 256LL) + 127) / 128 * 128, 1 << 30);
+    const bool tall = p.tiles > 2;
+    if (n_seq > 1) chunk = std::min(chunk, tall ? 512LL : 768LL);
+    chunk = std::max({chunk, tall ? 512LL : 256LL, (max_len + kTreeMaxChunks - 1LL) / kTreeMaxChunks});
+    p.chunk = (int)std::min<long long>((chunk + 127) / 128 * 128, 1 << 30);
     p.chunks = std::max(1, (int)((max_len + (long long)p.chunk - 1) / p.chunk));
     return p;
 }

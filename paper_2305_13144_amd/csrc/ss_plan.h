@@ -183,10 +183,11 @@ int gemm_mode();
 
 // Attention over a cache (k_attention_tree, k_attention_tree_tall): rows of a sequence and key/value head (its nodes times the query
 // heads that share the head) go to workgroups in blocks of 16 * tiles (8: the tall kernel), its slots in chunks.
-// One sequence: as many chunks as the chip holds workgroups at once (3 a unit, 2 with more than 16 rows), of at least 256 slots.  Several
-// differ in length, which only the device knows: at most 768 slots, so that the last chunks of long ones do not run alone.
-// 64 rows of up to 8000 slots (32 heads on 8, 8 bits): 384 slots 106 us, 512 111, 768 101, 1024 114, 2048 126, whole 117; one of 500,000 slots
-// 768 231, 2048 208, 8192 (488 workgroups) 187, 16384 220.
+// One sequence: as many chunks as the chip holds workgroups at once (3 a unit, 2 with more than 16 rows), of at least 256 slots (tall kernel
+// 512).  Several differ in length, which only the device knows: at most 768 slots (512), so that the last chunks of long ones do not run
+// alone.  32 heads on 8, 8 bits, us: 64 rows of up to 8000 slots 384 slots a chunk 105, 512 110, 768 97, 1024 113, whole 117; one row of
+// 500,000 slots 768 231, 2048 208, 8192 (488 workgroups) 187, 16384 220.  Tall: 16 rows of up to 16 nodes and 3000 slots 256 32, 512 29, 768
+// 37, 1024 40; 8 rows of up to 61 nodes and 6000 slots 53, 49, 44, 50; one row of 64 nodes and 8000 slots (bf16) 30, 26, 28, 30.
 constexpr int kTreeMaxChunks = 1024;
 struct TreePlan {
     int tiles, row_blocks, chunk, chunks;
