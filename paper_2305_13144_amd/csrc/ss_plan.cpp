@@ -396,7 +396,7 @@ TreePlan tree_plan(int n_seq, int n_kv, int rows, int max_len, int n_cu)
     const bool tall = p.tiles > 2;
     if (n_seq > 1) chunk = std::min(chunk, tall ? 512LL : 768LL);
     chunk = std::max({chunk, tall ? 512LL : 256LL, (max_len + kTreeMaxChunks - 1LL) / kTreeMaxChunks});
-    p.chunk = (int)std::min<long long>((chunk + 127) / 128 * 128, 1 << 30);
+    p.chunk = (int)std::min<long long>((chunk + 127) / 128 * 128, 1 << 29);
     p.chunks = std::max(1, (int)((max_len + (long long)p.chunk - 1) / p.chunk));
     return p;
 }

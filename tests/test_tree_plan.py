@@ -45,7 +45,7 @@ def test_plans_cover_every_slot(tmp_path):
     src = tmp_path / "plan.cpp"
     src.write_text(PROGRAM)
     exe = tmp_path / "plan"
-    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan", "-I", CSRC, str(src), os.path.join(CSRC, "ss_plan.cpp"),
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-I", CSRC, str(src), os.path.join(CSRC, "ss_plan.cpp"),
                     "-o", str(exe)], check=True)
     out = subprocess.run([str(exe)], capture_output=True, text=True)
     assert out.returncode == 0 and out.stdout.startswith("ok"), out.stdout + out.stderr
