@@ -365,12 +365,13 @@ def ss_bench_read_stream(w: Weights, iters: int, stream: Optional[int] = None):
 # `stream`, a HIP stream handle) and return once enqueued.
 
 _torch = None
+_raw_stream = None
 _ELEMENT = {}   # torch dtype -> element type
 
 
 def _with_torch():
     """torch, with the library on the same HIP runtime: pointers and streams of another one mean nothing to it."""
-    global _torch
+    global _torch, _raw_stream
     if _torch is None:
         import torch
 
@@ -381,6 +382,7 @@ def _with_torch():
             raise RuntimeError("torch and this library have loaded a HIP runtime each (" + ", ".join(sorted(runtimes)) +
                                "): import torch before the library is first used")
         _ELEMENT.update({torch.float16: SS_F16, torch.bfloat16: SS_BF16, torch.int8: SS_I8})
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)   # a microsecond less than current_stream()
         _torch = torch
     return _torch
 
@@ -430,12 +432,9 @@ class _Elsewhere:
             c.__exit__(*exc)
 
 
-def _enqueue(index: int, stream: Optional[int], call):
-    """call(stream handle) with `index` the current device and the stream current, the default one included."""
-    if stream is None and index == _torch.cuda.current_device():
-        return call(_torch.cuda.current_stream(index).cuda_stream)
-    with _Elsewhere(index, stream):
-        return call(_torch.cuda.current_stream(index).cuda_stream)
+def _stream(index: int) -> int:
+    """Handle of torch's current stream."""
+    return _raw_stream(index) if _raw_stream else _torch.cuda.current_stream(index).cuda_stream
 
 
 class Cache:
@@ -480,25 +479,30 @@ class Cache:
 
 def ss_cache_write(cache: Cache, k, v, seq, slot, stream: Optional[int] = None) -> None:
     """Keys and values [n, n_kv_heads, head_dim] of n tokens to slot[t] of sequence seq[t] (int32 [n]; -1: passed over)."""
-    index, n, kv, hd, i32 = cache.index, k.shape[0], cache.n_kv_heads, cache.head_dim, _torch.int32
-    kr, vr = _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd)
-    sq, sl = _table(seq, "seq", index, n, i32), _table(slot, "slot", index, n, i32)
-    _check(_enqueue(index, stream, lambda s: _lib.ss_cache_write(cache.struct, kr, vr, sq, sl, n, s)))
+    t, index = _torch, cache.index
+    if stream is not None or index != t.cuda.current_device():
+        with _Elsewhere(index, stream):
+            return ss_cache_write(cache, k, v, seq, slot)
+    n, kv, hd, i32 = k.shape[0], cache.n_kv_heads, cache.head_dim, t.int32
+    _check(_lib.ss_cache_write(cache.struct, _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd), _table(seq, "seq", index, n, i32),
+                               _table(slot, "slot", index, n, i32), n, _stream(index)))
 
 
 def ss_cache_read(cache: Cache, seq, slot, dtype=None, k=None, v=None, stream: Optional[int] = None):
     """(k, v) [n, n_kv_heads, head_dim]: what slot[t] of sequence seq[t] stands for.  Into k and v if they are given, whose rows of
     tokens that do not exist stay as they are; into new tensors of `dtype` (float16) otherwise, where those rows are undefined."""
-    t, index, n, kv, hd = _torch, cache.index, seq.numel(), cache.n_kv_heads, cache.head_dim
-    sq, sl = _table(seq, "seq", index, n, t.int32), _table(slot, "slot", index, n, t.int32)
-
-    def call(s):
-        ko = t.empty((n, kv, hd), dtype=dtype or t.float16, device=cache.device) if k is None else k
-        vo = t.empty((n, kv, hd), dtype=ko.dtype, device=cache.device) if v is None else v
-        _check(_lib.ss_cache_read(cache.struct, sq, sl, n, _rows(ko, "k", index, kv, hd), _rows(vo, "v", index, kv, hd), s))
-        return ko, vo
-
-    return _enqueue(index, stream, call)
+    t, index = _torch, cache.index
+    if stream is not None or index != t.cuda.current_device():
+        with _Elsewhere(index, stream):
+            return ss_cache_read(cache, seq, slot, dtype, k, v)
+    n, kv, hd, i32 = seq.numel(), cache.n_kv_heads, cache.head_dim, t.int32
+    if k is None:
+        k = t.empty((n, kv, hd), dtype=dtype or t.float16, device=cache.device)
+    if v is None:
+        v = t.empty_like(k, memory_format=t.contiguous_format)
+    _check(_lib.ss_cache_read(cache.struct, _table(seq, "seq", index, n, i32), _table(slot, "slot", index, n, i32), n, _rows(k, "k", index, kv, hd),
+                              _rows(v, "v", index, kv, hd), _stream(index)))
+    return k, v
 
 
 def ss_tree_mask(parents, max_nodes: int) -> np.ndarray:
@@ -523,40 +527,41 @@ def ss_attention_tree(q, cache: Cache, context, max_context: int, nodes=None, ma
     slots of history.  q [rows, heads, head_dim]; context int32 [n]; nodes int32 [n + 1] (None: a row each); mask int64
     [rows, words] as of ss_tree_mask (None: a chain); seq int32 [n] (None: sequence j).  scale: head_dim ** -0.5 if not given.
     workspace: a uint8 tensor (a new one if not given).  Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
-    t, index, hd, n = _torch, cache.index, cache.head_dim, context.numel()
-    qr, i32 = _rows(q, "q", index, None, hd), t.int32
+    t, index = _torch, cache.index
+    if stream is not None or index != t.cuda.current_device():
+        with _Elsewhere(index, stream):
+            return ss_attention_tree(q, cache, context, max_context, nodes, max_nodes, mask, seq, scale, out, workspace)
+    hd, n, i32 = cache.head_dim, context.numel(), t.int32
+    qr = _rows(q, "q", index, None, hd)
     rows, heads = q.shape[0], q.shape[1]
-    tables = (_table(seq, "seq", index, n, i32), _table(context, "context", index, n, i32), max_context,
-              _table(nodes, "nodes", index, n + 1, i32), max_nodes, _table(mask, "mask", index, rows * ((max(max_nodes, 1) + 63) // 64), t.int64),
-              hd ** -0.5 if scale is None else scale)
-
-    def call(s):
-        o = t.empty((rows, heads, hd), dtype=q.dtype, device=cache.device) if out is None else out
-        w = workspace
-        if w is None:
-            need = ss_attention_tree_workspace(heads, cache.n_kv_heads, hd, n, max_context, max_nodes)
-            w = t.empty(need, dtype=t.uint8, device=cache.device) if need else None
-        _check(_lib.ss_attention_tree(cache.struct, qr, _rows(o, "out", index, heads, hd), heads, n, *tables,
-                                      _table(w, "workspace", index, 0 if w is None else w.numel(), t.uint8), 0 if w is None else w.numel(), s))
-        return o
-
-    return _enqueue(index, stream, call)
+    if out is None:
+        out = t.empty_like(q, memory_format=t.contiguous_format)
+    if workspace is None:
+        need = C.c_size_t(0)
+        _check(_lib.ss_attention_tree_workspace(heads, cache.n_kv_heads, hd, n, max_context, max_nodes, need))
+        if need.value:
+            workspace = t.empty(need.value, dtype=t.uint8, device=cache.device)
+    size = 0 if workspace is None else workspace.numel()
+    _check(_lib.ss_attention_tree(cache.struct, qr, _rows(out, "out", index, heads, hd), heads, n, _table(seq, "seq", index, n, i32),
+                                  _table(context, "context", index, n, i32), max_context, _table(nodes, "nodes", index, n + 1, i32), max_nodes,
+                                  _table(mask, "mask", index, rows * ((max(max_nodes, 1) + 63) // 64), t.int64), hd ** -0.5 if scale is None else scale,
+                                  _table(workspace, "workspace", index, size, t.uint8), size, _stream(index)))
+    return out
 
 
 def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] = None, out=None, stream: Optional[int] = None):
     """Causal attention of packed prompts: rows offsets[i] .. offsets[i+1] - 1 (int32) are sequence i's tokens, at most max_len.  q [rows,
     heads, head_dim]; k, v [rows, kv_heads, head_dim].  Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
-    t = _with_torch()
-    index, (rows, heads, hd), kv, n = q.get_device(), q.shape, k.shape[1], offsets.numel() - 1
+    t, index = _with_torch(), q.get_device()
     if index < 0:
         _refuse(q, "q", index, "")
-    parts = _rows(q, "q", index, heads, hd), _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd)
-    at = _table(offsets, "offsets", index, n + 1, t.int32)
-
-    def call(s):
-        o = t.empty((rows, heads, hd), dtype=q.dtype, device=q.device) if out is None else out
-        _check(_lib.ss_attention_packed(*parts, _rows(o, "out", index, heads, hd), heads, kv, hd, at, n, max_len,
-                                        hd ** -0.5 if scale is None else scale, s))
-        return o
-
-    return _enqueue(index, stream, call)
+    if stream is not None or index != t.cuda.current_device():
+        with _Elsewhere(index, stream):
+            return ss_attention_packed(q, k, v, offsets, max_len, scale, out)
+    heads, hd, kv, n = q.shape[1], q.shape[2], k.shape[1], offsets.numel() - 1
+    if out is None:
+        out = t.empty_like(q, memory_format=t.contiguous_format)
+    _check(_lib.ss_attention_packed(_rows(q, "q", index, heads, hd), _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd),
+                                    _rows(out, "out", index, heads, hd), heads, kv, hd, _table(offsets, "offsets", index, n + 1, t.int32), n, max_len,
+                                    hd ** -0.5 if scale is None else scale, _stream(index)))
+    return out
