@@ -474,6 +474,9 @@ int check_cfg(const ss_model_cfg* c)
     return SS_OK;
 }
 
+// Bytes of a layer's keys and values in 8 bits.
+size_t cache8_layer_bytes(const ss_model_cfg& c, size_t slots) { return (2 * slots * ((size_t)c.d_model + 4 * (size_t)c.n_heads) + 255) & ~(size_t)255; }
+
 // ---------------------------------------------------------------------------------------- workspace
 // n_max token-rows in a forward, B micro-batch rows, n_sel rows whose logits are wanted,
 // slots = total key/value slots of the micro-batch; tree_shares: bytes of chunks of a forward over trees (0: there is none).
@@ -504,7 +507,7 @@ int ensure_workspace(const ss_weights* w, Lane& ln, int n_max, int B, int n_sel,
         {&ws.pd, ss::gemm_partial_rows_bound(n_max) * d * 4, false},
         {&ws.hsel, (size_t)ss::round_up(n_sel, 128) * d * 2, true},
         {&ws.logits, (size_t)ss::round_up(n_sel, 16) * V * 4, false},
-        {&ws.kv, (size_t)c.n_layers * 2 * slots * (w->cache8 ? d + c.n_heads * 4 : d * 2), false},
+        {&ws.kv, c.n_layers * (w->cache8 ? cache8_layer_bytes(c, slots) : 2 * slots * d * 2), false},
         {&ws.rows16, w->cache8 || trees ? nr * 3 * d * 2 : 0, false},
         {&ws.shares, std::max(decode_shares, tree_shares), false},
         {&ws.ints, n_i32 * 4, false},
@@ -565,7 +568,7 @@ ss::CacheView cache_view(const ss_weights* w, const Lane& ln, int layer)
     v.n_kv = c.n_heads;
     v.hd = c.head_dim;
     if (w->cache8) {
-        char* at = ln.ws.kv.as<char>() + (size_t)layer * 2 * slots * (d + c.n_heads * 4);
+        char* at = ln.ws.kv.as<char>() + layer * cache8_layer_bytes(c, slots);
         v.dtype = ss::kI8;
         v.k = at;
         v.v = at + slots * d;

@@ -67,6 +67,22 @@ def test_many_rows_with_an_8_bit_cache(model):
     assert np.abs(got - ref).max() <= 3e-2 * np.abs(ref).max()
 
 
+def test_one_head_and_odd_counts_of_slots_in_8_bits():
+    """The codes of later layers lie behind the scales of earlier ones, here an odd number of 4-byte words."""
+    shape = synth.ModelShape("one", 3, 64, 1, 64, 256, 256)
+    W = synth.make_weights(shape, seed=3, threads=2)
+    toks, offs = prompts(shape, [41, 12], 4)
+    om = OracleModel(shape, W, "f64")
+    gw = ss.Weights(shape, W)
+    try:
+        gw.set_option(ss.SS_OPT_CACHE_BITS, 8)
+        got = ss.ss_forward_logits(gw, toks, offs, [30, 7])
+    finally:
+        gw.close()
+    ref = np.concatenate([om.teacher_forced(toks[offs[i]:offs[i + 1]], first=n - 1) for i, n in enumerate((30, 7))])
+    assert np.abs(got - ref).max() <= 3e-2 * np.abs(ref).max()
+
+
 def test_generation_with_an_8_bit_cache(model):
     """Lengths, ends and counters are those of any cache; a row's tokens do not depend on flags, polling or the static workspace; and
     where the oracle's choice on the row's own prefix is clear, it is the row's."""
