@@ -422,7 +422,8 @@ int ss_bench_read_stream(ss_weights* w, int32_t iters, double* ms_out, int64_t* 
 #define SS_I8  3 /* caches only: 8-bit codes with one scale per vector (below)        */
 
 /* Rows of heads: element e of head h of row r at p + (r * row_stride + h * head_stride + e) elements.  p is 16-byte aligned, the
- * strides are multiples of 8 from 0 (a row or head that all share, of inputs) to 2^24. */
+ * strides are multiples of 8 from 0 (a row or head that all share, of inputs) to 2^24 for rows, to 2^40 for heads.  Rows that are
+ * written do not overlap. */
 typedef struct {
     void*   p;
     int64_t row_stride, head_stride; /* in elements */
@@ -456,8 +457,8 @@ typedef struct {
 int ss_cache_write(const ss_cache* cache, const ss_rows* k, const ss_rows* v, const int32_t* seq, const int32_t* slot, int32_t n,
                    void* hip_stream);
 
-/* The way back: row t of k and v is what slot[t] of sequence seq[t] stands for, rounded to the rows' type.  Rows of tokens that
- * do not exist stay as they are.  A slot may be read any number of times. */
+/* The way back: row t of k and v is what slot[t] of sequence seq[t] stands for, rounded to the rows' type (half: +-65504
+ * beyond its range).  Rows of tokens that do not exist stay as they are.  A slot may be read any number of times. */
 int ss_cache_read(const ss_cache* cache, const int32_t* seq, const int32_t* slot, int32_t n, const ss_rows* k, const ss_rows* v,
                   void* hip_stream);
 
@@ -469,6 +470,7 @@ int ss_cache_read(const ss_cache* cache, const int32_t* seq, const int32_t* slot
  * nodes (ss_cache_write has put them there).  Node t attends to the whole history and to those nodes that its mask names:
  *   out[t][head] = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale * <q[t][head], k_s>)
  * A row that sees nothing gets zeros.  Slots that a row does not see have no influence on it, whatever they hold.
+ * Results in half saturate at +-65504, as everything that is stored as half.
  *   q, out       [rows][n_heads][head_dim], of one type, that of the cache if it has 16 bits; head h uses key/value head
  *                h / (n_heads / n_kv_heads)
  *   seq          device, int32[n_seq], nullable: the sequence of the cache; NULL = the j-th is j.  A sequence that does not
@@ -496,7 +498,7 @@ int ss_tree_mask(const int32_t* parents, int32_t n, int32_t max_nodes, uint64_t*
 /*
  * Causal attention of whole prompts that lie behind each other: rows offsets[i] .. offsets[i+1] - 1 (device, int32[n_seq + 1]) are the
  * tokens of sequence i, none or up to max_len (what lies beyond is passed over); each attends to itself and the tokens of
- * its sequence before it.  Rows of no sequence stay as they are.
+ * its sequence before it.  Rows of no sequence stay as they are, results in half saturate at +-65504.
  *   q, out [rows][n_heads][head_dim], k, v [rows][n_kv_heads][head_dim], one type; head h uses key/value head h / (n_heads / n_kv_heads)
  */
 int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_rows* v, const ss_rows* out, int32_t n_heads, int32_t n_kv_heads,

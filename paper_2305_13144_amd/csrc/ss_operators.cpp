@@ -4,6 +4,7 @@
 
 #include <atomic>
 #include <climits>
+#include <cmath>
 
 #include "ss_internal.h"
 #include "ss_kernels.h"
@@ -37,10 +38,19 @@ int check_rows(const ss_rows* r, const char* name)
     if (!is_half(r->dtype)) return fail(SS_EINVAL, "%s: dtype must be SS_F16 or SS_BF16", name);
     if (r->rows < 0) return fail(SS_EINVAL, "%s: negative number of rows", name);
     if (r->rows > 0 && !r->p) return fail(SS_EINVAL, "%s: NULL pointer", name);
-    if (r->row_stride < 0 || r->head_stride < 0 || r->row_stride > (1 << 24)) return fail(SS_EINVAL, "%s: strides must be 0 to 2^24", name);
+    if (r->row_stride < 0 || r->head_stride < 0 || r->row_stride > (1 << 24) || r->head_stride > (1ll << 40))
+        return fail(SS_EINVAL, "%s: strides must be 0 to 2^24 (rows) and 2^40 (heads)", name);
     if (!aligned(r->p) || r->row_stride % 8 || r->head_stride % 8)
         return fail(SS_EINVAL, "%s must be 16-byte aligned, its strides multiples of 8 elements", name);
     return SS_OK;
+}
+
+// Rows that are written: no two heads of any two rows share an element, in the order [rows][heads] or [heads][rows].
+int check_apart(const ss_rows* r, const char* name, int64_t n_heads, int32_t head_dim)
+{
+    const bool by_rows = (n_heads == 1 || r->head_stride >= head_dim) && (r->rows < 2 || r->row_stride >= (n_heads - 1) * r->head_stride + head_dim);
+    const bool by_heads = (r->rows < 2 || r->row_stride >= head_dim) && (n_heads == 1 || r->head_stride >= (r->rows - 1) * r->row_stride + head_dim);
+    return by_rows || by_heads ? SS_OK : fail(SS_EINVAL, "%s: its rows overlap", name);
 }
 
 ss::CacheView view(const ss_cache* c)
@@ -126,6 +136,8 @@ extern "C" int ss_cache_read(const ss_cache* cache, const int32_t* seq, const in
 {
     ss::clear_error();
     if (int rc = check_token_list(cache, k, v, seq, slot, n)) return rc;
+    if (int rc = check_apart(k, "k", cache->n_kv_heads, cache->head_dim)) return rc;
+    if (int rc = check_apart(v, "v", cache->n_kv_heads, cache->head_dim)) return rc;
     if (n == 0 || cache->n_seq == 0) return SS_OK;
     ss::launch_cache_read(view(cache), view(k), view(v), k->dtype, seq, slot, n, (hipStream_t)hip_stream);
     return launched();
@@ -154,6 +166,8 @@ extern "C" int ss_attention_tree(const ss_cache* cache, const ss_rows* q, const 
     if (q->dtype != out->dtype) return fail(SS_EINVAL, "q and out differ in type");
     if (cache->dtype != SS_I8 && cache->dtype != q->dtype) return fail(SS_EINVAL, "a cache of 16 bits and q must have the same type");
     if (out->rows < q->rows) return fail(SS_EINVAL, "out has fewer rows than q");
+    if (!std::isfinite(scale)) return fail(SS_EINVAL, "scale must be finite");
+    if (int rc = check_apart(out, "out", n_heads, cache->head_dim)) return rc;
     if (!nodes && max_nodes != 1) return fail(SS_EINVAL, "nodes is NULL: max_nodes must be 1");
     if (!nodes && q->rows < n_seq) return fail(SS_EINVAL, "q has fewer than %d rows", n_seq);
     if (!seq && n_seq > cache->n_seq) return fail(SS_EINVAL, "the cache has fewer than %d sequences", n_seq);
@@ -213,6 +227,8 @@ extern "C" int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_
     if (k->rows < q->rows || v->rows < q->rows || out->rows < q->rows) return fail(SS_EINVAL, "k, v or out has fewer rows than q");
     if (n_heads > 65535) return fail(SS_EINVAL, "more than 65535 heads");
     if (n_seq < 0 || max_len < 0) return fail(SS_EINVAL, "negative number of sequences or length");
+    if (!std::isfinite(scale)) return fail(SS_EINVAL, "scale must be finite");
+    if (int rc = check_apart(out, "out", n_heads, head_dim)) return rc;
     if (n_seq > 65535) return fail(SS_EINVAL, "more than 65535 sequences");
     if (max_len > 64 * 65535) return fail(SS_EINVAL, "max_len is too large");
     if (n_seq == 0 || max_len == 0 || q->rows == 0) return SS_OK;

@@ -53,12 +53,12 @@ def read(lib, c=cache(), k=rows(), v=rows(), seq=P, slot=P, n=8):
 
 
 def tree(lib, c=cache(), q=rows(), out=rows(), heads=4, n_seq=4, seq=None, context=P, max_context=50, nodes=None, max_nodes=1, mask=None,
-         work=None, nbytes=0):
-    return lib.ss_attention_tree(c, q, out, heads, n_seq, seq, context, max_context, nodes, max_nodes, mask, 0.1, work, nbytes, None)
+         work=None, nbytes=0, scale=0.1):
+    return lib.ss_attention_tree(c, q, out, heads, n_seq, seq, context, max_context, nodes, max_nodes, mask, scale, work, nbytes, None)
 
 
-def packed(lib, q=rows(), k=rows(), v=rows(), out=rows(), heads=4, kv=2, dim=64, offsets=P, n_seq=2, max_len=8):
-    return lib.ss_attention_packed(q, k, v, out, heads, kv, dim, offsets, n_seq, max_len, 0.1, None)
+def packed(lib, q=rows(), k=rows(), v=rows(), out=rows(), heads=4, kv=2, dim=64, offsets=P, n_seq=2, max_len=8, scale=0.1):
+    return lib.ss_attention_packed(q, k, v, out, heads, kv, dim, offsets, n_seq, max_len, scale, None)
 
 
 @pytest.mark.parametrize("c,word", BAD_CACHES)
@@ -102,6 +102,7 @@ def test_calls_whose_parts_do_not_fit_are_refused(lib):
     refused(tree(lib, seq=P, n_seq=65536, q=rows(rows=2**40), out=rows(rows=2**40)), "sequences")
     refused(tree(lib, c=cache(n_seq=0, start=0, slots=0), seq=P), "no sequences")
     refused(tree(lib, q=rows(row_stride=-64)), "strides")
+    refused(tree(lib, q=rows(head_stride=2**60)), "strides")
     refused(packed(lib, heads=65536), "heads")
     refused(packed(lib, heads=5), "multiple")
     refused(packed(lib, dim=80), "head_dim")
@@ -112,6 +113,20 @@ def test_calls_whose_parts_do_not_fit_are_refused(lib):
     refused(packed(lib, max_len=-1), "negative")
     refused(packed(lib, n_seq=65536), "sequences")
     refused(packed(lib, max_len=1 << 30), "max_len")
+
+
+def test_results_that_overlap_and_scales_that_are_no_numbers_are_refused(lib):
+    for bad in (rows(row_stride=0), rows(head_stride=0), rows(row_stride=192, head_stride=64), rows(row_stride=64, head_stride=448), rows(head_stride=32)):
+        refused(tree(lib, out=bad), "overlap")
+        refused(packed(lib, out=bad), "overlap")
+    for bad in (rows(row_stride=64), rows(head_stride=32), rows(row_stride=0)):
+        refused(read(lib, k=bad), "overlap")
+        refused(read(lib, v=bad), "overlap")
+    for scale in (float("nan"), float("inf"), -float("inf")):
+        refused(tree(lib, scale=scale), "finite")
+        refused(packed(lib, scale=scale), "finite")
+    by_heads = rows(row_stride=64, head_stride=512)                # [heads][rows]
+    assert tree(lib, out=by_heads, n_seq=0, context=None) == ss.SS_OK and packed(lib, out=by_heads, n_seq=0) == ss.SS_OK
 
 
 def test_a_workspace_that_is_too_small_is_refused_with_its_size(lib):
