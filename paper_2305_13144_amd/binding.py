@@ -421,7 +421,7 @@ class _Elsewhere:
         t = _torch
         self.contexts = [t.cuda.device(index)]
         if stream is not None:
-            self.contexts.append(t.cuda.stream(t.cuda.ExternalStream(stream, device=index)))
+            self.contexts.append(t.cuda.stream(t.cuda.ExternalStream(stream, device=index) if stream else t.cuda.default_stream(index)))
 
     def __enter__(self):
         for c in self.contexts:

@@ -415,7 +415,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     constexpr int KL = ROW / 64;             // 16-byte loads per 16 slots and lane
     constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
-    __shared__ int s_odd;
+    __shared__ int s_odd[NW];
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
     const CacheView& c = a.c;
 
@@ -434,7 +434,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     const char *K = (const char*)c.k + head_base * ROW, *V = (const char*)c.v + head_base * ROW;
     const float *kscale = I8 ? c.k_scale + head_base : nullptr, *vscale = I8 ? c.v_scale + head_base : nullptr;
     const int first = s_begin + 32 * wave;
-    if (threadIdx.x == 0) s_odd = 0;
 
     // A step's operands as they come from memory; those of the next step are requested as soon as the registers are free.
     u32x4 kreg[2][KL];
@@ -545,6 +544,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
             }
     }
     f32x4 o[QT][ET];
+    bool odd = false;   // this wave has met a value that is not finite among slots that not every row sees
     float m_run[QT], l_run[QT], R[QT], R_inv[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
@@ -648,7 +648,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         }
         if constexpr (TAIL && !I8) {   // infinite and NaN values count as 0 here, so that no row meets them as 0 * x: see below
             constexpr uint32_t INF = std::is_same<M, _Float16>::value ? 0x7c00u : 0x7f80u;
-            bool odd = false;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
 #pragma unroll
@@ -657,7 +656,6 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
                     odd = odd || (lo | up);
                     vreg[i][w] = x & ~(lo | up);
                 }
-            if (odd) s_odd = 1;
         }
 #pragma unroll
         for (int t = 0; t < ET; ++t) {
@@ -678,6 +676,8 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     for (; s0 < s_end; s0 += 32 * NW) step(s0, std::true_type{});
 
     // the waves' sums together: each brings its own to the common maximum
+    odd = __any(odd);
+    if (lane == 0) s_odd[wave] = odd;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         l_run[u] = across<32>(across<16>(l_run[u], Add()), Add());
@@ -720,7 +720,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         }
         if (r >= n_rows) continue;
         if constexpr (!I8)
-            if (s_odd)   // rare: the values that counted as 0, to the rows that see them (a positive weight times infinity or NaN)
+            if (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3])   // rare: the values that counted as 0, to the rows that see them
                 for (int slot = s_begin + max(shared_end - s_begin, 0) / 32 * 32; slot < s_end; ++slot) {
                     if (!tree_seen(a, node0 + node[u], node[u], slot - ctx, 1)) continue;
                     const C* v = (const C*)(V + (int64_t)slot * ROW) + e0;
@@ -1010,6 +1010,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     const float l = across<32>(l_run, Add()), inv = 1.f / l;
     wait_copies_and_meet<0>();
     char* rows = &lds[0][0][0] + wave * QW * ROW;
+    const bool any_odd = odd_lds;
+    const float limit = any_odd ? 3.4028235e38f : __builtin_inff();   // half saturates; infinities only below, once they are summed
 #pragma unroll
     for (int t = 0; t < ET; ++t)
 #pragma unroll
@@ -1017,23 +1019,26 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
             T r[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const float x = o[t][4 * b + e] * inv;
-                if constexpr (std::is_same<T, _Float16>::value) r[e] = __builtin_bit_cast(_Float16, f2h(x));
-                else r[e] = (T)x;
+                float x = o[t][4 * b + e] * inv;
+                if (std::is_same<T, _Float16>::value && fabsf(x) <= limit) x = fminf(fmaxf(x, -65504.f), 65504.f);   // NaN stays
+                r[e] = (T)x;
             }
             *(uint2*)(rows + ql * ROW + (((4 * t + b) ^ key_turn(ql)) * 16 + (hi ^ (ql >> 4)) * 8)) = __builtin_bit_cast(uint2, r);
         }
-    if (odd_lds) {   // rare: the values that counted as 0, to the queries that see them (a positive weight times infinity or NaN)
-        for (int n = q0; n <= wave_last; ++n)
-            for (int e = lane; e < HD; e += 64) {
-                const float x = (float)((const T*)(Vg + (int64_t)n * v_row))[e];
-                if (fabsf(x) <= 3.4e38f) continue;
-                for (int r = max(n - wave_first, 0); r < QW; ++r) {
-                    T* to = (T*)(rows + r * ROW + (((e >> 3) ^ key_turn(r)) * 16 + ((e >> 2 & 1) ^ (r >> 4)) * 8)) + (e & 3);
-                    *to = (T)((float)*to + x);
+    if (any_odd)   // rare: the values that counted as 0, to the queries that see them (a positive weight times infinity or NaN)
+        for (int e = lane; e < HD; e += 64) {
+            float sum = 0.f;
+            for (int r = 0, n = q0; r < QW; ++r) {
+                for (; n <= min(wave_first + r, wave_last); ++n) {
+                    const float x = (float)((const T*)(Vg + (int64_t)n * v_row))[e];
+                    if (!(fabsf(x) <= 3.4028235e38f)) sum += x;
                 }
+                T* to = (T*)(rows + r * ROW + (((e >> 3) ^ key_turn(r)) * 16 + ((e >> 2 & 1) ^ (r >> 4)) * 8)) + (e & 3);
+                const float x = (float)*to + sum;
+                if constexpr (std::is_same<T, _Float16>::value) *to = __builtin_bit_cast(_Float16, f2h(x));
+                else *to = (T)x;
             }
-    }
+        }
 #pragma unroll
     for (int i = 0; i < QW / RPC; ++i) {
         const int r = i * RPC + lane / PIECES, piece = (lane % PIECES) ^ key_turn(r);

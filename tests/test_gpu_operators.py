@@ -48,7 +48,7 @@ def assert_attention(got, q, k, v, visible, scale, weight_type):
     total = p.sum(-1, keepdim=True)
     w = torch.where(total > 0, p / total.clamp_min(1e-300), 0.0)
     ref, A = w @ v, w @ v.abs()
-    D = (q.shape[1] + 8) * 2.0 ** -24 * scale * (q64.abs() @ k.abs().T.contiguous()).masked_fill(~visible, 0).amax(-1, keepdim=True)
+    D = (q.shape[1] + 8) * 2.0 ** -24 * abs(scale) * (q64.abs() @ k.abs().T.contiguous()).masked_fill(~visible, 0).amax(-1, keepdim=True)
     vmax = torch.where(visible.any(0, keepdim=True).T, v.abs(), 0.0).max() if n else 0.0
     tol = half_step(got.dtype) * ref.abs() + (half_step(weight_type) + 4 * D + 2.0 ** -18) * A + n * 2.0 ** -23 * vmax + 1e-30
     bad = (got.double() - ref).abs() > tol
@@ -184,7 +184,7 @@ def random_tree(r, n):
     return [int(r.integers(-1, t)) if t else -1 for t in range(n)]
 
 
-def check_tree(seed, ctx, nodes, kv, group, dim, dtype, held, chain=False, spread=0.0, max_context=None, empty_rows=False):
+def check_tree(seed, ctx, nodes, kv, group, dim, dtype, held, chain=False, spread=0.0, max_context=None, empty_rows=False, scale=None):
     r = np.random.default_rng(seed)
     heads, n = kv * group, len(ctx)
     slots = [a + b + int(r.integers(0, 9)) for a, b in zip(ctx, nodes)]
@@ -207,7 +207,7 @@ def check_tree(seed, ctx, nodes, kv, group, dim, dtype, held, chain=False, sprea
         bits = (packed.view(np.uint64)[:, np.arange(top) // 64] >> (np.arange(top) % 64).astype(np.uint64) & np.uint64(1)).astype(bool)
         mask = torch.tensor(packed, device="cuda")
     got = ss.ss_attention_tree(q, H.cache, i32(ctx), max(ctx) if max_context is None else max_context, nodes=i32(first.tolist()),
-                               max_nodes=top, mask=mask, out=out)
+                               max_nodes=top, mask=mask, out=out, scale=scale)
     assert got is out
     assert (out[first[-1]:] == 5).all()
     for i in range(n):
@@ -218,7 +218,8 @@ def check_tree(seed, ctx, nodes, kv, group, dim, dtype, held, chain=False, sprea
         see = torch.tensor(see, device="cuda")
         for h in range(heads):
             k, v = (H.rows(m, i, h // group, ctx[i] + nodes[i]) for m in ("k", "v"))
-            assert_attention(out[first[i]:first[i + 1], h], q[first[i]:first[i + 1], h], k, v, see, dim ** -0.5, F16 if held == I8 else held)
+            assert_attention(out[first[i]:first[i + 1], h], q[first[i]:first[i + 1], h], k, v, see, dim ** -0.5 if scale is None else scale,
+                             F16 if held == I8 else held)
     return H, q, out
 
 
@@ -264,6 +265,55 @@ def test_the_stated_context_only_shares_out_the_work(held, said):
 @pytest.mark.parametrize("dtype,held", HELD)
 def test_a_long_context_is_shared_out_and_joined(dtype, held):
     check_tree(7, [20000, 11, 4097], [3, 1, 20], 1, 4, 128, dtype, held)
+
+
+@pytest.mark.parametrize("dtype,held", HELD)
+@pytest.mark.parametrize("scale", [0.0, -0.1, 1.0])
+def test_scales_of_scores(dtype, held, scale):
+    check_tree(60, [130, 0], [3, 1], 2, 2, 128, dtype, held, scale=scale)
+    check_tree(61, [40, 0], [20, 30], 1, 4, 64, dtype, held, scale=scale)
+    if held != I8:
+        check_packed(62, [40, 200], 1, 2, 64, dtype, scale=scale)
+
+
+@pytest.mark.parametrize("dtype,most", [(F16, 65504.0), (BF16, math.inf)])
+@pytest.mark.parametrize("nodes", [1, 40])
+def test_infinite_values_reach_those_who_see_them(nodes, dtype, most):
+    """A value that is infinite makes that element of those who see it infinite (half: its largest number), with its sign, and no other."""
+    H = Held(63, [100], 1, 128, dtype)
+    q = randn(gen(64), nodes, 1, 128, dtype=dtype)
+    call = lambda: ss.ss_attention_tree(q, H.cache, i32([50]), 50, nodes=i32([0, nodes]), max_nodes=nodes)  # noqa: E731
+    clean = call()
+    H.raw["v"][50 + nodes - 1, 5], H.raw["v"][50 + nodes - 1, 77] = math.inf, -math.inf
+    got = call()
+    assert got[-1, 0, 5] == most and got[-1, 0, 77] == -most
+    got[-1, 0, [5, 77]] = clean[-1, 0, [5, 77]]
+    assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("dtype,most", [(F16, 65504.0), (BF16, math.inf)])
+def test_infinite_values_in_prompts(dtype, most):
+    """As above; of both signs they make a NaN of what sees both, wherever in the prompt they are."""
+    k, v, q = (randn(gen(s), 300, 1, 128, dtype=dtype) for s in (65, 66, 67))
+    call = lambda: ss.ss_attention_packed(q, k, v, i32([0, 300]), 300)  # noqa: E731
+    clean = call()
+    v[266, 0, 3] = -math.inf
+    v[5, 0, 70], v[270, 0, 70] = math.inf, -math.inf
+    got = call()
+    assert (got[266:, 0, 3] == -most).all() and (got[5:270, 0, 70] == most).all() and got[270:, 0, 70].isnan().all()
+    got[266:, 0, 3], got[5:, 0, 70] = clean[266:, 0, 3], clean[5:, 0, 70]
+    assert torch.equal(got, clean)
+
+
+def test_results_by_heads_and_inputs_that_all_share():
+    """Results as [heads][rows], and one row of queries for all nodes."""
+    H = Held(68, [60, 60], 2, 64, I8)
+    one = randn(gen(69), 1, 4, 64, dtype=BF16)
+    out = torch.empty(4, 2, 64, dtype=BF16, device="cuda").transpose(0, 1)
+    ss.ss_attention_tree(one.expand(2, 4, 64), H.cache, i32([30, 50]), 50, out=out)
+    want = ss.ss_attention_tree(one.repeat(2, 1, 1), H.cache, i32([30, 50]), 50)
+    assert torch.equal(out, want)
+    assert torch.equal(ss.ss_attention_tree(one.expand(2, 4, 64), H.cache, i32([30, 50]), 50, stream=0), want)
 
 
 @pytest.mark.parametrize("dtype,held", HELD)
