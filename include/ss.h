@@ -416,6 +416,8 @@ int ss_bench_read_stream(ss_weights* w, int32_t iters, double* ms_out, int64_t* 
  * are their own; graphs that may replay at the same time need workspaces of their own.  All pointers in the structures and all
  * tables are device pointers of the current device; tables are read when the work runs, not when it is enqueued, and entries
  * that lead outside the tensors are passed over, not followed.
+ * out may be q itself (the same rows and strides); otherwise results, caches that are written and workspaces share no memory with
+ * each other or with what is read.  Everything is forward only: there are no gradients.
  * Errors: SS_EINVAL (NULL, bad counts, types, strides or alignment; nothing was enqueued), SS_EDEVICE (launch failed).
  */
 #define SS_F16 2 /* IEEE half                                                        */

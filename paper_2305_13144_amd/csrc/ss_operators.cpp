@@ -2,6 +2,7 @@
 // enqueued; they allocate nothing and wait for nothing, so a caller may capture them into a graph.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <atomic>
 #include <climits>
 #include <cmath>
@@ -242,7 +243,7 @@ extern "C" int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_
     a.scale = scale;
     a.heads = n_heads;
     a.n_kv = n_kv_heads;
-    a.max_len = max_len;
+    a.max_len = (int32_t)std::min<int64_t>(max_len, q->rows);   // no sequence is longer: no workgroups for what a caller only allows
     ss::launch_attention_packed(a, head_dim, q->dtype, n_seq, (hipStream_t)hip_stream);
     return launched();
 }

@@ -316,6 +316,24 @@ def test_results_by_heads_and_inputs_that_all_share():
     assert torch.equal(ss.ss_attention_tree(one.expand(2, 4, 64), H.cache, i32([30, 50]), 50, stream=0), want)
 
 
+@pytest.mark.parametrize("nodes,context", [(1, 200), (1, 5000), (20, 200), (100, 3000)])
+@pytest.mark.parametrize("held", [F16, I8])
+def test_results_in_the_place_of_the_queries(held, nodes, context):
+    H = Held(72, [context + nodes] * 3, 2, 128, held)
+    q, table = randn(gen(73), 3 * nodes, 8, 128, dtype=F16), i32([0, nodes, 2 * nodes, 3 * nodes])
+    call = lambda q, out: ss.ss_attention_tree(q, H.cache, i32([context, context // 2, 0]), context, nodes=table, max_nodes=nodes, out=out)  # noqa: E731
+    want, own = call(q, None), q.clone()
+    assert call(own, own) is own and torch.equal(own, want)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_results_of_prompts_in_the_place_of_the_queries(dtype):
+    q, k, v = randn(gen(74), 700, 8, 64, dtype=dtype), randn(gen(75), 700, 2, 64, dtype=dtype), randn(gen(76), 700, 2, 64, dtype=dtype)
+    offsets = i32([0, 1, 130, 700])
+    want, own = ss.ss_attention_packed(q, k, v, offsets, 570), q.clone()
+    assert ss.ss_attention_packed(own, k, v, offsets, 64 * 65535, out=own) is own and torch.equal(own, want)
+
+
 @pytest.mark.parametrize("dtype,held", HELD)
 def test_many_small_weights_count_beside_a_large_one(dtype, held):
     """One slot of score 0 and thousands whose weights, 2^-15 each, are below half's normal range: together a quarter."""
