@@ -131,6 +131,29 @@ def test_a_group_with_an_8_bit_cache_does_not_depend_on_company(flags):
     gw.close()
 
 
+def test_the_other_entry_points_with_an_8_bit_cache(model):
+    """Sampled groups do not depend on lanes, logits of prompts are near the oracle's, and the measurements run."""
+    shape, gw, om = model
+    w = synth.make_group(shape, 20, 31, ("uniform", 4, 40), ("lognormal", 8.0, 0.6, 1, 20), 0.3, 20, 8, ("SORT", "BIN"), base_batch=8, max_batch=16)
+    toks, offs = prompts(shape, [25, 3], 9)
+    gw.set_option(ss.SS_OPT_CACHE_BITS, 8)
+    try:
+        got = []
+        for lanes in (1, 3):
+            gw.set_option(ss.SS_OPT_IN_FLIGHT, lanes)
+            got.append(ss.ss_run_group_generate(gw, w.prompt_tokens, w.prompt_offsets, w.pred_lens, 8, ss.make_policy(("SORT", "BIN"), 8, 20, 16),
+                                                temperature=0.7, seed=5, target_lens=w.target_lens))
+        everything = ss.ss_forward_logits(gw, toks, offs, [25, 3], all_prompt_logits=True)
+        assert (ss.ss_bench_decode_steps_in_flight(gw, np.zeros(3 * 50, np.int32), 3, 50, 2) > 0).all()
+        assert (ss.ss_bench_weight_stream(gw, 3, 2)[0] > 0).all()
+    finally:
+        gw.set_option(ss.SS_OPT_CACHE_BITS, 16)
+        gw.set_option(ss.SS_OPT_IN_FLIGHT, 4)
+    assert np.array_equal(got[0]["tokens"], got[1]["tokens"]) and np.array_equal(got[0]["lens"], got[1]["lens"])
+    ref = np.concatenate([om.teacher_forced(toks[offs[i]:offs[i + 1]], first=0) for i in range(2)])
+    assert everything.shape == ref.shape and np.abs(everything - ref).max() <= 3e-2 * np.abs(ref).max()
+
+
 def test_the_option_takes_8_and_16(model):
     shape, gw, om = model
     for bad in (0, 1, 4, 32, -8):
