@@ -232,6 +232,7 @@ __global__ __launch_bounds__(256) void k_cache_read(CacheView c, RowsView k, Row
 
 // The engine's way into the cache.  As k_rope_append: row j's sums of q|k|v, whose columns are in the order of qkv_col, rotated at its
 // position; here a vector is HD / 8 lanes', 4 elements of each half per lane.  Keys and values are coded from their fp32 values.
+// Bound by its bytes (fp32 slices in, halves and codes out) and, in decode steps, by the launch: the codes need no pass of their own.
 template <int HD, typename CACHE>
 __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* __restrict__ part, int ksplit, size_t part_stride,
                                                       const float* __restrict__ rcos, const float* __restrict__ rsin, f16_t* __restrict__ rows,
@@ -306,8 +307,11 @@ __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* _
 // 8-bit caches: codes become halves exactly (1152 + code as a half's bits, less 1152), the key's scale multiplies the score
 // and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R < 1 with R a power
 // of two above the scales that the row has met so far.  A row of bf16 queries is brought into half's range by a power of two.
-// Slots that a row must not see weigh 0 whatever they hold: scores by selection, values through value_sums where one is
-// infinite or NaN.
+// Slots that a row must not see weigh 0 whatever they hold: scores by selection; infinite and NaN values of steps that not every row sees
+// count as 0 in the products and are added at the end to the rows that see them.
+// Bound by the cache's bytes at long contexts (64 rows to 8000 slots, 32 heads on 8, 8 bits: 91 us, 5.7 TB/s but for the ragged ends), at short
+// ones by the launch and the latencies of table, slots and join (16 rows to 250 slots, 32 heads, halves: 12 us).  Operands are
+// requested again as their registers fall free: 3 waves a SIMD, where a second set of registers leaves 2 and a fourth wave spills (98 -> 203 us).
 template <typename C, typename T>
 struct MathType { typedef T type; };           // 16-bit cache: its own type
 template <typename T>
@@ -744,7 +748,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
 
 // Adds up the chunks of rows whose slots were shared out.  A group of HD / 4 lanes adds up chunks like the waves above; WIDE: the groups of
 // a workgroup take the chunks of one row in turn (few rows, many chunks: the time is that of the loads one after another), else a
-// row each.
+// row each.  15616 rows of few chunks: 5.4 us, with a workgroup a row 17.8; one row of 32 heads at 3900 slots: 3.8 us with WIDE.
 template <int HD, typename T, bool WIDE>
 __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 {
@@ -808,6 +812,9 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 //   values   the same keys of element lane % 32: four neighbouring keys of one element, what the transposed LDS read returns
 // Keys and values are copied into LDS as they lie in memory (two tiles, one on its way while the other is used), pieces of 16 bytes
 // changing places within a row so that what is read at once lies in different banks.
+// Bound by power: 12288 tokens, 32 heads on 8 of 128: 1.09 to 1.21 ms by the card, 1.02 to 1.13 PFLOP/s of the half square that counts, where
+// zeros take 0.88 (the clock falls to 1.8 GHz).  256 prompts to 256 tokens, 32 heads: 215 us, 164 of them bytes.  8 waves a workgroup:
+// 1199 -> 1224 and 238 -> 275 us; tiles of 32 keys and 2 waves: 216 -> 237 for the short prompts.
 constexpr int kPackTile = 64, kPackQueries = 32;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -1056,6 +1063,8 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
 // What k_attention_tree computes, for units of more rows than a wave or two can hold: a wave takes 32 rows as the packed kernel takes 32
 // queries, the four waves of a workgroup share tiles of 64 slots in LDS, and slots of 8-bit caches become halves once on their way
 // there, not once per wave.  Copies of 16-bit slots go straight into LDS; codes pass through registers, requested a tile ahead.
+// Bound by vector work, 415 instructions a wave and tile beside 32 products (8 trees to 61 nodes at up to 6000 slots, 32 heads on 8, 8 bits:
+// 37 us; the kernel above in blocks of 32 rows opens the codes once per block: 75 -> 42 when this one was first measured).
 template <int HD, typename T, typename C>
 __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
 {
