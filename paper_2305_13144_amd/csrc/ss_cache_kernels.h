@@ -50,6 +50,24 @@ __device__ __forceinline__ u32x4 from_floats(const float (&f)[8])
     return __builtin_bit_cast(u32x4, h);
 }
 
+// What a weight's exponent s * sc takes off, of the maximum m that the weights are relative to.  Its rounding, up to 2^-24 of it, is a
+// factor common to all of a row's slots, but where it is large no factor that a weight can hold (from 2^28 on half's range is left, from 2^31
+// on the exponential's): there the differences are formed first.  A branch of the wave that ordinary scores never take.
+template <typename V, int N>
+__device__ __forceinline__ float exponent_top(float m, float sc, V (&s)[N])
+{
+    float top = fmaxf(m * sc, kLowest);
+    if (__any(fabsf(top) > 0x1p22f)) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] -= m;
+        top = 0.f;
+    }
+    return top;
+}
+
+// A chunk's maximum as it is kept for the join: finite, so that differences are numbers.
+__device__ __forceinline__ float part_top(float m) { return fminf(fmaxf(m, kLowest), -kLowest); }
+
 // First slot's vector of head h of sequence i in a cache, or -1 if the tables do not describe a slab inside it.
 __device__ __forceinline__ int64_t slab_of(const CacheView& c, int i, int* slots)
 {
@@ -633,7 +651,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
                     for (int t = 0; t < ET; ++t) o[u][t] *= down;
                 }
             }
-            const float m_sc = fmaxf(m_run[u] * sc, kLowest);   // its rounding is a factor common to all of a row's slots
+            const float m_sc = I8 ? m_run[u] : exponent_top(m_run[u], sc, s[u]);
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -736,7 +754,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
             float* to = a.part + ((((size_t)j * a.chunks + chunk) * c.n_kv + h) * a.max_nodes * G + r) * (HD + 4);
 #pragma unroll
             for (int t = 0; t < ET; t += 4) *(float4*)(to + e0 + t) = make_float4(x[t], x[t + 1], x[t + 2], x[t + 3]);
-            if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(fmaxf(m_all[u] * sc, kLowest), l_all[u]);
+            if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(part_top(m_all[u] * sc), l_all[u]);
         } else {
             const float inv = l_all[u] != 0.f ? 1.f / l_all[u] : 0.f;   // a row that sees nothing gets zeros
 #pragma unroll
@@ -952,7 +970,7 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
 #pragma unroll
             for (int t = 0; t < ET; ++t) o[t] *= alpha;
         }
-        const float m_sc = fmaxf(m_run * sc, kLowest);   // its rounding is a factor common to all of a query's keys
+        const float m_sc = exponent_top(m_run, sc, s);
         t8 pb[2 * NB];
 #pragma unroll
         for (int kt = 0; kt < NB; ++kt)
@@ -1256,7 +1274,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
             }
         }
         if constexpr (I8) __builtin_amdgcn_sched_barrier(0);
-        const float m_sc = fmaxf(m_run * sc, kLowest);
+        const float m_sc = I8 ? m_run : exponent_top(m_run, sc, s);
         m8 pb[4];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -1325,7 +1343,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
     if (r0 + wave * QW + ql >= n_rows) return;
     const float f = (I8 ? R : 1.f) * (n_chunks > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f);   // a row that sees nothing gets zeros
     float* const part = a.part + ((((size_t)j * a.chunks + chunk) * c.n_kv + h) * a.max_nodes * G + row) * (HD + 4);
-    if (n_chunks > 1 && hi == 0) *(float2*)(part + HD) = make_float2(fmaxf(m_run * sc, kLowest), l);
+    if (n_chunks > 1 && hi == 0) *(float2*)(part + HD) = make_float2(part_top(m_run * sc), l);
 #pragma unroll
     for (int t = 0; t < ET; ++t)
 #pragma unroll

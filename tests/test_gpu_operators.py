@@ -582,3 +582,44 @@ def test_a_whole_answer_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, captured)), seed
+
+
+# ------------------------------------------------------------------------------------------------ large scores
+def check_best_slot(got, q, k, v, visible, scale):
+    """Where the best score leads by more than what fp32 sums of products leave open, the result is that slot's value (one rounding of
+    the result; a weight of one and its sum have none).  Returns how many rows are decided so."""
+    s = ((q.double() @ k.T.contiguous()) * scale).masked_fill(~visible, -math.inf)
+    best = s.topk(2, -1)
+    open_ = 4 * (q.shape[1] + 8) * 2.0 ** -24 * abs(scale) * (q.double().abs() @ k.abs().T.contiguous()).masked_fill(~visible, 0).amax(-1)
+    sure = best.values[:, 0] - best.values[:, 1] > open_ + 60                              # 2^-86: no other slot has a weight
+    want = v[best.indices[:, 0]]
+    assert torch.isfinite(got).all()
+    assert ((got.double() - want).abs() <= (half_step(got.dtype) * want.abs()))[sure].all()
+    return int(sure.sum())
+
+
+@pytest.mark.parametrize("dtype,size", [(F16, 1e4), (BF16, 1e6), (BF16, 1e15), (BF16, 2e18)])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+@pytest.mark.parametrize("nodes,context", [(1, 60), (3, 400), (9, 70), (20, 900)])
+def test_large_scores(nodes, context, scale, dtype, size):
+    """Scores from 2^30 on, whose steps in fp32 are larger than the exponential's range."""
+    group, dim = 3, 128
+    H = Held(84, [context + nodes], 1, dim, dtype)
+    H.raw["k"].copy_((H.raw["k"].double() * size).to(dtype))
+    q = (randn(gen(85), nodes, group, dim).double() * size).to(dtype)
+    got = ss.ss_attention_tree(q, H.cache, i32([context]), context, nodes=i32([0, nodes]), max_nodes=nodes, scale=scale)
+    k, v = (H.rows(m, 0, 0, context + nodes) for m in ("k", "v"))
+    see = torch.ones(nodes, context + nodes, dtype=torch.bool, device="cuda").tril(context)
+    assert sum(check_best_slot(got[:, h], q[:, h], k, v, see, scale) for h in range(group)) >= nodes * group // 2
+
+
+@pytest.mark.parametrize("dtype,size", [(F16, 1e4), (BF16, 1e6), (BF16, 1e15), (BF16, 2e18)])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_large_scores_in_prompts(dim, scale, dtype, size):
+    n = 300
+    q, k = ((randn(gen(s), n, 1, dim).double() * size).to(dtype) for s in (86, 87))
+    v = randn(gen(88), n, 1, dim, dtype=dtype)
+    got = ss.ss_attention_packed(q, k, v, i32([0, n]), n, scale=scale)
+    see = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
+    assert check_best_slot(got[:, 0], q[:, 0], k[:, 0].double(), v[:, 0].double(), see, scale) >= n // 2
