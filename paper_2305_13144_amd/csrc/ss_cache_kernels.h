@@ -65,6 +65,14 @@ __device__ __forceinline__ float exponent_top(float m, float sc, V (&s)[N])
     return top;
 }
 
+// The power of two that brings a row whose largest magnitude is `top` (in bf16) to 2^14 to 2^15, and its inverse.  2^-100 and less count as that.
+__device__ __forceinline__ float half_power(float top, float* inverse)
+{
+    const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);   // top is below 2^(ex + 1)
+    *inverse = __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+    return __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
+}
+
 // A chunk's maximum as it is kept for the join: finite, so that differences are numbers.
 __device__ __forceinline__ float part_top(float m) { return fminf(fmaxf(m, kLowest), -kLowest); }
 
@@ -324,7 +332,7 @@ __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* _
 // fill the chip (tree_plan), whose sums k_tree_join adds up.
 // 8-bit caches: codes become halves exactly (1152 + code as a half's bits, less 1152), the key's scale multiplies the score
 // and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R < 1 with R a power
-// of two above the scales that the row has met so far.  A row of bf16 queries is brought into half's range by a power of two.
+// of two above the scales that the row has met so far.  A row of bf16 queries is brought into half's range by a power of two of its own.
 // Slots that a row must not see weigh 0 whatever they hold: scores by selection; infinite and NaN values of steps that not every row sees
 // count as 0 in the products and are added at the end to the rows that see them.
 // Bound by the cache's bytes at long contexts (64 rows to 8000 slots, 32 heads on 8, 8 bits: 91 us, 5.7 TB/s but for the ragged ends), at short
@@ -522,9 +530,10 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     }
 
     // queries, and what brings their scores to units of log2: for 16-bit caches a factor sc > 0 (a negative one turns the
-    // queries over), else the key's scale times qscale
-    const float log2_scale = a.scale * 1.44269504088896341f, sc = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
-    float qscale = log2_scale;
+    // queries over), else the key's scale times log2_scale, and with bf16 queries the row's power of two in sc
+    constexpr bool SCALED = !I8 || !std::is_same<M, T>::value;   // sc is not 1
+    const float log2_scale = a.scale * 1.44269504088896341f;
+    float sc[QT];
     m8 qf[QT][KS];
     int node[QT];
     u32x4 qreg[QT][KS];
@@ -539,31 +548,30 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     if constexpr (std::is_same<M, T>::value) {
         const uint32_t flip = !I8 && a.scale < 0.f ? 0x80008000u : 0u;
 #pragma unroll
-        for (int u = 0; u < QT; ++u)
+        for (int u = 0; u < QT; ++u) {
+            sc[u] = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
 #pragma unroll
             for (int i = 0; i < KS; ++i) qf[u][i] = __builtin_bit_cast(m8, qreg[u][i] ^ u32x4{flip, flip, flip, flip});
-    } else {   // bf16 queries, half arithmetic: the largest magnitude of the rows becomes 2^14 to 2^15
-        float top = 0.f, x[8];
+        }
+    } else {   // bf16 queries, half arithmetic: the largest magnitude of each row becomes 2^14 to 2^15
 #pragma unroll
-        for (int u = 0; u < QT; ++u)
+        for (int u = 0; u < QT; ++u) {
+            float top = 0.f, x[8];
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 to_floats<T>(qreg[u][i], x);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
             }
-        top = wave_max(top);
-        const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);   // the largest is below 2^(ex + 1)
-        const float down = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-        qscale *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
-#pragma unroll
-        for (int u = 0; u < QT; ++u)
+            top = across<32>(across<16>(top, Max()), Max());
+            const float down = half_power(top, &sc[u]);
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 to_floats<T>(qreg[u][i], x);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) qf[u][i][e] = (_Float16)(x[e] * down);
             }
+        }
     }
     f32x4 o[QT][ET];
     bool odd = false;   // this wave has met a value that is not finite among slots that not every row sees
@@ -605,7 +613,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) kq[kt][i] = ks[kt][i] * qscale;
+                for (int i = 0; i < 4; ++i) kq[kt][i] = ks[kt][i] * log2_scale;
         if (s_next < s_end) load_keys(s_next);
         m8 pb[QT];
 #pragma unroll
@@ -627,8 +635,8 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
                 }
             mt = across<32>(across<16>(mt, Max()), Max());
             // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1
-            if (__any((mt - m_run[u]) * sc > 8.f)) {
-                const float m_new = fmaxf(m_run[u], mt), alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc);
+            if (__any((mt - m_run[u]) * sc[u] > 8.f)) {
+                const float m_new = fmaxf(m_run[u], mt), alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc[u]);
                 m_run[u] = m_new;
                 l_run[u] *= alpha;
 #pragma unroll
@@ -651,12 +659,12 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
                     for (int t = 0; t < ET; ++t) o[u][t] *= down;
                 }
             }
-            const float m_sc = I8 ? m_run[u] : exponent_top(m_run[u], sc, s[u]);
+            const float m_sc = I8 ? fmaxf(m_run[u] * sc[u], kLowest) : exponent_top(m_run[u], sc[u], s[u]);   // 8 bits: sc is a power of two
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(I8 ? s[u][kt][i] - m_sc : fmaf(s[u][kt][i], sc, -m_sc));
+                    const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[u][kt][i], sc[u], -m_sc) : s[u][kt][i] - m_sc);
                     if constexpr (I8) {
                         l_run[u] += p;
                         pb[u][kt * 4 + i] = (M)(TAIL && !(seen[kt] >> i & 1) ? 0.f : p * (vs[kt][i] * R_inv[u]));
@@ -717,8 +725,8 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         for (int w = 0; w < NW; ++w) m_all[u] = fmaxf(m_all[u], s_m[w][u * 16 + ql]);
         l_all[u] = 0.f;
 #pragma unroll
-        for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f((s_m[w][u * 16 + ql] - m_all[u]) * sc);
-        const float f = __builtin_amdgcn_exp2f((m_run[u] - m_all[u]) * sc) * (I8 ? R[u] : 1.f);
+        for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f((s_m[w][u * 16 + ql] - m_all[u]) * sc[u]);
+        const float f = __builtin_amdgcn_exp2f((m_run[u] - m_all[u]) * sc[u]) * (I8 ? R[u] : 1.f);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -754,7 +762,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
             float* to = a.part + ((((size_t)j * a.chunks + chunk) * c.n_kv + h) * a.max_nodes * G + r) * (HD + 4);
 #pragma unroll
             for (int t = 0; t < ET; t += 4) *(float4*)(to + e0 + t) = make_float4(x[t], x[t + 1], x[t + 2], x[t + 3]);
-            if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(part_top(m_all[u] * sc), l_all[u]);
+            if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(part_top(m_all[u] * sc[u]), l_all[u]);
         } else {
             const float inv = l_all[u] != 0.f ? 1.f / l_all[u] : 0.f;   // a row that sees nothing gets zeros
 #pragma unroll
@@ -1095,7 +1103,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
     constexpr int PT = HD / 64;   // 16-byte pieces of codes per thread
     __shared__ __attribute__((aligned(1024))) char lds[2][2][TILE];
     __shared__ __attribute__((aligned(16))) float s_ks[2][KT], s_vs[2][KT];
-    __shared__ float s_top[2], s_q[NW];
+    __shared__ float s_top[2];
     __shared__ int s_odd;
     const CacheView& c = a.c;
     const int G = a.heads / c.n_kv, rb = blockIdx.x / c.n_kv, h = blockIdx.x - rb * c.n_kv, chunk = blockIdx.y, j = blockIdx.z;
@@ -1139,7 +1147,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
             }
         }
     };
-    float qscale = a.scale * 1.44269504088896341f;
+    const float log2_scale = a.scale * 1.44269504088896341f;
     auto stage = [&](int b) {   // codes to halves
         if constexpr (I8) {
             const int r = tid >> 2;
@@ -1158,7 +1166,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
                     *(u32x4*)(to + TILE + (to_v ^ (i * 128 + k * 16))) = halves(vreg[i][2 * k], vreg[i][2 * k + 1]);
                 }
             if (tid < KT) {
-                s_ks[b][tid] = sreg * qscale;
+                s_ks[b][tid] = sreg * log2_scale;
             } else if (tid < 2 * KT) {
                 s_vs[b][tid - KT] = sreg;
                 const float top = wave_max(sreg);
@@ -1169,10 +1177,11 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
     if (n_tiles > 0) request(0, 0);
     if (tid == 0) s_odd = 0;
 
-    // queries: as in k_attention_tree, one power of two for the workgroup
+    // queries and sc: as in k_attention_tree
+    constexpr bool SCALED = !I8 || !std::is_same<M, T>::value;
     const int row = min(r0 + wave * QW + ql, n_rows - 1), node = row / G;
     const bool busy = r0 + wave * QW < n_rows;
-    const float sc = I8 ? 1.f : fmaxf(fabsf(qscale), 1e-37f);
+    float sc = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
     m8 qf[KS];
     {
         const T* qp = (const T*)a.q.p + (int64_t)(node0 + node) * a.q.row + (int64_t)(h * G + row - node * G) * a.q.head + 8 * hi;
@@ -1191,13 +1200,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
             }
-            top = wave_max(top);
-            if (lane == 0) s_q[wave] = top;
-            __syncthreads();
-            top = fmaxf(fmaxf(s_q[0], s_q[1]), fmaxf(s_q[2], s_q[3]));
-            const int ex = max((int)(__float_as_uint(top) >> 23) - 127, -100);
-            const float down = __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
-            qscale *= __uint_as_float((uint32_t)(127 - 14 + ex) << 23);
+            const float down = half_power(across<32>(top, Max()), &sc);
 #pragma unroll
             for (int i = 0; i < KS; ++i) {
                 to_floats<T>(w[i], x);
@@ -1274,7 +1277,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
             }
         }
         if constexpr (I8) __builtin_amdgcn_sched_barrier(0);
-        const float m_sc = I8 ? m_run : exponent_top(m_run, sc, s);
+        const float m_sc = I8 ? fmaxf(m_run * sc, kLowest) : exponent_top(m_run, sc, s);
         m8 pb[4];
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
@@ -1284,7 +1287,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
                 if constexpr (I8) vq = *(const f32x4*)&s_vs[b][kt * 32 + 8 * g + 4 * hi];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(I8 ? s[kt][4 * g + e] - m_sc : fmaf(s[kt][4 * g + e], sc, -m_sc));
+                    const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[kt][4 * g + e], sc, -m_sc) : s[kt][4 * g + e] - m_sc);
                     float w = p;
                     if constexpr (I8) {
                         l_run += p;

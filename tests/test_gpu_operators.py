@@ -585,16 +585,17 @@ def test_a_whole_answer_on_another_stream_and_in_a_graph():
 
 
 # ------------------------------------------------------------------------------------------------ large scores
-def check_best_slot(got, q, k, v, visible, scale):
+def check_best_slot(got, q, k, v, visible, scale, weight=0.0):
     """Where the best score leads by more than what fp32 sums of products leave open, the result is that slot's value (one rounding of
-    the result; a weight of one and its sum have none).  Returns how many rows are decided so."""
+    the result; with 16 bits a weight and its sum are the same number).  Returns how many rows are decided so.
+    weight: with 8 bits the result is half(p scale / R) R code / p, by the one rounding to half within 2^-11 of scale code."""
     s = ((q.double() @ k.T.contiguous()) * scale).masked_fill(~visible, -math.inf)
     best = s.topk(2, -1)
     open_ = 4 * (q.shape[1] + 8) * 2.0 ** -24 * abs(scale) * (q.double().abs() @ k.abs().T.contiguous()).masked_fill(~visible, 0).amax(-1)
     sure = best.values[:, 0] - best.values[:, 1] > open_ + 60                              # 2^-86: no other slot has a weight
     want = v[best.indices[:, 0]]
     assert torch.isfinite(got).all()
-    assert ((got.double() - want).abs() <= (half_step(got.dtype) * want.abs()))[sure].all()
+    assert ((got.double() - want).abs() <= (half_step(got.dtype) + weight) * want.abs())[sure].all()
     return int(sure.sum())
 
 
@@ -623,3 +624,53 @@ def test_large_scores_in_prompts(dim, scale, dtype, size):
     got = ss.ss_attention_packed(q, k, v, i32([0, n]), n, scale=scale)
     see = torch.ones(n, n, dtype=torch.bool, device="cuda").tril()
     assert check_best_slot(got[:, 0], q[:, 0], k[:, 0].double(), v[:, 0].double(), see, scale) >= n // 2
+
+
+# ------------------------------------------------------------------------------------------------ rows and slots of very different size
+@pytest.mark.parametrize("dtype,held", HELD)
+@pytest.mark.parametrize("nodes,kv,group,dim,context", [(4, 2, 4, 128, 40), (8, 1, 4, 64, 300), (40, 1, 8, 128, 90), (33, 2, 1, 64, 700), (8, 1, 2, 128, 6000)])
+def test_rows_have_nothing_to_do_with_their_neighbours(nodes, kv, group, dim, context, dtype, held):
+    """Queries that are infinite, no numbers, huge or tiny beside ordinary ones (other nodes, and other heads of the same node): each row
+    is what it is by its own definition.  A huge row's answer is the value of its best slot."""
+    heads, big = kv * group, 1e30 if dtype == BF16 else 6e4
+    H = Held(80, [context + nodes], kv, dim, held)
+    q = randn(gen(81), nodes, heads, dim, dtype=dtype)
+    odd = {(0, 0): "inf", (1, heads - 1): "nan", (2, 0): "huge", (nodes - 1, heads - 1): "tiny"}
+    q[0, 0, 3], q[1, heads - 1, dim - 1] = -math.inf, math.nan
+    q[2, 0] = (q[2, 0].double() * big / 8).to(dtype)
+    q[nodes - 1, heads - 1] = (q[nodes - 1, heads - 1].double() * (1e-30 if dtype == BF16 else 1e-3)).to(dtype)
+    got = ss.ss_attention_tree(q, H.cache, i32([context]), context, nodes=i32([0, nodes]), max_nodes=nodes)
+    see = torch.ones(nodes, context + nodes, dtype=torch.bool, device="cuda").tril(context)
+    for h in range(heads):
+        k, v = (H.rows(m, 0, h // group, context + nodes) for m in ("k", "v"))
+        plain = torch.tensor([odd.get((t, h)) in (None, "tiny") for t in range(nodes)], device="cuda")
+        assert_attention(got[plain, h], q[plain, h], k, v, see[plain], dim ** -0.5, F16 if held == I8 else held)
+        for t in range(nodes):
+            if odd.get((t, h)) in ("inf", "nan"):
+                assert got[t, h].isnan().all()
+            elif odd.get((t, h)) == "huge":
+                s = torch.where(see[t], k @ q[t, h].double(), -math.inf)
+                best = s.topk(2)
+                if (best.values[0] - best.values[1]) * dim ** -0.5 > 2.0 ** -12 * (k.abs() @ q[t, h].double().abs()).max() + 60:   # no other slot has a weight
+                    want = v[best.indices[0]]
+                    assert ((got[t, h].double() - want).abs() <= (half_step(dtype) + 2.0 ** -10) * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype,held", HELD)
+@pytest.mark.parametrize("nodes,group", [(12, 1), (30, 1), (150, 2)])
+def test_large_queries_that_see_little(nodes, group, dtype, held):
+    """Queries of 2^13 and more whose rows see nothing, their last node alone, or a node of the last steps: what they do not see comes first."""
+    H = Held(89, [nodes], 1, 128, held)
+    q = (randn(gen(90), nodes, group, 128) * 2.0 ** (20 if dtype == BF16 else 12)).to(dtype)
+    bits = torch.zeros(nodes, nodes, dtype=torch.bool)
+    bits[1::3, nodes - 1] = True
+    bits[2::3, nodes - 2:] = True
+    words = (nodes + 63) // 64
+    mask = torch.tensor([[sum(int(b) << i for i, b in enumerate(row[64 * w:64 * w + 64])) for w in range(words)] for row in bits.tolist()], device="cuda")
+    got = ss.ss_attention_tree(q, H.cache, i32([0]), 0, nodes=i32([0, nodes]), max_nodes=nodes, mask=mask)
+    assert (got[0::3] == 0).all()
+    v = H.rows("v", 0, 0, nodes)
+    assert ((got[1::3].double() - v[-1]).abs() <= (half_step(dtype) + 2.0 ** -11) * v[-1].abs()).all()   # one slot: its weight is rounded, 8 bits
+    k, see = H.rows("k", 0, 0, nodes), bits.cuda()
+    for h in range(group):
+        check_best_slot(got[2::3, h], q[2::3, h], k, v, see[2::3], 128 ** -0.5, 2.0 ** -11 if held == I8 else 0.0)
