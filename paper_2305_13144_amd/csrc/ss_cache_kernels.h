@@ -73,6 +73,24 @@ __device__ __forceinline__ float half_power(float top, float* inverse)
     return __uint_as_float((uint32_t)(127 + 14 - ex) << 23);
 }
 
+// R of a row over an 8-bit cache.  The largest product top = p * scale that the row has met is at least 2^6 R, and a product up to 2^15 R
+// is held without a change of R: half's largest number is 2^16, and what rounds in its subnormals is off by at most 2^-25 R, 2^-31 of the
+// largest.  Where the weights' maximum has moved (by `alpha`), R moves with it, as the products that it was made for no longer count.
+struct WeightUnit {
+    float R = 0.f;
+    __device__ __forceinline__ float largest() const { return R * 0x1p15f; }
+    __device__ __forceinline__ float inverse() const { return __uint_as_float(0x7f000000u - __float_as_uint(R)); }
+    // `top`: of the products that come; returns what the sums so far, in the old unit, are to be multiplied by
+    __device__ __forceinline__ float follow(float alpha, float top)
+    {
+        const float old = R * alpha;
+        const uint32_t two = __float_as_uint(fmaxf(old * 64.f, top)) & 0x7f800000u;
+        const uint32_t bits = min(max(two, 7u << 23) - (6u << 23), 0x7e800000u);   // 2^-126 to 2^126
+        R = __uint_as_float(bits);
+        return old * inverse();
+    }
+};
+
 // A chunk's maximum as it is kept for the join: finite, so that differences are numbers.
 __device__ __forceinline__ float part_top(float m) { return fminf(fmaxf(m, kLowest), -kLowest); }
 
@@ -331,8 +349,8 @@ __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* _
 // over a unit's steps and join their sums through LDS at the end; a unit's slots are cut into chunks for as many workgroups as
 // fill the chip (tree_plan), whose sums k_tree_join adds up.
 // 8-bit caches: codes become halves exactly (1152 + code as a half's bits, less 1152), the key's scale multiplies the score
-// and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R < 1 with R a power
-// of two above the scales that the row has met so far.  A row of bf16 queries is brought into half's range by a power of two of its own.
+// and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R with R a power of two that follows
+// the largest p * scale of the row (WeightUnit): a slot of large values and no weight takes no bits from the others.  A row of bf16 queries is brought into half's range by a power of two of its own.
 // Slots that a row must not see weigh 0 whatever they hold: scores by selection; infinite and NaN values of steps that not every row sees
 // count as 0 in the products and are added at the end to the rows that see them.
 // Bound by the cache's bytes at long contexts (64 rows to 8000 slots, 32 heads on 8, 8 bits: 91 us, 5.7 TB/s but for the ragged ends), at short
@@ -575,13 +593,14 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     }
     f32x4 o[QT][ET];
     bool odd = false;   // this wave has met a value that is not finite among slots that not every row sees
-    float m_run[QT], l_run[QT], R[QT], R_inv[QT];
+    float m_run[QT], l_run[QT];
+    WeightUnit unit[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
 #pragma unroll
         for (int t = 0; t < ET; ++t) o[u][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
         m_run[u] = kLowest;
-        l_run[u] = R[u] = R_inv[u] = 0.f;
+        l_run[u] = 0.f;
     }
     auto step = [&](int s0, auto tail_step) {
         constexpr bool TAIL = decltype(tail_step)::value;   // some slot is a node's, or there is none
@@ -635,31 +654,19 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
                 }
             mt = across<32>(across<16>(mt, Max()), Max());
             // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1
-            if (__any((mt - m_run[u]) * sc[u] > 8.f)) {
-                const float m_new = fmaxf(m_run[u], mt), alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc[u]);
+            float alpha = 1.f;
+            const bool moves = __any((mt - m_run[u]) * sc[u] > 8.f);
+            if (moves) {
+                const float m_new = fmaxf(m_run[u], mt);
+                alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc[u]);
                 m_run[u] = m_new;
                 l_run[u] *= alpha;
+                if constexpr (!I8)
 #pragma unroll
-                for (int t = 0; t < ET; ++t) o[u][t] *= alpha;
-            }
-            if constexpr (I8) {   // a power of two above the scales that the row has met
-                float top = 0.f;
-#pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) top = fmaxf(top, TAIL && !(seen[kt] >> i & 1) ? 0.f : vs[kt][i]);
-                if (__any(top > R[u])) {
-                    top = across<32>(across<16>(top, Max()), Max());
-                    const uint32_t two = min(__float_as_uint(top) + 0x01000000u, 0x7f000000u) & 0x7f800000u;
-                    const float R_new = top > R[u] ? __uint_as_float(two) : R[u];
-                    const float down = R[u] * __uint_as_float(0x7f000000u - __float_as_uint(R_new));
-                    R[u] = R_new;
-                    R_inv[u] = R_new > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(R_new)) : 0.f;
-#pragma unroll
-                    for (int t = 0; t < ET; ++t) o[u][t] *= down;
-                }
+                    for (int t = 0; t < ET; ++t) o[u][t] *= alpha;
             }
             const float m_sc = I8 ? fmaxf(m_run[u] * sc[u], kLowest) : exponent_top(m_run[u], sc[u], s[u]);   // 8 bits: sc is a power of two
+            float top = 0.f;
 #pragma unroll
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -667,11 +674,24 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
                     const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[u][kt][i], sc[u], -m_sc) : s[u][kt][i] - m_sc);
                     if constexpr (I8) {
                         l_run[u] += p;
-                        pb[u][kt * 4 + i] = (M)(TAIL && !(seen[kt] >> i & 1) ? 0.f : p * (vs[kt][i] * R_inv[u]));
+                        s[u][kt][i] = TAIL && !(seen[kt] >> i & 1) ? 0.f : p * vs[kt][i];
+                        top = fmaxf(top, fabsf(s[u][kt][i]));
                     } else {
                         pb[u][kt * 4 + i] = (M)p;
                     }
                 }
+            if constexpr (I8) {
+                if (moves || __any(top > unit[u].largest())) {
+                    const float f = unit[u].follow(alpha, across<32>(across<16>(top, Max()), Max()));
+#pragma unroll
+                    for (int t = 0; t < ET; ++t) o[u][t] *= f;
+                }
+                const float inv = unit[u].inverse();
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pb[u][kt * 4 + i] = (M)(s[u][kt][i] * inv);
+            }
             if constexpr (!I8)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) l_run[u] = add_pair<M>(__builtin_bit_cast(u32x4, pb[u])[i], l_run[u]);
@@ -726,7 +746,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
         l_all[u] = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f((s_m[w][u * 16 + ql] - m_all[u]) * sc[u]);
-        const float f = __builtin_amdgcn_exp2f((m_run[u] - m_all[u]) * sc[u]) * (I8 ? R[u] : 1.f);
+        const float f = __builtin_amdgcn_exp2f((m_run[u] - m_all[u]) * sc[u]) * (I8 ? unit[u].R : 1.f);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -1103,7 +1123,6 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
     constexpr int PT = HD / 64;   // 16-byte pieces of codes per thread
     __shared__ __attribute__((aligned(1024))) char lds[2][2][TILE];
     __shared__ __attribute__((aligned(16))) float s_ks[2][KT], s_vs[2][KT];
-    __shared__ float s_top[2];
     __shared__ int s_odd;
     const CacheView& c = a.c;
     const int G = a.heads / c.n_kv, rb = blockIdx.x / c.n_kv, h = blockIdx.x - rb * c.n_kv, chunk = blockIdx.y, j = blockIdx.z;
@@ -1169,8 +1188,6 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
                 s_ks[b][tid] = sreg * log2_scale;
             } else if (tid < 2 * KT) {
                 s_vs[b][tid - KT] = sreg;
-                const float top = wave_max(sreg);
-                if (tid == KT) s_top[b] = top;
             }
         }
     };
@@ -1214,7 +1231,8 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
     for (int t = 0; t < ET; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float m_run = kLowest, l_run = 0.f, R = 0.f, R_inv = 0.f;
+    float m_run = kLowest, l_run = 0.f;
+    WeightUnit unit;
     const unsigned k_at = ql * ROW + (hi ^ key_turn(ql)) * 16;
     const int v_r = 4 * hi + ((lane & 15) >> 2);
     unsigned v_at[ET];
@@ -1237,48 +1255,39 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
         if constexpr (I8) __builtin_amdgcn_sched_barrier(0);   // the scales' reads stay behind: their registers are the keys'
         uint64_t seen = ~0ull;
         if constexpr (TAIL) seen = tree_seen(a, node0 + node, node, k0 - ctx, s_end - k0) >> (4 * hi);
-        float mt = kLowest, top = 0.f;
+        float mt = kLowest;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                f32x4 kq, vq;
+                f32x4 kq;
                 if constexpr (I8) kq = *(const f32x4*)&s_ks[b][kt * 32 + 8 * g + 4 * hi];
-                if constexpr (I8 && TAIL) vq = *(const f32x4*)&s_vs[b][kt * 32 + 8 * g + 4 * hi];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const bool sees = !TAIL || (seen >> (kt * 32 + 8 * g + e) & 1);
                     float x = s[kt][4 * g + e];
                     if constexpr (I8) x *= kq[e];
                     if (!sees) x = -__builtin_inff();
-                    if constexpr (I8 && TAIL) top = fmaxf(top, sees ? vq[e] : 0.f);
                     s[kt][4 * g + e] = x;
                     mt = fmaxf(mt, x);
                 }
             }
         mt = across<32>(mt, Max());
-        if (__any((mt - m_run) * sc > 8.f)) {   // see k_attention_tree
-            const float m_new = fmaxf(m_run, mt), alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
+        float alpha = 1.f;   // see k_attention_tree
+        const bool moves = __any((mt - m_run) * sc > 8.f);
+        if (moves) {
+            const float m_new = fmaxf(m_run, mt);
+            alpha = __builtin_amdgcn_exp2f((m_run - m_new) * sc);
             m_run = m_new;
             l_run *= alpha;
+            if constexpr (!I8)
 #pragma unroll
-            for (int t = 0; t < ET; ++t) o[t] *= alpha;
-        }
-        if constexpr (I8) {
-            top = TAIL ? across<32>(top, Max()) : s_top[b];
-            if (__any(top > R)) {
-                const uint32_t two = min(__float_as_uint(top) + 0x01000000u, 0x7f000000u) & 0x7f800000u;
-                const float R_new = top > R ? __uint_as_float(two) : R;
-                const float down = R * __uint_as_float(0x7f000000u - __float_as_uint(R_new));
-                R = R_new;
-                R_inv = R_new > 0.f ? __uint_as_float(0x7f000000u - __float_as_uint(R_new)) : 0.f;
-#pragma unroll
-                for (int t = 0; t < ET; ++t) o[t] *= down;
-            }
+                for (int t = 0; t < ET; ++t) o[t] *= alpha;
         }
         if constexpr (I8) __builtin_amdgcn_sched_barrier(0);
         const float m_sc = I8 ? fmaxf(m_run * sc, kLowest) : exponent_top(m_run, sc, s);
         m8 pb[4];
+        float top = 0.f;
 #pragma unroll
         for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
@@ -1288,14 +1297,27 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[kt][4 * g + e], sc, -m_sc) : s[kt][4 * g + e] - m_sc);
-                    float w = p;
                     if constexpr (I8) {
                         l_run += p;
-                        w = TAIL && !(seen >> (kt * 32 + 8 * g + e) & 1) ? 0.f : p * (vq[e] * R_inv);
+                        s[kt][4 * g + e] = TAIL && !(seen >> (kt * 32 + 8 * g + e) & 1) ? 0.f : p * vq[e];
+                        top = fmaxf(top, fabsf(s[kt][4 * g + e]));
+                    } else {
+                        pb[kt * 2 + (g >> 1)][(g & 1) * 4 + e] = (M)p;
                     }
-                    pb[kt * 2 + (g >> 1)][(g & 1) * 4 + e] = (M)w;
                 }
             }
+        if constexpr (I8) {
+            if (moves || __any(top > unit.largest())) {
+                const float f = unit.follow(alpha, across<32>(top, Max()));
+#pragma unroll
+                for (int t = 0; t < ET; ++t) o[t] *= f;
+            }
+            const float inv = unit.inverse();
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) pb[kt * 2 + (i >> 3)][i & 7] = (M)(s[kt][i] * inv);
+        }
         if constexpr (!I8)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -1344,7 +1366,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
     const float l = across<32>(l_run, Add());
     wait_copies_and_meet<0>();
     if (r0 + wave * QW + ql >= n_rows) return;
-    const float f = (I8 ? R : 1.f) * (n_chunks > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f);   // a row that sees nothing gets zeros
+    const float f = (I8 ? unit.R : 1.f) * (n_chunks > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f);   // a row that sees nothing gets zeros
     float* const part = a.part + ((((size_t)j * a.chunks + chunk) * c.n_kv + h) * a.max_nodes * G + row) * (HD + 4);
     if (n_chunks > 1 && hi == 0) *(float2*)(part + HD) = make_float2(part_top(m_run * sc), l);
 #pragma unroll

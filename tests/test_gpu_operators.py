@@ -674,3 +674,38 @@ def test_large_queries_that_see_little(nodes, group, dtype, held):
     k, see = H.rows("k", 0, 0, nodes), bits.cuda()
     for h in range(group):
         check_best_slot(got[2::3, h], q[2::3, h], k, v, see[2::3], 128 ** -0.5, 2.0 ** -11 if held == I8 else 0.0)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("nodes,group", [(1, 1), (5, 4), (60, 2)])
+@pytest.mark.parametrize("far", [0, 12, 20, 40, 100])
+def test_a_slot_of_large_values_and_no_weight(nodes, group, far, dtype):
+    """One slot whose values are 2^far times the others' and whose weight is 2^-far / 16 or less: the others count as without it.
+
+    Tolerance, A and D as above: per slot a rounding to half of weight times scale, relative 2^-11 above half's normal range, below it
+    2^-25 in units of which the largest product that the row met is at least 2^6: over n slots n 2^-31 of that product times 127."""
+    dim, context = 128, 200
+    H = Held(82, [context + nodes], 1, dim, I8)
+    k, unit = H.raw["k"], H.raw["k_scale"]
+    first = int(H.start[0])
+    k[:, 0] = 0                                     # the first element of a key is the far slot's alone
+    k[first + 70] = 0
+    k[first + 70, 0] = -127
+    unit[first + 70] = 1
+    H.raw["v_scale"][first + 70] *= 2.0 ** far
+    q = randn(gen(83), nodes, group, dim, dtype=dtype)
+    q[..., 0] = (far + 4 + 12) * math.log(2) * dim ** 0.5 / 127   # 12: the others' scores lie well above -12 in powers of two
+    got = ss.ss_attention_tree(q, H.cache, i32([context]), context, nodes=i32([0, nodes]), max_nodes=nodes)
+    kk, vv = (H.rows(m, 0, 0, context + nodes) for m in ("k", "v"))
+    see = torch.ones(nodes, context + nodes, dtype=torch.bool, device="cuda").tril(context)
+    scale = H.raw["v_scale"][first:first + context + nodes].double()
+    for h in range(group):
+        q64 = q[:, h].double()
+        s = ((q64 @ kk.T.contiguous()) * dim ** -0.5).masked_fill(~see, -math.inf)
+        w = torch.softmax(s, -1)
+        assert (w[:, 70] * 2.0 ** far <= 1 / 16).all()
+        ref, A = w @ vv, w @ vv.abs()
+        D = (dim + 8) * 2.0 ** -24 * dim ** -0.5 * (q64.abs() @ kk.abs().T.contiguous()).masked_fill(~see, 0).amax(-1, keepdim=True)
+        tol = half_step(dtype) * ref.abs() + (half_step(F16) + 4 * D + 2.0 ** -18) * A + kk.shape[0] * 2.0 ** -31 * 127 * (w * scale).amax(-1, keepdim=True)
+        bad = (got[:, h].double() - ref).abs() > tol
+        assert not bad.any(), (bad.sum().item(), (got[:, h].double() - ref).abs().max().item())
