@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "ss_device.h"
+#include "ss_plan.h"
 
 namespace ss {
 
@@ -100,7 +101,7 @@ __device__ __forceinline__ int64_t slab_of(const CacheView& c, int i, int* slots
     const int64_t at = c.start[i];
     const int n = c.slots[i];
     *slots = n;
-    return at >= 0 && n >= 0 && at + n <= c.total ? at * c.n_kv : -1;
+    return slab_inside(at, n, c.total) ? at * c.n_kv : -1;
 }
 
 // ------------------------------------------------------------------------------------------ cache: write and read
@@ -391,7 +392,7 @@ __device__ __forceinline__ TreeSeq tree_sequence(const TreeArgs& a, int j)
         s.slots = c.slots[there];
     }
     if (j < live && s.node0 >= 0 && count > 0 && s.node0 + (int64_t)count <= a.q.rows) s.n_nodes = count;
-    if (seq >= 0 && seq < c.n_seq && at >= 0 && s.slots >= 0 && at + s.slots <= c.total) {
+    if (seq >= 0 && seq < c.n_seq && slab_inside(at, s.slots, c.total)) {
         s.base = at * c.n_kv;
         s.len = (int)min((int64_t)s.ctx + s.n_nodes, (int64_t)min(s.slots, 0x7fffff00));   // a step beyond it is still a number
     }

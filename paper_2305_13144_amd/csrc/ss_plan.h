@@ -181,6 +181,12 @@ PassUnits pass_units(const std::vector<int>& order, const std::vector<int>& rows
 void set_gemm_mode(int mode);
 int gemm_mode();
 
+// Whether `slots` slots from `start` on lie in a cache of `total`: no sum that an entry of a caller's table could carry past 64 bits.
+constexpr bool slab_inside(int64_t start, int slots, int64_t total)
+{
+    return start >= 0 && slots >= 0 && slots <= total && start <= total - slots;
+}
+
 // Attention over a cache (k_attention_tree, k_attention_tree_tall): rows of a sequence and key/value head (its nodes times the query
 // heads that share the head) go to workgroups in blocks of 16 * tiles (8: the tall kernel), its slots in chunks.
 // One sequence: as many chunks as the chip holds workgroups at once (3 a unit, 2 with more than 16 rows), of at least 256 slots (tall kernel
