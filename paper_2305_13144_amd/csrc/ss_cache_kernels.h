@@ -376,14 +376,14 @@ __device__ __forceinline__ TreeSeq tree_sequence(const TreeArgs& a, int j)
     const CacheView& c = a.c;
     TreeSeq s{j, 0, 0, 0, 0, 0};
     // what does not depend on other tables is read at once
-    int seq = j, count = 1;
+    int seq = j, end = j + 1;
     const int live = a.d_n ? *a.d_n : a.n_seq, own = min(j, c.n_seq - 1);
     int64_t at = c.start[own];
     s.slots = c.slots[own];
     s.ctx = max(a.context[j], 0);
     if (a.nodes) {
         s.node0 = a.nodes[j];
-        count = min(a.nodes[j + 1] - s.node0, a.max_nodes);
+        end = a.nodes[j + 1];
     }
     if (a.seq) {
         seq = a.seq[j];
@@ -391,7 +391,7 @@ __device__ __forceinline__ TreeSeq tree_sequence(const TreeArgs& a, int j)
         at = c.start[there];
         s.slots = c.slots[there];
     }
-    if (j < live && s.node0 >= 0 && count > 0 && s.node0 + (int64_t)count <= a.q.rows) s.n_nodes = count;
+    if (j < live) s.n_nodes = (int)table_rows(s.node0, end, a.max_nodes, a.q.rows);
     if (seq >= 0 && seq < c.n_seq && slab_inside(at, s.slots, c.total)) {
         s.base = at * c.n_kv;
         s.len = (int)min((int64_t)s.ctx + s.n_nodes, (int64_t)min(s.slots, 0x7fffff00));   // a step beyond it is still a number
@@ -897,9 +897,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
     // query heads that share a head of keys and values are on one die
     const int G = a.heads / a.n_kv, hk = blockIdx.x % a.n_kv, h = hk * G + blockIdx.x / a.n_kv;
     const int i_seq = blockIdx.y, qt = gridDim.z - 1 - blockIdx.z;
-    const int first = a.offsets[i_seq], count = a.lengths ? a.lengths[i_seq] : a.offsets[i_seq + 1] - first;
-    if (first < 0 || first + (int64_t)count > a.q.rows) return;
-    const int p = min(count, a.max_len);
+    const int first = a.offsets[i_seq];
+    const int end = a.lengths ? first + a.lengths[i_seq] : a.offsets[i_seq + 1];
+    const int p = (int)min(table_rows(first, end, INT64_MAX, a.q.rows), (int64_t)a.max_len);
     const int q0 = qt * QW * NW;
     if (q0 >= p) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

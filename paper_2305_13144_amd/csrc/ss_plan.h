@@ -187,6 +187,14 @@ constexpr bool slab_inside(int64_t start, int slots, int64_t total)
     return start >= 0 && slots >= 0 && slots <= total && start <= total - slots;
 }
 
+// Rows first .. end - 1 of a caller's table: how many there are, 0 where they go down or lead outside `rows`, at most `most` of them where
+// only the first `most` have to be inside (nodes).
+constexpr int64_t table_rows(int first, int end, int64_t most, int64_t rows)
+{
+    const int64_t n = (int64_t)end - first < most ? (int64_t)end - first : most;
+    return first >= 0 && n > 0 && first + n <= rows ? n : 0;
+}
+
 // Attention over a cache (k_attention_tree, k_attention_tree_tall): rows of a sequence and key/value head (its nodes times the query
 // heads that share the head) go to workgroups in blocks of 16 * tiles (8: the tall kernel), its slots in chunks.
 // One sequence: as many chunks as the chip holds workgroups at once (3 a unit, 2 with more than 16 rows), of at least 256 slots (tall kernel

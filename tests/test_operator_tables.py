@@ -29,3 +29,21 @@ def test_slabs_beyond_the_cache_are_outside_wherever_they_start(tmp_path):
                 }
             }
 """)
+
+
+def test_rows_of_tables_that_go_down_or_lead_outside_are_none(tmp_path):
+    run(tmp_path, r"""
+    const int some[] = {INT_MIN, INT_MIN + 5, -1, 0, 1, 5, 79, 80, 81, INT_MAX - 1, INT_MAX};
+    for (int64_t rows : {(int64_t)0, (int64_t)1, (int64_t)80, (int64_t)INT_MAX, INT64_MAX})
+        for (int64_t most : {(int64_t)1, (int64_t)64, (int64_t)1024, INT64_MAX})
+            for (int first : some)
+                for (int end : some) {
+                    wide want = (wide)end - first;
+                    if (want > most) want = most;
+                    if (first < 0 || want < 0 || first + want > rows) want = 0;
+                    if (ss::table_rows(first, end, most, rows) != (int64_t)want) {
+                        std::printf("%d to %d, at most %lld of %lld\n", first, end, (long long)most, (long long)rows);
+                        return 1;
+                    }
+                }
+""")
