@@ -361,8 +361,10 @@ def ss_bench_read_stream(w: Weights, iters: int, stream: Optional[int] = None):
 
 
 # ---------------------------------------------------------------------------------------------------- operators on device tensors
-# Tensors are torch's, used where they lie: nothing is copied.  The calls go to torch's current stream of the tensors' device (or to
-# `stream`, a HIP stream handle) and return once enqueued.
+# Tensors are torch's, used where they lie: nothing is copied.  The calls go to torch's current stream of the tensors' device and return once
+# enqueued.  Given another `stream` (a HIP stream handle, 0: the default stream) they go there, behind what the current stream holds so
+# far, and the tensors' memory is not given to others before that work is done; whoever reads the results on another
+# stream has it wait for this one, as with torch's own.  (A graph that is being captured there cannot wait for work outside it.)
 
 _torch = None
 _raw_stream = None
@@ -414,27 +416,26 @@ def _table(t, name: str, index: int, count: int, dtype):
     return t.data_ptr()
 
 
-class _Elsewhere:
-    """Launches and allocations on a device that is not the current one, or on a given stream."""
-
-    def __init__(self, index: int, stream: Optional[int]):
-        t = _torch
-        self.contexts = [t.cuda.device(index)]
-        if stream is not None:
-            self.contexts.append(t.cuda.stream(t.cuda.ExternalStream(stream, device=index) if stream else t.cuda.default_stream(index)))
-
-    def __enter__(self):
-        for c in self.contexts:
-            c.__enter__()
-
-    def __exit__(self, *exc):
-        for c in reversed(self.contexts):
-            c.__exit__(*exc)
-
-
 def _stream(index: int) -> int:
     """Handle of torch's current stream."""
     return _raw_stream(index) if _raw_stream else _torch.cuda.current_stream(index).cuda_stream
+
+
+def _on(stream: Optional[int], index: int, *tensors) -> int:
+    """Handle of the stream that a call goes to, given one or none, in order behind the current one and with the tensors kept."""
+    now = _stream(index)
+    if stream is None or stream == now:
+        return now
+    t = _torch.cuda
+    there = t.ExternalStream(stream, device=index) if stream else t.default_stream(index)
+    with t.stream(there):
+        captured = t.is_current_stream_capturing()
+    if not captured or t.is_current_stream_capturing():
+        there.wait_stream(t.current_stream(index))
+    for x in tensors:
+        if x is not None:
+            x.record_stream(there)
+    return stream
 
 
 class Cache:
@@ -462,6 +463,7 @@ class Cache:
         self.n_seq, self.n_kv_heads, self.head_dim, self.total_slots = n, n_kv_heads, head_dim, total
         self.device, self.index = k.device, index
         self.struct = ss_cache(*ptr, total, n, n_kv_heads, head_dim, dtype)
+        self.tensors = (k, v, start, slots, k_scale, v_scale)
 
     @classmethod
     def allocate(cls, slots: Sequence[int], n_kv_heads: int, head_dim: int, dtype, device="cuda") -> "Cache":
@@ -480,28 +482,28 @@ class Cache:
 def ss_cache_write(cache: Cache, k, v, seq, slot, stream: Optional[int] = None) -> None:
     """Keys and values [n, n_kv_heads, head_dim] of n tokens to slot[t] of sequence seq[t] (int32 [n]; -1: passed over)."""
     t, index = _torch, cache.index
-    if stream is not None or index != t.cuda.current_device():
-        with _Elsewhere(index, stream):
-            return ss_cache_write(cache, k, v, seq, slot)
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_cache_write(cache, k, v, seq, slot, stream)
     n, kv, hd, i32 = k.shape[0], cache.n_kv_heads, cache.head_dim, t.int32
     _check(_lib.ss_cache_write(cache.struct, _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd), _table(seq, "seq", index, n, i32),
-                               _table(slot, "slot", index, n, i32), n, _stream(index)))
+                               _table(slot, "slot", index, n, i32), n, _on(stream, index, k, v, seq, slot, *cache.tensors)))
 
 
 def ss_cache_read(cache: Cache, seq, slot, dtype=None, k=None, v=None, stream: Optional[int] = None):
     """(k, v) [n, n_kv_heads, head_dim]: what slot[t] of sequence seq[t] stands for.  Into k and v if they are given, whose rows of
     tokens that do not exist stay as they are; into new tensors of `dtype` (float16) otherwise, where those rows are undefined."""
     t, index = _torch, cache.index
-    if stream is not None or index != t.cuda.current_device():
-        with _Elsewhere(index, stream):
-            return ss_cache_read(cache, seq, slot, dtype, k, v)
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_cache_read(cache, seq, slot, dtype, k, v, stream)
     n, kv, hd, i32 = seq.numel(), cache.n_kv_heads, cache.head_dim, t.int32
     if k is None:
         k = t.empty((n, kv, hd), dtype=dtype or t.float16, device=cache.device)
     if v is None:
         v = t.empty_like(k, memory_format=t.contiguous_format)
     _check(_lib.ss_cache_read(cache.struct, _table(seq, "seq", index, n, i32), _table(slot, "slot", index, n, i32), n, _rows(k, "k", index, kv, hd),
-                              _rows(v, "v", index, kv, hd), _stream(index)))
+                              _rows(v, "v", index, kv, hd), _on(stream, index, k, v, seq, slot, *cache.tensors)))
     return k, v
 
 
@@ -528,9 +530,9 @@ def ss_attention_tree(q, cache: Cache, context, max_context: int, nodes=None, ma
     [rows, words] as of ss_tree_mask (None: a chain); seq int32 [n] (None: sequence j).  scale: head_dim ** -0.5 if not given.
     workspace: a uint8 tensor (a new one if not given).  Returns out, a new tensor if not given (rows of no sequence are then undefined)."""
     t, index = _torch, cache.index
-    if stream is not None or index != t.cuda.current_device():
-        with _Elsewhere(index, stream):
-            return ss_attention_tree(q, cache, context, max_context, nodes, max_nodes, mask, seq, scale, out, workspace)
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_attention_tree(q, cache, context, max_context, nodes, max_nodes, mask, seq, scale, out, workspace, stream)
     hd, n, i32 = cache.head_dim, context.numel(), t.int32
     qr = _rows(q, "q", index, None, hd)
     rows, heads = q.shape[0], q.shape[1]
@@ -545,7 +547,8 @@ def ss_attention_tree(q, cache: Cache, context, max_context: int, nodes=None, ma
     _check(_lib.ss_attention_tree(cache.struct, qr, _rows(out, "out", index, heads, hd), heads, n, _table(seq, "seq", index, n, i32),
                                   _table(context, "context", index, n, i32), max_context, _table(nodes, "nodes", index, n + 1, i32), max_nodes,
                                   _table(mask, "mask", index, rows * ((max(max_nodes, 1) + 63) // 64), t.int64), hd ** -0.5 if scale is None else scale,
-                                  _table(workspace, "workspace", index, size, t.uint8), size, _stream(index)))
+                                  _table(workspace, "workspace", index, size, t.uint8), size,
+                                  _on(stream, index, q, out, seq, context, nodes, mask, workspace, *cache.tensors)))
     return out
 
 
@@ -555,13 +558,13 @@ def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] =
     t, index = _with_torch(), q.get_device()
     if index < 0:
         _refuse(q, "q", index, "")
-    if stream is not None or index != t.cuda.current_device():
-        with _Elsewhere(index, stream):
-            return ss_attention_packed(q, k, v, offsets, max_len, scale, out)
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_attention_packed(q, k, v, offsets, max_len, scale, out, stream)
     heads, hd, kv, n = q.shape[1], q.shape[2], k.shape[1], offsets.numel() - 1
     if out is None:
         out = t.empty_like(q, memory_format=t.contiguous_format)
     _check(_lib.ss_attention_packed(_rows(q, "q", index, heads, hd), _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd),
                                     _rows(out, "out", index, heads, hd), heads, kv, hd, _table(offsets, "offsets", index, n + 1, t.int32), n, max_len,
-                                    hd ** -0.5 if scale is None else scale, _stream(index)))
+                                    hd ** -0.5 if scale is None else scale, _on(stream, index, q, k, v, out, offsets)))
     return out

@@ -709,3 +709,71 @@ def test_a_slot_of_large_values_and_no_weight(nodes, group, far, dtype):
         tol = half_step(dtype) * ref.abs() + (half_step(F16) + 4 * D + 2.0 ** -18) * A + kk.shape[0] * 2.0 ** -31 * 127 * (w * scale).amax(-1, keepdim=True)
         bad = (got[:, h].double() - ref).abs() > tol
         assert not bad.any(), (bad.sum().item(), (got[:, h].double() - ref).abs().max().item())
+
+
+# ------------------------------------------------------------------------------------------------ streams
+def busy():
+    """Some milliseconds of work on the current stream."""
+    a = torch.ones(4096, 4096, device="cuda")
+    for _ in range(20):
+        a = a @ a * 2.0 ** -12
+    return a
+
+
+def calls_on(stream, H, x, tables):
+    """Every operator, its inputs and tables made by the current stream just before, nothing of them kept."""
+    q, k, v = x.clone(), x[:, :2].clone(), x[:, 2:4].clone()
+    seq, slot, context, nodes = (lambda a=a: a.clone() for a in tables)
+    ss.ss_cache_write(H.cache, k, v, seq(), slot(), stream=stream)
+    res = list(ss.ss_cache_read(H.cache, seq(), slot(), F16, stream=stream))
+    res.append(ss.ss_attention_tree(q, H.cache, context(), 40, nodes=nodes(), max_nodes=3, stream=stream))
+    res.append(ss.ss_attention_packed(x.clone(), k.clone(), v.clone(), nodes(), 3, stream=stream))
+    return res
+
+
+def held_calls(seed):
+    H, x = Held(seed, [60, 60], 2, 128, I8), randn(gen(seed + 1), 4, 8, 128, dtype=F16)
+    tables = i32([0, 0, 0, 1]), i32([40, 41, 42, 5]), i32([40, 5]), i32([0, 3, 4])
+    return H, x, tables, calls_on(None, H, x, tables), torch.cuda.Stream()
+
+
+def test_a_given_stream_waits_for_what_the_current_one_holds():
+    H, x, tables, want, side = held_calls(91)
+    torch.cuda.synchronize()
+    late = torch.zeros_like(x)
+    busy()
+    late.copy_(x)
+    got = calls_on(side.cuda_stream, H, late, tables)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_a_given_stream_keeps_the_memory_that_it_reads():
+    H, x, tables, want, side = held_calls(93)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        busy()                                                    # side reads late
+    got = calls_on(side.cuda_stream, H, x, tables)
+    junk = [torch.full((n,), 1000, dtype=torch.int16, device="cuda") for n in (x.numel(), x.numel() // 4, 256, 8, 4, 2) for _ in range(12)]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(junk) == 72
+
+
+def test_a_given_stream_in_a_captured_graph():
+    """A branch of a captured graph, on the stream given; and the stream itself being captured."""
+    H, x, side = Held(95, [60, 60], 2, 128, I8), randn(gen(96), 4, 8, 128, dtype=F16), torch.cuda.Stream()
+    call = lambda stream: ss.ss_attention_tree(x, H.cache, i32_40, 40, stream=stream)  # noqa: E731
+    i32_40, graph = i32([40, 5]), torch.cuda.CUDAGraph()
+    x = x[:2]
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        a = call(side.cuda_stream)
+        torch.cuda.current_stream().wait_stream(side)
+        b = call(torch.cuda.current_stream().cuda_stream)
+    for seed in (97, 98, 99):
+        x.copy_(randn(gen(seed), *x.shape, dtype=F16))
+        want = call(None).clone()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(a, want) and torch.equal(b, want)
