@@ -365,6 +365,7 @@ def ss_bench_read_stream(w: Weights, iters: int, stream: Optional[int] = None):
 # enqueued.  Given another `stream` (a HIP stream handle, 0: the default stream) they go there, behind what the current stream holds so
 # far, and the tensors' memory is not given to others before that work is done; whoever reads the results on another
 # stream has it wait for this one, as with torch's own.  (A graph that is being captured there cannot wait for work outside it.)
+# Forward only: tensors that require gradients are refused unless gradients are off (torch.no_grad(), or detach()).
 
 _torch = None
 _raw_stream = None
@@ -399,6 +400,8 @@ def _refuse(t, name: str, index: int, what: str):
 
 def _rows(t, name: str, index: int, heads: Optional[int], head_dim: int) -> ss_rows:
     """[rows, heads, head_dim] of float16 or bfloat16 with any strides but the last; on device `index`."""
+    if t.requires_grad and _torch.is_grad_enabled():
+        raise ValueError(f"{name} requires gradients, and this operator has none: call it under torch.no_grad(), or with {name}.detach()")
     shape, dtype = t.shape, _ELEMENT.get(t.dtype, SS_I8)
     if t.get_device() != index or len(shape) != 3 or shape[2] != head_dim or (heads is not None and shape[1] != heads) or dtype == SS_I8:
         _refuse(t, name, index, f"[rows, {'heads' if heads is None else heads}, {head_dim}] of float16 or bfloat16")

@@ -777,3 +777,20 @@ def test_a_given_stream_in_a_captured_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(a, want) and torch.equal(b, want)
+
+
+def test_inputs_that_require_gradients_are_refused():
+    """A result without a gradient would pass for a constant.  Without gradients the call is as always."""
+    H, x, tables, want, side = held_calls(100)
+    x = x.requires_grad_()
+    seq, slot, context, nodes = tables
+    k = x[:, :2]
+    for call in (lambda: ss.ss_cache_write(H.cache, k, k.detach(), seq, slot), lambda: ss.ss_cache_write(H.cache, k.detach(), k, seq, slot),
+                 lambda: ss.ss_attention_tree(x, H.cache, context, 40, nodes=nodes, max_nodes=3),
+                 lambda: ss.ss_attention_tree(x.detach(), H.cache, context, 40, nodes=nodes, max_nodes=3, out=torch.zeros_like(x).requires_grad_()),
+                 lambda: ss.ss_attention_packed(x.detach(), k.detach(), k, nodes, 3), lambda: ss.ss_attention_packed(x, k.detach(), k.detach(), nodes, 3)):
+        with pytest.raises(ValueError, match="gradients"):
+            call()
+    with torch.no_grad():
+        got = calls_on(None, H, x, tables)
+    assert all(torch.equal(a, b) and not a.requires_grad for a, b in zip(got, want))

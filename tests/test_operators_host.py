@@ -175,3 +175,15 @@ def test_tensors_that_do_not_fit_are_refused_by_the_binding(lib):
                  torch.zeros(1, dtype=torch.int32), 2, 64)
     with pytest.raises(ValueError, match="GPU"):
         ss.ss_attention_packed(host, host, host, torch.zeros(2, dtype=torch.int32), 4)
+
+
+def test_rows_that_require_gradients_are_refused(lib):
+    ss._with_torch()
+    x = torch.zeros(4, 2, 64, dtype=torch.float16, requires_grad=True)
+    with pytest.raises(ValueError, match="q requires gradients"):
+        ss._rows(x, "q", -1, 2, 64)                                # -1: the host, where nothing is launched
+    with pytest.raises(ValueError, match="gradients"):
+        ss._rows((x * 2)[1:], "q", -1, 2, 64)
+    with torch.no_grad():
+        assert ss._rows(x, "q", -1, 2, 64).rows == 4
+    assert ss._rows(x.detach(), "q", -1, None, 64).row_stride == 128
