@@ -450,6 +450,8 @@ typedef struct {
     int32_t dtype;                       /* SS_F16, SS_BF16, SS_I8 */
 } ss_cache;
 
+#define SS_CACHE_MAX_TOKENS 268435440 /* of a call below; and n * n_kv_heads < 2^31 */
+
 /*
  * Keys and values of n tokens into the cache: token t goes to slot[t] of sequence seq[t] (device, int32[n]); tokens whose
  * sequence or slot does not exist (-1, say, for padding) are passed over.  A pair (seq, slot) may occur once per call.

@@ -94,6 +94,8 @@ int check_token_list(const ss_cache* c, const ss_rows* k, const ss_rows* v, cons
     if (k->dtype != v->dtype) return fail(SS_EINVAL, "k and v differ in type");
     if (k->rows < n || v->rows < n) return fail(SS_EINVAL, "k and v have fewer than %d rows", n);
     if (n > 0 && (!seq || !slot)) return fail(SS_EINVAL, "seq or slot is NULL");
+    // workgroups of 256 threads take 16 tokens each, and a grid has fewer than 2^32 threads a dimension
+    if (n > SS_CACHE_MAX_TOKENS) return fail(SS_EINVAL, "more than %d tokens", SS_CACHE_MAX_TOKENS);
     if ((int64_t)n * c->n_kv_heads > INT_MAX) return fail(SS_EINVAL, "more than 2^31 vectors");
     return SS_OK;
 }

@@ -187,3 +187,14 @@ def test_rows_that_require_gradients_are_refused(lib):
     with torch.no_grad():
         assert ss._rows(x, "q", -1, 2, 64).rows == 4
     assert ss._rows(x.detach(), "q", -1, None, 64).row_stride == 128
+
+
+def test_more_tokens_than_a_launch_takes_are_refused(lib):
+    """Rows of stride 0 let any number of tokens share a vector."""
+    one, all_ = cache(n_kv_heads=1), rows(row_stride=0, rows=2**31 - 1)
+    for n in (2**28 - 15, 2**28, 2**31 - 16, 2**31 - 1):
+        refused(write(lib, c=one, k=all_, v=all_, n=n), "tokens")
+        refused(read(lib, c=one, k=rows(rows=2**31 - 1), v=rows(rows=2**31 - 1), n=n), "tokens")
+    nothing = cache(n_kv_heads=1, n_seq=0, start=0, slots=0)
+    assert write(lib, c=nothing, k=all_, v=all_, n=2**28 - 16) == ss.SS_OK
+    refused(write(lib, c=cache(n_kv_heads=9), k=all_, v=all_, n=2**28 - 16), "vectors")
