@@ -60,8 +60,12 @@ ss::CacheView view(const ss_cache* c)
 }
 ss::RowsView view(const ss_rows* r) { return {r->p, r->row_stride, r->head_stride, r->rows}; }
 
-int launched()
+// Runs f, which launches, and says what became of it.  An error that an earlier call of the caller's left behind is not this call's.
+template <class F>
+int launch(F f)
 {
+    (void)hipGetLastError();
+    f();
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? SS_OK : fail(SS_EDEVICE, "launch failed: %s", hipGetErrorString(e));
 }
@@ -130,8 +134,7 @@ extern "C" int ss_cache_write(const ss_cache* cache, const ss_rows* k, const ss_
     ss::clear_error();
     if (int rc = check_token_list(cache, k, v, seq, slot, n)) return rc;
     if (n == 0 || cache->n_seq == 0) return SS_OK;
-    ss::launch_cache_write(view(cache), view(k), view(v), k->dtype, seq, slot, n, (hipStream_t)hip_stream);
-    return launched();
+    return launch([&] { ss::launch_cache_write(view(cache), view(k), view(v), k->dtype, seq, slot, n, (hipStream_t)hip_stream); });
 }
 
 extern "C" int ss_cache_read(const ss_cache* cache, const int32_t* seq, const int32_t* slot, int32_t n, const ss_rows* k, const ss_rows* v,
@@ -142,8 +145,7 @@ extern "C" int ss_cache_read(const ss_cache* cache, const int32_t* seq, const in
     if (int rc = check_apart(k, "k", cache->n_kv_heads, cache->head_dim)) return rc;
     if (int rc = check_apart(v, "v", cache->n_kv_heads, cache->head_dim)) return rc;
     if (n == 0 || cache->n_seq == 0) return SS_OK;
-    ss::launch_cache_read(view(cache), view(k), view(v), k->dtype, seq, slot, n, (hipStream_t)hip_stream);
-    return launched();
+    return launch([&] { ss::launch_cache_read(view(cache), view(k), view(v), k->dtype, seq, slot, n, (hipStream_t)hip_stream); });
 }
 
 extern "C" int ss_attention_tree_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n_seq, int32_t max_context,
@@ -199,8 +201,7 @@ extern "C" int ss_attention_tree(const ss_cache* cache, const ss_rows* q, const 
     a.chunk = p.chunk;
     a.chunks = p.chunks;
     a.row_blocks = p.row_blocks;
-    ss::launch_attention_tree(a, q->dtype, p.tiles, (hipStream_t)hip_stream);
-    return launched();
+    return launch([&] { ss::launch_attention_tree(a, q->dtype, p.tiles, (hipStream_t)hip_stream); });
 }
 
 extern "C" int ss_tree_mask(const int32_t* parents, int32_t n, int32_t max_nodes, uint64_t* mask)
@@ -246,6 +247,5 @@ extern "C" int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_
     a.heads = n_heads;
     a.n_kv = n_kv_heads;
     a.max_len = (int32_t)std::min<int64_t>(max_len, q->rows);   // no sequence is longer: no workgroups for what a caller only allows
-    ss::launch_attention_packed(a, head_dim, q->dtype, n_seq, (hipStream_t)hip_stream);
-    return launched();
+    return launch([&] { ss::launch_attention_packed(a, head_dim, q->dtype, n_seq, (hipStream_t)hip_stream); });
 }

@@ -9,6 +9,7 @@ value is rounded to, relative to the value (2^-11 for half, 2^-8 for bf16):
                                           each slot: n 2^-23 max|v| covers both it and the scales' power of two
   the scores, sums of dim products in fp32 and the exponential    each weight by at most 4 D relative, D = (dim + 8) 2^-24 scale max sum|q||k|
 """
+import ctypes
 import math
 
 import numpy as np
@@ -794,3 +795,17 @@ def test_inputs_that_require_gradients_are_refused():
     with torch.no_grad():
         got = calls_on(None, H, x, tables)
     assert all(torch.equal(a, b) and not a.requires_grad for a, b in zip(got, want))
+
+
+def test_an_error_that_others_left_behind_is_not_the_calls():
+    """A device that does not exist is refused by the runtime, which remembers it; the operators' launches are in order all the same."""
+    with open("/proc/self/maps") as f:
+        runtime = ctypes.CDLL(next(line.split()[-1] for line in f if "libamdhip64" in line))
+    H, x, tables, want, side = held_calls(102)
+    seq, slot, context, nodes = tables
+    for call in (lambda: ss.ss_cache_write(H.cache, x[:, :2], x[:, 2:4], seq, slot), lambda: ss.ss_cache_read(H.cache, seq, slot, k=x[:, :2], v=x[:, 2:4]),
+                 lambda: ss.ss_attention_tree(x, H.cache, context, 40, nodes=nodes, max_nodes=3),
+                 lambda: ss.ss_attention_packed(x, x[:, :2], x[:, 2:4], nodes, 3)):
+        torch.cuda.synchronize()
+        assert runtime.hipSetDevice(100000) != 0
+        call()
