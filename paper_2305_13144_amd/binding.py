@@ -441,6 +441,13 @@ def _on(stream: Optional[int], index: int, *tensors) -> int:
     return stream
 
 
+def _count(n: int, name: str) -> int:
+    """An argument of 32 bits: ctypes would cut a larger one to another number."""
+    if not -2**31 <= n < 2**31:
+        raise ValueError(f"{name} must be a number of 32 bits: it is {n}")
+    return n
+
+
 class Cache:
     """The key/value cache of one layer (ss_cache): a view of tensors that the caller owns.
 
@@ -473,8 +480,10 @@ class Cache:
         """An empty cache of torch.float16, bfloat16 or int8 with a slab of slots[i] slots for sequence i, one behind the other."""
         t = _with_torch()
         n = np.asarray(slots, dtype=np.int64)
-        if n.ndim != 1 or (n < 0).any():
-            raise ValueError("slots must be a list of numbers >= 0")
+        if n.ndim != 1 or (n < 0).any() or (n >= 2**31).any():
+            raise ValueError("slots must be a list of numbers >= 0 and below 2^31")
+        if n_kv_heads < 1 or head_dim not in (64, 128):
+            raise ValueError("n_kv_heads must be positive, head_dim 64 or 128")
         total = int(n.sum())
         k, v = (t.zeros(total * n_kv_heads * head_dim, dtype=dtype, device=device) for _ in range(2))
         scales = [t.zeros(total * n_kv_heads, device=device) if dtype == t.int8 else None for _ in range(2)]
@@ -513,7 +522,7 @@ def ss_cache_read(cache: Cache, seq, slot, dtype=None, k=None, v=None, stream: O
 def ss_tree_mask(parents, max_nodes: int) -> np.ndarray:
     """int64 [n, (max_nodes + 63) // 64] on the host: the bits of the nodes that each node of a tree sees (itself and those above it);
     parents[t] < t, -1 for a node below the history."""
-    p = _i32(parents)
+    p, max_nodes = _i32(parents), _count(max_nodes, "max_nodes")
     mask = np.zeros((len(p), (max(max_nodes, 1) + 63) // 64), np.int64)
     _check(lib().ss_tree_mask(_ptr(p), len(p), max_nodes, _ptr(mask)))
     return mask
@@ -522,6 +531,8 @@ def ss_tree_mask(parents, max_nodes: int) -> np.ndarray:
 def ss_attention_tree_workspace(n_heads: int, n_kv_heads: int, head_dim: int, n_seq: int, max_context: int, max_nodes: int = 1) -> int:
     """Bytes of workspace that ss_attention_tree takes for these counts on the current device."""
     need = C.c_size_t(0)
+    for n, name in ((n_heads, "n_heads"), (n_kv_heads, "n_kv_heads"), (n_seq, "n_seq"), (max_context, "max_context"), (max_nodes, "max_nodes")):
+        _count(n, name)
     _check(lib().ss_attention_tree_workspace(n_heads, n_kv_heads, head_dim, n_seq, max_context, max_nodes, need))
     return need.value
 
@@ -537,6 +548,8 @@ def ss_attention_tree(q, cache: Cache, context, max_context: int, nodes=None, ma
         with t.cuda.device(index):
             return ss_attention_tree(q, cache, context, max_context, nodes, max_nodes, mask, seq, scale, out, workspace, stream)
     hd, n, i32 = cache.head_dim, context.numel(), t.int32
+    _count(max_context, "max_context")
+    _count(max_nodes, "max_nodes")
     qr = _rows(q, "q", index, None, hd)
     rows, heads = q.shape[0], q.shape[1]
     if out is None:
@@ -564,6 +577,7 @@ def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] =
     if index != t.cuda.current_device():
         with t.cuda.device(index):
             return ss_attention_packed(q, k, v, offsets, max_len, scale, out, stream)
+    _count(max_len, "max_len")
     heads, hd, kv, n = q.shape[1], q.shape[2], k.shape[1], offsets.numel() - 1
     if out is None:
         out = t.empty_like(q, memory_format=t.contiguous_format)

@@ -809,3 +809,15 @@ def test_an_error_that_others_left_behind_is_not_the_calls():
         torch.cuda.synchronize()
         assert runtime.hipSetDevice(100000) != 0
         call()
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    H, x, tables, want, side = held_calls(104)
+    seq, slot, context, nodes = tables
+    for big in (2**32 + 3, 2**31):
+        with pytest.raises(ValueError, match="max_context"):
+            ss.ss_attention_tree(x, H.cache, context, big, nodes=nodes, max_nodes=3)
+        with pytest.raises(ValueError, match="max_nodes"):
+            ss.ss_attention_tree(x, H.cache, context, 40, nodes=nodes, max_nodes=big)
+        with pytest.raises(ValueError, match="max_len"):
+            ss.ss_attention_packed(x, x[:, :2], x[:, 2:4], nodes, big)

@@ -198,3 +198,22 @@ def test_more_tokens_than_a_launch_takes_are_refused(lib):
     nothing = cache(n_kv_heads=1, n_seq=0, start=0, slots=0)
     assert write(lib, c=nothing, k=all_, v=all_, n=2**28 - 16) == ss.SS_OK
     refused(write(lib, c=cache(n_kv_heads=9), k=all_, v=all_, n=2**28 - 16), "vectors")
+
+
+def test_numbers_beyond_32_bits_are_refused_by_the_binding(lib):
+    """2^32 + 5 would be 5 where the library takes 32 bits, and 2^31 slots none."""
+    for n in (2**32 + 5, 2**31, -2**31 - 1):
+        with pytest.raises(ValueError, match="max_nodes"):
+            ss.ss_tree_mask([-1], n)
+        with pytest.raises(ValueError, match="max_context"):
+            ss.ss_attention_tree_workspace(4, 2, 64, 1, n, 1)
+        with pytest.raises(ValueError, match="n_seq"):
+            ss.ss_attention_tree_workspace(4, 2, 64, n, 100, 1)
+        with pytest.raises(ValueError, match="max_len"):
+            ss._count(n, "max_len")
+    for slots in ([2**31], [3, 2**32 + 5], [-1], [[2, 3]]):
+        with pytest.raises(ValueError, match="slots must be a list"):
+            ss.Cache.allocate(slots, 1, 64, torch.int8, device="meta")
+    for kv, dim in ((0, 64), (-2, 64), (2, 96)):
+        with pytest.raises(ValueError, match="head_dim 64 or 128"):
+            ss.Cache.allocate([4], kv, dim, torch.int8, device="meta")
