@@ -263,6 +263,10 @@ def ss_tree_logits(w: Weights, prompt_tokens, prompt_offsets, node_tokens, node_
     """[B + nodes, vocab]: for each row the logits of its prompt's last position, then those of its drafted nodes."""
     pt, po, nt, no, pa = (_i32(a) for a in (prompt_tokens, prompt_offsets, node_tokens, node_offsets, parents))
     B = len(po) - 1
+    if B < 1 or len(no) != B + 1:
+        raise ValueError(f"prompt_offsets and node_offsets must both have rows + 1 entries: they have {len(po)} and {len(no)}")
+    if len(pt) < po[-1] or no[-1] < 0 or len(nt) < no[-1] or len(pa) < no[-1]:
+        raise ValueError(f"{len(pt)} prompt tokens, {len(nt)} node tokens and {len(pa)} parents are fewer than the offsets say ({po[-1]}, {no[-1]}, {no[-1]})")
     out = np.empty((B + int(no[-1]), w.shape.vocab), np.float32)
     _check(lib().ss_tree_logits(w.h, _ptr(pt), _ptr(po), B, _ptr(nt), _ptr(no), _ptr(pa), _ptr(out), stream))
     return out

@@ -217,3 +217,18 @@ def test_numbers_beyond_32_bits_are_refused_by_the_binding(lib):
     for kv, dim in ((0, 64), (-2, 64), (2, 96)):
         with pytest.raises(ValueError, match="head_dim 64 or 128"):
             ss.Cache.allocate([4], kv, dim, torch.int8, device="meta")
+
+
+def test_tables_of_trees_that_are_too_short_are_refused_by_the_binding(lib):
+    """The library would read behind them.  (Without a model the whole ones are refused by the library, before it reads anything.)"""
+    class NoModel:
+        h, shape = None, type("Shape", (), dict(vocab=16))
+
+    ok = dict(prompt_tokens=[1, 2, 3], prompt_offsets=[0, 2, 3], node_tokens=[4, 5], node_offsets=[0, 2, 2], parents=[-1, 0])
+    for change in (dict(node_offsets=[0, 2]), dict(node_offsets=[0, 1, 2, 2]), dict(node_offsets=[]), dict(prompt_offsets=[0], node_offsets=[0]),
+                   dict(prompt_offsets=[], node_offsets=[]), dict(prompt_tokens=[1, 2]), dict(node_tokens=[4]), dict(parents=[-1]), dict(node_offsets=[0, 2, -1])):
+        with pytest.raises(ValueError, match="offsets"):
+            ss.ss_tree_logits(NoModel, **{**ok, **change})
+    with pytest.raises(ss.SsError) as e:
+        ss.ss_tree_logits(NoModel, **ok)
+    assert e.value.code == ss.SS_EINVAL
