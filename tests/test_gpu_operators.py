@@ -821,3 +821,105 @@ def test_numbers_beyond_32_bits_are_refused():
             ss.ss_attention_tree(x, H.cache, context, 40, nodes=nodes, max_nodes=big)
         with pytest.raises(ValueError, match="max_len"):
             ss.ss_attention_packed(x, x[:, :2], x[:, 2:4], nodes, big)
+
+
+# ------------------------------------------------------------------------------------------------ every slot once, and no more than the roundings
+def assert_roundings(got, q, k, v, visible, scale, held, unit=None):
+    """As assert_attention, with the roundings of each weight alone.  Weights w of sum 1, the largest w_max:
+      16 bits of bf16   each w by 2^-8 of itself
+      half              each by 2^-11 of itself or, where it is a subnormal, by 2^-25 of a unit that is no larger than w_max, and never by
+                        more than itself: sum over slots min(w, 2^-25 w_max) |v|
+      8 bits            each w scale by 2^-11 of itself or 2^-25 R with 2^6 R at most the largest w scale: sum min(w |v|, 2^-31 127 max(w scale))
+    unit: the values' scales [slots], with 8 bits."""
+    q64 = q.double()
+    s = ((q64 @ k.T.contiguous()) * scale).masked_fill(~visible, -math.inf)
+    w = torch.softmax(s, -1)
+    ref, A = w @ v, w @ v.abs()
+    D = (q.shape[1] + 8) * 2.0 ** -24 * abs(scale) * (q64.abs() @ k.abs().T.contiguous()).masked_fill(~visible, 0).amax(-1, keepdim=True)
+    small = torch.zeros_like(ref)
+    if held == F16:
+        small = torch.minimum(w, 2.0 ** -25 * w.amax(-1, keepdim=True)) @ v.abs()
+    elif held == I8:
+        most = 2.0 ** -31 * 127 * (w * unit).amax(-1)
+        small = torch.stack([torch.minimum(row[:, None] * v.abs(), m).sum(0) for row, m in zip(w, most)])
+    tol = half_step(got.dtype) * ref.abs() + (half_step(BF16 if held == BF16 else F16) + 4 * D + 2.0 ** -18) * A + small
+    bad = (got.double() - ref).abs() > tol
+    assert torch.isfinite(got).all()
+    assert not bad.any(), (bad.sum().item(), ((got.double() - ref).abs() / tol).max().item())
+
+
+@pytest.mark.parametrize("dtype,held", HELD)
+@pytest.mark.parametrize("nodes,group", [([1, 1, 1], 1), ([3, 1, 2], 4), ([6, 1, 8], 4), ([17, 1, 20], 4)])
+def test_long_contexts_to_the_roundings(nodes, group, dtype, held):
+    ctx, dim = [20000, 11, 4097], 128
+    H = Held(106, [a + b + 3 for a, b in zip(ctx, nodes)], 1, dim, held)
+    first = np.concatenate([[0], np.cumsum(nodes)])
+    q = randn(gen(107), int(first[-1]), group, dim, dtype=dtype)
+    got = ss.ss_attention_tree(q, H.cache, i32(ctx), max(ctx), nodes=i32(first.tolist()), max_nodes=max(nodes))
+    for i, n in enumerate(nodes):
+        k, v = (H.rows(m, i, 0, ctx[i] + n) for m in ("k", "v"))
+        at = int(H.start[i])
+        unit = H.raw["v_scale"][at:at + ctx[i] + n].double() if held == I8 else None
+        see = torch.ones(n, ctx[i] + n, dtype=torch.bool, device="cuda").tril(ctx[i])
+        for h in range(group):
+            assert_roundings(got[first[i]:first[i + 1], h], q[first[i]:first[i + 1], h], k, v, see, dim ** -0.5, held, unit)
+
+
+@pytest.mark.parametrize("dtype,held", HELD)
+@pytest.mark.parametrize("nodes,group", [([1], 4), ([4, 1], 4), ([8, 2], 4), ([20], 4), ([33, 1, 70], 1)])
+@pytest.mark.parametrize("said", [None, 0, 100000])
+def test_every_slot_counts_once(nodes, group, said, dtype, held):
+    """Equal weights, and values that say to which of 128 runs of neighbouring slots a slot belongs: a result is the share of the run among
+    what the row sees, which one slot too few or too many changes by 1 / (slots of a run) of itself, 1/56 and more here."""
+    dim, n = 128, len(nodes)
+    ctx = [7000, 130, 1999][:n]
+    slots = [a + b for a, b in zip(ctx, nodes)]
+    H = Held(108, slots, 1, dim, held)
+    for i in range(n):
+        run = -(-slots[i] // 128)
+        ones = torch.nn.functional.one_hot(torch.arange(slots[i], device="cuda") // run, dim)
+        H.raw["v"][int(H.start[i]):int(H.start[i]) + slots[i]] = (ones * (127 if held == I8 else 1)).to(held)
+    if held == I8:
+        H.raw["v_scale"].fill_(0.5)
+    first = np.concatenate([[0], np.cumsum(nodes)])
+    q = randn(gen(109), int(first[-1]), group, dim, dtype=dtype)
+    got = ss.ss_attention_tree(q, H.cache, i32(ctx), max(ctx) if said is None else said, nodes=i32(first.tolist()), max_nodes=max(nodes), scale=0.0)
+    for i in range(n):
+        v = H.rows("v", i, 0, slots[i])
+        for t in range(nodes[i]):
+            want = v[:ctx[i] + t + 1].sum(0) / (ctx[i] + t + 1)       # weights of 1 and halves of powers of two are exact in half
+            assert ((got[first[i] + t].double() - want).abs() <= (half_step(dtype) + 2.0 ** -20) * want).all(), (i, t)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_every_token_of_a_prompt_counts_once(dim, dtype):
+    lens, heads = [2500, 1, 129, 640], 2
+    first = np.concatenate([[0], np.cumsum(lens)])
+    q, k = randn(gen(110), int(first[-1]), heads, dim, dtype=dtype), randn(gen(111), int(first[-1]), 1, dim, dtype=dtype)
+    v = torch.cat([torch.nn.functional.one_hot(torch.arange(n, device="cuda") // -(-n // dim), dim) for n in lens])[:, None]
+    got = ss.ss_attention_packed(q, k, v.to(dtype), i32(first.tolist()), max(lens), scale=0.0)
+    for i, n in enumerate(lens):
+        seen = v[first[i]:first[i + 1], 0].double().cumsum(0) / torch.arange(1, n + 1, device="cuda")[:, None]
+        assert ((got[first[i]:first[i + 1]].double() - seen[:, None]).abs() <= (half_step(dtype) + 2.0 ** -20) * seen[:, None]).all(), i
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_prompts_written_in_8_bits_and_attended(dtype):
+    """Prompts into the cache, drafts behind them, and their attention, to the roundings of what the cache then stands for."""
+    kv, group, dim, lens, extra = 2, 4, 128, [70, 1, 200], [5, 3, 9]
+    whole = [a + b for a, b in zip(lens, extra)]
+    c, first = ss.Cache.allocate(whole, kv, dim, I8), np.concatenate([[0], np.cumsum(extra)])
+    for part, base in ((lens, [0, 0, 0]), (extra, lens)):
+        k, v = (randn(gen(112 + sum(part) + i), sum(part), kv, dim, dtype=dtype) for i in range(2))
+        ss.ss_cache_write(c, k, v, i32(np.repeat(np.arange(3), part).tolist()), i32(np.concatenate([b + np.arange(n) for b, n in zip(base, part)]).tolist()))
+    q = randn(gen(120), sum(extra), kv * group, dim, dtype=dtype)
+    got = ss.ss_attention_tree(q, c, i32(lens), max(lens), nodes=i32(first.tolist()), max_nodes=max(extra))
+    start = np.concatenate([[0], np.cumsum(whole)])
+    for i in range(3):
+        see = torch.ones(extra[i], whole[i], dtype=torch.bool, device="cuda").tril(lens[i])
+        for h in range(kv * group):
+            at = int(start[i]) * kv + h // group * whole[i]
+            units = [x[at:at + whole[i]].double() for x in (c.k_scale, c.v_scale)]
+            k, v = (x.view(-1, dim)[at:at + whole[i]].double() * u[:, None] for x, u in zip((c.k, c.v), units))
+            assert_roundings(got[first[i]:first[i + 1], h], q[first[i]:first[i + 1], h], k, v, see, dim ** -0.5, I8, units[1])
