@@ -267,6 +267,8 @@ int ss_forward_logits(ss_weights* w, const int32_t* tokens, const int32_t* offse
  *   node_offsets  host, int32[B+1] from 0, not decreasing; a row may have no nodes, at most SS_TREE_MAX_NODES (below)
  *   parents       host, int32[node_offsets[B]]: an earlier node of the same row, counted from the row's first, or -1
  *   logits_out    host, float32, [vocab] rows: for each row that of its prompt's last position, then those of its nodes
+ * Whatever the cache holds, the nodes' queries are rounded to half (2^-11) before their attention, where over a 16-bit cache those of prompts
+ * keep 22 bits and those of decode steps stay in float32.
  * Errors: SS_EINVAL (as ss_forward_logits; bad nodes; a node beyond 4096 positions), SS_ENOMEM, SS_EDEVICE, SS_ESTATE.
  */
 int ss_tree_logits(ss_weights* w, const int32_t* prompt_tokens, const int32_t* prompt_offsets, int32_t B, const int32_t* node_tokens,
@@ -473,7 +475,8 @@ int ss_cache_read(const ss_cache* cache, const int32_t* seq, const int32_t* slot
  * the call has context[j] slots of history and behind them, in slots context[j], context[j] + 1, ..., the keys and values of its
  * nodes (ss_cache_write has put them there).  Node t attends to the whole history and to those nodes that its mask names:
  *   out[t][head] = sum_s p_s v_s / sum_s p_s,   p_s = exp(scale * <q[t][head], k_s>)
- * A row that sees nothing gets zeros.  Slots that a row does not see have no influence on it, whatever they hold.
+ * A row that sees nothing gets zeros.  Slots that a row does not see have no influence on it, whatever they hold, nor have other rows'
+ * queries; a value that it sees and that is infinite or NaN leaves that element of its result infinite or NaN.
  * Results in half saturate at +-65504, as everything that is stored as half.
  *   q, out       [rows][n_heads][head_dim], of one type, that of the cache if it has 16 bits; head h uses key/value head
  *                h / (n_heads / n_kv_heads)

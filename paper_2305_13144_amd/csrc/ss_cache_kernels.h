@@ -351,11 +351,15 @@ __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* _
 // fill the chip (tree_plan), whose sums k_tree_join adds up.
 // 8-bit caches: codes become halves exactly (1152 + code as a half's bits, less 1152), the key's scale multiplies the score
 // and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R with R a power of two that follows
-// the largest p * scale of the row (WeightUnit): a slot of large values and no weight takes no bits from the others.  A row of bf16 queries is brought into half's range by a power of two of its own.
+// the largest p * scale of the row (WeightUnit): a slot of large values and no weight takes no bits from the others.  Their sum stays that of the
+// unrounded p, as what is rounded has the scale in it: each weight is off by half a step of half, 2^-11 (relative error of a long row 0.0003, where
+// the result's own rounding makes 0.0002).  Over 16-bit caches a weight is rounded to the values' type, which the matrix instructions want
+// of both operands (bf16: 2^-8 each, 0.0020 where the result's rounding makes 0.0016), and the sum is that of the rounded weights.  A row of bf16 queries is brought into half's range by a power of two of its own:
+// exact down to 2^-29 of its largest element, 8 bits being fewer than 11.
 // Slots that a row must not see weigh 0 whatever they hold: scores by selection; infinite and NaN values of steps that not every row sees
 // count as 0 in the products and are added at the end to the rows that see them.
-// Bound by the cache's bytes at long contexts (64 rows to 8000 slots, 32 heads on 8, 8 bits: 91 us, 5.7 TB/s but for the ragged ends), at short
-// ones by the launch and the latencies of table, slots and join (16 rows to 250 slots, 32 heads, halves: 12 us).  Operands are
+// Bound by the cache's bytes at long contexts (64 rows to 8000 slots, 32 heads on 8, 8 bits: 89 to 92 us, 5.7 TB/s but for 2552 chunks of unlike length), at short
+// ones by a chain of latencies: table, slots, the second of two steps one behind the other, barriers, join (16 rows to 250 slots, 32 heads, halves: 12 us).  Operands are
 // requested again as their registers fall free: 3 waves a SIMD, where a second set of registers leaves 2 and a fourth wave spills (98 -> 203 us).
 template <typename C, typename T>
 struct MathType { typedef T type; };           // 16-bit cache: its own type
@@ -857,10 +861,12 @@ __global__ __launch_bounds__(256) void k_tree_join(TreeArgs a)
 // queries, so that a query's numbers are in two lanes and the weights are already the operand that O^T += V^T P^T takes:
 //   weights  lane (query = lane % 32, hi = lane / 32) holds keys 8b + 4hi + (0..3), b = 0..3, of a block; two b's are an operand
 //   values   the same keys of element lane % 32: four neighbouring keys of one element, what the transposed LDS read returns
+// Weights are rounded to the values' type, as above, and their sum is that of the rounded ones.
 // Keys and values are copied into LDS as they lie in memory (two tiles, one on its way while the other is used), pieces of 16 bytes
 // changing places within a row so that what is read at once lies in different banks.
 // Bound by power: 12288 tokens, 32 heads on 8 of 128: 1.09 to 1.21 ms by the card, 1.02 to 1.13 PFLOP/s of the half square that counts, where
-// zeros take 0.88 (the clock falls to 1.8 GHz).  256 prompts to 256 tokens, 32 heads: 215 us, 164 of them bytes.  8 waves a workgroup:
+// zeros take 0.88 (the clock falls to 1.8 GHz, the matrix units are busy 58 % of its cycles).  Several long prompts also by the launch's end,
+// their workgroups being of unlike length: six to 4001 tokens 254 us, 0.96 PFLOP/s.  256 prompts to 256 tokens, 32 heads: 215 us, 164 of them bytes.  8 waves a workgroup:
 // 1199 -> 1224 and 238 -> 275 us; tiles of 32 keys and 2 waves: 216 -> 237 for the short prompts.
 constexpr int kPackTile = 64, kPackQueries = 32;
 
@@ -1110,8 +1116,9 @@ __global__ __launch_bounds__(64 * NW, 2) void k_attention_packed(PackedArgs a)
 // What k_attention_tree computes, for units of more rows than a wave or two can hold: a wave takes 32 rows as the packed kernel takes 32
 // queries, the four waves of a workgroup share tiles of 64 slots in LDS, and slots of 8-bit caches become halves once on their way
 // there, not once per wave.  Copies of 16-bit slots go straight into LDS; codes pass through registers, requested a tile ahead.
-// Bound by vector work, 415 instructions a wave and tile beside 32 products (8 trees to 61 nodes at up to 6000 slots, 32 heads on 8, 8 bits:
-// 37 us; the kernel above in blocks of 32 rows opens the codes once per block: 75 -> 42 when this one was first measured).
+// Bound by vector work and by rows that are not there: 8 trees to 61 nodes at up to 6000 slots, 32 heads on 8, 8 bits, 40 us: 21 vector
+// instructions a product, the matrix units 7 % busy; half of the workgroups' rows exist, as a sequence of 3 nodes has as many workgroups as one of 61.
+// The kernel above in blocks of 32 rows opens the codes once per block: 75 -> 42 when this one was first measured.
 template <int HD, typename T, typename C>
 __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
 {
@@ -1455,7 +1462,10 @@ static void attention_tree(const TreeArgs& a, int tiles, hipStream_t s)
     else if (tiles == 2) k_attention_tree<HD, T, C, 2><<<grid, 256, 0, s>>>(a);
     else k_attention_tree_tall<HD, T, C><<<grid, 256, 0, s>>>(a);
     if (a.chunks < 2) return;
-    // a row's chunks one after another are slower than a workgroup's start where there are more than a few and the rows leave units idle
+    // A row's chunks one after another are slower than a workgroup's start where there are more than a few and the rows leave units idle.
+    // Whole calls, us, a workgroup a row / a group of lanes a row: 32 rows of 9 chunks 13.4 / 14.2, of 16 14.3 / 16.0, of 24 48.7 / 51.8, of 92
+    // 82.1 / 91.9; 512 rows of 24 54.5 / 57.7; 1024 of 11 35.9 / 34.9 and 58.6 / 58.8, 2048 99.0 / 98.1; beyond 4096 the other way: 8192 327.2 / 321.6,
+    // 15616 of 12 56.9 / 46.0.
     const int rows = a.max_nodes * (a.heads / a.c.n_kv), groups = 1024 / HD;
     if (a.chunks > 8 && (int64_t)rows * a.c.n_kv * a.n_seq <= 4096) k_tree_join<HD, T, true><<<dim3(rows, a.c.n_kv, a.n_seq), 256, 0, s>>>(a);
     else k_tree_join<HD, T, false><<<dim3((rows + groups - 1) / groups, a.c.n_kv, a.n_seq), 256, 0, s>>>(a);

@@ -200,8 +200,15 @@ constexpr int64_t table_rows(int first, int end, int64_t most, int64_t rows)
 // One sequence: as many chunks as the chip holds workgroups at once (3 a unit, 2 with more than 16 rows), of at least 256 slots (tall kernel
 // 512).  Several differ in length, which only the device knows: at most 768 slots (512), so that the last chunks of long ones do not run
 // alone.  32 heads on 8, 8 bits, us: 64 rows of up to 8000 slots 384 slots a chunk 105, 512 110, 768 97, 1024 113, whole 117; one row of
-// 500,000 slots 768 231, 2048 208, 8192 (488 workgroups) 187, 16384 220.  Tall: 16 rows of up to 16 nodes and 3000 slots 256 32, 512 29, 768
-// 37, 1024 40; 8 rows of up to 61 nodes and 6000 slots 53, 49, 44, 50; one row of 64 nodes and 8000 slots (bf16) 30, 26, 28, 30.
+// 500,000 slots 768 231, 2048 208, 8192 (488 workgroups) 187, 16384 220.
+// The tall kernel's 512 is the one constant that is least off: over twelve calls (1 to 64 trees of 16 to 100 nodes, 1000 to 30,000 slots, both widths
+// of cache) 9 % slower on average than the best of 256 to 1536, 23 % at worst; 384 13 %, 640 12 %, 768 15 %.  16 rows of up to 16 nodes and 3000
+// slots 256 32, 512 28, 768 37, 1024 37; 8 rows of up to 61 nodes and 6000 slots 50, 46, 42, 49 (16 bits 41, 36, 32, 36); one row of 64 nodes and
+// 8000 slots (bf16) 30, 26, 27, 29.
+// The tall kernel from 33 rows on, blocks of 32 rows against it: over 16 bits 40 rows (64 trees of up to 5 nodes and 2000 slots, 64 heads on 8) 72 / 65,
+// 64 74 / 71, 128 114 / 82, 36 rows (16 trees) 39 / 26, but 33 to 64 rows of one tree at 701 slots 15 to 16 / 17 to 18.  Over 8 bits it
+// breaks even later: 36 rows 35 / 29, but 40 57 / 76, 64 59 / 82, 96 60 / 86, 80 (8 trees) 24 / 26; 128 99 / 92, 244 75 / 46.  One row count serves both, as
+// the workspace's size is asked for without the cache's type.
 constexpr int kTreeMaxChunks = 1024;
 struct TreePlan {
     int tiles, row_blocks, chunk, chunks;
