@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* _
 // unrounded p, as what is rounded has the scale in it: each weight is off by half a step of half, 2^-11 (relative error of a long row 0.0003, where
 // the result's own rounding makes 0.0002).  Over 16-bit caches a weight is rounded to the values' type, which the matrix instructions want
 // of both operands (bf16: 2^-8 each, 0.0020 where the result's rounding makes 0.0016), and the sum is that of the rounded weights.  A row of bf16 queries is brought into half's range by a power of two of its own:
-// exact down to 2^-29 of its largest element, 8 bits being fewer than 11.
+// exact down to 2^-31 of its largest element, 8 bits being fewer than 11.
 // Slots that a row must not see weigh 0 whatever they hold: scores by selection; infinite and NaN values of steps that not every row sees
 // count as 0 in the products and are added at the end to the rows that see them.
 // Bound by the cache's bytes at long contexts (64 rows to 8000 slots, 32 heads on 8, 8 bits: 89 to 92 us, 5.7 TB/s but for 2552 chunks of unlike length), at short
