@@ -66,6 +66,14 @@ __device__ __forceinline__ float exponent_top(float m, float sc, V (&s)[N])
     return top;
 }
 
+// score - top, where the score is a product.  Both are to be the rounded numbers: with the product inside the difference (one fma) its rounding,
+// which is in the top, would remain of the largest score.
+__device__ __forceinline__ float below_top(float score, float top)
+{
+#pragma clang fp contract(off)
+    return score - top;
+}
+
 // The power of two that brings a row whose largest magnitude is `top` (in bf16) to 2^14 to 2^15, and its inverse.  2^-100 and less count as that.
 __device__ __forceinline__ float half_power(float top, float* inverse)
 {
@@ -676,7 +684,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
             for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[u][kt][i], sc[u], -m_sc) : s[u][kt][i] - m_sc);
+                    const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[u][kt][i], sc[u], -m_sc) : below_top(s[u][kt][i], m_sc));
                     if constexpr (I8) {
                         l_run[u] += p;
                         s[u][kt][i] = TAIL && !(seen[kt] >> i & 1) ? 0.f : p * vs[kt][i];
@@ -1304,7 +1312,7 @@ __global__ __launch_bounds__(256, 2) void k_attention_tree_tall(TreeArgs a)
                 if constexpr (I8) vq = *(const f32x4*)&s_vs[b][kt * 32 + 8 * g + 4 * hi];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[kt][4 * g + e], sc, -m_sc) : s[kt][4 * g + e] - m_sc);
+                    const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[kt][4 * g + e], sc, -m_sc) : below_top(s[kt][4 * g + e], m_sc));
                     if constexpr (I8) {
                         l_run += p;
                         s[kt][4 * g + e] = TAIL && !(seen >> (kt * 32 + 8 * g + e) & 1) ? 0.f : p * vq[e];

@@ -923,3 +923,41 @@ def test_prompts_written_in_8_bits_and_attended(dtype):
             units = [x[at:at + whole[i]].double() for x in (c.k_scale, c.v_scale)]
             k, v = (x.view(-1, dim)[at:at + whole[i]].double() * u[:, None] for x, u in zip((c.k, c.v), units))
             assert_roundings(got[first[i]:first[i + 1], h], q[first[i]:first[i + 1], h], k, v, see, dim ** -0.5, I8, units[1])
+
+
+@pytest.mark.parametrize("held", [BF16, I8])
+@pytest.mark.parametrize("nodes,group", [(2, 2), (20, 1), (40, 3)])
+@pytest.mark.parametrize("power", [-116, -100, -60, 60, 100, 116])
+def test_queries_and_keys_whose_sizes_cancel(nodes, group, power, held):
+    """Queries times 2^power, keys times 2^-power: ordinary scores, at both ends of bf16's range."""
+    dim, context = 128, 150
+    H = Held(121, [context + nodes], 1, dim, held)
+    q = randn(gen(122), nodes, group, dim, dtype=BF16)
+    call = lambda q: ss.ss_attention_tree(q, H.cache, i32([context]), context, nodes=i32([0, nodes]), max_nodes=nodes)  # noqa: E731
+    see = torch.ones(nodes, context + nodes, dtype=torch.bool, device="cuda").tril(context)
+    if held == I8:
+        H.raw["k_scale"].mul_(2.0 ** -power)
+        unit = H.raw["v_scale"].double()
+    else:
+        H.raw["k"].mul_(2.0 ** -power)
+        unit = None
+    q = (q.double() * 2.0 ** power).to(BF16)
+    got = call(q)
+    k, v = (H.rows(m, 0, 0, context + nodes) for m in ("k", "v"))
+    for h in range(group):
+        assert_roundings(got[:, h], q[:, h], k, v, see, dim ** -0.5, held, unit)
+
+
+@pytest.mark.parametrize("dtype,size", [(F16, 1e4), (BF16, 1e6), (BF16, 1e15), (BF16, 2e18)])
+@pytest.mark.parametrize("scale", [1.0, -1.0])
+@pytest.mark.parametrize("nodes,context", [(1, 60), (3, 400), (9, 70), (20, 900)])
+def test_large_scores_over_8_bits(nodes, context, scale, dtype, size):
+    """As test_large_scores."""
+    group, dim = 3, 128
+    H = Held(123, [context + nodes], 1, dim, I8)
+    H.raw["k_scale"].mul_(size)
+    q = (randn(gen(124), nodes, group, dim).double() * size).to(dtype)
+    got = ss.ss_attention_tree(q, H.cache, i32([context]), context, nodes=i32([0, nodes]), max_nodes=nodes, scale=scale)
+    k, v = (H.rows(m, 0, 0, context + nodes) for m in ("k", "v"))
+    see = torch.ones(nodes, context + nodes, dtype=torch.bool, device="cuda").tril(context)
+    assert sum(check_best_slot(got[:, h], q[:, h], k, v, see, scale, 2.0 ** -11) for h in range(group)) >= nodes * group // 2
