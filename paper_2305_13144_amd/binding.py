@@ -582,6 +582,9 @@ def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] =
         with t.cuda.device(index):
             return ss_attention_packed(q, k, v, offsets, max_len, scale, out, stream)
     _count(max_len, "max_len")
+    for x, name in ((q, "q"), (k, "k")):
+        if x.dim() != 3:
+            _refuse(x, name, index, "[rows, heads, head_dim] of float16 or bfloat16")
     heads, hd, kv, n = q.shape[1], q.shape[2], k.shape[1], offsets.numel() - 1
     if out is None:
         out = t.empty_like(q, memory_format=t.contiguous_format)

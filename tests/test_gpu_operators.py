@@ -961,3 +961,16 @@ def test_large_scores_over_8_bits(nodes, context, scale, dtype, size):
     k, v = (H.rows(m, 0, 0, context + nodes) for m in ("k", "v"))
     see = torch.ones(nodes, context + nodes, dtype=torch.bool, device="cuda").tril(context)
     assert sum(check_best_slot(got[:, h], q[:, h], k, v, see, scale, 2.0 ** -11) for h in range(group)) >= nodes * group // 2
+
+
+def test_tensors_of_other_dimensions_are_refused():
+    H, x, tables, want, side = held_calls(125)
+    seq, slot, context, nodes = tables
+    k = x[:, :2]
+    for bad in (x[:, 0], x[None]):
+        for call in (lambda: ss.ss_attention_packed(bad, k, k, nodes, 3), lambda: ss.ss_attention_packed(x, bad, k, nodes, 3),
+                     lambda: ss.ss_attention_packed(x, k, bad, nodes, 3), lambda: ss.ss_attention_packed(x, k, k, nodes, 3, out=bad),
+                     lambda: ss.ss_attention_tree(bad, H.cache, context, 40, nodes=nodes, max_nodes=3), lambda: ss.ss_cache_write(H.cache, bad, k, seq, slot),
+                     lambda: ss.ss_cache_write(H.cache, k, bad, seq, slot), lambda: ss.ss_cache_read(H.cache, seq, slot, k=bad)):
+            with pytest.raises(ValueError, match="must be"):
+                call()
