@@ -360,8 +360,11 @@ __global__ __launch_bounds__(256) void k_rotate_store(MbState st, const float* _
 // 8-bit caches: codes become halves exactly (1152 + code as a half's bits, less 1152), the key's scale multiplies the score
 // and the value's the weight.  Weights are rounded to half, so they are held as w = p * scale / R with R a power of two that follows
 // the largest p * scale of the row (WeightUnit): a slot of large values and no weight takes no bits from the others.  Their sum stays that of the
-// unrounded p, as what is rounded has the scale in it: each weight is off by half a step of half, 2^-11 (relative error of a long row 0.0003, where
-// the result's own rounding makes 0.0002).  Over 16-bit caches a weight is rounded to the values' type, which the matrix instructions want
+// unrounded p, as what is rounded has the scale in it, so that the rounding of a large weight does not cancel: each is off by half a step of half, 2^-11.
+// Beside results in bf16 that is nothing.  Results in half of up to 16 rows take the weight as the sum of two halves, a second product for
+// what the first leaves (relative error of a long row 0.00029 -> 0.00021, the result's own rounding; 64 rows of 32 heads at 3000 slots 106 -> 108 us,
+// with heads of 64 60 -> 63); with more rows the vector work and the products bound it (40 -> 43 us in blocks of 32 rows, 46 -> 53 in the
+// kernel for more), and their results keep the one rounding.  Over 16-bit caches a weight is rounded to the values' type, which the matrix instructions want
 // of both operands (bf16: 2^-8 each, 0.0020 where the result's rounding makes 0.0016), and the sum is that of the rounded weights.  A row of bf16 queries is brought into half's range by a power of two of its own:
 // exact down to 2^-31 of its largest element, 8 bits being fewer than 11.
 // Slots that a row must not see weigh 0 whatever they hold: scores by selection; infinite and NaN values of steps that not every row sees
@@ -466,7 +469,7 @@ __device__ __forceinline__ float add_pair(uint32_t a, float sum)
 }
 
 template <int HD, typename T, typename C, int QT>
-__global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArgs a)
+__global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attention_tree(TreeArgs a)
 {
     typedef typename MathType<C, T>::type M;
     typedef typename Half<M>::x8 m8;
@@ -475,6 +478,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
     constexpr int ROW = HD * sizeof(C);      // bytes of a vector
     constexpr int KL = ROW / 64;             // 16-byte loads per 16 slots and lane
     constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
+    constexpr bool PAIRS = I8 && std::is_same<T, _Float16>::value && QT == 1;   // weights as sums of two halves
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
     __shared__ int s_odd[NW];
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
@@ -647,7 +651,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
 #pragma unroll
                 for (int i = 0; i < 4; ++i) kq[kt][i] = ks[kt][i] * log2_scale;
         if (s_next < s_end) load_keys(s_next);
-        m8 pb[QT];
+        m8 pb[QT], rest[QT];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             float mt = kLowest;
@@ -703,7 +707,10 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) pb[u][kt * 4 + i] = (M)(s[u][kt][i] * inv);
+                    for (int i = 0; i < 4; ++i) {
+                        pb[u][kt * 4 + i] = (M)(s[u][kt][i] * inv);
+                        if constexpr (PAIRS) rest[u][kt * 4 + i] = (M)fmaf(s[u][kt][i], inv, -(float)pb[u][kt * 4 + i]);
+                    }
             }
             if constexpr (!I8)
 #pragma unroll
@@ -730,7 +737,10 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void k_attention_tree(TreeArg
             }
             const m8 vf = __builtin_bit_cast(m8, w);
 #pragma unroll
-            for (int u = 0; u < QT; ++u) o[u][t] = Half<M>::mma(vf, pb[u], o[u][t]);
+            for (int u = 0; u < QT; ++u) {
+                o[u][t] = Half<M>::mma(vf, pb[u], o[u][t]);
+                if constexpr (PAIRS) o[u][t] = Half<M>::mma(vf, rest[u], o[u][t]);
+            }
         }
         if (s_next < s_end) load_values(s_next);
     };

@@ -974,3 +974,26 @@ def test_tensors_of_other_dimensions_are_refused():
                      lambda: ss.ss_cache_write(H.cache, k, bad, seq, slot), lambda: ss.ss_cache_read(H.cache, seq, slot, k=bad)):
             with pytest.raises(ValueError, match="must be"):
                 call()
+
+
+@pytest.mark.parametrize("nodes,group,dim,context", [(1, 1, 128, 3900), (1, 16, 64, 700), (4, 4, 128, 300), (16, 1, 64, 60)])
+@pytest.mark.parametrize("lowest", [0, 3, 20])
+def test_half_results_of_few_rows_over_8_bits_have_one_rounding(nodes, group, dim, context, lowest):
+    """Up to 16 rows a unit weights are pairs of halves: off by 2^-22 of themselves (2^-11 of what the first leaves, 2^-11), or where they are
+    subnormal by 2^-25 R with 2^6 R at most the largest product, times codes up to 127.  Scores are whole numbers of powers of two from 0 to
+    -20, exact but for scale log2(e), which is 1 within 2^-23: 20 2^-23 ln 2 of a weight, 2^-18 with the exponential and the sums."""
+    H = Held(126, [context + nodes], 1, dim, I8)
+    H.raw["k"].zero_()
+    H.raw["k"][:, 0] = -torch.randint(0, lowest + 1, (len(H.raw["k"]),), device="cuda", generator=gen(127)).to(I8)
+    H.raw["k_scale"].fill_(1)
+    q = torch.zeros(nodes, group, dim, dtype=F16, device="cuda")
+    q[..., 0] = 1
+    got = ss.ss_attention_tree(q, H.cache, i32([context]), context, nodes=i32([0, nodes]), max_nodes=nodes, scale=math.log(2))
+    at = slice(int(H.start[0]), int(H.start[0]) + context + nodes)
+    v, unit = H.rows("v", 0, 0, context + nodes), H.raw["v_scale"].double()[at]
+    p = torch.exp2(H.raw["k"][at, 0].double()).expand(nodes, -1) * torch.ones(nodes, context + nodes, device="cuda").tril(context)
+    w = p / p.sum(-1, keepdim=True)
+    ref, A = w @ v, w @ v.abs()
+    tol = half_step(F16) * ref.abs() + (2.0 ** -22 + 2.0 ** -18) * A + len(v) * 2.0 ** -31 * 127 * (w * unit).amax(-1, keepdim=True)
+    bad = (got.double() - ref[:, None]).abs() > tol[:, None]
+    assert not bad.any(), (bad.sum().item(), ((got.double() - ref[:, None]).abs() / tol[:, None]).max().item())
