@@ -511,6 +511,147 @@ int ss_tree_mask(const int32_t* parents, int32_t n, int32_t max_nodes, uint64_t*
 int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_rows* v, const ss_rows* out, int32_t n_heads, int32_t n_kv_heads,
                         int32_t head_dim, const int32_t* offsets, int32_t n_seq, int32_t max_len, float scale, void* hip_stream);
 
+/* ------------------------------------------------------------------ caches in pages, and beam search over them */
+
+/*
+ * A pool of pages holds the keys and values of one layer: element e of head h in slot s of page p is at
+ * ((p * n_kv_heads + h) * page_slots + s) * head_dim + e of k and v.  SS_I8: as in ss_cache, the scale of a vector at (p * n_kv_heads + h) *
+ * page_slots + s.
+ */
+typedef struct {
+    void *k, *v;              /* device, 16-byte aligned, n_pages * n_kv_heads * page_slots * head_dim elements */
+    float *k_scale, *v_scale; /* device, 16-byte aligned, n_pages * n_kv_heads * page_slots, SS_I8 only         */
+    int32_t n_pages;
+    int32_t page_slots;       /* 16, 32, 64, 128 or 256 */
+    int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */
+    int32_t dtype;            /* SS_F16, SS_BF16, SS_I8 */
+} ss_pages;
+
+/*
+ * Whose pages they are, in every layer alike: position t of row i is slot t % page_slots of page pages[i * stride + t / page_slots].  A length
+ * below 0 counts as 0, one beyond stride * page_slots as that; entries behind a row's length are not looked at.  A page may be in several
+ * rows (they share what they have in common).  An entry that is no page (-1, say) holds nothing: its positions are not written, not read and
+ * not attended to.
+ */
+typedef struct {
+    int32_t* pages;   /* device, int32[n_rows * stride] */
+    int32_t* lengths; /* device, int32[n_rows]: positions that the row has */
+    int32_t n_rows, stride;
+    int32_t page_slots, n_pages; /* of the pools */
+} ss_page_table;
+
+#define SS_PAGES_MAX_ROWS 8192 /* of a table that forks or is made dense */
+
+/*
+ * Keys and values of n tokens into their pages: token t goes to position pos[t] of row row[t] (device, int32[n]); both NULL: to the last
+ * position of row t (the decode step, after ss_pages_fork has made room).  Tokens whose row, position (not below the row's length) or page
+ * does not exist are passed over.  A place may be written once per call.  k, v and what they become as in ss_cache_write; ss_pages_read
+ * is the way back, as ss_cache_read.
+ */
+int ss_pages_write(const ss_pages* pages, const ss_page_table* table, const ss_rows* k, const ss_rows* v, const int32_t* row,
+                   const int32_t* pos, int32_t n, void* hip_stream);
+int ss_pages_read(const ss_pages* pages, const ss_page_table* table, const int32_t* row, const int32_t* pos, int32_t n, const ss_rows* k,
+                  const ss_rows* v, void* hip_stream);
+
+#define SS_PAGES_MAX_GROUP 32
+
+/*
+ * Attention of one new token per row over the pages of its row of the table, its own key and value among them (ss_pages_write has put them
+ * there): out[j][head] = sum_s p_s v_s / sum_s p_s, p_s = exp(scale * <q[j][head], k_s>), over the positions s below the row's length.  A row
+ * that sees nothing gets zeros; what it does not see, and infinite and NaN values, as in ss_attention_tree.
+ *   q, out      [n][n_heads][head_dim], of one type, that of the pool if it has 16 bits; head h uses key/value head h / (n_heads / n_kv_heads)
+ *   rows        device, int32[n], nullable: the table's row of the j-th query; NULL = row j.  A row that does not exist gets zeros
+ *   max_length  the largest length (host; it only chooses how the work is shared out: a longer row is attended all the same)
+ *   group       n is a multiple of it: queries j * group .. j * group + group - 1 are looked at together, and where their rows hold the same
+ *               page in the same entry (the beams of a prompt do) it is read once for all of them.  1 to SS_PAGES_MAX_GROUP.  It changes the time, and
+ *               results by roundings, nothing else
+ *   workspace   device, 16-byte aligned, at least the bytes that ss_attention_pages_workspace gives for the same counts and stride on the
+ *               same device (0: may be NULL); its contents need not be kept and do not matter
+ */
+int ss_attention_pages(const ss_pages* pages, const ss_page_table* table, const ss_rows* q, const ss_rows* out, int32_t n_heads, int32_t n,
+                       const int32_t* rows, int32_t max_length, int32_t group, float scale, void* workspace, size_t workspace_bytes,
+                       void* hip_stream);
+int ss_attention_pages_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_slots, int32_t stride, int32_t n,
+                                 int32_t max_length, int32_t group, size_t* bytes);
+
+/*
+ * A step of the rows of a table: row i of `to` takes over the pages of row parent[i] of `from` and grows by grow[i] positions.  Rows that are
+ * nobody's parent are let go; a page that no row of `to` holds is free.  Free pages are handed out lowest number first, row after row and
+ * in a row entry after entry.  Where a row grows into its last page (its length is no multiple of page_slots) and another row of `to` holds that
+ * page too, they must not both write there: of the rows that do, the lowest keeps the page if no row holds it that does not, and each other
+ * gets a free page in its place, before those that it grows by, and its pair in src and dst, for ss_pages_copy to copy the contents.
+ *   from, to    tables of the same page_slots and n_pages; `to` (its entries behind a row's last page become -1, its lengths are set) shares
+ *               no memory with `from`.  A row that would grow beyond its stride stays as long as that
+ *   parent      device, int32[to->n_rows], nullable: NULL = row i continues row i.  A row without a parent (-1, no such row) begins empty
+ *   grow        device, int32[to->n_rows], nullable: NULL = 1 for each row that has a parent and 0 for the others.  Negative: 0
+ *   held        device, uint8[n_pages], nullable: nonzero = somebody else holds the page too: it is not free, and nobody writes into it
+ *   src, dst    device, int32[to->n_rows]: the pages to copy for row i, -1 where there are none
+ *   missing     device, int32[1]: pages that there were not, 0 if all went well.  The rows that lack them have -1 in their places (if it is the copy of a
+ *               last page, they have lost its positions): the caller takes `from` once more, with fewer rows or less to grow
+ *   workspace   device, 16-byte aligned, ss_pages_workspace bytes; contents do not matter
+ * To let rows go, or to begin new ones beside those that are there: parent; to grow without a fork: parent NULL.  Entries of `from` that are no
+ * page stay as they are (-1).
+ */
+int ss_pages_fork(const ss_page_table* from, const ss_page_table* to, const int32_t* parent, const int32_t* grow, const uint8_t* held,
+                  int32_t* src, int32_t* dst, int32_t* missing, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * New numbers for the pages in use, so that they are 0 .. counts[0] - 1: the k-th page in use from counts[0] on (in the order of numbers)
+ * takes the number of the k-th free page below it, the others keep theirs.
+ *   from, to    tables of the same shape; `to` gets the new numbers (-1 behind a row's last page, and for entries that are no page) and the
+ *               lengths.  `to` may be `from` itself; else they share no memory
+ *   held        as above: such pages are in use too, whoever holds them finds them by `place`
+ *   src, dst    device, int32[n_pages / 2]: the pages to copy, for ss_pages_copy with &counts[1]; -1 behind them
+ *   place       device, int32[n_pages], nullable: the new number of each page, -1 for free ones
+ *   counts      device, int32[2]: pages in use; pages to copy
+ *   workspace   as above
+ */
+int ss_pages_compact(const ss_page_table* from, const ss_page_table* to, const uint8_t* held, int32_t* src, int32_t* dst, int32_t* place,
+                     int32_t* counts, void* workspace, size_t workspace_bytes, void* hip_stream);
+int ss_pages_workspace(int32_t n_pages, size_t* bytes);
+
+/*
+ * Copies page src[i] to page dst[i] (device, int32[n]) for i below n and, if `count` (device, int32[1], nullable) is given, below *count, in each
+ * of n_layers pools alike (host: an array of pools that differ in nothing but their pointers).  Pairs with a number that is no page
+ * are passed over.  No page may be the destination of two pairs, or of one and the source of another.
+ */
+int ss_pages_copy(const ss_pages* layers, int32_t n_layers, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* count,
+                  void* hip_stream);
+
+#define SS_BEAM_MAX 64
+
+/* The state of beams, one entry (row) each. */
+typedef struct {
+    float*   totals;  /* sum of the log probabilities of the beam's tokens; a beam whose sum is not finite has no continuation            */
+    int32_t* lengths; /* tokens so far.  NULL if there are no histories and length_power is 0; a length below 0 counts as 0, none grows beyond 2^31 - 1 */
+    uint8_t* ended;   /* nonzero: the beam takes no further token.  NULL: none has ended (as input), not wanted (as output)           */
+    int32_t* history; /* int32[rows][history_stride]: the beam's tokens, nullable                                                     */
+    int32_t  history_stride;
+} ss_beams;
+
+/*
+ * A step of beam search.  Each of n_groups groups has `beams` beams (row g * beams + b) and, for each that has not ended, the logits of its next
+ * token.  Candidates are (b, v): beam b continued by token v, with the sum total_b + ((logit - m) - log sum exp(logits - m)), m the row's largest
+ * logit, and length + 1;
+ * of a beam that has ended only itself, with its sum and length, as (b, end_id) (end_id -1: as (b, 0), and its token is -1).  Their rank is
+ * sum / length^length_power (a length of 0 counts as 1).  Of a group's candidates the `keep` with the largest rank are taken in that order, of equal ones first that with the
+ * lower b * vocab + v.  Logits that are infinite or NaN are no candidates and have no part in the sum.
+ *   logits       device, [n_groups * beams][vocab] of SS_F32, SS_F16 or SS_BF16, aligned as its elements are; rows `row_stride` elements apart.
+ *                Rows of beams that have ended are not read
+ *   now          the beams' state; next: that of the taken candidates (n_groups * keep rows), shares no memory with `now`.  next->ended: the
+ *                candidate had ended, or its token is end_id.  next->history: the parent's tokens and the new one, as far as there is room, -1 behind
+ *                them; given exactly if now->history is
+ *   parent       device, int32[n_groups * keep]: the row that the candidate continues, as ss_pages_fork takes it
+ *   token        device, int32[n_groups * keep]
+ * A group with fewer candidates has none in its last places: parent and token -1, sum -inf, length 0, ended.
+ * 1 <= beams, keep <= SS_BEAM_MAX.  Ranks and sums are formed in float64 (log sum exp to about 2^-23), sums rounded to float32 once per step.
+ *   workspace    device, 16-byte aligned, ss_beam_select_workspace bytes; contents do not matter
+ */
+int ss_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep,
+                   const ss_beams* now, const ss_beams* next, int32_t* parent, int32_t* token, int32_t end_id, float length_power,
+                   void* workspace, size_t workspace_bytes, void* hip_stream);
+int ss_beam_select_workspace(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep, size_t* bytes);
+
 #ifdef __cplusplus
 }
 #endif

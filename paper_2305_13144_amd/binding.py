@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import numpy as np
 
@@ -22,12 +22,15 @@ SS_OPT_IN_FLIGHT, SS_IN_FLIGHT_MAX, SS_IN_FLIGHT_DEFAULT = 2, 4, 4
 SS_OPT_WEIGHT_COPIES, SS_OPT_CACHE_BITS = 3, 4
 SS_BF16, SS_F32, SS_F16, SS_I8 = 0, 1, 2, 3
 SS_TREE_MAX_NODES = 1024
+SS_PAGES_MAX_ROWS, SS_PAGES_MAX_GROUP, SS_BEAM_MAX = 8192, 32, 64
 FLAG_BITS = dict(SORT=SS_SORT, BIN=SS_BIN, FCR=SS_FCR, VBS=SS_VBS, COMPACT=SS_COMPACT)
 
 EXPORTS = ["ss_last_error", "ss_set_verbose", "ss_set_gemm_mode", "ss_schedule", "ss_schedule_failures", "ss_plan_free", "ss_weights_create",
            "ss_weights_destroy", "ss_set_option", "ss_decode_microbatch", "ss_decode_microbatch_static", "ss_forward_logits", "ss_tree_logits", "ss_run_group", "ss_generate_microbatch",
            "ss_run_group_generate", "ss_bench_decode_step", "ss_bench_decode_steps_in_flight", "ss_bench_weight_stream", "ss_bench_read_stream",
-           "ss_cache_write", "ss_cache_read", "ss_attention_tree", "ss_attention_tree_workspace", "ss_tree_mask", "ss_attention_packed"]
+           "ss_cache_write", "ss_cache_read", "ss_attention_tree", "ss_attention_tree_workspace", "ss_tree_mask", "ss_attention_packed",
+           "ss_pages_write", "ss_pages_read", "ss_attention_pages", "ss_attention_pages_workspace", "ss_pages_fork", "ss_pages_compact",
+           "ss_pages_workspace", "ss_pages_copy", "ss_beam_select", "ss_beam_select_workspace"]
 
 
 class SsError(RuntimeError):
@@ -79,6 +82,21 @@ class ss_cache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("start", C.c_void_p),
                 ("slots", C.c_void_p), ("total_slots", C.c_int64), ("n_seq", C.c_int32), ("n_kv_heads", C.c_int32),
                 ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ss_pages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_slots", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class ss_page_table(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("lengths", C.c_void_p), ("n_rows", C.c_int32), ("stride", C.c_int32),
+                ("page_slots", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class ss_beams(C.Structure):
+    _fields_ = [("totals", C.c_void_p), ("lengths", C.c_void_p), ("ended", C.c_void_p), ("history", C.c_void_p),
+                ("history_stride", C.c_int32)]
 
 
 def _struct_dict(s: C.Structure) -> dict:
@@ -134,6 +152,17 @@ def lib():
         L.ss_tree_mask.argtypes = [vp, C.c_int32, C.c_int32, vp]
         L.ss_attention_packed.argtypes = [rows, rows, rows, rows, C.c_int32, C.c_int32, C.c_int32, vp, C.c_int32, C.c_int32,
                                           C.c_float, vp]
+        pages, table, beams, i32 = C.POINTER(ss_pages), C.POINTER(ss_page_table), C.POINTER(ss_beams), C.c_int32
+        L.ss_pages_write.argtypes = [pages, table, rows, rows, vp, vp, i32, vp]
+        L.ss_pages_read.argtypes = [pages, table, vp, vp, i32, rows, rows, vp]
+        L.ss_attention_pages.argtypes = [pages, table, rows, rows, i32, i32, vp, i32, i32, C.c_float, vp, C.c_size_t, vp]
+        L.ss_attention_pages_workspace.argtypes = [i32] * 8 + [C.POINTER(C.c_size_t)]
+        L.ss_pages_fork.argtypes = [table, table, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.ss_pages_compact.argtypes = [table, table, vp, vp, vp, vp, vp, vp, C.c_size_t, vp]
+        L.ss_pages_workspace.argtypes = [i32, C.POINTER(C.c_size_t)]
+        L.ss_pages_copy.argtypes = [pages, i32, vp, vp, i32, vp, vp]
+        L.ss_beam_select.argtypes = [vp, i32, C.c_int64, i32, i32, i32, i32, beams, beams, vp, vp, i32, C.c_float, vp, C.c_size_t, vp]
+        L.ss_beam_select_workspace.argtypes = [i32] * 4 + [C.POINTER(C.c_size_t)]
         for name in EXPORTS:
             if name not in ("ss_last_error", "ss_set_verbose", "ss_set_gemm_mode", "ss_plan_free", "ss_weights_destroy"):
                 getattr(L, name).restype = C.c_int
@@ -591,4 +620,306 @@ def ss_attention_packed(q, k, v, offsets, max_len: int, scale: Optional[float] =
     _check(_lib.ss_attention_packed(_rows(q, "q", index, heads, hd), _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd),
                                     _rows(out, "out", index, heads, hd), heads, kv, hd, _table(offsets, "offsets", index, n + 1, t.int32), n, max_len,
                                     hd ** -0.5 if scale is None else scale, _on(stream, index, q, k, v, out, offsets)))
+    return out
+
+
+# ---------------------------------------------------------------------------------------------------- caches in pages, beam search
+
+
+class Pages:
+    """The pool of pages of one layer (ss_pages): a view of tensors that the caller owns.
+
+    k, v              flat, pages * n_kv_heads * page_slots * head_dim elements of float16, bfloat16 or int8
+    k_scale, v_scale  flat float32, pages * n_kv_heads * page_slots, with int8
+    """
+
+    def __init__(self, k, v, page_slots: int, n_kv_heads: int, head_dim: int, k_scale=None, v_scale=None):
+        t = _with_torch()
+        if n_kv_heads < 1 or head_dim not in (64, 128) or page_slots not in (16, 32, 64, 128, 256):
+            raise ValueError("n_kv_heads must be positive, head_dim 64 or 128, page_slots 16, 32, 64, 128 or 256")
+        vectors = n_kv_heads * page_slots
+        if k.dtype not in _ELEMENT or not k.is_cuda or k.numel() % (vectors * head_dim) or k.numel() == 0:
+            _refuse(k, "k", k.get_device(), "whole pages, at least one, of float16, bfloat16 or int8")
+        index, dtype, n = k.get_device(), _ELEMENT[k.dtype], k.numel() // (vectors * head_dim)
+        _count(n, "the number of pages")
+        if (dtype == SS_I8) != (k_scale is not None) or (dtype == SS_I8) != (v_scale is not None):
+            raise ValueError("k_scale and v_scale belong to int8 pages, and only to them")
+        ptr = [_table(x, name, index, k.numel(), k.dtype) for x, name in ((k, "k"), (v, "v"))]
+        ptr += [_table(x, name, index, n * vectors, t.float32) for x, name in ((k_scale, "k_scale"), (v_scale, "v_scale"))]
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.page_slots, self.n_kv_heads, self.head_dim = n, page_slots, n_kv_heads, head_dim
+        self.device, self.index = k.device, index
+        self.struct = ss_pages(*ptr, n, page_slots, n_kv_heads, head_dim, dtype)
+        self.tensors = (k, v, k_scale, v_scale)
+
+    @classmethod
+    def allocate(cls, n_pages: int, page_slots: int, n_kv_heads: int, head_dim: int, dtype, device="cuda") -> "Pages":
+        """Empty pages of torch.float16, bfloat16 or int8."""
+        t = _with_torch()
+        if min(n_pages, page_slots, n_kv_heads, head_dim) < 1:
+            raise ValueError("n_pages, page_slots, n_kv_heads and head_dim must be positive")
+        vectors = n_pages * n_kv_heads * page_slots
+        k, v = (t.zeros(vectors * head_dim, dtype=dtype, device=device) for _ in range(2))
+        scales = [t.zeros(vectors, device=device) if dtype == t.int8 else None for _ in range(2)]
+        return cls(k, v, page_slots, n_kv_heads, head_dim, *scales)
+
+
+class PageTable:
+    """Which pages hold the positions of each row, in every layer alike (ss_page_table): a view of tensors that the caller owns.
+
+    pages    int32 [rows, stride]: page of positions page_slots * e .. page_slots * (e + 1) - 1 in entry e; -1: none
+    lengths  int32 [rows]
+    """
+
+    def __init__(self, pages, lengths, page_slots: int, n_pages: int):
+        t = _with_torch()
+        if page_slots not in (16, 32, 64, 128, 256) or n_pages < 1:
+            raise ValueError("page_slots must be 16, 32, 64, 128 or 256, n_pages positive")
+        index = lengths.get_device()
+        if index < 0:
+            _refuse(lengths, "lengths", index, "")
+        if pages.dim() != 2 or pages.shape[0] != lengths.numel():
+            _refuse(pages, "pages", index, f"[{lengths.numel()}, entries] of {t.int32}")
+        rows, stride = pages.shape
+        _count(n_pages, "n_pages")
+        _count(rows, "the number of rows")
+        _count(stride, "the number of entries")
+        self.struct = ss_page_table(_table(pages, "pages", index, rows * stride, t.int32), _table(lengths, "lengths", index, rows, t.int32),
+                                    rows, stride, page_slots, n_pages)
+        self.pages, self.lengths, self.page_slots, self.n_pages = pages, lengths, page_slots, n_pages
+        self.rows, self.stride, self.device, self.index = rows, stride, lengths.device, index
+        self.tensors = (pages, lengths)
+
+    @classmethod
+    def allocate(cls, rows: int, stride: int, page_slots: int, n_pages: int, device="cuda") -> "PageTable":
+        """`rows` rows without pages, with room for `stride` each."""
+        t = _with_torch()
+        return cls(t.full((rows, stride), -1, dtype=t.int32, device=device), t.zeros(rows, dtype=t.int32, device=device), page_slots, n_pages)
+
+
+def _same_device(index: int, *others):
+    for name, x in others:
+        if x.index != index:
+            raise ValueError(f"{name} must be on cuda:{index}: it is on {x.device}")
+
+
+def ss_pages_write(pages: Pages, table: PageTable, k, v, row=None, pos=None, stream: Optional[int] = None) -> None:
+    """Keys and values [n, n_kv_heads, head_dim] of n tokens to position pos[t] of row row[t] (int32 [n]; -1: passed over); without row and
+    pos, of one token per row to its last position."""
+    t, index = _torch, pages.index
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_pages_write(pages, table, k, v, row, pos, stream)
+    _same_device(index, ("table", table))
+    n, kv, hd, i32 = k.shape[0], pages.n_kv_heads, pages.head_dim, t.int32
+    _check(_lib.ss_pages_write(pages.struct, table.struct, _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd), _table(row, "row", index, n, i32),
+                               _table(pos, "pos", index, n, i32), _count(n, "the number of tokens"), _on(stream, index, k, v, row, pos, *pages.tensors, *table.tensors)))
+
+
+def ss_pages_read(pages: Pages, table: PageTable, row=None, pos=None, dtype=None, k=None, v=None, stream: Optional[int] = None):
+    """(k, v) [n, n_kv_heads, head_dim]: what position pos[t] of row row[t] stands for; without row and pos, the last position of each row.
+    Into k and v if they are given, whose rows of tokens that do not exist stay as they are; into new tensors of `dtype` (float16)
+    otherwise, where those rows are undefined."""
+    t, index = _torch, pages.index
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_pages_read(pages, table, row, pos, dtype, k, v, stream)
+    _same_device(index, ("table", table))
+    n, kv, hd, i32 = table.rows if row is None else row.numel(), pages.n_kv_heads, pages.head_dim, t.int32
+    if k is None:
+        k = t.empty((n, kv, hd), dtype=dtype or t.float16, device=pages.device)
+    if v is None:
+        v = t.empty_like(k, memory_format=t.contiguous_format)
+    _check(_lib.ss_pages_read(pages.struct, table.struct, _table(row, "row", index, n, i32), _table(pos, "pos", index, n, i32), _count(n, "the number of tokens"),
+                              _rows(k, "k", index, kv, hd), _rows(v, "v", index, kv, hd), _on(stream, index, k, v, row, pos, *pages.tensors, *table.tensors)))
+    return k, v
+
+
+def ss_attention_pages_workspace(n_heads: int, n_kv_heads: int, head_dim: int, page_slots: int, stride: int, n: int, max_length: int,
+                                 group: int = 1) -> int:
+    """Bytes of workspace that ss_attention_pages takes for these counts, and a table of `stride` entries a row, on the current device."""
+    need = C.c_size_t(0)
+    for x, name in ((n_heads, "n_heads"), (n_kv_heads, "n_kv_heads"), (stride, "stride"), (n, "n"), (max_length, "max_length"), (group, "group")):
+        _count(x, name)
+    _check(lib().ss_attention_pages_workspace(n_heads, n_kv_heads, head_dim, page_slots, stride, n, max_length, group, need))
+    return need.value
+
+
+def ss_attention_pages(q, pages: Pages, table: PageTable, max_length: int, group: int = 1, rows=None, scale: Optional[float] = None, out=None,
+                       workspace=None, stream: Optional[int] = None):
+    """Attention of one token per row, q [n, heads, head_dim], over the pages of its row of the table (rows int32 [n]; None: row j), which
+    hold its own key and value too.  Queries j * group .. are looked at together: pages that their rows share are read once.  scale: head_dim
+    ** -0.5 if not given.  workspace: a uint8 tensor (a new one if not given).  Returns out, a new tensor if not given."""
+    t, index = _torch, pages.index
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_attention_pages(q, pages, table, max_length, group, rows, scale, out, workspace, stream)
+    _same_device(index, ("table", table))
+    hd, n = pages.head_dim, q.shape[0]
+    _count(n, "the number of rows")
+    _count(max_length, "max_length")
+    _count(group, "group")
+    qr = _rows(q, "q", index, None, hd)
+    heads = q.shape[1]
+    if out is None:
+        out = t.empty_like(q, memory_format=t.contiguous_format)
+    if workspace is None:
+        need = C.c_size_t(0)
+        _check(_lib.ss_attention_pages_workspace(heads, pages.n_kv_heads, hd, pages.page_slots, table.stride, n, max_length, group, need))
+        if need.value:
+            workspace = t.empty(need.value, dtype=t.uint8, device=pages.device)
+    size = 0 if workspace is None else workspace.numel()
+    _check(_lib.ss_attention_pages(pages.struct, table.struct, qr, _rows(out, "out", index, heads, hd), heads, n, _table(rows, "rows", index, n, t.int32),
+                                   max_length, group, hd ** -0.5 if scale is None else scale, _table(workspace, "workspace", index, size, t.uint8), size,
+                                   _on(stream, index, q, out, rows, workspace, *pages.tensors, *table.tensors)))
+    return out
+
+
+def ss_pages_workspace(n_pages: int) -> int:
+    """Bytes of workspace that ss_pages_fork and ss_pages_compact take."""
+    need = C.c_size_t(0)
+    _check(lib().ss_pages_workspace(_count(n_pages, "n_pages"), need))
+    return need.value
+
+
+def ss_pages_fork(table: PageTable, to: PageTable, parent=None, grow=None, held=None, src=None, dst=None, missing=None, workspace=None,
+                  stream: Optional[int] = None):
+    """Row i of `to` takes over the pages of row parent[i] of `table` (int32 [to.rows]; None: row i; -1: none) and grows by grow[i] positions (int32; None: 1
+    where there is a parent).  held uint8 [n_pages]: nonzero, somebody else holds the page too.  Returns (src, dst, missing), int32, new tensors if not
+    given: the pages that ss_pages_copy has to copy for each row, -1 for none, and how many pages there were too few."""
+    t, index = _torch, table.index
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_pages_fork(table, to, parent, grow, held, src, dst, missing, workspace, stream)
+    _same_device(index, ("to", to))
+    n, i32 = to.rows, t.int32
+    if src is None:
+        src = t.empty(n, dtype=i32, device=table.device)
+    if dst is None:
+        dst = t.empty(n, dtype=i32, device=table.device)
+    if missing is None:
+        missing = t.empty(1, dtype=i32, device=table.device)
+    if workspace is None:
+        workspace = t.empty(8 * table.n_pages, dtype=t.uint8, device=table.device)
+    size = workspace.numel()
+    _check(_lib.ss_pages_fork(table.struct, to.struct, _table(parent, "parent", index, n, i32), _table(grow, "grow", index, n, i32),
+                              _table(held, "held", index, table.n_pages, t.uint8), _table(src, "src", index, n, i32), _table(dst, "dst", index, n, i32),
+                              _table(missing, "missing", index, 1, i32), _table(workspace, "workspace", index, size, t.uint8), size,
+                              _on(stream, index, parent, grow, held, src, dst, missing, workspace, *table.tensors, *to.tensors)))
+    return src, dst, missing
+
+
+def ss_pages_compact(table: PageTable, to: Optional[PageTable] = None, held=None, src=None, dst=None, place=None, counts=None, workspace=None,
+                     stream: Optional[int] = None):
+    """The pages in use get the numbers 0 .. counts[0] - 1, in `to` (None: in the table itself).  Returns (src, dst, place, counts), int32, new tensors if not
+    given: the pages to copy (ss_pages_copy with counts[1:]), the new number of every page (-1: free), and how many are in use and move."""
+    t, index = _torch, table.index
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_pages_compact(table, to, held, src, dst, place, counts, workspace, stream)
+    if to is None:
+        to = table
+    _same_device(index, ("to", to))
+    n, i32 = table.n_pages, t.int32
+    if src is None:
+        src = t.empty(n // 2, dtype=i32, device=table.device)
+    if dst is None:
+        dst = t.empty(n // 2, dtype=i32, device=table.device)
+    if place is None:
+        place = t.empty(n, dtype=i32, device=table.device)
+    if counts is None:
+        counts = t.empty(2, dtype=i32, device=table.device)
+    if workspace is None:
+        workspace = t.empty(8 * n, dtype=t.uint8, device=table.device)
+    size = workspace.numel()
+    _check(_lib.ss_pages_compact(table.struct, to.struct, _table(held, "held", index, n, t.uint8), _table(src, "src", index, n // 2, i32),
+                                 _table(dst, "dst", index, n // 2, i32), _table(place, "place", index, n, i32), _table(counts, "counts", index, 2, i32),
+                                 _table(workspace, "workspace", index, size, t.uint8), size,
+                                 _on(stream, index, held, src, dst, place, counts, workspace, *table.tensors, *to.tensors)))
+    return src, dst, place, counts
+
+
+def ss_pages_copy(layers: Sequence[Pages], src, dst, count=None, stream: Optional[int] = None) -> None:
+    """Page src[i] to page dst[i] (int32 [n]; -1: passed over) in every layer, for i below count[0] if `count` (int32 [1]) is given."""
+    if not layers:
+        return
+    t, index = _torch, layers[0].index
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_pages_copy(layers, src, dst, count, stream)
+    for x in layers:
+        if x.index != index:
+            raise ValueError(f"every layer must be on cuda:{index}: one is on {x.device}")
+    n, i32 = src.numel(), t.int32
+    structs = (ss_pages * len(layers))(*[x.struct for x in layers])
+    _check(_lib.ss_pages_copy(structs, len(layers), _table(src, "src", index, n, i32), _table(dst, "dst", index, n, i32), _count(n, "the number of pairs"),
+                              _table(count, "count", index, 1, i32), _on(stream, index, src, dst, count, *(y for x in layers for y in x.tensors))))
+
+
+class Beams(NamedTuple):
+    """What ss_beam_select returns: the candidates that were taken, `keep` of each group."""
+    parent: object    # int32 [groups * keep]: the row that each continues (ss_pages_fork's parent), -1: none
+    token: object     # int32 [groups * keep]
+    totals: object    # float32 [groups, keep]
+    lengths: object   # int32 [groups * keep], None without lengths
+    ended: object     # uint8 [groups * keep]
+    history: object   # int32 [groups * keep, width], None without histories
+
+
+def ss_beam_select_workspace(n_groups: int, beams: int, vocab: int, keep: int) -> int:
+    """Bytes of workspace that ss_beam_select takes."""
+    need = C.c_size_t(0)
+    for x, name in ((n_groups, "n_groups"), (beams, "beams"), (vocab, "vocab"), (keep, "keep")):
+        _count(x, name)
+    _check(lib().ss_beam_select_workspace(n_groups, beams, vocab, keep, need))
+    return need.value
+
+
+def ss_beam_select(logits, totals, keep: int, lengths=None, ended=None, end_id: int = -1, length_power: float = 0.0, history=None, out: Optional[Beams] = None,
+                   workspace=None, stream: Optional[int] = None) -> Beams:
+    """A step of beam search: of all continuations of the beams of each group the `keep` best, by the sum of their tokens' log probabilities over
+    length ** length_power.  logits [groups * beams, vocab] of float32, float16 or bfloat16; totals float32 [groups, beams]; lengths int32 and ended uint8
+    [groups * beams]; history int32 [groups * beams, width].  Returns the new state in new tensors, or in `out`'s."""
+    t = _with_torch()
+    index = logits.get_device()
+    if index < 0:
+        _refuse(logits, "logits", index, "")
+    if index != t.cuda.current_device():
+        with t.cuda.device(index):
+            return ss_beam_select(logits, totals, keep, lengths, ended, end_id, length_power, history, out, workspace, stream)
+    for x, name in ((logits, "logits"), (totals, "totals")):
+        if x.requires_grad and t.is_grad_enabled():
+            raise ValueError(f"{name} requires gradients, and this operator has none: call it under torch.no_grad(), or with {name}.detach()")
+    dtype = SS_F32 if logits.dtype is t.float32 else _ELEMENT.get(logits.dtype, SS_I8)
+    if totals.dim() != 2:
+        _refuse(totals, "totals", index, "[groups, beams] of float32")
+    groups, beams = totals.shape
+    if logits.dim() != 2 or logits.shape[0] != groups * beams or dtype == SS_I8 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _refuse(logits, "logits", index, f"[{groups * beams}, vocab] of float32, float16 or bfloat16 whose last dimension is contiguous")
+    for x, name in ((keep, "keep"), (end_id, "end_id"), (logits.shape[0], "the number of rows"), (logits.shape[1], "vocab")):
+        _count(x, name)
+    vocab, rows, n, i32, dev = logits.shape[1], groups * beams, groups * max(keep, 0), t.int32, logits.device
+    if history is not None and (history.dim() != 2 or history.shape[0] != rows):
+        _refuse(history, "history", index, f"[{rows}, width] of int32")
+    width = 0 if history is None else history.shape[1]
+    if out is None:
+        out = Beams(t.empty(n, dtype=i32, device=dev), t.empty(n, dtype=i32, device=dev), t.empty((groups, max(keep, 0)), dtype=t.float32, device=dev),
+                    None if lengths is None else t.empty(n, dtype=i32, device=dev), t.empty(n, dtype=t.uint8, device=dev),
+                    None if history is None else t.empty((n, width), dtype=i32, device=dev))
+    if out.history is not None and (out.history.dim() != 2 or out.history.shape[0] != n):
+        _refuse(out.history, "out.history", index, f"[{n}, width] of int32")
+    new_width = 0 if out.history is None else out.history.shape[1]
+    _count(max(width, new_width), "the width of histories")
+    now = ss_beams(_table(totals, "totals", index, rows, t.float32), _table(lengths, "lengths", index, rows, i32), _table(ended, "ended", index, rows, t.uint8),
+                   _table(history, "history", index, rows * width, i32), width)
+    to = ss_beams(_table(out.totals, "out.totals", index, n, t.float32), _table(out.lengths, "out.lengths", index, n, i32),
+                  _table(out.ended, "out.ended", index, n, t.uint8), _table(out.history, "out.history", index, n * new_width, i32), new_width)
+    if workspace is None:
+        need = C.c_size_t(0)
+        _check(_lib.ss_beam_select_workspace(groups, beams, vocab, keep, need))
+        workspace = t.empty(need.value, dtype=t.uint8, device=dev)
+    size = workspace.numel()
+    _check(_lib.ss_beam_select(logits.data_ptr(), dtype, logits.stride(0), groups, beams, vocab, keep, now, to, _table(out.parent, "out.parent", index, n, i32),
+                               _table(out.token, "out.token", index, n, i32), end_id, length_power, _table(workspace, "workspace", index, size, t.uint8), size,
+                               _on(stream, index, logits, totals, lengths, ended, history, workspace, *out)))
     return out

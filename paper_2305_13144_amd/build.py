@@ -7,7 +7,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libss.so")
-SOURCES = ["ss_common.cpp", "ss_sched.cpp", "ss_plan.cpp", "ss_operators.cpp", "ss_kernels.hip", "ss_engine.hip"]
+SOURCES = ["ss_common.cpp", "ss_sched.cpp", "ss_plan.cpp", "ss_operators.cpp", "ss_kernels.hip", "ss_page_kernels.hip", "ss_beam_kernels.hip", "ss_engine.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pthread", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

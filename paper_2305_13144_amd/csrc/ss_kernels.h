@@ -146,7 +146,7 @@ void launch_read_stream(const f16_t* p, size_t bytes, uint32_t* sink, hipStream_
 void launch_fill_i32(int32_t* p, int32_t v, size_t n, hipStream_t s);
 
 // ---- operators on device tensors (ss_cache_kernels.h)
-constexpr int kBF16 = 0, kF16 = 2, kI8 = 3;   // element types: SS_BF16, SS_F16, SS_I8
+constexpr int kBF16 = 0, kF32 = 1, kF16 = 2, kI8 = 3;   // element types: SS_BF16, SS_F32, SS_F16, SS_I8
 
 // A layer's key/value cache: element e of head h in slot s of sequence i at (start[i] * n_kv + h * slots[i] + s) * hd + e.
 struct CacheView {
@@ -196,6 +196,71 @@ void launch_attention_packed(const PackedArgs& a, int hd, int token, int n_seq, 
 // halves into rows [n][q d | k d | v d].
 void launch_rotate_store(const MbState& st, const float* qkv_part, int ksplit, size_t part_stride, const float* rope_cos, const float* rope_sin,
                          f16_t* rows, int dense_kv, const CacheView& c, const int32_t* slot, int d, int n_max, hipStream_t s);
+
+// ---- caches in pages (ss_page_kernels.hip)
+// A layer's pool: element e of head h in slot s of page p at ((p * n_kv + h) * page + s) * hd + e.
+struct PagesView {
+    void *k, *v;
+    float *k_scale, *v_scale;   // kI8: one per vector
+    int n_pages, page, n_kv, hd, dtype;
+};
+struct TableView {
+    int32_t *pages, *lengths;
+    int rows, stride, page, n_pages;
+};
+// Token t at position pos[t] of row row[t], or with row == nullptr at the last position of row t.
+void launch_pages_write(const PagesView& p, const TableView& t, const RowsView& k, const RowsView& v, int token, const int32_t* row,
+                        const int32_t* pos, int n, hipStream_t s);
+void launch_pages_read(const PagesView& p, const TableView& t, const RowsView& k, const RowsView& v, int token, const int32_t* row,
+                       const int32_t* pos, int n, hipStream_t s);
+struct PageAttentionArgs {
+    PagesView p;
+    TableView t;
+    RowsView q, out;
+    const int32_t* rows;   // [n] rows of the table, or null
+    float scale;
+    int n, group, heads;
+};
+void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s);
+struct ForkArgs {
+    TableView from, to;
+    const int32_t *parent, *grow;
+    const uint8_t* held;
+    int32_t *src, *dst, *missing;
+    int32_t* claim;        // [n_pages] workspace
+};
+void launch_pages_fork(const ForkArgs& a, hipStream_t s);
+struct CompactArgs {
+    TableView from, to;
+    const uint8_t* held;
+    int32_t *src, *dst, *place, *counts;
+    int32_t *used, *code;  // [n_pages] workspace each
+};
+void launch_pages_compact(const CompactArgs& a, hipStream_t s);
+// `layers`: host array.
+void launch_pages_copy(const PagesView* layers, int n_layers, const int32_t* src, const int32_t* dst, int n, const int32_t* count, hipStream_t s);
+
+// ---- beam search (ss_beam_kernels.hip)
+struct BeamArgs {
+    const void* logits;
+    int64_t row_stride;
+    int n_groups, beams, vocab, keep, chunks;   // chunks: beam_chunks
+    const float* totals;
+    const int32_t* lengths;
+    const uint8_t* ended;
+    const int32_t* history;
+    int history_stride;
+    float* next_totals;
+    int32_t* next_lengths;
+    uint8_t* next_ended;
+    int32_t* next_history;
+    int next_history_stride;
+    int32_t *parent, *token;
+    int end_id;
+    float power;
+    float* part;   // [rows][chunks]: the chunk's largest logit and the sum of exp(logit - largest) beside it (2), its best candidates' logits (keep) and tokens (keep)
+};
+void launch_beam_select(const BeamArgs& a, int dtype, hipStream_t s);
 
 }  // namespace ss
 

@@ -6,6 +6,7 @@
 #include <atomic>
 #include <climits>
 #include <cmath>
+#include <vector>
 
 #include "ss_internal.h"
 #include "ss_kernels.h"
@@ -14,10 +15,12 @@ namespace {
 
 using ss::fail;
 
-static_assert(ss::kBF16 == SS_BF16 && ss::kF16 == SS_F16 && ss::kI8 == SS_I8, "element types");
+static_assert(ss::kBF16 == SS_BF16 && ss::kF32 == SS_F32 && ss::kF16 == SS_F16 && ss::kI8 == SS_I8, "element types");
+static_assert(ss::kBeamMax == SS_BEAM_MAX, "beams");
 
 bool is_half(int32_t dtype) { return dtype == SS_F16 || dtype == SS_BF16; }
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
+bool is_page_size(int32_t n) { return n == 16 || n == 32 || n == 64 || n == 128 || n == 256; }
 
 int check_cache(const ss_cache* c)
 {
@@ -124,6 +127,99 @@ ss::TreePlan plan_of(int32_t n_heads, int32_t n_kv_heads, int32_t n_seq, int32_t
 size_t part_bytes(const ss::TreePlan& p, int32_t n_heads, int32_t head_dim, int32_t n_seq, int32_t max_nodes)
 {
     return p.chunks > 1 ? (size_t)n_seq * p.chunks * max_nodes * n_heads * (head_dim + 4) * 4 : 0;
+}
+
+int check_pages(const ss_pages* p)
+{
+    if (!p) return fail(SS_EINVAL, "pages is NULL");
+    if (p->head_dim != 64 && p->head_dim != 128) return fail(SS_EINVAL, "pages: head_dim must be 64 or 128");
+    if (!is_half(p->dtype) && p->dtype != SS_I8) return fail(SS_EINVAL, "pages: dtype must be SS_F16, SS_BF16 or SS_I8");
+    if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return fail(SS_EINVAL, "pages: 1 to 65535 heads");
+    if (p->n_pages < 1) return fail(SS_EINVAL, "pages: there must be a page");
+    if (!is_page_size(p->page_slots)) return fail(SS_EINVAL, "pages: page_slots must be 16, 32, 64, 128 or 256");
+    if (!p->k || !p->v) return fail(SS_EINVAL, "pages: k or v is NULL");
+    if (!aligned(p->k) || !aligned(p->v)) return fail(SS_EINVAL, "pages: k and v must be 16-byte aligned");
+    if (p->dtype == SS_I8 && (!p->k_scale || !p->v_scale)) return fail(SS_EINVAL, "pages: SS_I8 needs k_scale and v_scale");
+    if (p->dtype == SS_I8 && (!aligned(p->k_scale) || !aligned(p->v_scale))) return fail(SS_EINVAL, "pages: k_scale and v_scale must be 16-byte aligned");
+    return SS_OK;
+}
+
+int check_table(const ss_page_table* t, const char* name)
+{
+    if (!t) return fail(SS_EINVAL, "%s is NULL", name);
+    if (t->n_rows < 0 || t->stride < 0) return fail(SS_EINVAL, "%s: negative number of rows or entries", name);
+    if (t->n_pages < 1) return fail(SS_EINVAL, "%s: there must be a page", name);
+    if (!is_page_size(t->page_slots)) return fail(SS_EINVAL, "%s: page_slots must be 16, 32, 64, 128 or 256", name);
+    if ((int64_t)t->stride * t->page_slots > INT_MAX - 1024) return fail(SS_EINVAL, "%s: rows of more than 2^31 positions", name);
+    if ((int64_t)t->n_rows * t->stride > INT_MAX) return fail(SS_EINVAL, "%s: more than 2^31 entries", name);
+    if (t->n_rows > 0 && (!t->lengths || (t->stride > 0 && !t->pages))) return fail(SS_EINVAL, "%s: pages or lengths is NULL", name);
+    return SS_OK;
+}
+
+int check_pages_and_table(const ss_pages* p, const ss_page_table* t)
+{
+    if (int rc = check_pages(p)) return rc;
+    if (int rc = check_table(t, "table")) return rc;
+    if (t->page_slots != p->page_slots || t->n_pages != p->n_pages) return fail(SS_EINVAL, "table and pages differ in page_slots or n_pages");
+    return SS_OK;
+}
+
+int check_page_tokens(const ss_pages* p, const ss_page_table* t, const ss_rows* k, const ss_rows* v, const int32_t* row, const int32_t* pos, int32_t n)
+{
+    if (int rc = check_pages_and_table(p, t)) return rc;
+    if (int rc = check_rows(k, "k")) return rc;
+    if (int rc = check_rows(v, "v")) return rc;
+    if (n < 0) return fail(SS_EINVAL, "negative number of tokens");
+    if (k->dtype != v->dtype) return fail(SS_EINVAL, "k and v differ in type");
+    if (k->rows < n || v->rows < n) return fail(SS_EINVAL, "k and v have fewer than %d rows", n);
+    if (!row != !pos) return fail(SS_EINVAL, "row and pos are given together or not at all");
+    if (n > SS_CACHE_MAX_TOKENS) return fail(SS_EINVAL, "more than %d tokens", SS_CACHE_MAX_TOKENS);
+    if ((int64_t)n * p->n_kv_heads > INT_MAX) return fail(SS_EINVAL, "more than 2^31 vectors");
+    return SS_OK;
+}
+
+int check_two_tables(const ss_page_table* from, const ss_page_table* to)
+{
+    if (int rc = check_table(from, "from")) return rc;
+    if (int rc = check_table(to, "to")) return rc;
+    if (from->page_slots != to->page_slots || from->n_pages != to->n_pages) return fail(SS_EINVAL, "from and to differ in page_slots or n_pages");
+    if (from->n_rows > SS_PAGES_MAX_ROWS || to->n_rows > SS_PAGES_MAX_ROWS) return fail(SS_EINVAL, "more than %d rows", SS_PAGES_MAX_ROWS);
+    return SS_OK;
+}
+
+size_t pages_workspace(int32_t n_pages) { return (size_t)n_pages * 8; }
+
+int check_workspace(const void* workspace, size_t given, size_t need)
+{
+    if (need > given || (need > 0 && !workspace))
+        return fail(SS_EINVAL, "this call needs %zu bytes of workspace, it was given %zu", need, workspace ? given : (size_t)0);
+    if (need > 0 && !aligned(workspace)) return fail(SS_EINVAL, "workspace must be 16-byte aligned");
+    return SS_OK;
+}
+
+ss::PagesView view(const ss_pages* p) { return {p->k, p->v, p->k_scale, p->v_scale, p->n_pages, p->page_slots, p->n_kv_heads, p->head_dim, p->dtype}; }
+ss::TableView view(const ss_page_table* t) { return {t->pages, t->lengths, t->n_rows, t->stride, t->page_slots, t->n_pages}; }
+
+int check_page_attention(int32_t n_heads, int32_t n_kv_heads, int32_t n, int32_t max_length, int32_t group)
+{
+    if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return fail(SS_EINVAL, "n_heads must be a multiple of the key/value heads");
+    if (n_heads > 65535) return fail(SS_EINVAL, "more than 65535 heads");
+    if (n < 0 || max_length < 0) return fail(SS_EINVAL, "negative number of rows or length");
+    if (n > 65535) return fail(SS_EINVAL, "more than 65535 rows");
+    if (group < 1 || group > SS_PAGES_MAX_GROUP) return fail(SS_EINVAL, "group must be 1 to %d", SS_PAGES_MAX_GROUP);
+    if (n % group) return fail(SS_EINVAL, "%d rows are no whole groups of %d", n, group);
+    return SS_OK;
+}
+
+size_t attention_workspace() { return 0; }
+
+int check_beams(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep)
+{
+    if (beams < 1 || beams > SS_BEAM_MAX) return fail(SS_EINVAL, "beams must be 1 to %d", SS_BEAM_MAX);
+    if (keep < 1 || keep > SS_BEAM_MAX) return fail(SS_EINVAL, "keep must be 1 to %d", SS_BEAM_MAX);
+    if (vocab < 1) return fail(SS_EINVAL, "vocab must be positive");
+    if (n_groups < 0 || (int64_t)n_groups * beams > 65535) return fail(SS_EINVAL, "0 to 65535 rows of beams");
+    return SS_OK;
 }
 
 }  // namespace
@@ -248,4 +344,179 @@ extern "C" int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_
     a.n_kv = n_kv_heads;
     a.max_len = (int32_t)std::min<int64_t>(max_len, q->rows);   // no sequence is longer: no workgroups for what a caller only allows
     return launch([&] { ss::launch_attention_packed(a, head_dim, q->dtype, n_seq, (hipStream_t)hip_stream); });
+}
+
+extern "C" int ss_pages_write(const ss_pages* pages, const ss_page_table* table, const ss_rows* k, const ss_rows* v, const int32_t* row,
+                              const int32_t* pos, int32_t n, void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_page_tokens(pages, table, k, v, row, pos, n)) return rc;
+    if (n == 0 || table->n_rows == 0 || table->stride == 0) return SS_OK;
+    return launch([&] { ss::launch_pages_write(view(pages), view(table), view(k), view(v), k->dtype, row, pos, n, (hipStream_t)hip_stream); });
+}
+
+extern "C" int ss_pages_read(const ss_pages* pages, const ss_page_table* table, const int32_t* row, const int32_t* pos, int32_t n,
+                             const ss_rows* k, const ss_rows* v, void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_page_tokens(pages, table, k, v, row, pos, n)) return rc;
+    if (int rc = check_apart(k, "k", pages->n_kv_heads, pages->head_dim)) return rc;
+    if (int rc = check_apart(v, "v", pages->n_kv_heads, pages->head_dim)) return rc;
+    if (n == 0 || table->n_rows == 0 || table->stride == 0) return SS_OK;
+    return launch([&] { ss::launch_pages_read(view(pages), view(table), view(k), view(v), k->dtype, row, pos, n, (hipStream_t)hip_stream); });
+}
+
+extern "C" int ss_attention_pages_workspace(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_slots, int32_t stride, int32_t n,
+                                            int32_t max_length, int32_t group, size_t* bytes)
+{
+    ss::clear_error();
+    if (!bytes) return fail(SS_EINVAL, "bytes is NULL");
+    if (head_dim != 64 && head_dim != 128) return fail(SS_EINVAL, "head_dim must be 64 or 128");
+    if (!is_page_size(page_slots)) return fail(SS_EINVAL, "page_slots must be 16, 32, 64, 128 or 256");
+    if (stride < 0 || (int64_t)stride * page_slots > INT_MAX - 1024) return fail(SS_EINVAL, "rows of negative length or of more than 2^31 positions");
+    if (int rc = check_page_attention(n_heads, n_kv_heads, n, max_length, group)) return rc;
+    *bytes = attention_workspace();
+    return SS_OK;
+}
+
+extern "C" int ss_attention_pages(const ss_pages* pages, const ss_page_table* table, const ss_rows* q, const ss_rows* out, int32_t n_heads,
+                                  int32_t n, const int32_t* rows, int32_t max_length, int32_t group, float scale, void* workspace,
+                                  size_t workspace_bytes, void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_pages_and_table(pages, table)) return rc;
+    if (int rc = check_rows(q, "q")) return rc;
+    if (int rc = check_rows(out, "out")) return rc;
+    if (int rc = check_page_attention(n_heads, pages->n_kv_heads, n, max_length, group)) return rc;
+    if (q->dtype != out->dtype) return fail(SS_EINVAL, "q and out differ in type");
+    if (pages->dtype != SS_I8 && pages->dtype != q->dtype) return fail(SS_EINVAL, "pages of 16 bits and q must have the same type");
+    if (q->rows < n || out->rows < n) return fail(SS_EINVAL, "q or out has fewer than %d rows", n);
+    if (!std::isfinite(scale)) return fail(SS_EINVAL, "scale must be finite");
+    if (int rc = check_apart(out, "out", n_heads, pages->head_dim)) return rc;
+    if (!rows && n > table->n_rows) return fail(SS_EINVAL, "the table has fewer than %d rows", n);
+    if (int rc = check_workspace(workspace, workspace_bytes, attention_workspace())) return rc;
+    if (n == 0) return SS_OK;
+    ss::PageAttentionArgs a{};
+    a.p = view(pages);
+    a.t = view(table);
+    a.q = view(q);
+    a.out = view(out);
+    a.rows = rows;
+    a.scale = scale;
+    a.n = n;
+    a.group = group;
+    a.heads = n_heads;
+    return launch([&] { ss::launch_attention_pages(a, q->dtype, (hipStream_t)hip_stream); });
+}
+
+extern "C" int ss_pages_workspace(int32_t n_pages, size_t* bytes)
+{
+    ss::clear_error();
+    if (!bytes) return fail(SS_EINVAL, "bytes is NULL");
+    if (n_pages < 1) return fail(SS_EINVAL, "there must be a page");
+    *bytes = pages_workspace(n_pages);
+    return SS_OK;
+}
+
+extern "C" int ss_pages_fork(const ss_page_table* from, const ss_page_table* to, const int32_t* parent, const int32_t* grow,
+                             const uint8_t* held, int32_t* src, int32_t* dst, int32_t* missing, void* workspace, size_t workspace_bytes,
+                             void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_two_tables(from, to)) return rc;
+    if ((to->n_rows > 0 && (!src || !dst)) || !missing) return fail(SS_EINVAL, "src, dst or missing is NULL");
+    if (from->n_rows > 0 && to->n_rows > 0 && ((from->stride > 0 && from->pages == to->pages) || from->lengths == to->lengths))
+        return fail(SS_EINVAL, "to must not be from: rows change places");
+    if (int rc = check_workspace(workspace, workspace_bytes, pages_workspace(to->n_pages))) return rc;
+    ss::ForkArgs a{view(from), view(to), parent, grow, held, src, dst, missing, (int32_t*)workspace};
+    return launch([&] { ss::launch_pages_fork(a, (hipStream_t)hip_stream); });
+}
+
+extern "C" int ss_pages_compact(const ss_page_table* from, const ss_page_table* to, const uint8_t* held, int32_t* src, int32_t* dst,
+                                int32_t* place, int32_t* counts, void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_two_tables(from, to)) return rc;
+    if (from->n_rows != to->n_rows || from->stride != to->stride) return fail(SS_EINVAL, "from and to differ in rows or stride");
+    if ((from->n_pages > 1 && (!src || !dst)) || !counts) return fail(SS_EINVAL, "src, dst or counts is NULL");
+    if (int rc = check_workspace(workspace, workspace_bytes, pages_workspace(from->n_pages))) return rc;
+    ss::CompactArgs a{view(from), view(to), held, src, dst, place, counts, (int32_t*)workspace, (int32_t*)workspace + from->n_pages};
+    return launch([&] { ss::launch_pages_compact(a, (hipStream_t)hip_stream); });
+}
+
+extern "C" int ss_pages_copy(const ss_pages* layers, int32_t n_layers, const int32_t* src, const int32_t* dst, int32_t n, const int32_t* count,
+                             void* hip_stream)
+{
+    ss::clear_error();
+    if (n_layers < 0 || n < 0) return fail(SS_EINVAL, "negative number of layers or pages");
+    if (n_layers > 0 && !layers) return fail(SS_EINVAL, "layers is NULL");
+    for (int32_t l = 0; l < n_layers; ++l) {
+        if (int rc = check_pages(layers + l)) return rc;
+        const ss_pages &x = layers[l], &y = layers[0];
+        if (x.n_pages != y.n_pages || x.page_slots != y.page_slots || x.n_kv_heads != y.n_kv_heads || x.head_dim != y.head_dim || x.dtype != y.dtype)
+            return fail(SS_EINVAL, "layer %d is not like the first", l);
+    }
+    if (n > 0 && (!src || !dst)) return fail(SS_EINVAL, "src or dst is NULL");
+    if (n == 0 || n_layers == 0) return SS_OK;
+    std::vector<ss::PagesView> views;
+    return ss::no_throw([&] {
+        for (int32_t l = 0; l < n_layers; ++l) views.push_back(view(layers + l));
+        return launch([&] { ss::launch_pages_copy(views.data(), n_layers, src, dst, n, count, (hipStream_t)hip_stream); });
+    });
+}
+
+extern "C" int ss_beam_select_workspace(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep, size_t* bytes)
+{
+    ss::clear_error();
+    if (!bytes) return fail(SS_EINVAL, "bytes is NULL");
+    if (int rc = check_beams(n_groups, beams, vocab, keep)) return rc;
+    *bytes = ss::beam_part_floats(n_groups * beams, vocab, keep) * 4;
+    return SS_OK;
+}
+
+extern "C" int ss_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep,
+                              const ss_beams* now, const ss_beams* next, int32_t* parent, int32_t* token, int32_t end_id, float length_power,
+                              void* workspace, size_t workspace_bytes, void* hip_stream)
+{
+    ss::clear_error();
+    if (int rc = check_beams(n_groups, beams, vocab, keep)) return rc;
+    if (dtype != SS_F32 && !is_half(dtype)) return fail(SS_EINVAL, "logits: dtype must be SS_F32, SS_F16 or SS_BF16");
+    if (!now || !next) return fail(SS_EINVAL, "now or next is NULL");
+    if (end_id < -1 || end_id >= vocab) return fail(SS_EINVAL, "end_id must be -1 or a token");
+    if (!std::isfinite(length_power)) return fail(SS_EINVAL, "length_power must be finite");
+    if (row_stride < 0 || row_stride > (1ll << 40)) return fail(SS_EINVAL, "logits: row_stride must be 0 to 2^40");
+    if ((uintptr_t)logits % (dtype == SS_F32 ? 4 : 2)) return fail(SS_EINVAL, "logits are not aligned as their elements");
+    if (!now->history != !next->history) return fail(SS_EINVAL, "now and next both have histories, or neither");
+    if (now->history && (now->history_stride < 0 || next->history_stride < 0)) return fail(SS_EINVAL, "negative history_stride");
+    if ((length_power != 0.f || now->history || next->lengths) && !now->lengths) return fail(SS_EINVAL, "lengths is NULL: histories, new lengths and length_power need them");
+    if (n_groups == 0) return SS_OK;
+    if (!logits || !now->totals || !next->totals || !parent || !token) return fail(SS_EINVAL, "logits, totals, parent or token is NULL");
+    if (now->totals == next->totals || (now->lengths && now->lengths == next->lengths) || (now->ended && now->ended == next->ended) ||
+        (now->history && now->history == next->history))
+        return fail(SS_EINVAL, "next must not be now: beams change places");
+    if (int rc = check_workspace(workspace, workspace_bytes, ss::beam_part_floats(n_groups * beams, vocab, keep) * 4)) return rc;
+    ss::BeamArgs a{};
+    a.logits = logits;
+    a.row_stride = row_stride;
+    a.n_groups = n_groups;
+    a.beams = beams;
+    a.vocab = vocab;
+    a.keep = keep;
+    a.chunks = ss::beam_chunks(vocab);
+    a.totals = now->totals;
+    a.lengths = now->lengths;
+    a.ended = now->ended;
+    a.history = now->history;
+    a.history_stride = now->history_stride;
+    a.next_totals = next->totals;
+    a.next_lengths = next->lengths;
+    a.next_ended = next->ended;
+    a.next_history = next->history;
+    a.next_history_stride = next->history_stride;
+    a.parent = parent;
+    a.token = token;
+    a.end_id = end_id;
+    a.power = length_power;
+    a.part = (float*)workspace;
+    return launch([&] { ss::launch_beam_select(a, dtype, (hipStream_t)hip_stream); });
 }

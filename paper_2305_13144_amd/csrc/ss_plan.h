@@ -224,6 +224,11 @@ constexpr int tree_chunks(int len, int chunk, int most)
     return len <= chunk ? 1 : len > (most - 1) * (long long)chunk ? most : (len + chunk - 1) / chunk;
 }
 
+// Beam search: logits of a workgroup, and how many such chunks a row has.
+constexpr int kBeamMax = 64, kBeamChunk = 8192;
+constexpr int beam_chunks(int vocab) { return vocab / kBeamChunk + (vocab % kBeamChunk != 0); }
+constexpr size_t beam_part_floats(int rows, int vocab, int keep) { return (size_t)rows * beam_chunks(vocab) * (2 + 2 * (size_t)keep); }
+
 }  // namespace ss
 
 #endif
