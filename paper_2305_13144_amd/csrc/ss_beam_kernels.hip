@@ -45,7 +45,7 @@ __device__ __forceinline__ Best<V> block_best(Best<V> b, Best<V>* lds)   // 256 
 }
 
 // Tokens of a beam of this length, and with one more.
-__device__ __forceinline__ int beam_length(int length, bool more) { return min(max(length, 0), INT_MAX - 1) + more; }
+__device__ __forceinline__ int beam_length(int length, bool more) { return min(max(length, 0), INT_MAX - more) + more; }
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)

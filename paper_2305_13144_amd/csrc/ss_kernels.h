@@ -220,6 +220,13 @@ struct PageAttentionArgs {
     const int32_t* rows;   // [n] rows of the table, or null
     float scale;
     int n, group, heads;
+    int tiles, row_blocks, workers;   // page_plan
+    // workspace
+    float* part;           // workers > 0: [workers][2][16 * tiles][hd + 4]: sums, their maximum, their weight
+    void* records;         //              [workers]: 16 bytes each
+    int32_t* item_counts;  // group > 1: [n / group]
+    void* items;           //            [n / group][items_stride]: 16 bytes each
+    int64_t items_stride;
 };
 void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s);
 struct ForkArgs {

@@ -117,56 +117,594 @@ __global__ __launch_bounds__(256) void k_pages_read(PagesView c, TableView tb, R
     }
 }
 
-// ------------------------------------------------------------------------------------------ attention
-// A workgroup takes one query head of one row: a thread a position, then a thread an element.
-template <int HD, typename T, typename C>
-__global__ __launch_bounds__(256) void k_attention_pages(PageAttentionArgs a)
-{
-    constexpr bool I8 = std::is_same<C, int8_t>::value;
-    __shared__ float s_q[HD], s_p[256], s_red[4];
-    __shared__ int64_t s_at[256];
-    const int h = blockIdx.x, j = blockIdx.y, hk = h / (a.heads / a.p.n_kv), t = threadIdx.x, P = a.t.page;
-    const int r = a.rows ? a.rows[j] : j;
-    const int len = r >= 0 && r < a.t.rows ? row_length(a.t, r) : 0;
-    if (t < HD) s_q[t] = (float)((const T*)a.q.p)[(int64_t)j * a.q.row + (int64_t)h * a.q.head + t] * a.scale;
-    float m = kLowest, l = 0.f, o = 0.f;
-    for (int s0 = 0; s0 < len; s0 += 256) {
-        __syncthreads();
-        const int s = s0 + t;
-        int64_t at = -1;
-        if (s < len) {
-            const int p = a.t.pages[(int64_t)r * a.t.stride + s / P];
-            if (is_page(a.t, p)) at = ((int64_t)p * a.p.n_kv + hk) * P + s % P;
+// Sum over the workgroup's NT threads, in each of them, and of those before a thread.
+template <int NT>
+struct Scan {
+    int before, all;
+    __device__ __forceinline__ Scan(int x, int* lds)   // lds: NT / 64 + 1
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        int s = x;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(s, d);
+            if (lane >= d) s += o;
         }
-        float x = -__builtin_inff();
-        if (at >= 0) {
-            x = 0.f;
-            for (int e = 0; e < HD; ++e) x = fmaf(s_q[e], (float)((const C*)a.p.k)[at * HD + e], x);
-            if constexpr (I8) x *= a.p.k_scale[at];
+        __syncthreads();
+        if (lane == 63) lds[wave] = s;
+        __syncthreads();
+        before = s - x;
+        all = 0;
+#pragma unroll
+        for (int w = 0; w < NT / 64; ++w) {
+            if (w < wave) before += lds[w];
+            all += lds[w];
         }
-        const float top = wave_max(x);
-        if ((t & 63) == 0) s_red[t >> 6] = top;
-        __syncthreads();
-        const float m_new = fmaxf(m, fmaxf(fmaxf(s_red[0], s_red[1]), fmaxf(s_red[2], s_red[3])));
-        const float alpha = __expf(m - m_new), p = at >= 0 ? __expf(x - m_new) : 0.f;
-        m = m_new;
-        __syncthreads();
-        const float sum = wave_sum(p);
-        if ((t & 63) == 0) s_red[t >> 6] = sum;
-        s_p[t] = p;
-        s_at[t] = at;
-        __syncthreads();
-        l = l * alpha + ((s_red[0] + s_red[1]) + (s_red[2] + s_red[3]));
-        o *= alpha;
-        if (t < HD)
-            for (int i = 0; i < 256; ++i)
-                if (s_at[i] >= 0) o = fmaf(s_p[i], (float)((const C*)a.p.v)[s_at[i] * HD + t] * (I8 ? a.p.v_scale[s_at[i]] : 1.f), o);
     }
-    if (t >= HD) return;
-    o = l != 0.f ? o / l : 0.f;
-    T* to = (T*)a.out.p + (int64_t)j * a.out.row + (int64_t)h * a.out.head + t;
-    if constexpr (std::is_same<T, _Float16>::value) *to = __builtin_bit_cast(_Float16, f2h(o));
-    else *to = (T)o;
+};
+
+// ------------------------------------------------------------------------------------------ attention
+// A unit is one key/value head of a group of rows: its rows r = row of the group * G + (head within its G), in blocks of 16 * QT.  Its slots come in
+// items: 16 neighbouring slots of one page, with the positions that they are and the rows of the group that hold the page there.  Of a single row the
+// items are its table; of a group k_page_items lists every page once per entry, however many rows hold it.
+// The mathematics of a step of two items is that of k_attention_tree (ss_cache_kernels.h): S^T = K Q^T, an online softmax in powers of two whose weights
+// are the operand of O^T += V^T P^T as they lie, nothing staged in LDS; what differs is where slots lie and who sees them.  An item is always
+// whole in memory, so nothing is clamped; scores of slots that a row does not see are set to -inf.  Values of such slots meet weights of 0: in 8 bits
+// they are finite whatever lies there (the scale is left out), in 16 bits an infinity or NaN shows in the sums, and the piece is done again,
+// slot by slot (k_attention_pages' `careful`).
+// With long rows the items of all units lie in one row and every worker (as many as the chip holds at once) takes an equal share of it, whatever
+// the rows' lengths: of the units that it meets the whole ones are finished, of the first and last a part is kept, and k_page_join adds up the parts of
+// units that several workers share.  Short rows: a workgroup a unit, no join.
+struct PageItem {
+    int page, p0;
+    unsigned mask;   // rows of the group
+    int full;        // seen by all rows of the group in all slots
+};
+static_assert(sizeof(PageItem) == 16, "four words");
+
+// Of the j-th group: items, and the i-th of them.
+__device__ __forceinline__ int attended_row(const PageAttentionArgs& a, int q) { return a.rows ? a.rows[q] : q; }
+__device__ __forceinline__ int attended_length(const PageAttentionArgs& a, int r) { return r >= 0 && r < a.t.rows ? row_length(a.t, r) : 0; }
+__device__ __forceinline__ int group_items(const PageAttentionArgs& a, int j)
+{
+    return a.group == 1 ? (attended_length(a, attended_row(a, j)) + 15) >> 4 : a.item_counts[j];
+}
+__device__ __forceinline__ PageItem group_item(const PageAttentionArgs& a, int j, int row, int len, int i)
+{
+    if (a.group > 1) return ((const PageItem*)a.items)[(int64_t)j * a.items_stride + i];
+    const int p0 = 16 * i, p = a.t.pages[(int64_t)row * a.t.stride + p0 / a.t.page];
+    if (!is_page(a.t, p)) return {0, p0, 0u, 0};
+    return {p, p0, 1u, p0 + 16 <= len};
+}
+
+// The items of a group, by position and there by the first row that holds the page.
+constexpr int kItemThreads = 1024;
+__global__ __launch_bounds__(kItemThreads) void k_page_items(PageAttentionArgs a)
+{
+    __shared__ int s_page[kItemThreads], s_len[32], s_row[32], s_scan[kItemThreads / 64 + 1];
+    const int j = blockIdx.x, g = a.group, t = threadIdx.x, P = a.t.page;
+    if (t < g) {
+        const int r = attended_row(a, j * g + t);
+        s_row[t] = r;
+        s_len[t] = attended_length(a, r);
+    }
+    __syncthreads();
+    int most = 0, least = INT_MAX;
+    for (int b = 0; b < g; ++b) {
+        most = max(most, s_len[b]);
+        least = min(least, s_len[b]);
+    }
+    const int entries = pages_of(most, P), per = kItemThreads / g, b = t % g;
+    PageItem* out = (PageItem*)a.items + (int64_t)j * a.items_stride;
+    const unsigned all = g == 32 ? ~0u : (1u << g) - 1;
+    int count = 0;
+    for (int e0 = 0; e0 < entries; e0 += per) {
+        const int e = e0 + t / g;
+        int page = -1;
+        if (t < per * g && e < pages_of(s_len[b], P)) {
+            page = a.t.pages[(int64_t)s_row[b] * a.t.stride + e];
+            if (!is_page(a.t, page)) page = -1;
+        }
+        __syncthreads();
+        s_page[t] = page;
+        __syncthreads();
+        unsigned mask = 0;
+        int len = 0;
+        if (page >= 0)
+            for (int c = 0; c < g; ++c)
+                if (s_page[t - b + c] == page) {
+                    mask |= 1u << c;
+                    len = max(len, s_len[c]);
+                }
+        const int tiles = page >= 0 && __ffs(mask) - 1 == b ? (min(len - e * P, P) + 15) >> 4 : 0;
+        const Scan<kItemThreads> s(tiles, s_scan);
+        for (int i = 0; i < tiles; ++i) {
+            const int p0 = e * P + 16 * i;
+            out[count + s.before + i] = {page, p0, mask, mask == all && p0 + 16 <= least};
+        }
+        count += s.all;
+    }
+    if (t == 0) a.item_counts[j] = count;
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void page_store(const PageAttentionArgs& a, int q, int head, int e0, const float (&x)[N])
+{
+    T r[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        if constexpr (std::is_same<T, _Float16>::value) r[i] = __builtin_bit_cast(_Float16, f2h(x[i]));
+        else r[i] = (T)x[i];
+    }
+    typedef uint32_t words __attribute__((ext_vector_type(N * 2 / 4)));
+    *(words*)((T*)a.out.p + (int64_t)q * a.out.row + (int64_t)head * a.out.head + e0) = __builtin_bit_cast(words, r);
+}
+
+// What all lanes hold alike, in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32);
+}
+
+// A worker's record: the unit that it begins and does not end (j < 0: none), and the worker that does.
+struct PageRecord {
+    int j, hb, last, pad;
+};
+
+constexpr int kItemsAtOnce = 512;
+
+template <int HD, typename T, typename C, int QT, bool DEALT>
+__global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attention_pages(PageAttentionArgs a)
+{
+    typedef typename MathType<C, T>::type M;
+    typedef typename Half<M>::x8 m8;
+    constexpr bool I8 = std::is_same<C, int8_t>::value;
+    constexpr int KS = HD / 32, ET = HD / 16, NW = 4, ROWS = 16 * QT;
+    constexpr int ROW = HD * sizeof(C);      // bytes of a vector
+    constexpr int KL = ROW / 64;             // 16-byte loads per 16 slots and lane
+    constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
+    constexpr bool PAIRS = I8 && std::is_same<T, _Float16>::value && QT == 1;   // weights as sums of two halves
+    __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
+    __shared__ int s_odd[NW], s_scan[2];
+    __shared__ int64_t s_wide[NW], s_off;
+    __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
+    __shared__ PageItem s_item[kItemsAtOnce];
+
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 15, g = lane >> 4;
+    const int n_kv = a.p.n_kv, G = a.heads / n_kv, units = n_kv * a.row_blocks, n_groups = a.n / a.group, P = a.t.page;
+    const int unit_rows = a.group * G;
+
+    // ---- one unit's items i0 .. i1 - 1, all of them if whole; else the sums go to part
+    auto piece = [&](int j, int hb, int i0, int i1, bool whole, float* part) {
+        const int rb = hb / n_kv, h = hb - rb * n_kv, r0 = rb * ROWS, n_rows = min(unit_rows - r0, ROWS);
+        const int row0 = uniform(attended_row(a, j * a.group)), len0 = a.group == 1 ? uniform(attended_length(a, row0)) : 0;
+        const char *K = (const char*)a.p.k + (int64_t)h * P * ROW, *V = (const char*)a.p.v + (int64_t)h * P * ROW;
+        const float *kscale = I8 ? a.p.k_scale + (int64_t)h * P : nullptr, *vscale = I8 ? a.p.v_scale + (int64_t)h * P : nullptr;
+
+        // A step's operands as they come from memory; those of the next step are requested as soon as the registers are free.
+        u32x4 kreg[2][KL];
+        uint32_t vreg[8][VW];
+        f32x4 ks[2], vs[2];
+        const unsigned k_off = ql * ROW + 16 * g, v_off = 4 * g * ROW + ET * ql * (int)sizeof(C);
+        auto load16 = [](const char* p) { return __builtin_nontemporal_load((const u32x4*)p); };
+        auto slot_of = [&](int page, int p0) { return (int64_t)page * ((int64_t)n_kv * P) + (p0 & (P - 1)); };   // of head 0
+        auto load_keys = [&](const int64_t (&at)[2]) {
+#pragma unroll
+            for (int kt = 0; kt < 2; ++kt) {
+                const char* p = K + at[kt] * ROW;
+#pragma unroll
+                for (int i = 0; i < KL; ++i) kreg[kt][i] = load16(p + k_off + 64 * i);
+                if constexpr (I8) ks[kt] = *(const f32x4*)(kscale + at[kt] + 4 * g);
+            }
+        };
+        auto load_values = [&](const int64_t (&at)[2]) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const char* p = V + at[i >> 2] * ROW + v_off + (i & 3) * ROW;
+                if constexpr (VW == 4) {
+                    const u32x4 w = load16(p);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vreg[i][e] = w[e];
+                } else if constexpr (VW == 2) {
+                    const u32x2 w = __builtin_nontemporal_load((const u32x2*)p);
+                    vreg[i][0] = w[0];
+                    vreg[i][1] = w[1];
+                } else {
+                    vreg[i][0] = __builtin_nontemporal_load((const uint32_t*)p);
+                }
+            }
+            if constexpr (I8)
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) vs[kt] = *(const f32x4*)(vscale + at[kt] + 4 * g);
+        };
+
+        // queries, and what brings their scores to units of log2, as in k_attention_tree
+        constexpr bool SCALED = !I8 || !std::is_same<M, T>::value;   // sc is not 1
+        const float log2_scale = a.scale * 1.44269504088896341f;
+        float sc[QT];
+        m8 qf[QT][KS];
+        int len[QT], bit[QT];   // of this lane's row: its length and its place in the group
+        u32x4 qreg[QT][KS];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            const int r = min(r0 + u * 16 + ql, unit_rows - 1), b = r / G;
+            const T* qp = (const T*)a.q.p + (int64_t)(j * a.group + b) * a.q.row + (int64_t)(h * G + r - b * G) * a.q.head;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) qreg[u][i] = *(const u32x4*)(I8 ? qp + 64 * (i >> 1) + 16 * g + 8 * (i & 1) : qp + 32 * i + 8 * g);
+            bit[u] = b;
+            len[u] = a.group == 1 ? len0 : attended_length(a, attended_row(a, j * a.group + b));
+        }
+        if constexpr (std::is_same<M, T>::value) {
+            const uint32_t flip = !I8 && a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                sc[u] = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
+#pragma unroll
+                for (int i = 0; i < KS; ++i) qf[u][i] = __builtin_bit_cast(m8, qreg[u][i] ^ u32x4{flip, flip, flip, flip});
+            }
+        } else {   // bf16 queries, half arithmetic: the largest magnitude of each row becomes 2^14 to 2^15
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                float top = 0.f, x[8];
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    to_floats<T>(qreg[u][i], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+                }
+                top = across<32>(across<16>(top, Max()), Max());
+                const float down = half_power(top, &sc[u]);
+#pragma unroll
+                for (int i = 0; i < KS; ++i) {
+                    to_floats<T>(qreg[u][i], x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) qf[u][i][e] = (_Float16)(x[e] * down);
+                }
+            }
+        }
+        f32x4 o[QT][ET];
+        float m_run[QT], l_run[QT];
+        WeightUnit unit[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+#pragma unroll
+            for (int e = 0; e < ET; ++e) o[u][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            m_run[u] = kLowest;
+            l_run[u] = 0.f;
+        }
+        for (int c0 = i0; c0 < i1; c0 += kItemsAtOnce) {
+            const int here = min(i1 - c0, kItemsAtOnce), steps = (here + 1) >> 1;
+            __syncthreads();
+            for (int i = t; i < 2 * steps; i += 256) s_item[i] = i < here ? group_item(a, j, row0, len0, c0 + i) : PageItem{0, 0, 0u, 0};
+            __syncthreads();
+            // places of a step's two items (a wave's: scalar), who sees them
+            auto place = [&](int step, int64_t (&at)[2]) {
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) at[kt] = slot_of(uniform(s_item[2 * step + kt].page), uniform(s_item[2 * step + kt].p0));
+            };
+            int64_t at[2];
+            if (wave < steps) {
+                place(wave, at);
+                load_keys(at);
+                load_values(at);
+            }
+            for (int step = wave; step < steps; step += NW) {
+                const bool more = step + NW < steps;
+                if (more) place(step + NW, at);
+                const PageItem it[2] = {s_item[2 * step], s_item[2 * step + 1]};
+                const bool full = uniform(it[0].full & it[1].full);
+                f32x4 s[QT][2];
+#pragma unroll
+                for (int kt = 0; kt < 2; ++kt) {
+                    m8 kf[KS];
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        if constexpr (I8) {
+                            const uint32_t lo = kreg[kt][i >> 1][2 * (i & 1)], up = kreg[kt][i >> 1][2 * (i & 1) + 1];
+                            const u32x4 w = {code_pair(lo, lo, 0x0c010c00u), code_pair(lo, lo, 0x0c030c02u), code_pair(up, up, 0x0c010c00u),
+                                             code_pair(up, up, 0x0c030c02u)};
+                            kf[i] = __builtin_bit_cast(m8, w);
+                        } else {
+                            kf[i] = __builtin_bit_cast(m8, kreg[kt][i]);
+                        }
+                    }
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) {
+                        s[u][kt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) s[u][kt] = Half<M>::mma(kf[i], qf[u][i], s[u][kt]);
+                    }
+                }
+                f32x4 kq[2];
+                if constexpr (I8)
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) kq[kt][i] = ks[kt][i] * log2_scale;
+                if (more) load_keys(at);
+                m8 pb[QT], rest[QT];
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    f32x4 w[2];   // the values' scales, 0 for those that the row does not see
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt) {
+                        if constexpr (I8) {
+                            w[kt] = vs[kt];
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) s[u][kt][i] *= kq[kt][i];
+                        }
+                        if (!full) {
+                            const int seen = it[kt].mask >> bit[u] & 1 ? len[u] - it[kt].p0 - 4 * g : 0;   // of this lane's four slots
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (i >= seen) {
+                                    s[u][kt][i] = -__builtin_inff();
+                                    if constexpr (I8) w[kt][i] = 0.f;
+                                }
+                        }
+                    }
+                    float mt = kLowest;
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[u][kt][i]);
+                    mt = across<32>(across<16>(mt, Max()), Max());
+                    // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1
+                    float alpha = 1.f;
+                    const bool moves = __any((mt - m_run[u]) * sc[u] > 8.f);
+                    if (moves) {
+                        const float m_new = fmaxf(m_run[u], mt);
+                        alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc[u]);
+                        m_run[u] = m_new;
+                        l_run[u] *= alpha;
+                        if constexpr (!I8)
+#pragma unroll
+                            for (int e = 0; e < ET; ++e) o[u][e] *= alpha;
+                    }
+                    const float m_sc = I8 ? fmaxf(m_run[u] * sc[u], kLowest) : exponent_top(m_run[u], sc[u], s[u]);   // 8 bits: sc is a power of two
+                    float top = 0.f;
+#pragma unroll
+                    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float p = __builtin_amdgcn_exp2f(SCALED ? fmaf(s[u][kt][i], sc[u], -m_sc) : below_top(s[u][kt][i], m_sc));
+                            if constexpr (I8) {
+                                l_run[u] += p;
+                                s[u][kt][i] = p * w[kt][i];
+                                top = fmaxf(top, fabsf(s[u][kt][i]));
+                            } else {
+                                pb[u][kt * 4 + i] = (M)p;
+                            }
+                        }
+                    if constexpr (I8) {
+                        if (moves || __any(top > unit[u].largest())) {
+                            const float f = unit[u].follow(alpha, across<32>(across<16>(top, Max()), Max()));
+#pragma unroll
+                            for (int e = 0; e < ET; ++e) o[u][e] *= f;
+                        }
+                        const float inv = unit[u].inverse();
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                pb[u][kt * 4 + i] = (M)(s[u][kt][i] * inv);
+                                if constexpr (PAIRS) rest[u][kt * 4 + i] = (M)fmaf(s[u][kt][i], inv, -(float)pb[u][kt * 4 + i]);
+                            }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) l_run[u] = add_pair<M>(__builtin_bit_cast(u32x4, pb[u])[i], l_run[u]);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < ET; ++e) {
+                    u32x4 w;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if constexpr (I8) w[i] = code_pair(vreg[2 * i][e >> 2], vreg[2 * i + 1][e >> 2], 0x0c040c00u + (e & 3) * 0x00010001u);
+                        else w[i] = __builtin_amdgcn_perm(vreg[2 * i + 1][e >> 1], vreg[2 * i][e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+                    }
+                    const m8 vf = __builtin_bit_cast(m8, w);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) {
+                        o[u][e] = Half<M>::mma(vf, pb[u], o[u][e]);
+                        if constexpr (PAIRS) o[u][e] = Half<M>::mma(vf, rest[u], o[u][e]);
+                    }
+                }
+                if (more) load_values(at);
+            }
+        }
+
+        // the waves' sums together: each brings its own to the common maximum
+        bool odd = false;
+        if constexpr (!I8) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int e = 0; e < ET; ++e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) odd = odd || !(fabsf(o[u][e][i]) <= 3.4e38f);
+            odd = __any(odd);
+        }
+        if (lane == 0) s_odd[wave] = odd;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            l_run[u] = across<32>(across<16>(l_run[u], Add()), Add());
+            if (g == 0) {
+                s_m[wave][u * 16 + ql] = m_run[u];
+                s_l[wave][u * 16 + ql] = l_run[u];
+            }
+        }
+        __syncthreads();
+        float m_all[QT], l_all[QT];
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            m_all[u] = kLowest;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) m_all[u] = fmaxf(m_all[u], s_m[w][u * 16 + ql]);
+            l_all[u] = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) l_all[u] += s_l[w][u * 16 + ql] * __builtin_amdgcn_exp2f((s_m[w][u * 16 + ql] - m_all[u]) * sc[u]);
+            const float f = __builtin_amdgcn_exp2f((m_run[u] - m_all[u]) * sc[u]) * (I8 ? unit[u].R : 1.f);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < ET; e += 4) {
+                    const float4 x = make_float4(o[u][e][i] * f, o[u][e + 1][i] * f, o[u][e + 2][i] * f, o[u][e + 3][i] * f);
+                    *(float4*)&s_o[wave][u][i][lane][e] = x;
+                }
+        }
+        const bool careful = !I8 && (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3]);
+        __syncthreads();
+        // wave i takes elements ET * (4g + i) .. of every row: ET neighbours per lane
+        const int e0 = ET * (4 * g + wave);
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            const int r = u * 16 + ql, b = (r0 + r) / G;
+            float x[ET];
+#pragma unroll
+            for (int e = 0; e < ET; ++e) {
+                x[e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < NW; ++w) x[e] += s_o[w][u][wave][lane][e];
+            }
+            if (r >= n_rows) continue;
+            if (careful) {   // rare: infinite or NaN values, or slots that hold them and are not seen: these sums slot by slot, relative to the same maximum
+#pragma unroll
+                for (int e = 0; e < ET; ++e) x[e] = 0.f;
+                const float flip = a.scale < 0.f ? -1.f : 1.f;
+                const T* qp = (const T*)a.q.p + (int64_t)(j * a.group + b) * a.q.row + (int64_t)(h * G + r0 + r - b * G) * a.q.head;
+                for (int i = i0; i < i1; ++i) {
+                    const PageItem one = group_item(a, j, row0, len0, i);
+                    const int seen = one.mask >> bit[u] & 1 ? min(len[u] - one.p0, 16) : 0;
+                    for (int slot = 0; slot < seen; ++slot) {
+                        const int64_t at = (slot_of(one.page, one.p0) + slot) * HD;
+                        float score = 0.f;
+                        for (int e = 0; e < HD; ++e) score = fmaf((float)qp[e] * flip, (float)((const C*)K)[at + e], score);
+                        const float p = __builtin_amdgcn_exp2f((score - m_all[u]) * sc[u]);
+#pragma unroll
+                        for (int e = 0; e < ET; ++e) x[e] = fmaf(p, (float)((const C*)V)[at + e0 + e], x[e]);
+                    }
+                }
+            }
+            if (!whole) {
+                float* to = part + (size_t)r * (HD + 4);
+#pragma unroll
+                for (int e = 0; e < ET; e += 4) *(float4*)(to + e0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(part_top(m_all[u] * sc[u]), l_all[u]);
+            } else {
+                const float inv = l_all[u] != 0.f ? 1.f / l_all[u] : 0.f;   // a row that sees nothing gets zeros
+#pragma unroll
+                for (int e = 0; e < ET; ++e) x[e] *= inv;
+                page_store<T, ET>(a, j * a.group + b, h * G + r0 + r - b * G, e0, x);
+            }
+        }
+    };
+
+    if constexpr (!DEALT) {
+        const int j = blockIdx.y;
+        piece(j, blockIdx.x, 0, group_items(a, j), true, nullptr);
+    } else {
+        // all items of the units before each of the groups, thread by thread; this worker's share
+        const int w = blockIdx.x, per = (n_groups + 255) / 256, first = min(t * per, n_groups), end = min(first + per, n_groups);
+        int64_t sum = 0;
+        for (int j = first; j < end; ++j) sum += group_items(a, j);
+        int64_t before = sum;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int64_t x = __shfl_up(before, d);
+            if (lane >= d) before += x;
+        }
+        if (lane == 63) s_wide[wave] = before;
+        __syncthreads();
+        before -= sum;
+        int64_t total = 0;
+#pragma unroll
+        for (int i = 0; i < NW; ++i) {
+            if (i < wave) before += s_wide[i];
+            total += s_wide[i];
+        }
+        total = uniform(total * units);
+        const int64_t share = (max((total + a.workers - 1) / a.workers, (int64_t)kPageShare) + 1) & ~(int64_t)1, start = w * share, mine_all = min(share, total - start);
+        for (int j = w; j < n_groups; j += a.workers)   // groups that see nothing are nobody's share
+            if (group_items(a, j) == 0)
+                for (int e = t; e < a.group * a.heads * (HD / 8); e += 256) {
+                    const int r = e / (HD / 8);
+                    const float zero[8] = {};
+                    page_store<T, 8>(a, j * a.group + r / a.heads, r % a.heads, e % (HD / 8) * 8, zero);
+                }
+        PageRecord* record = (PageRecord*)a.records + w;
+        if (start >= total) {
+            if (t == 0) *record = {-1, 0, 0, 0};
+            return;
+        }
+        if (before * units <= start && start < (before + sum) * units) {
+            int j = first;
+            int64_t off = start - before * units;
+            while (true) {
+                const int64_t n = (int64_t)group_items(a, j) * units;
+                if (off < n) break;
+                off -= n;
+                ++j;
+            }
+            s_scan[0] = j;
+            s_off = off;
+        }
+        __syncthreads();
+        int j = uniform(s_scan[0]), count = uniform(group_items(a, j));
+        const int64_t off = uniform(s_off);
+        int hb = (int)(off / count), i0 = (int)(off % count);
+        int64_t left = mine_all;
+        PageRecord mine = {-1, 0, 0, 0};
+        while (true) {
+            const int i1 = (int)min((int64_t)count, i0 + left);
+            const bool whole = i0 == 0 && i1 == count;
+            float* part = a.part + ((size_t)w * 2 + (i0 == 0)) * ROWS * (HD + 4);
+            if (i0 == 0 && i1 < count) mine = {j, hb, (int)((start + (mine_all - left) + count - 1) / share), 0};
+            piece(j, hb, i0, i1, whole, part);
+            left -= i1 - i0;
+            if (left <= 0) break;
+            i0 = 0;
+            if (++hb == units) {
+                hb = 0;
+                do count = uniform(group_items(a, ++j));
+                while (count == 0);
+            }
+        }
+        if (t == 0) *record = mine;
+    }
+}
+
+// Adds up the parts of the unit that worker blockIdx.x begins and others go on with: its own, kept second, and theirs, kept first.
+template <int HD, typename T, int QT>
+__global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
+{
+    constexpr int LPG = HD / 4, GROUPS = 256 / LPG, ROWS = 16 * QT;
+    const int w = blockIdx.x;
+    const PageRecord rec = ((const PageRecord*)a.records)[w];
+    if (rec.j < 0) return;
+    const int group = threadIdx.x / LPG, e = threadIdx.x % LPG;
+    const int n_kv = a.p.n_kv, G = a.heads / n_kv, rb = rec.hb / n_kv, h = rec.hb - rb * n_kv, r0 = rb * ROWS, n_rows = min(a.group * G - r0, ROWS);
+    for (int r = group; r < n_rows; r += GROUPS) {
+        float m = kLowest, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int k = w; k <= rec.last; ++k) {
+            const float* q = a.part + (((size_t)k * 2 + (k == w)) * ROWS + r) * (HD + 4);
+            const float4 y = *(const float4*)(q + 4 * e);
+            const float2 ml = *(const float2*)(q + HD);
+            const float m_new = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - m_new), f_k = __builtin_amdgcn_exp2f(ml.x - m_new);
+            m = m_new;
+            l = l * f + ml.y * f_k;
+            x[0] = x[0] * f + y.x * f_k;
+            x[1] = x[1] * f + y.y * f_k;
+            x[2] = x[2] * f + y.z * f_k;
+            x[3] = x[3] * f + y.w * f_k;
+        }
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= inv;
+        const int b = (r0 + r) / G;
+        page_store<T, 4>(a, rec.j * a.group + b, h * G + r0 + r - b * G, 4 * e, x);
+    }
 }
 
 // ------------------------------------------------------------------------------------------ fork
@@ -224,32 +762,6 @@ __global__ __launch_bounds__(256) void k_pages_inherit(ForkArgs a)
         a.src[i] = a.dst[i] = -1;
     }
 }
-
-// Sum over the workgroup's NT threads, in each of them, and of those before a thread.
-template <int NT>
-struct Scan {
-    int before, all;
-    __device__ __forceinline__ Scan(int x, int* lds)   // lds: NT / 64 + 1
-    {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-        int s = x;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(s, d);
-            if (lane >= d) s += o;
-        }
-        __syncthreads();
-        if (lane == 63) lds[wave] = s;
-        __syncthreads();
-        before = s - x;
-        all = 0;
-#pragma unroll
-        for (int w = 0; w < NT / 64; ++w) {
-            if (w < wave) before += lds[w];
-            all += lds[w];
-        }
-    }
-};
 
 constexpr int kForkThreads = 1024, kForkPages = 4096;   // pages of a workgroup
 
@@ -438,11 +950,25 @@ void launch_pages_read(const PagesView& p, const TableView& t, const RowsView& k
 
 void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s)
 {
+    if (a.group > 1) k_page_items<<<a.n / a.group, kItemThreads, 0, s>>>(a);
+    auto go = [&](auto dim, auto t, auto e, auto tiles) {
+        constexpr int HD = decltype(dim)::value, QT = decltype(tiles)::value;
+        typedef decltype(t) T;
+        typedef decltype(e) C;
+        if (a.workers == 0) {
+            k_attention_pages<HD, T, C, QT, false><<<dim3(a.p.n_kv * a.row_blocks, a.n / a.group), 256, 0, s>>>(a);
+        } else {
+            k_attention_pages<HD, T, C, QT, true><<<a.workers, 256, 0, s>>>(a);
+            k_page_join<HD, T, QT><<<a.workers, 256, 0, s>>>(a);
+        }
+    };
     with_types(a.p.hd, token, a.p.dtype, [&](auto dim, auto t, auto e) {
         typedef decltype(t) T;
         typedef decltype(e) C;
-        if constexpr (std::is_same<C, int8_t>::value || std::is_same<C, T>::value)
-            k_attention_pages<decltype(dim)::value, T, C><<<dim3(a.heads, a.n), 256, 0, s>>>(a);
+        if constexpr (std::is_same<C, int8_t>::value || std::is_same<C, T>::value) {
+            if (a.tiles == 1) go(dim, t, e, std::integral_constant<int, 1>{});
+            else go(dim, t, e, std::integral_constant<int, 2>{});
+        }
     });
 }
 

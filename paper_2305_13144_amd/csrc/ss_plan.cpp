@@ -410,4 +410,32 @@ void tree_mask(const int* parents, int n, int words, uint64_t* mask)
     }
 }
 
+PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_length, int n_cu)
+{
+    PagePlan p;
+    const long long rows = (long long)group * heads_each;
+    p.tiles = rows <= 16 ? 1 : 2;
+    p.row_blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
+    p.workers = 0;
+    if (max_length > kPageWholeSlots) {
+        const long long units = std::max(1LL, (long long)(n / group) * n_kv * p.row_blocks), at_once = (p.tiles == 2 ? 2LL : hd == 64 ? 4LL : 3LL) * n_cu;
+        const long long items = (long long)group * ((max_length + 15LL) / 16);   // of a unit, at most
+        p.workers = (int)std::max(1LL, std::min(at_once, (items + kPageShare - 1) / kPageShare * units));
+    }
+    return p;
+}
+
+PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int stride)
+{
+    auto whole = [](size_t b) { return (b + 15) / 16 * 16; };
+    PageSpace s;
+    s.records = (size_t)p.workers * 2 * 16 * p.tiles * (hd + 4) * 4;
+    s.counts = s.records + (size_t)p.workers * 16;
+    const size_t groups = group > 1 ? n / group : 0;
+    s.items = s.counts + whole(groups * 4);
+    s.items_stride = (long long)group * stride * (page / 16);
+    s.bytes = s.items + groups * (size_t)s.items_stride * 16;
+    return s;
+}
+
 }  // namespace ss

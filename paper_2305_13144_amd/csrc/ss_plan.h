@@ -224,6 +224,20 @@ constexpr int tree_chunks(int len, int chunk, int most)
     return len <= chunk ? 1 : len > (most - 1) * (long long)chunk ? most : (len + chunk - 1) / chunk;
 }
 
+// Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles; workers that share out the items of all
+// units (0: a workgroup a unit).  A share has at least kPageShare items of 16 slots.
+constexpr int kPageShare = 8, kPageWholeSlots = 512;
+struct PagePlan {
+    int tiles, row_blocks, workers;
+};
+PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_length, int n_cu);
+// Its workspace: where its parts begin and how large it is (bytes, all multiples of 16).
+struct PageSpace {
+    size_t records, counts, items, bytes;   // the parts of workers begin at 0
+    long long items_stride;
+};
+PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int stride);
+
 // Beam search: logits of a workgroup, and how many such chunks a row has.
 constexpr int kBeamMax = 64, kBeamChunk = 8192;
 constexpr int beam_chunks(int vocab) { return vocab / kBeamChunk + (vocab % kBeamChunk != 0); }
