@@ -631,7 +631,7 @@ typedef struct {
 
 /*
  * A step of beam search.  Each of n_groups groups has `beams` beams (row g * beams + b) and, for each that has not ended, the logits of its next
- * token.  Candidates are (b, v): beam b continued by token v, with the sum total_b + ((logit - m) - log sum exp(logits - m)), m the row's largest
+ * token.  Candidates are (b, v): beam b continued by token v, with the sum total_b + ((logit - m) - log sum exp(logits - m)), m near the row's largest
  * logit, and length + 1;
  * of a beam that has ended only itself, with its sum and length, as (b, end_id) (end_id -1: as (b, 0), and its token is -1).  Their rank is
  * sum / length^length_power (a length of 0 counts as 1).  Of a group's candidates the `keep` with the largest rank are taken in that order, of equal ones first that with the

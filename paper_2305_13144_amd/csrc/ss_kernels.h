@@ -251,7 +251,7 @@ void launch_pages_copy(const PagesView* layers, int n_layers, const int32_t* src
 struct BeamArgs {
     const void* logits;
     int64_t row_stride;
-    int n_groups, beams, vocab, keep, chunks;   // chunks: beam_chunks
+    int n_groups, beams, vocab, keep, slices;   // beam_slices
     const float* totals;
     const int32_t* lengths;
     const uint8_t* ended;
@@ -265,7 +265,7 @@ struct BeamArgs {
     int32_t *parent, *token;
     int end_id;
     float power;
-    float* part;   // [rows][chunks]: the chunk's largest logit and the sum of exp(logit - largest) beside it (2), its best candidates' logits (keep) and tokens (keep)
+    float* part;   // [rows][slices][beam_part_floats]
 };
 void launch_beam_select(const BeamArgs& a, int dtype, hipStream_t s);
 

@@ -225,6 +225,11 @@ int check_beams(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep)
     return SS_OK;
 }
 
+size_t beam_workspace(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep)
+{
+    return (size_t)n_groups * beams * ss::beam_slices(n_groups, beams, vocab, keep, compute_units()) * ss::beam_part_floats(keep) * 4;
+}
+
 }  // namespace
 
 extern "C" int ss_cache_write(const ss_cache* cache, const ss_rows* k, const ss_rows* v, const int32_t* seq, const int32_t* slot, int32_t n,
@@ -483,7 +488,7 @@ extern "C" int ss_beam_select_workspace(int32_t n_groups, int32_t beams, int32_t
     ss::clear_error();
     if (!bytes) return fail(SS_EINVAL, "bytes is NULL");
     if (int rc = check_beams(n_groups, beams, vocab, keep)) return rc;
-    *bytes = ss::beam_part_floats(n_groups * beams, vocab, keep) * 4;
+    *bytes = beam_workspace(n_groups, beams, vocab, keep);
     return SS_OK;
 }
 
@@ -507,7 +512,7 @@ extern "C" int ss_beam_select(const void* logits, int32_t dtype, int64_t row_str
     if (now->totals == next->totals || (now->lengths && now->lengths == next->lengths) || (now->ended && now->ended == next->ended) ||
         (now->history && now->history == next->history))
         return fail(SS_EINVAL, "next must not be now: beams change places");
-    if (int rc = check_workspace(workspace, workspace_bytes, ss::beam_part_floats(n_groups * beams, vocab, keep) * 4)) return rc;
+    if (int rc = check_workspace(workspace, workspace_bytes, beam_workspace(n_groups, beams, vocab, keep))) return rc;
     ss::BeamArgs a{};
     a.logits = logits;
     a.row_stride = row_stride;
@@ -515,7 +520,7 @@ extern "C" int ss_beam_select(const void* logits, int32_t dtype, int64_t row_str
     a.beams = beams;
     a.vocab = vocab;
     a.keep = keep;
-    a.chunks = ss::beam_chunks(vocab);
+    a.slices = ss::beam_slices(n_groups, beams, vocab, keep, compute_units());
     a.totals = now->totals;
     a.lengths = now->lengths;
     a.ended = now->ended;

@@ -238,10 +238,11 @@ struct PageSpace {
 };
 PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int stride);
 
-// Beam search: logits of a workgroup, and how many such chunks a row has.
-constexpr int kBeamMax = 64, kBeamChunk = 8192;
-constexpr int beam_chunks(int vocab) { return vocab / kBeamChunk + (vocab % kBeamChunk != 0); }
-constexpr size_t beam_part_floats(int rows, int vocab, int keep) { return (size_t)rows * beam_chunks(vocab) * (2 + 2 * (size_t)keep); }
+// Beam search: workgroups that share out a row's logits, so many that all rows together fill the chip, that a wave has a few steps of 1 KiB, and that a
+// group's candidates are no more than kBeamRanked (or a slice a row).  A slice's part of the workspace: reference, sum (fp64), logits, tokens.
+constexpr int kBeamMax = 64, kBeamRanked = 1024;
+constexpr int beam_part_floats(int keep) { return 4 + 2 * keep; }
+int beam_slices(int n_groups, int beams, int vocab, int keep, int n_cu);
 
 }  // namespace ss
 
