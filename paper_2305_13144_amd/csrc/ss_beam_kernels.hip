@@ -53,54 +53,96 @@ __device__ __forceinline__ double wave_sum(double x)
     return x;
 }
 
-// The best candidates that a wave has met, lane k the k-th: larger logits first, of equal ones lower tokens.
+// A number's bits, ordered as the numbers.
+__device__ __forceinline__ uint32_t ordered(float x)
+{
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// A number that at least n of four values of each lane are not below: the n-th largest but for its last 16 bits, bit by bit; -inf where that is -inf.
+__device__ __forceinline__ float nth_largest(const f32x4& x, int n)
+{
+    uint32_t t = 0;
+    for (int b = 31; b >= 16; --b) {
+        int there = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) there += __popcll(__ballot(ordered(x[i]) >= (t | 1u << b)));
+        if (there >= n) t |= 1u << b;
+    }
+    const float least = __uint_as_float(t & 0x80000000u ? t & 0x7fffffffu : ~t);
+    return least >= -3.4028235e38f ? least : -__builtin_inff();   // -inf without its last bits is a NaN
+}
+
+// The candidates that a wave has met and not ruled out, in no order, in LDS.
 struct Shortlist {
-    float v = -__builtin_inff();
-    int i = INT_MAX;
-    // x, of all lanes alike, takes its place.
-    __device__ __forceinline__ void insert(float x, int xi)
+    float* v;
+    int* i;   // tokens
+    int count;
+
+    // Only the n best stay (larger logits, of equal ones lower tokens), where there are more; returns the n-th's logit.
+    __device__ __forceinline__ float cut(int n)
     {
-        const int lane = threadIdx.x & 63, at = __popcll(__ballot(v > x || (v == x && i < xi)));
-        const float ov = __shfl_up(v, 1);
-        const int oi = __shfl_up(i, 1);
-        if (lane > at) {
-            v = ov;
-            i = oi;
+        const int lane = threadIdx.x & 63, rounds = (count + 63) >> 6;
+        auto held = [&](int r) { return r * 64 + lane < count ? ordered(v[r * 64 + lane]) : 0u; };   // 0: none, below all
+        auto at_least = [&](auto f) {
+            int there = 0;
+            for (int r = 0; r < rounds; ++r) there += __popcll(__ballot(f(r)));
+            return there;
+        };
+        uint32_t t = 0;
+        for (int b = 31; b >= 0; --b)
+            if (at_least([&](int r) { return held(r) >= (t | 1u << b); }) >= n) t |= 1u << b;
+        // of those that are equal to it the first ones: tokens below `to`
+        const int equal = n - at_least([&](int r) { return held(r) > t; });
+        int to = INT_MAX;
+        if (at_least([&](int r) { return held(r) == t; }) > equal) {
+            to = 0;
+            for (int b = 30; b >= 0; --b)   // the largest number that no more than `equal` tokens are below
+                if (at_least([&](int r) { return held(r) == t && i[r * 64 + lane] < (to | 1 << b); }) <= equal) to |= 1 << b;
         }
-        if (lane == at) {
-            v = x;
-            i = xi;
+        int kept = 0;
+        for (int r = 0; r < rounds; ++r) {   // what is written is what has been read
+            const uint32_t h = held(r);
+            const int token = h ? i[r * 64 + lane] : 0;
+            const bool stays = h > t || (h == t && token < to);
+            const uint64_t all = __ballot(stays);
+            const float x = h ? v[r * 64 + lane] : 0.f;
+            if (stays) {
+                const int at = kept + __popcll(all & ((1ull << lane) - 1));
+                v[at] = x;
+                i[at] = token;
+            }
+            kept += __popcll(all);
         }
+        count = kept;
+        return __uint_as_float(t & 0x80000000u ? t & 0x7fffffffu : ~t);
     }
 };
-
-// The n-th largest of the lanes' values, -inf if there are fewer (NaN counts as above all).
-__device__ __forceinline__ float nth_largest(float x, int n)
-{
-    const uint32_t u = __float_as_uint(x), key = u & 0x80000000u ? ~u : u | 0x80000000u;   // ordered as the numbers
-    uint32_t t = 0;
-    for (int b = 31; b >= 0; --b)
-        if (__popcll(__ballot(key >= (t | 1u << b))) >= n) t |= 1u << b;
-    return __uint_as_float(t & 0x80000000u ? t & 0x7fffffffu : ~t);
-}
 
 // A wave goes through its part of a row in order, 64 x 16 bytes a step, kBeamAhead steps requested at a time.
 //   sum         of exp(x - ref): ref is the largest logit of the first steps, and moves where one is more than 80 above it (rare).  Those of 16 bytes
 //               are added in fp32 and their sums in fp64, as thousands of terms follow each other
-//   shortlist   a step whose largest logit is not above the last on the list (and not below what `keep` lanes have in the first steps) costs one
-//               comparison; each logit that is takes a turn of the wave.  About keep * (2 + log(steps)) turns of 80 cycles where logits come in no order
+//   candidates  a lane keeps the largest of its 16 bytes' largest logits, with its step, and the second largest: 4 instructions a step, whatever
+//               the order of the logits.  The keep-th largest of the workgroup's lanes, `least`, is what none of the keep best is below; so those are
+//               in the 16 bytes that a lane remembers, read again, and where a lane's second is not below it either, in the whole of what
+//               that lane has read (some 1 in 30 waves).  Where that is so in many lanes, as with few distinct logits, the wave goes through all of
+//               its part again
 // NaN and +inf, which are no candidates, would show in the sum: then the wave goes through its part once more and takes them as -inf.
-// Bound by the bytes and, at 16 bits, by the vector units (about 9 instructions a logit, 4 of them the exponential's).
-constexpr int kBeamAhead = 4;
+// Bound by the bytes and, at 16 bits, by the vector units (about 9 instructions a logit, 4 of them the exponential's).  Lists in order of the lanes of a
+// wave, into which every logit above the last went by itself, took 17 of 57 us (96 x 8 rows over 100003 tokens), one that grew to 64 and
+// was then cut to its best 35 of 78.
+constexpr int kBeamAhead = 4, kBeamList = 64, kBeamLanes = 6;
 
 template <typename T>
 __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
 {
     typedef LogitVector<T> Vec;
-    constexpr int N = Vec::N, NW = 4;
-    __shared__ float s_v[NW * kBeamMax], s_ref[NW];
-    __shared__ int s_i[NW * kBeamMax];
+    constexpr int N = Vec::N, NW = 4, CAP = kBeamList + 64 * N;
+    __shared__ float s_v[NW * CAP], s_ref[NW];
+    __shared__ int s_i[NW * CAP], s_count[NW];
     __shared__ double s_sum[NW];
+    __shared__ __attribute__((aligned(16))) float s_first[256];
     const int row = blockIdx.y, slice = blockIdx.x, t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     if (a.ended && a.ended[row]) return;
     const T* x = (const T*)a.logits + (int64_t)row * a.row_stride;
@@ -108,15 +150,11 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
     const int64_t steps_all = ((int64_t)mis + a.vocab + 64 * N - 1) / (64 * N), workers = (int64_t)a.slices * NW, me = (int64_t)slice * NW + wave;
     const int first = (int)(steps_all * me / workers), end = (int)(steps_all * (me + 1) / workers);
 
-    Shortlist list;
-    float ref = 0.f;
-    double sum = 0;
-    // step s: 16 bytes a lane; at the row's ends element by element, -inf beside it
-    auto load = [&](int s, u32x4& r) {
-        const int64_t e0 = (int64_t)s * (64 * N) - mis;
-        const int64_t e = e0 + lane * N;
-        if (e0 >= 0 && e0 + 64 * N <= a.vocab) {
-            r = __builtin_nontemporal_load((const u32x4*)(x + e));
+    // 16 bytes: those of a lane in a step; at the row's ends element by element, -inf beside it
+    auto place = [&](int s, int l) { return (int64_t)s * (64 * N) - mis + l * N; };
+    auto load_one = [&](int64_t e, u32x4& r) {
+        if (e >= 0 && e + N <= a.vocab) {
+            r = *(const u32x4*)(x + e);
             return;
         }
         T part[N];
@@ -124,22 +162,29 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
         for (int i = 0; i < N; ++i) part[i] = e + i >= 0 && e + i < a.vocab ? x[e + i] : (T)(-__builtin_inff());
         r = __builtin_bit_cast(u32x4, part);
     };
+    auto load = [&](int s, u32x4& r) {
+        if (place(s, 0) >= 0 && place(s, 64) <= a.vocab) r = __builtin_nontemporal_load((const u32x4*)(x + place(s, lane)));
+        else load_one(place(s, lane), r);
+    };
+    auto clean = [&](float (&v)[N]) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = v[i] <= 3.4028235e38f ? v[i] : -__builtin_inff();
+    };
+    auto largest = [&](const float (&v)[N]) {
+        float m = v[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
+        return m;
+    };
+
+    float ref, best, second;   // of this lane's 16 bytes, by their largest logits
+    int best_step;
+    double sum;
     auto pass = [&](auto clean_pass) {
         constexpr bool CLEAN = decltype(clean_pass)::value;
-        list = Shortlist{};
-        sum = 0;
         auto open = [&](const u32x4& r, float (&v)[N]) {
             Vec::open(r, v);
-            if constexpr (CLEAN)
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    if (!(v[i] <= 3.4028235e38f)) v[i] = -__builtin_inff();
-        };
-        auto largest = [&](const float (&v)[N]) {
-            float m = v[0];
-#pragma unroll
-            for (int i = 1; i < N; ++i) m = fmaxf(m, v[i]);
-            return m;
+            if constexpr (CLEAN) clean(v);
         };
         u32x4 now[kBeamAhead], next[kBeamAhead];
 #pragma unroll
@@ -147,23 +192,18 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
             next[k] = u32x4{0, 0, 0, 0};
             if (first + k < end) load(first + k, next[k]);
         }
-        float mine = -__builtin_inff();
+        ref = -3.0e38f;
 #pragma unroll
         for (int k = 0; k < kBeamAhead; ++k)
             if (first + k < end) {
                 float v[N];
                 open(next[k], v);
-                mine = fmaxf(mine, largest(v));
+                ref = fmaxf(ref, largest(v));
             }
-        ref = fmaxf(wave_max(mine), -3.0e38f);
-        // what is below the keep-th of the lanes' largest is not among the wave's keep best; `above`: only what is above it can be
-        const float floor = nth_largest(mine, a.keep);
-        float above = floor > -3.4028235e38f ? -__builtin_inff() : floor, last_v = -__builtin_inff();
-        int last_i = INT_MAX;
-        if (floor > -3.4028235e38f) {   // the next number below
-            const uint32_t u = __float_as_uint(floor);
-            above = __uint_as_float(u == 0 || u == 0x80000000u ? 0x80000001u : u & 0x80000000u ? u + 1 : u - 1);
-        }
+        ref = wave_max(ref);
+        best = second = -__builtin_inff();
+        best_step = first;
+        sum = 0;
         for (int s = first; s < end; s += kBeamAhead) {
 #pragma unroll
             for (int k = 0; k < kBeamAhead; ++k) now[k] = next[k];
@@ -189,34 +229,66 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
 #pragma unroll
                     for (int i = 0; i < w; ++i) p[i] += p[i + w];
                 sum += (double)p[0];
-                if (!__any(top > above)) continue;
-                const int token = (int)((int64_t)(s + k) * (64 * N) - mis) + lane * N;
-#pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    uint64_t turn = __ballot(v[i] > above);
-                    while (turn) {
-                        const int l = __ffsll((unsigned long long)turn) - 1;
-                        list.insert(__int_as_float(__builtin_amdgcn_readlane(__float_as_int(v[i]), l)), __builtin_amdgcn_readlane(token + i, l));
-                        last_v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(list.v), a.keep - 1));
-                        last_i = __builtin_amdgcn_readlane(list.i, a.keep - 1);
-                        turn &= turn - 1;
-                        turn &= __ballot(v[i] > last_v || (v[i] == last_v && token + i < last_i));
-                    }
-                }
-                above = fmaxf(above, last_v);
+                second = fmaxf(second, fminf(best, top));
+                best_step = top > best ? s + k : best_step;
+                best = fmaxf(best, top);
             }
         }
         sum = wave_sum(sum);
         return fabs(sum) <= 1e300;
     };
     if (!pass(std::false_type{})) pass(std::true_type{});
+    s_first[t] = best;
+    __syncthreads();
+    const float least = nth_largest(*(const f32x4*)(s_first + 4 * lane), a.keep);
+
+    Shortlist list{s_v + wave * CAP, s_i + wave * CAP, 0};
+    auto collect = [&](bool have, const u32x4& r, int64_t e, float above) {   // of a lane's 16 bytes at e; cut: only the best stay, and the last's logit
+        float v[N];
+        Vec::open(r, v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const bool goes = have && v[i] >= least && v[i] > above && v[i] <= 3.4028235e38f;
+            const uint64_t all = __ballot(goes);
+            if (goes) {
+                const int at = list.count + __popcll(all & ((1ull << lane) - 1));
+                list.v[at] = v[i];
+                list.i[at] = (int)(e + i);
+            }
+            list.count += __popcll(all);
+        }
+        return list.count > kBeamList ? list.cut(a.keep) : -__builtin_inff();
+    };
+    constexpr float kNothing = -__builtin_inff();
+    const bool here = best >= least && best > kNothing;
+    uint64_t more = __ballot(here && second >= least && second > kNothing);
+    if (__popcll(more) <= kBeamLanes) {
+        u32x4 r{0, 0, 0, 0};
+        const int64_t e = place(best_step, lane);
+        if (here) load_one(e, r);
+        if (__any(here)) collect(here, r, e, kNothing);
+        for (; more; more &= more - 1) {
+            const int l = __ffsll((unsigned long long)more) - 1, known = __builtin_amdgcn_readlane(best_step, l);
+            for (int s0 = first; s0 < end; s0 += 64) {
+                const int s = s0 + lane;
+                const int64_t at = place(s, l);
+                const bool have = s < end && s != known;
+                if (have) load_one(at, r);
+                collect(have, r, at, kNothing);
+            }
+        }
+    } else {
+        float above = kNothing;   // once the list has been cut: `keep` of its candidates, all before those to come, are not below it
+        for (int s = first; s < end; ++s) {
+            u32x4 r;
+            load(s, r);
+            above = fmaxf(above, collect(true, r, place(s, lane), above));
+        }
+    }
 
     // the waves' together
-    if (lane < a.keep) {
-        s_v[wave * a.keep + lane] = list.v;
-        s_i[wave * a.keep + lane] = list.i;
-    }
     if (lane == 0) {
+        s_count[wave] = list.count;
         s_ref[wave] = ref;
         s_sum[wave] = sum;
     }
@@ -230,49 +302,104 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
         out[0] = top;
         *(double*)(out + 2) = all;
     }
-    const int n = NW * a.keep;
-    if (t >= n) return;
-    const float v = s_v[t];
-    const int i = s_i[t];
-    int before = 0;   // entries without a candidate, all alike, keep their order
-    for (int k = 0; k < n; ++k) before += s_v[k] > v || (s_v[k] == v && (s_i[k] < i || (s_i[k] == i && k < t)));
-    if (before < a.keep) {
-        out[4 + before] = v;
-        out[4 + a.keep + before] = __int_as_float(i == INT_MAX ? -1 : i);
+    int n = 0;
+    for (int w = 0; w < NW; ++w) n += s_count[w];
+    if (lane < s_count[wave]) {   // at most kBeamList of a wave
+        const float v = list.v[lane];
+        const int i = list.i[lane];
+        int before = 0;
+        for (int w = 0; w < NW; ++w) {
+            const int there = s_count[w];
+#pragma unroll 8
+            for (int k = 0; k < there; ++k) before += (s_v[w * CAP + k] > v) | ((s_v[w * CAP + k] == v) & (s_i[w * CAP + k] < i));
+        }
+        if (before < a.keep) {
+            out[4 + before] = v;
+            out[4 + a.keep + before] = __int_as_float(i);
+        }
     }
+    if (t >= n && t < a.keep) out[4 + a.keep + t] = __int_as_float(-1);   // fewer candidates than places
 }
 
 // Tokens of a beam of this length, and with one more.
 __device__ __forceinline__ int beam_length(int length, bool more) { return min(max(length, 0), INT_MAX - more) + more; }
 
-// Up to kBeamRanked candidates find their places by counting those before them; more (then a row is one slice) are taken one by one, a lane of
-// the first wave holding the best of its beam that is left.
+// Up to kBeamRanked candidates find their places by counting those before them, once each wave has left out what is not among its best; more (then a row is one slice) are taken one by one, a lane of
+// the first wave holding the best of its beam that is left.  Bound by a chain of latencies (a launch's start, two loads behind each other, fp64 exp,
+// log and pow of a lane per beam): all that does not depend on other loads is requested at the start.
 __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
 {
-    __shared__ double s_top[kBeamMax], s_log[kBeamMax], s_total[kBeamMax], s_power[kBeamMax], s_rank[kBeamRanked];
-    __shared__ uint64_t s_key[kBeamRanked];   // beam and token: of equal ranks the lower one is first
-    __shared__ int s_over[kBeamMax], s_row[kBeamMax], s_token[kBeamMax];
-    const int g = blockIdx.x, t = threadIdx.x, per = beam_part_floats(a.keep), lists = a.slices * a.keep, n = a.beams * lists;
+    struct Ranked {
+        double rank;
+        uint64_t key;   // beam and token: of equal ranks the lower one is first
+    };
     constexpr uint64_t kNone = ~0ull;
-    if (t < a.beams) {
-        const int row = g * a.beams + t;
-        const bool over = a.ended && a.ended[row];
-        const float* p = a.part + (int64_t)row * a.slices * per;
-        double m = -__builtin_inf(), l = 0;
-        if (!over) {
-            for (int c = 0; c < a.slices; ++c) m = fmax(m, (double)p[c * per]);
-            for (int c = 0; c < a.slices; ++c) l += *(const double*)(p + c * per + 2) * exp((double)p[c * per] - m);
+    constexpr int PER = kBeamRanked / 256;
+    __shared__ Ranked s_c[kBeamRanked];
+    __shared__ double s_top[kBeamMax], s_log[kBeamMax], s_total[kBeamMax], s_power[kBeamMax];
+    __shared__ int s_over[kBeamMax], s_row[kBeamMax], s_token[kBeamMax], s_len[kBeamMax], s_kept[4];
+    const int g = blockIdx.x, t = threadIdx.x, per = beam_part_floats(a.keep), lists = a.slices * a.keep, n = a.beams * lists, sums = a.beams * a.slices;
+    const float* part = a.part + (int64_t)g * a.beams * a.slices * per;
+    const bool ranked = n <= kBeamRanked;
+    // (sums <= n: with one slice a row there are at most kBeamMax of them)
+    float ref[PER], cand[PER];
+    double sum_of[PER];
+    int token_of[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = t + 256 * k;
+        if (c < sums) {
+            ref[k] = part[c * per];
+            sum_of[k] = *(const double*)(part + c * per + 2);
         }
+        if (ranked && c < n) {
+            const float* p = part + (int64_t)(c / a.keep) * per + 4 + c % a.keep;
+            cand[k] = *p;
+            token_of[k] = __float_as_int(p[a.keep]);
+        }
+    }
+    if (t < a.beams) {
+        const int row = g * a.beams + t, len = a.lengths ? a.lengths[row] : 0;
+        const bool over = a.ended && a.ended[row];
         s_over[t] = over;
-        s_top[t] = m;
-        s_log[t] = log(l);
+        s_len[t] = len;
         s_total[t] = a.totals[row];
-        s_power[t] = a.power != 0.f ? pow((double)max(beam_length(a.lengths[row], !over), 1), (double)a.power) : 1.0;
+        s_power[t] = a.power != 0.f ? pow((double)max(beam_length(len, !over), 1), (double)a.power) : 1.0;
     }
     if (t < a.keep) s_row[t] = s_token[t] = -1;
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = t + 256 * k;
+        if (c < sums) s_c[c].rank = ref[k];
+    }
     __syncthreads();
-    // the e-th candidate of a beam: its rank, and its sum
-    auto candidate = [&](int beam, int e, double* sum, uint64_t* key) {
+    double share[PER];   // a slice's sum, relative to its row's largest reference
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = t + 256 * k;
+        if (c >= sums) break;
+        const int beam = c / a.slices;
+        if (s_over[beam]) continue;
+        double m = s_c[beam * a.slices].rank;
+        for (int o = 1; o < a.slices; ++o) m = fmax(m, s_c[beam * a.slices + o].rank);
+        share[k] = sum_of[k] * exp((double)ref[k] - m);
+        s_top[beam] = m;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const int c = t + 256 * k;
+        if (c < sums) s_c[c].rank = share[k];
+    }
+    __syncthreads();
+    if (t < a.beams && !s_over[t]) {
+        double l = s_c[t * a.slices].rank;
+        for (int o = 1; o < a.slices; ++o) l += s_c[t * a.slices + o].rank;
+        s_log[t] = log(l);
+    }
+    __syncthreads();
+    // a candidate of a beam, its e-th: its rank and its sum
+    auto candidate = [&](int beam, int e, float logit, int token, double* sum, uint64_t* key) {
         *key = kNone;
         *sum = -__builtin_inf();
         if (!(fabs(s_total[beam]) <= 3.5e38)) return -__builtin_inf();
@@ -281,10 +408,8 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
             *sum = s_total[beam];
             *key = (uint64_t)beam << 32 | (uint32_t)max(a.end_id, 0);
         } else {
-            const float* p = a.part + (((int64_t)g * a.beams + beam) * a.slices + e / a.keep) * per + 4 + e % a.keep;
-            const int token = __float_as_int(p[a.keep]);
             if (token < 0) return -__builtin_inf();
-            *sum = s_total[beam] + (((double)p[0] - s_top[beam]) - s_log[beam]);
+            *sum = s_total[beam] + (((double)logit - s_top[beam]) - s_log[beam]);
             *key = (uint64_t)beam << 32 | (uint32_t)token;
         }
         return *sum / s_power[beam];
@@ -298,34 +423,69 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
         a.parent[at] = row;
         a.token[at] = token;
         a.next_totals[at] = (float)sum;
-        if (a.next_lengths) a.next_lengths[at] = beam_length(a.lengths[row], !over);
+        if (a.next_lengths) a.next_lengths[at] = beam_length(s_len[beam], !over);
         if (a.next_ended) a.next_ended[at] = over || token == a.end_id;
     };
-    if (n <= kBeamRanked) {
-        double sums[kBeamRanked / 256];
-        for (int c = t, k = 0; c < n; c += 256, ++k) s_rank[c] = candidate(c / lists, c % lists, &sums[k], &s_key[c]);
-        __syncthreads();
-        for (int c = t, k = 0; c < n; c += 256, ++k) {
-            const double r = s_rank[c];
-            const uint64_t key = s_key[c];
-            if (key == kNone) continue;
-            int before = 0;
-            for (int o = 0; o < n; ++o) before += s_key[o] != kNone && (s_rank[o] > r || (s_rank[o] == r && s_key[o] < key));
-            if (before < a.keep) take(before, key, sums[k]);
+    if (ranked) {
+        // of each wave's candidates those that are not below its keep-th, as floats, which are ordered alike
+        Ranked mine[PER];
+        double sum[PER];
+        uint32_t as_float[PER];
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            const int c = t + 256 * k;
+            mine[k] = {-__builtin_inf(), kNone};
+            if (c < n) mine[k].rank = candidate(c / lists, c % lists, cand[k], token_of[k], &sum[k], &mine[k].key);
+            as_float[k] = ordered((float)mine[k].rank);
         }
+        uint32_t least = 0;
+        for (int b = 31; b >= 0; --b) {
+            int there = 0;
+#pragma unroll
+            for (int k = 0; k < PER; ++k)
+                if (256 * k < n) there += __popcll(__ballot(as_float[k] >= (least | 1u << b)));
+            if (there >= a.keep) least |= 1u << b;
+        }
+        int kept = 0;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) {
+            if (256 * k >= n) break;
+            const bool stays = mine[k].key != kNone && as_float[k] >= least;
+            const uint64_t all = __ballot(stays);
+            if (stays) s_c[(t >> 6) * (64 * PER) + kept + __popcll(all & ((1ull << (t & 63)) - 1))] = mine[k];
+            else mine[k].key = kNone;
+            kept += __popcll(all);
+        }
+        if ((t & 63) == 0) s_kept[t >> 6] = kept;
+        __syncthreads();
+        int before[PER] = {};
+        for (int w = 0; w < 4; ++w)
+            for (int o = 0; o < s_kept[w]; ++o) {
+                const Ranked x = s_c[w * (64 * PER) + o];
+#pragma unroll
+                for (int k = 0; k < PER; ++k)
+                    if (256 * k < n) before[k] += x.rank > mine[k].rank || (x.rank == mine[k].rank && x.key < mine[k].key);
+            }
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (mine[k].key != kNone && before[k] < a.keep) take(before[k], mine[k].key, sum[k]);
     } else if (t < 64) {
         int at = 0;
         double sum = 0, rank = -__builtin_inf();
         uint64_t key = kNone;
-        if (t < a.beams) rank = candidate(t, 0, &sum, &key);
+        auto head = [&] {
+            const float* p = part + (int64_t)t * per + 4 + at;
+            rank = candidate(t, at, *p, __float_as_int(p[a.keep]), &sum, &key);
+        };
+        if (t < a.beams) head();
         for (int place = 0; place < a.keep; ++place) {
-            double r = key == kNone ? -__builtin_inf() : rank;
+            double r = rank;
             uint64_t best = key;
 #pragma unroll
             for (int d = 32; d > 0; d >>= 1) {
                 const double o = __shfl_xor(r, d);
                 const uint64_t ok = __shfl_xor((unsigned long long)best, d);
-                if (ok != kNone && (best == kNone || o > r || (o == r && ok < best))) {
+                if (o > r || (o == r && ok < best)) {
                     r = o;
                     best = ok;
                 }
@@ -333,7 +493,11 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
             if (best == kNone) break;
             if (key == best) {
                 take(place, key, sum);
-                rank = ++at < lists ? candidate(t, at, &sum, &key) : (key = kNone, 0.0);
+                if (++at < a.keep) head();
+                else {
+                    rank = -__builtin_inf();
+                    key = kNone;
+                }
             }
         }
     }
@@ -346,13 +510,24 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
         if (a.next_ended) a.next_ended[at] = 1;
     }
     if (!a.next_history) return;
+    constexpr int AT_ONCE = 8;   // a wave takes a history, so many loads at a time
     const int width = a.next_history_stride;
-    for (int k = 0; k < a.keep; ++k) {
-        const int row = s_row[k], len = row < 0 ? 0 : max(a.lengths[row], 0), token = s_token[k], kept = min(len, a.history_stride);
+    for (int k = t >> 6; k < a.keep; k += 4) {
+        const int row = s_row[k], len = row < 0 ? 0 : max(s_len[row - g * a.beams], 0), token = s_token[k], kept = min(len, a.history_stride);
         const int32_t* from = a.history + (int64_t)max(row, 0) * a.history_stride;
         int32_t* to = a.next_history + ((int64_t)g * a.keep + k) * width;
-#pragma unroll 4
-        for (int i = t; i < width; i += 256) to[i] = i < kept ? from[i] : i == len ? token : -1;
+        for (int i0 = t & 63; i0 < width; i0 += 64 * AT_ONCE) {
+            int x[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                const int i = i0 + 64 * u;
+                x[u] = i == len ? token : -1;
+                if (i < kept) x[u] = from[i];
+            }
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (i0 + 64 * u < width) to[i0 + 64 * u] = x[u];
+        }
     }
 }
 

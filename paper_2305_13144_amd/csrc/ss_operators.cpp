@@ -225,9 +225,10 @@ int check_beams(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep)
     return SS_OK;
 }
 
+// Whatever the logits' type is: that of 32 bits has the most slices.
 size_t beam_workspace(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep)
 {
-    return (size_t)n_groups * beams * ss::beam_slices(n_groups, beams, vocab, keep, compute_units()) * ss::beam_part_floats(keep) * 4;
+    return (size_t)n_groups * beams * ss::beam_slices(n_groups, beams, vocab, keep, 4, compute_units()) * ss::beam_part_floats(keep) * 4;
 }
 
 }  // namespace
@@ -520,7 +521,7 @@ extern "C" int ss_beam_select(const void* logits, int32_t dtype, int64_t row_str
     a.beams = beams;
     a.vocab = vocab;
     a.keep = keep;
-    a.slices = ss::beam_slices(n_groups, beams, vocab, keep, compute_units());
+    a.slices = ss::beam_slices(n_groups, beams, vocab, keep, dtype == SS_F32 ? 4 : 2, compute_units());
     a.totals = now->totals;
     a.lengths = now->lengths;
     a.ended = now->ended;

@@ -438,10 +438,10 @@ PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int 
     return s;
 }
 
-int beam_slices(int n_groups, int beams, int vocab, int keep, int n_cu)
+int beam_slices(int n_groups, int beams, int vocab, int keep, int size, int n_cu)
 {
     const long long rows = std::max(1LL, (long long)n_groups * beams);
-    const long long fill = (4LL * n_cu + rows - 1) / rows, steps = (vocab + 8191LL) / 8192;   // 4 waves of 4 steps of 512
+    const long long fill = (2LL * n_cu + rows - 1) / rows, steps = ((long long)vocab * size + 16383) / 16384;   // 4 waves of 4 steps
     const long long few = std::max(1, kBeamRanked / (beams * keep));
     return (int)std::max(1LL, std::min({fill, steps, few}));
 }

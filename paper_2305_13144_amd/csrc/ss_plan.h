@@ -242,7 +242,7 @@ PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int 
 // group's candidates are no more than kBeamRanked (or a slice a row).  A slice's part of the workspace: reference, sum (fp64), logits, tokens.
 constexpr int kBeamMax = 64, kBeamRanked = 1024;
 constexpr int beam_part_floats(int keep) { return 4 + 2 * keep; }
-int beam_slices(int n_groups, int beams, int vocab, int keep, int n_cu);
+int beam_slices(int n_groups, int beams, int vocab, int keep, int size, int n_cu);   // size: bytes of a logit
 
 }  // namespace ss
 
