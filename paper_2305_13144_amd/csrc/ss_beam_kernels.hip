@@ -438,8 +438,8 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
             if (c < n) mine[k].rank = candidate(c / lists, c % lists, cand[k], token_of[k], &sum[k], &mine[k].key);
             as_float[k] = ordered((float)mine[k].rank);
         }
-        uint32_t least = 0;
-        for (int b = 31; b >= 0; --b) {
+        uint32_t least = 0;   // but for its last bits
+        for (int b = 31; b >= 12; --b) {
             int there = 0;
 #pragma unroll
             for (int k = 0; k < PER; ++k)

@@ -252,6 +252,11 @@ struct PageRecord {
     int j, hb, last, pad;
 };
 
+// Of a thread: what its groups are on a line of all groups, and what is before them; the whole line.
+struct Prefix {
+    int64_t before, own, all;
+};
+
 constexpr int kItemsAtOnce = 512;
 
 template <int HD, typename T, typename C, int QT, bool DEALT>
@@ -266,8 +271,8 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
     constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
     constexpr bool PAIRS = I8 && std::is_same<T, _Float16>::value && QT == 1;   // weights as sums of two halves
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
-    __shared__ int s_odd[NW], s_scan[2];
-    __shared__ int64_t s_wide[NW], s_off;
+    __shared__ int s_odd[NW], s_scan;
+    __shared__ int64_t s_wide[3][NW], s_off;
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
     __shared__ PageItem s_item[kItemsAtOnce];
 
@@ -605,27 +610,43 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
         const int j = blockIdx.y;
         piece(j, blockIdx.x, 0, group_items(a, j), true, nullptr);
     } else {
-        // all items of the units before each of the groups, thread by thread; this worker's share
-        const int w = blockIdx.x, per = (n_groups + 255) / 256, first = min(t * per, n_groups), end = min(first + per, n_groups);
-        int64_t sum = 0;
-        for (int j = first; j < end; ++j) sum += group_items(a, j);
-        int64_t before = sum;
+        // Two ways to share out the items, both found by every worker for itself from the groups' counts, a thread a group (or some):
+        //   whole parts   every unit is cut into equal parts of at most `share` items, and a worker takes one: where all parts have a worker with a share
+        //                 not much above the average
+        //   stretches     all units in a row, and a worker takes the items of its stretch of it, of one unit or several.  A unit that a worker begins
+        //                 costs it a chain of latencies: it counts as `start` items more
+        const int w = blockIdx.x, per = (n_groups + 255) / 256, g0 = min(t * per, n_groups), g1 = min(g0 + per, n_groups);
+        auto sum_of = [&](auto f, int64_t* lds) {   // of all threads' f(j) over their groups; what is before this thread
+            int64_t sum = 0;
+            for (int j = g0; j < g1; ++j) sum += f(group_items(a, j));
+            int64_t before = sum;
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t x = __shfl_up(before, d);
-            if (lane >= d) before += x;
-        }
-        if (lane == 63) s_wide[wave] = before;
-        __syncthreads();
-        before -= sum;
-        int64_t total = 0;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int64_t x = __shfl_up(before, d);
+                if (lane >= d) before += x;
+            }
+            if (lane == 63) lds[wave] = before;
+            __syncthreads();
+            before -= sum;
+            int64_t total = 0;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            if (i < wave) before += s_wide[i];
-            total += s_wide[i];
-        }
-        total = uniform(total * units);
-        const int64_t share = (max((total + a.workers - 1) / a.workers, (int64_t)kPageShare) + 1) & ~(int64_t)1, start = w * share, mine_all = min(share, total - start);
+            for (int i = 0; i < NW; ++i) {
+                if (i < wave) before += lds[i];
+                total += lds[i];
+            }
+            return Prefix{before, sum, uniform(total)};
+        };
+        const Prefix items = sum_of([](int n) { return (int64_t)n; }, s_wide[0]);
+        const int64_t average = (items.all * units + a.workers - 1) / a.workers;
+        const int wide = (int)min(max(average + (average >> 3) + kPageStart / 2, (int64_t)kPageShare), (int64_t)1 << 28);
+        const Prefix parts = sum_of([&](int n) { return (int64_t)((n + wide - 1) / wide); }, s_wide[1]);
+        const bool whole_parts = parts.all * units <= a.workers;
+        const int start_cost = whole_parts ? 0 : (int)min(average >> 2, (int64_t)kPageStart);
+        const Prefix line = whole_parts ? parts : sum_of([&](int n) { return (int64_t)(n > 0 ? n + start_cost : 0); }, s_wide[2]);
+        const int64_t total = line.all * units;
+        const int64_t share = whole_parts ? 1 : (max((total + a.workers - 1) / a.workers, (int64_t)kPageShare) + 1) & ~(int64_t)1;
+        const int64_t from = w * share, mine_all = min(share, total - from);
+        auto length = [&](int n) { return whole_parts ? (n + wide - 1) / wide : n > 0 ? n + start_cost : 0; };   // of a unit on the line
         for (int j = w; j < n_groups; j += a.workers)   // groups that see nothing are nobody's share
             if (group_items(a, j) == 0)
                 for (int e = t; e < a.group * a.heads * (HD / 8); e += 256) {
@@ -634,77 +655,113 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                     page_store<T, 8>(a, j * a.group + r / a.heads, r % a.heads, e % (HD / 8) * 8, zero);
                 }
         PageRecord* record = (PageRecord*)a.records + w;
-        if (start >= total) {
+        if (from >= total) {
             if (t == 0) *record = {-1, 0, 0, 0};
             return;
         }
-        if (before * units <= start && start < (before + sum) * units) {
-            int j = first;
-            int64_t off = start - before * units;
+        if (line.before * units <= from && from < (line.before + line.own) * units) {
+            int j = g0;
+            int64_t off = from - line.before * units;
             while (true) {
-                const int64_t n = (int64_t)group_items(a, j) * units;
+                const int64_t n = (int64_t)length(group_items(a, j)) * units;
                 if (off < n) break;
                 off -= n;
                 ++j;
             }
-            s_scan[0] = j;
+            s_scan = j;
             s_off = off;
         }
         __syncthreads();
-        int j = uniform(s_scan[0]), count = uniform(group_items(a, j));
+        int j = uniform(s_scan), count = uniform(group_items(a, j));
         const int64_t off = uniform(s_off);
-        int hb = (int)(off / count), i0 = (int)(off % count);
-        int64_t left = mine_all;
         PageRecord mine = {-1, 0, 0, 0};
-        while (true) {
-            const int i1 = (int)min((int64_t)count, i0 + left);
-            const bool whole = i0 == 0 && i1 == count;
-            float* part = a.part + ((size_t)w * 2 + (i0 == 0)) * ROWS * (HD + 4);
-            if (i0 == 0 && i1 < count) mine = {j, hb, (int)((start + (mine_all - left) + count - 1) / share), 0};
-            piece(j, hb, i0, i1, whole, part);
-            left -= i1 - i0;
-            if (left <= 0) break;
-            i0 = 0;
-            if (++hb == units) {
-                hb = 0;
-                do count = uniform(group_items(a, ++j));
-                while (count == 0);
+        if (whole_parts) {
+            const int n = length(count), hb = (int)(off / n), k = (int)(off % n);
+            const int i0 = (int)((int64_t)count * k / n), i1 = (int)((int64_t)count * (k + 1) / n);
+            if (k == 0 && n > 1) mine = {j, hb, w + n - 1, 0};
+            piece(j, hb, i0, i1, n == 1, a.part + ((size_t)w * 2 + (k == 0)) * ROWS * (HD + 4));
+        } else {
+            int hb = (int)(off / length(count)), v0 = (int)(off % length(count));
+            int64_t left = mine_all;
+            while (true) {
+                const int v1 = (int)min((int64_t)length(count), v0 + left), i0 = max(v0 - start_cost, 0), i1 = max(v1 - start_cost, 0);
+                if (i0 < i1) {
+                    const bool whole = i0 == 0 && i1 == count;
+                    if (i0 == 0 && i1 < count) mine = {j, hb, (int)((from + (mine_all - left) - v0 + length(count) - 1) / share), 0};
+                    piece(j, hb, i0, i1, whole, a.part + ((size_t)w * 2 + (i0 == 0)) * ROWS * (HD + 4));
+                }
+                left -= v1 - v0;
+                if (left <= 0) break;
+                v0 = 0;
+                if (++hb == units) {
+                    hb = 0;
+                    do count = uniform(group_items(a, ++j));
+                    while (count == 0);
+                }
             }
         }
         if (t == 0) *record = mine;
     }
 }
 
-// Adds up the parts of the unit that worker blockIdx.x begins and others go on with: its own, kept second, and theirs, kept first.
+// Adds up the parts of the unit that worker blockIdx.x begins and others go on with: its own, kept second, and theirs, kept first.  A workgroup takes as
+// many rows as it has groups of HD / 4 lanes; with fewer rows the groups share out a row's parts.  Loads of four parts at a time: the time is that of
+// their latencies.
 template <int HD, typename T, int QT>
 __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
 {
     constexpr int LPG = HD / 4, GROUPS = 256 / LPG, ROWS = 16 * QT;
+    __shared__ float s_m[GROUPS], s_l[GROUPS];
+    __shared__ float4 s_x[GROUPS][LPG];
     const int w = blockIdx.x;
     const PageRecord rec = ((const PageRecord*)a.records)[w];
     if (rec.j < 0) return;
-    const int group = threadIdx.x / LPG, e = threadIdx.x % LPG;
-    const int n_kv = a.p.n_kv, G = a.heads / n_kv, rb = rec.hb / n_kv, h = rec.hb - rb * n_kv, r0 = rb * ROWS, n_rows = min(a.group * G - r0, ROWS);
-    for (int r = group; r < n_rows; r += GROUPS) {
-        float m = kLowest, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int k = w; k <= rec.last; ++k) {
-            const float* q = a.part + (((size_t)k * 2 + (k == w)) * ROWS + r) * (HD + 4);
-            const float4 y = *(const float4*)(q + 4 * e);
-            const float2 ml = *(const float2*)(q + HD);
-            const float m_new = fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - m_new), f_k = __builtin_amdgcn_exp2f(ml.x - m_new);
-            m = m_new;
-            l = l * f + ml.y * f_k;
-            x[0] = x[0] * f + y.x * f_k;
-            x[1] = x[1] * f + y.y * f_k;
-            x[2] = x[2] * f + y.z * f_k;
-            x[3] = x[3] * f + y.w * f_k;
-        }
-        const float inv = l != 0.f ? 1.f / l : 0.f;
+    const int group = threadIdx.x / LPG, e = threadIdx.x % LPG, first = blockIdx.y * GROUPS;
+    const int n_kv = a.p.n_kv, G = a.heads / n_kv, rb = rec.hb / n_kv, h = rec.hb - rb * n_kv, r0 = rb * ROWS;
+    const int n_rows = min(min(a.group * G - r0, ROWS) - first, GROUPS);
+    if (n_rows <= 0) return;
+    int sharers = 1;
+    while (2 * sharers * n_rows <= GROUPS) sharers *= 2;
+    const int r = first + group / sharers, turn = group % sharers, n = rec.last - w + 1;
+    const bool there = group / sharers < n_rows;
+    float m = kLowest, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
+    auto add = [&](float m_k, float l_k, const float4& y) {
+        const float m_new = fmaxf(m, m_k), f = __builtin_amdgcn_exp2f(m - m_new), f_k = __builtin_amdgcn_exp2f(m_k - m_new);
+        m = m_new;
+        l = l * f + l_k * f_k;
+        x[0] = x[0] * f + y.x * f_k;
+        x[1] = x[1] * f + y.y * f_k;
+        x[2] = x[2] * f + y.z * f_k;
+        x[3] = x[3] * f + y.w * f_k;
+    };
+    if (there)
+        for (int k = turn; k < n; k += 4 * sharers) {
+            float4 y[4];
+            float2 ml[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] *= inv;
-        const int b = (r0 + r) / G;
-        page_store<T, 4>(a, rec.j * a.group + b, h * G + r0 + r - b * G, 4 * e, x);
+            for (int i = 0; i < 4; ++i) {
+                const int part = min(k + i * sharers, n - 1);
+                const float* q = a.part + (((size_t)(w + part) * 2 + (part == 0)) * ROWS + r) * (HD + 4);
+                y[i] = *(const float4*)(q + 4 * e);
+                ml[i] = *(const float2*)(q + HD);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k + i * sharers < n) add(ml[i].x, ml[i].y, y[i]);
+        }
+    s_x[group][e] = make_float4(x[0], x[1], x[2], x[3]);
+    if (e == 0) {
+        s_m[group] = m;
+        s_l[group] = l;
     }
+    __syncthreads();
+    if (!there || turn > 0) return;
+    for (int k = 1; k < sharers; ++k) add(s_m[group + k], s_l[group + k], s_x[group + k][e]);
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] *= inv;
+    const int b = (r0 + r) / G;
+    page_store<T, 4>(a, rec.j * a.group + b, h * G + r0 + r - b * G, 4 * e, x);
 }
 
 // ------------------------------------------------------------------------------------------ fork
@@ -959,7 +1016,7 @@ void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s
             k_attention_pages<HD, T, C, QT, false><<<dim3(a.p.n_kv * a.row_blocks, a.n / a.group), 256, 0, s>>>(a);
         } else {
             k_attention_pages<HD, T, C, QT, true><<<a.workers, 256, 0, s>>>(a);
-            k_page_join<HD, T, QT><<<a.workers, 256, 0, s>>>(a);
+            k_page_join<HD, T, QT><<<dim3(a.workers, 16 * QT * HD / 1024), 256, 0, s>>>(a);
         }
     };
     with_types(a.p.hd, token, a.p.dtype, [&](auto dim, auto t, auto e) {

@@ -226,7 +226,7 @@ constexpr int tree_chunks(int len, int chunk, int most)
 
 // Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles; workers that share out the items of all
 // units (0: a workgroup a unit).  A share has at least kPageShare items of 16 slots.
-constexpr int kPageShare = 8, kPageWholeSlots = 512;
+constexpr int kPageShare = 8, kPageStart = 10, kPageWholeSlots = 512;
 struct PagePlan {
     int tiles, row_blocks, workers;
 };
