@@ -208,6 +208,7 @@ int check_page_attention(int32_t n_heads, int32_t n_kv_heads, int32_t n, int32_t
     if (n > 65535) return fail(SS_EINVAL, "more than 65535 rows");
     if (group < 1 || group > SS_PAGES_MAX_GROUP) return fail(SS_EINVAL, "group must be 1 to %d", SS_PAGES_MAX_GROUP);
     if (n % group) return fail(SS_EINVAL, "%d rows are no whole groups of %d", n, group);
+    if ((int64_t)n / group * n_kv_heads * (((int64_t)group * (n_heads / n_kv_heads) + 15) / 16) > 1 << 22) return fail(SS_EINVAL, "too many rows and heads");
     return SS_OK;
 }
 
@@ -384,7 +385,7 @@ extern "C" int ss_attention_pages_workspace(int32_t n_heads, int32_t n_kv_heads,
     if (!is_page_size(page_slots)) return fail(SS_EINVAL, "page_slots must be 16, 32, 64, 128 or 256");
     if (stride < 0 || (int64_t)stride * page_slots > INT_MAX - 1024) return fail(SS_EINVAL, "rows of negative length or of more than 2^31 positions");
     if (int rc = check_page_attention(n_heads, n_kv_heads, n, max_length, group)) return rc;
-    *bytes = ss::page_space(plan_of_pages(n_heads, n_kv_heads, head_dim, n, max_length, group), n, group, head_dim, page_slots, stride).bytes;
+    *bytes = ss::page_space(plan_of_pages(n_heads, n_kv_heads, head_dim, n, max_length, group), n, group, n_kv_heads, head_dim, page_slots, stride).bytes;
     return SS_OK;
 }
 
@@ -405,11 +406,12 @@ extern "C" int ss_attention_pages(const ss_pages* pages, const ss_page_table* ta
     if (!rows && n > table->n_rows) return fail(SS_EINVAL, "the table has fewer than %d rows", n);
     if (n == 0) return SS_OK;
     const ss::PagePlan p = plan_of_pages(n_heads, pages->n_kv_heads, pages->head_dim, n, max_length, group);
-    const ss::PageSpace space = ss::page_space(p, n, group, pages->head_dim, table->page_slots, table->stride);
+    const ss::PageSpace space = ss::page_space(p, n, group, pages->n_kv_heads, pages->head_dim, table->page_slots, table->stride);
     if (int rc = check_workspace(workspace, workspace_bytes, space.bytes)) return rc;
     ss::PageAttentionArgs a{};
     a.tiles = p.tiles;
     a.row_blocks = p.row_blocks;
+    a.parts = p.parts;
     a.workers = p.workers;
     a.part = (float*)workspace;
     a.records = (char*)workspace + space.records;

@@ -152,9 +152,9 @@ struct Scan {
 // whole in memory, so nothing is clamped; scores of slots that a row does not see are set to -inf.  Values of such slots meet weights of 0: in 8 bits
 // they are finite whatever lies there (the scale is left out), in 16 bits an infinity or NaN shows in the sums, and the piece is done again,
 // slot by slot (k_attention_pages' `careful`).
-// With long rows the items of all units lie in one row and every worker (as many as the chip holds at once) takes an equal share of it, whatever
-// the rows' lengths: of the units that it meets the whole ones are finished, of the first and last a part is kept, and k_page_join adds up the parts of
-// units that several workers share.  Short rows: a workgroup a unit, no join.
+// Who takes what (page_plan): short rows a workgroup a unit; one long row, or few that are not very long, a workgroup one of `parts` equal parts of a unit; else
+// (DEALT) units are cut into parts of about the same number of items, so many that the chip goes through several rounds of them, whatever the rows'
+// lengths: equal parts take unlike times (54 to 97 us where there was one for each place on the chip).  k_page_join adds up the parts of units.
 struct PageItem {
     int page, p0;
     unsigned mask;   // rows of the group
@@ -247,17 +247,78 @@ __device__ __forceinline__ int64_t uniform(int64_t x)
     return (int64_t)((uint64_t)(uint32_t)uniform((int)x) | (uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32);
 }
 
-// A worker's record: the unit that it begins and does not end (j < 0: none), and the worker that does.
-struct PageRecord {
-    int j, hb, last, pad;
-};
+__device__ __forceinline__ int64_t lane_value(int64_t x, int l)
+{
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, l) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32);
+}
 
-// Of a thread: what its groups are on a line of all groups, and what is before them; the whole line.
-struct Prefix {
-    int64_t before, own, all;
-};
+// Sum over the lanes up to each (DPP controls: rows shifted by 1, 2, 4 and 8, then row ends to the rows behind).
+template <int C, int R>
+__device__ __forceinline__ int from_before(int x) { return __builtin_amdgcn_update_dpp(0, x, C, R, 0xf, false); }
+template <int C, int R>
+__device__ __forceinline__ int64_t from_before(int64_t x)
+{
+    return (int64_t)((uint64_t)(uint32_t)from_before<C, R>((int)x) | (uint64_t)(uint32_t)from_before<C, R>((int)(x >> 32)) << 32);
+}
+template <typename I>
+__device__ __forceinline__ I wave_prefix(I x)
+{
+    x += from_before<0x111, 0xf>(x);
+    x += from_before<0x112, 0xf>(x);
+    x += from_before<0x114, 0xf>(x);
+    x += from_before<0x118, 0xf>(x);
+    x += from_before<0x142, 0xa>(x);
+    x += from_before<0x143, 0xc>(x);
+    return x;
+}
 
-constexpr int kItemsAtOnce = 512;
+// Parts of a unit of `count` items, and where the k-th of n begins.
+__device__ __forceinline__ int page_parts(int count, int most) { return max(min(most, (count + kPageShare - 1) / kPageShare), 1); }
+__device__ __forceinline__ int page_cut(int count, int k, int n) { return (int)((uint32_t)count / (uint32_t)n) * k + (int)((uint32_t)count % (uint32_t)n * (uint32_t)k / (uint32_t)n); }
+
+// What a workgroup of k_attention_pages gets where the groups' counts decide: the k-th of n parts of unit hb of group j (j < 0: nothing).  All parts of all
+// units in a row, a unit cut into equal parts of at most `wide` items; every wave finds its place by itself, a lane a group (or some), so that there is
+// nothing to wait for.
+struct PageShare {
+    int j, hb, k, n, count, wide;
+};
+__device__ __forceinline__ PageShare page_share(const PageAttentionArgs& a, int units, int n_groups)
+{
+    const int lane = threadIdx.x & 63, per = (n_groups + 63) / 64, g0 = min(lane * per, n_groups), g1 = min(g0 + per, n_groups);
+    const int only = per == 1 && g0 < g1 ? group_items(a, g0) : 0;
+    auto items_of = [&](int j) { return per == 1 ? only : group_items(a, j); };   // of a lane's own group
+    int64_t sum = 0;
+    for (int j = g0; j < g1; ++j) sum += items_of(j);
+    const int64_t all = lane_value(wave_prefix(sum), 63) * units;
+    // (a division of 64 bits takes microseconds)
+    const int64_t wide64 = all < 1 << 30 ? ((uint32_t)all + (uint32_t)a.workers - 1) / (uint32_t)a.workers : (all + a.workers - 1) / a.workers;
+    PageShare s{-1, 0, 0, 0, 0, uniform((int)min(max(wide64, (int64_t)kPageShare), (int64_t)1 << 28))};
+    auto parts_of = [&](int n) { return (int)((uint32_t)(n + s.wide - 1) / (uint32_t)s.wide); };
+    int parts = 0;   // no more than a.workers / units and one a group
+    for (int j = g0; j < g1; ++j) parts += parts_of(items_of(j));
+    const int upto = wave_prefix(parts);
+    const int64_t from = (int64_t)(upto - parts) * units;
+    const bool here = (int)blockIdx.x >= from && (int)blockIdx.x < from + (int64_t)parts * units;
+    const uint64_t whose = __ballot(here);
+    if (!whose) return s;
+    int my_j = g0, my_n = 0, my_parts = 0, off = (int)(blockIdx.x - from);
+    if (here)
+        while (true) {
+            my_n = items_of(my_j);
+            my_parts = parts_of(my_n);
+            if (off < my_parts * units) break;
+            off -= my_parts * units;
+            ++my_j;
+        }
+    const int owner = __ffsll((unsigned long long)whose) - 1;
+    s.j = __builtin_amdgcn_readlane(my_j, owner);
+    s.count = __builtin_amdgcn_readlane(my_n, owner);
+    s.n = __builtin_amdgcn_readlane(my_parts, owner);
+    off = __builtin_amdgcn_readlane(off, owner);
+    s.hb = uniform((int)((uint32_t)off / (uint32_t)s.n));
+    s.k = off - s.hb * s.n;
+    return s;
+}
 
 template <int HD, typename T, typename C, int QT, bool DEALT>
 __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attention_pages(PageAttentionArgs a)
@@ -271,10 +332,8 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
     constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
     constexpr bool PAIRS = I8 && std::is_same<T, _Float16>::value && QT == 1;   // weights as sums of two halves
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
-    __shared__ int s_odd[NW], s_scan;
-    __shared__ int64_t s_wide[3][NW], s_off;
+    __shared__ int s_odd[NW];
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];
-    __shared__ PageItem s_item[kItemsAtOnce];
 
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), ql = lane & 15, g = lane >> 4;
     const int n_kv = a.p.n_kv, G = a.heads / n_kv, units = n_kv * a.row_blocks, n_groups = a.n / a.group, P = a.t.page;
@@ -378,27 +437,41 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
             m_run[u] = kLowest;
             l_run[u] = 0.f;
         }
-        for (int c0 = i0; c0 < i1; c0 += kItemsAtOnce) {
-            const int here = min(i1 - c0, kItemsAtOnce), steps = (here + 1) >> 1;
-            __syncthreads();
-            for (int i = t; i < 2 * steps; i += 256) s_item[i] = i < here ? group_item(a, j, row0, len0, c0 + i) : PageItem{0, 0, 0u, 0};
-            __syncthreads();
-            // places of a step's two items (a wave's: scalar), who sees them
-            auto place = [&](int step, int64_t (&at)[2]) {
+        // A wave takes every fourth step of two items; its lanes hold those of its next 32 steps.
+        const int n_items = i1 - i0, steps = (n_items + 1) >> 1;
+        PageItem held;
+        auto fetch = [&](int step) {
+            const int i = 2 * (step + NW * (lane >> 1)) + (lane & 1);
+            held = PageItem{0, 0, 0u, 0};
+            if (i < n_items) held = group_item(a, j, row0, len0, i0 + i);
+        };
+        int p0[2], full = 0, turn = 0;   // of the step whose operands are under way
+        unsigned mask[2];
+        int64_t at[2];
+        auto place = [&](int step) {
+            if ((turn & 31) == 0) fetch(step);
+            full = 1;
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt) at[kt] = slot_of(uniform(s_item[2 * step + kt].page), uniform(s_item[2 * step + kt].p0));
-            };
-            int64_t at[2];
-            if (wave < steps) {
-                place(wave, at);
-                load_keys(at);
-                load_values(at);
+            for (int kt = 0; kt < 2; ++kt) {
+                const int l = 2 * (turn & 31) + kt;
+                p0[kt] = __builtin_amdgcn_readlane(held.p0, l);
+                mask[kt] = (unsigned)__builtin_amdgcn_readlane((int)held.mask, l);
+                full &= __builtin_amdgcn_readlane(held.full, l);
+                at[kt] = slot_of(__builtin_amdgcn_readlane(held.page, l), p0[kt]);
             }
-            for (int step = wave; step < steps; step += NW) {
+            ++turn;
+        };
+        if (wave < steps) {
+            place(wave);
+            load_keys(at);
+            load_values(at);
+        }
+        for (int step = wave; step < steps; step += NW) {
+            {
                 const bool more = step + NW < steps;
-                if (more) place(step + NW, at);
-                const PageItem it[2] = {s_item[2 * step], s_item[2 * step + 1]};
-                const bool full = uniform(it[0].full & it[1].full);
+                const int it_p0[2] = {p0[0], p0[1]}, all = full;
+                const unsigned it_mask[2] = {mask[0], mask[1]};
+                if (more) place(step + NW);
                 f32x4 s[QT][2];
 #pragma unroll
                 for (int kt = 0; kt < 2; ++kt) {
@@ -439,8 +512,8 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
 #pragma unroll
                             for (int i = 0; i < 4; ++i) s[u][kt][i] *= kq[kt][i];
                         }
-                        if (!full) {
-                            const int seen = it[kt].mask >> bit[u] & 1 ? len[u] - it[kt].p0 - 4 * g : 0;   // of this lane's four slots
+                        if (!all) {
+                            const int seen = it_mask[kt] >> bit[u] & 1 ? len[u] - it_p0[kt] - 4 * g : 0;   // of this lane's four slots
 #pragma unroll
                             for (int i = 0; i < 4; ++i)
                                 if (i >= seen) {
@@ -607,104 +680,26 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
     };
 
     if constexpr (!DEALT) {
-        const int j = blockIdx.y;
-        piece(j, blockIdx.x, 0, group_items(a, j), true, nullptr);
+        const int j = blockIdx.z, hb = blockIdx.x, k = blockIdx.y, count = group_items(a, j), n = page_parts(count, a.parts);
+        if (k >= n) return;
+        piece(j, hb, page_cut(count, k, n), page_cut(count, k + 1, n), n == 1, a.part + (((size_t)j * units + hb) * a.parts + k) * ROWS * (HD + 4));
     } else {
-        // Two ways to share out the items, both found by every worker for itself from the groups' counts, a thread a group (or some):
-        //   whole parts   every unit is cut into equal parts of at most `share` items, and a worker takes one: where all parts have a worker with a share
-        //                 not much above the average
-        //   stretches     all units in a row, and a worker takes the items of its stretch of it, of one unit or several.  A unit that a worker begins
-        //                 costs it a chain of latencies: it counts as `start` items more
-        const int w = blockIdx.x, per = (n_groups + 255) / 256, g0 = min(t * per, n_groups), g1 = min(g0 + per, n_groups);
-        auto sum_of = [&](auto f, int64_t* lds) {   // of all threads' f(j) over their groups; what is before this thread
-            int64_t sum = 0;
-            for (int j = g0; j < g1; ++j) sum += f(group_items(a, j));
-            int64_t before = sum;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int64_t x = __shfl_up(before, d);
-                if (lane >= d) before += x;
+        const int w = blockIdx.x;
+        if (w < n_groups && group_items(a, w) == 0)   // groups that see nothing are nobody's part
+            for (int e = t; e < a.group * a.heads * (HD / 8); e += 256) {
+                const int r = e / (HD / 8);
+                const float zero[8] = {};
+                page_store<T, 8>(a, w * a.group + r / a.heads, r % a.heads, e % (HD / 8) * 8, zero);
             }
-            if (lane == 63) lds[wave] = before;
-            __syncthreads();
-            before -= sum;
-            int64_t total = 0;
-#pragma unroll
-            for (int i = 0; i < NW; ++i) {
-                if (i < wave) before += lds[i];
-                total += lds[i];
-            }
-            return Prefix{before, sum, uniform(total)};
-        };
-        const Prefix items = sum_of([](int n) { return (int64_t)n; }, s_wide[0]);
-        const int64_t average = (items.all * units + a.workers - 1) / a.workers;
-        const int wide = (int)min(max(average + (average >> 3) + kPageStart / 2, (int64_t)kPageShare), (int64_t)1 << 28);
-        const Prefix parts = sum_of([&](int n) { return (int64_t)((n + wide - 1) / wide); }, s_wide[1]);
-        const bool whole_parts = parts.all * units <= a.workers;
-        const int start_cost = whole_parts ? 0 : (int)min(average >> 2, (int64_t)kPageStart);
-        const Prefix line = whole_parts ? parts : sum_of([&](int n) { return (int64_t)(n > 0 ? n + start_cost : 0); }, s_wide[2]);
-        const int64_t total = line.all * units;
-        const int64_t share = whole_parts ? 1 : (max((total + a.workers - 1) / a.workers, (int64_t)kPageShare) + 1) & ~(int64_t)1;
-        const int64_t from = w * share, mine_all = min(share, total - from);
-        auto length = [&](int n) { return whole_parts ? (n + wide - 1) / wide : n > 0 ? n + start_cost : 0; };   // of a unit on the line
-        for (int j = w; j < n_groups; j += a.workers)   // groups that see nothing are nobody's share
-            if (group_items(a, j) == 0)
-                for (int e = t; e < a.group * a.heads * (HD / 8); e += 256) {
-                    const int r = e / (HD / 8);
-                    const float zero[8] = {};
-                    page_store<T, 8>(a, j * a.group + r / a.heads, r % a.heads, e % (HD / 8) * 8, zero);
-                }
-        PageRecord* record = (PageRecord*)a.records + w;
-        if (from >= total) {
-            if (t == 0) *record = {-1, 0, 0, 0};
-            return;
-        }
-        if (line.before * units <= from && from < (line.before + line.own) * units) {
-            int j = g0;
-            int64_t off = from - line.before * units;
-            while (true) {
-                const int64_t n = (int64_t)length(group_items(a, j)) * units;
-                if (off < n) break;
-                off -= n;
-                ++j;
-            }
-            s_scan = j;
-            s_off = off;
-        }
-        __syncthreads();
-        int j = uniform(s_scan), count = uniform(group_items(a, j));
-        const int64_t off = uniform(s_off);
-        PageRecord mine = {-1, 0, 0, 0};
-        if (whole_parts) {
-            const int n = length(count), hb = (int)(off / n), k = (int)(off % n);
-            const int i0 = (int)((int64_t)count * k / n), i1 = (int)((int64_t)count * (k + 1) / n);
-            if (k == 0 && n > 1) mine = {j, hb, w + n - 1, 0};
-            piece(j, hb, i0, i1, n == 1, a.part + ((size_t)w * 2 + (k == 0)) * ROWS * (HD + 4));
-        } else {
-            int hb = (int)(off / length(count)), v0 = (int)(off % length(count));
-            int64_t left = mine_all;
-            while (true) {
-                const int v1 = (int)min((int64_t)length(count), v0 + left), i0 = max(v0 - start_cost, 0), i1 = max(v1 - start_cost, 0);
-                if (i0 < i1) {
-                    const bool whole = i0 == 0 && i1 == count;
-                    if (i0 == 0 && i1 < count) mine = {j, hb, (int)((from + (mine_all - left) - v0 + length(count) - 1) / share), 0};
-                    piece(j, hb, i0, i1, whole, a.part + ((size_t)w * 2 + (i0 == 0)) * ROWS * (HD + 4));
-                }
-                left -= v1 - v0;
-                if (left <= 0) break;
-                v0 = 0;
-                if (++hb == units) {
-                    hb = 0;
-                    do count = uniform(group_items(a, ++j));
-                    while (count == 0);
-                }
-            }
-        }
-        if (t == 0) *record = mine;
+        const PageShare sh = page_share(a, units, n_groups);
+        if (w == 0 && t == 0) *(int32_t*)a.records = sh.wide;
+        if (sh.j < 0) return;
+        if (sh.k == 0 && t == 0) ((int32_t*)a.records)[4 + sh.j * units + sh.hb] = w;
+        piece(sh.j, sh.hb, page_cut(sh.count, sh.k, sh.n), page_cut(sh.count, sh.k + 1, sh.n), sh.n == 1, a.part + (size_t)w * ROWS * (HD + 4));
     }
 }
 
-// Adds up the parts of the unit that worker blockIdx.x begins and others go on with: its own, kept second, and theirs, kept first.  A workgroup takes as
+// Adds up the parts of the blockIdx.x-th unit, which lie behind each other.  A workgroup takes as
 // many rows as it has groups of HD / 4 lanes; with fewer rows the groups share out a row's parts.  Loads of four parts at a time: the time is that of
 // their latencies.
 template <int HD, typename T, int QT>
@@ -713,16 +708,18 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
     constexpr int LPG = HD / 4, GROUPS = 256 / LPG, ROWS = 16 * QT;
     __shared__ float s_m[GROUPS], s_l[GROUPS];
     __shared__ float4 s_x[GROUPS][LPG];
-    const int w = blockIdx.x;
-    const PageRecord rec = ((const PageRecord*)a.records)[w];
-    if (rec.j < 0) return;
+    const int unit = blockIdx.x, n_kv = a.p.n_kv, G = a.heads / n_kv, units = n_kv * a.row_blocks, j = unit / units, hb = unit % units;
+    const int count = group_items(a, j), wide = a.parts > 0 ? 0 : *(const int32_t*)a.records, first_part = a.parts > 0 ? unit * a.parts : ((const int32_t*)a.records)[4 + unit];
+    const int n = a.parts > 0 ? page_parts(count, a.parts) : (int)((uint32_t)(count + wide - 1) / (uint32_t)wide);
+    if (n < 2) return;
     const int group = threadIdx.x / LPG, e = threadIdx.x % LPG, first = blockIdx.y * GROUPS;
-    const int n_kv = a.p.n_kv, G = a.heads / n_kv, rb = rec.hb / n_kv, h = rec.hb - rb * n_kv, r0 = rb * ROWS;
+    const int rb = hb / n_kv, h = hb - rb * n_kv, r0 = rb * ROWS;
+    const float* parts = a.part + (size_t)first_part * ROWS * (HD + 4);
     const int n_rows = min(min(a.group * G - r0, ROWS) - first, GROUPS);
     if (n_rows <= 0) return;
     int sharers = 1;
     while (2 * sharers * n_rows <= GROUPS) sharers *= 2;
-    const int r = first + group / sharers, turn = group % sharers, n = rec.last - w + 1;
+    const int r = first + group / sharers, turn = group % sharers;
     const bool there = group / sharers < n_rows;
     float m = kLowest, l = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
     auto add = [&](float m_k, float l_k, const float4& y) {
@@ -741,7 +738,7 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int part = min(k + i * sharers, n - 1);
-                const float* q = a.part + (((size_t)(w + part) * 2 + (part == 0)) * ROWS + r) * (HD + 4);
+                const float* q = parts + ((size_t)part * ROWS + r) * (HD + 4);
                 y[i] = *(const float4*)(q + 4 * e);
                 ml[i] = *(const float2*)(q + HD);
             }
@@ -761,7 +758,7 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] *= inv;
     const int b = (r0 + r) / G;
-    page_store<T, 4>(a, rec.j * a.group + b, h * G + r0 + r - b * G, 4 * e, x);
+    page_store<T, 4>(a, j * a.group + b, h * G + r0 + r - b * G, 4 * e, x);
 }
 
 // ------------------------------------------------------------------------------------------ fork
@@ -1012,12 +1009,10 @@ void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s
         constexpr int HD = decltype(dim)::value, QT = decltype(tiles)::value;
         typedef decltype(t) T;
         typedef decltype(e) C;
-        if (a.workers == 0) {
-            k_attention_pages<HD, T, C, QT, false><<<dim3(a.p.n_kv * a.row_blocks, a.n / a.group), 256, 0, s>>>(a);
-        } else {
-            k_attention_pages<HD, T, C, QT, true><<<a.workers, 256, 0, s>>>(a);
-            k_page_join<HD, T, QT><<<dim3(a.workers, 16 * QT * HD / 1024), 256, 0, s>>>(a);
-        }
+        const int units = a.p.n_kv * a.row_blocks, groups = a.n / a.group;
+        if (a.parts > 0) k_attention_pages<HD, T, C, QT, false><<<dim3(units, a.parts, groups), 256, 0, s>>>(a);
+        else k_attention_pages<HD, T, C, QT, true><<<a.workers + units * groups, 256, 0, s>>>(a);
+        if (a.parts != 1) k_page_join<HD, T, QT><<<dim3(units * groups, 16 * QT * HD / 1024), 256, 0, s>>>(a);
     };
     with_types(a.p.hd, token, a.p.dtype, [&](auto dim, auto t, auto e) {
         typedef decltype(t) T;

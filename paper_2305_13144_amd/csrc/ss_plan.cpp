@@ -417,20 +417,26 @@ PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_l
     p.tiles = rows <= 16 ? 1 : 2;
     p.row_blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
     p.workers = 0;
-    if (max_length > kPageWholeSlots) {
-        const long long units = std::max(1LL, (long long)(n / group) * n_kv * p.row_blocks), at_once = (p.tiles == 2 ? 2LL : hd == 64 ? 4LL : 3LL) * n_cu;
-        const long long items = (long long)group * ((max_length + 15LL) / 16);   // of a unit, at most
-        p.workers = (int)std::max(1LL, std::min(at_once, (items + kPageShare - 1) / kPageShare * units));
+    p.parts = 1;
+    if (max_length <= kPageWholeSlots) return p;
+    const long long groups = std::max(1, n / group), units = groups * n_kv * p.row_blocks, at_once = (p.tiles == 2 ? 2LL : hd == 64 ? 4LL : 3LL) * n_cu;
+    const long long items = (long long)group * ((max_length + 15LL) / 16);   // of a unit, at most
+    if (groups == 1 || items * units <= at_once * kPageFew) {
+        p.parts = (int)std::max(1LL, std::min(at_once / units, (items + kPageShare - 1) / kPageShare));
+    } else {
+        p.parts = 0;
+        p.workers = (int)at_once * kPageRounds;
     }
     return p;
 }
 
-PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int stride)
+PageSpace page_space(const PagePlan& p, int n, int group, int n_kv, int hd, int page, int stride)
 {
     auto whole = [](size_t b) { return (b + 15) / 16 * 16; };
     PageSpace s;
-    s.records = (size_t)p.workers * 2 * 16 * p.tiles * (hd + 4) * 4;
-    s.counts = s.records + (size_t)p.workers * 16;
+    const size_t units = (size_t)(n / group) * n_kv * p.row_blocks, kept = p.parts == 0 ? p.workers + units : p.parts == 1 ? 0 : units * p.parts;
+    s.records = kept * 16 * p.tiles * (hd + 4) * 4;
+    s.counts = s.records + (p.parts == 0 ? whole((units + 4) * 4) : 0);
     const size_t groups = group > 1 ? n / group : 0;
     s.items = s.counts + whole(groups * 4);
     s.items_stride = (long long)group * stride * (page / 16);

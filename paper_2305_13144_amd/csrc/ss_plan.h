@@ -224,11 +224,12 @@ constexpr int tree_chunks(int len, int chunk, int most)
     return len <= chunk ? 1 : len > (most - 1) * (long long)chunk ? most : (len + chunk - 1) / chunk;
 }
 
-// Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles; workers that share out the items of all
-// units (0: a workgroup a unit).  A share has at least kPageShare items of 16 slots.
-constexpr int kPageShare = 8, kPageStart = 10, kPageWholeSlots = 512;
+// Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles.  parts > 0: a unit's items of 16 slots are cut into
+// so many equal parts, of at least kPageShare items, a workgroup each (1: no join); parts == 0: into parts of one size, that there are about `workers` of,
+// found from the rows' lengths, which costs microseconds first, and is worth it where there are more than kPageFew items for a place on the chip.
+constexpr int kPageShare = 8, kPageRounds = 4, kPageWholeSlots = 512, kPageFew = 24;
 struct PagePlan {
-    int tiles, row_blocks, workers;
+    int tiles, row_blocks, parts, workers;
 };
 PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_length, int n_cu);
 // Its workspace: where its parts begin and how large it is (bytes, all multiples of 16).
@@ -236,7 +237,7 @@ struct PageSpace {
     size_t records, counts, items, bytes;   // the parts of workers begin at 0
     long long items_stride;
 };
-PageSpace page_space(const PagePlan& p, int n, int group, int hd, int page, int stride);
+PageSpace page_space(const PagePlan& p, int n, int group, int n_kv, int hd, int page, int stride);
 
 // Beam search: workgroups that share out a row's logits, so many that all rows together fill the chip, that a wave has a few steps of 1 KiB, and that a
 // group's candidates are no more than kBeamRanked (or a slice a row).  A slice's part of the workspace: reference, sum (fp64), logits, tokens.

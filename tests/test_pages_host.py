@@ -119,6 +119,8 @@ def test_attention_that_does_not_fit_is_refused(lib):
     refused(attend(lib, most=-1), "negative")
     refused(attend(lib, n=65536), "65535")
     refused(attend(lib, n=9, rows=P), "fewer")
+    many = rows(rows=65535, row_stride=2**20)
+    refused(attend(lib, n=65535, rows=P, q=many, out=many, p=pages(n_kv_heads=65), heads=65), "too many")
     refused(attend(lib, t=table(n_rows=7)), "table has fewer")
     refused(attend(lib, out=rows(rows=7)), "fewer")
     refused(attend(lib, out=rows(dtype=ss.SS_BF16)), "type")
