@@ -220,10 +220,10 @@ struct PageAttentionArgs {
     const int32_t* rows;   // [n] rows of the table, or null
     float scale;
     int n, group, heads;
-    int tiles, row_blocks, parts, workers;   // page_plan
+    int tiles, row_blocks, parts, at_once;   // page_plan
     // workspace
-    float* part;           // parts > 1: [units of all groups][parts], parts == 0: [workers + units]; [16 * tiles][hd + 4]: sums, their maximum, their weight
-    void* records;         // parts == 0: a part's greatest number of items, ..., from the fourth on each unit's first part
+    float* part;           // parts > 1: [units of all groups][parts], parts == 0: [page_grid]; [16 * tiles][hd + 4]: sums, their maximum, their weight
+    void* notes;           // parts == 0: PageNotes
     int32_t* item_counts;  // group > 1: [n / group]
     void* items;           //            [n / group][items_stride]: 16 bytes each
     int64_t items_stride;

@@ -412,9 +412,9 @@ extern "C" int ss_attention_pages(const ss_pages* pages, const ss_page_table* ta
     a.tiles = p.tiles;
     a.row_blocks = p.row_blocks;
     a.parts = p.parts;
-    a.workers = p.workers;
+    a.at_once = p.at_once;
     a.part = (float*)workspace;
-    a.records = (char*)workspace + space.records;
+    a.notes = (char*)workspace + space.notes;
     a.item_counts = (int32_t*)((char*)workspace + space.counts);
     a.items = (char*)workspace + space.items;
     a.items_stride = space.items_stride;

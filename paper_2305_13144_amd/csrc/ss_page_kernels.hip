@@ -153,8 +153,7 @@ struct Scan {
 // they are finite whatever lies there (the scale is left out), in 16 bits an infinity or NaN shows in the sums, and the piece is done again,
 // slot by slot (k_attention_pages' `careful`).
 // Who takes what (page_plan): short rows a workgroup a unit; one long row, or few that are not very long, a workgroup one of `parts` equal parts of a unit; else
-// (DEALT) units are cut into parts of about the same number of items, so many that the chip goes through several rounds of them, whatever the rows'
-// lengths: equal parts take unlike times (54 to 97 us where there was one for each place on the chip).  k_page_join adds up the parts of units.
+// (DEALT) units are cut by the rows' lengths (PageCuts).  k_page_join adds up the parts of units.
 struct PageItem {
     int page, p0;
     unsigned mask;   // rows of the group
@@ -276,11 +275,34 @@ __device__ __forceinline__ I wave_prefix(I x)
 __device__ __forceinline__ int page_parts(int count, int most) { return max(min(most, (count + kPageShare - 1) / kPageShare), 1); }
 __device__ __forceinline__ int page_cut(int count, int k, int n) { return (int)((uint32_t)count / (uint32_t)n) * k + (int)((uint32_t)count % (uint32_t)n * (uint32_t)k / (uint32_t)n); }
 
-// What a workgroup of k_attention_pages gets where the groups' counts decide: the k-th of n parts of unit hb of group j (j < 0: nothing).  All parts of all
-// units in a row, a unit cut into equal parts of at most `wide` items; every wave finds its place by itself, a lane a group (or some), so that there is
-// nothing to wait for.
+// How units are cut where the groups' counts decide, the same for all.  Of many items for each of the `at_once` workgroups that the chip holds: large parts
+// of what falls to one of them, as many as fit into the unit, and what is left in one part or two.  All large parts come first, and the small ones
+// fill in as workgroups end, which those of one size do at unlike times (54 to 97 us).  (Equal parts, 64 rows to 8000 slots: half of what falls to
+// one 107 us, a quarter 110; large ones of three quarters, small ones of a fifth 108.)
+// Of few items: one round of equal parts where a width not much above the average allows it, since a part costs microseconds before its first
+// item.  Where more parts would come of it than there are workgroups: equal ones.
+struct PageCuts {
+    int large, small;   // items
+    __device__ __forceinline__ int large_of(int n) const { return large > 0 ? (int)((uint32_t)n / (uint32_t)large) : 0; }
+    __device__ __forceinline__ int small_of(int n) const { return (int)((uint32_t)(n - large_of(n) * large + small - 1) / (uint32_t)small); }
+    // items of the k-th part of n, large ones first: from the first to the last's end
+    __device__ __forceinline__ void part(int n, int k, int* i0, int* i1) const
+    {
+        const int l = large_of(n);
+        *i0 = k * large;
+        *i1 = *i0 + large;
+        if (k < l) return;
+        const int rest = n - l * large, parts = small_of(n);
+        *i0 = l * large + page_cut(rest, k - l, parts);
+        *i1 = l * large + page_cut(rest, k - l + 1, parts);
+    }
+};
+
+// What a workgroup gets: the k-th part of unit hb of group j (j < 0: nothing).  Every wave finds its place by itself, a lane a group (or some), so
+// that there is nothing to wait for.
 struct PageShare {
-    int j, hb, k, n, count, wide;
+    int j, hb, k, count;
+    PageCuts cuts;
 };
 __device__ __forceinline__ PageShare page_share(const PageAttentionArgs& a, int units, int n_groups)
 {
@@ -291,34 +313,75 @@ __device__ __forceinline__ PageShare page_share(const PageAttentionArgs& a, int 
     for (int j = g0; j < g1; ++j) sum += items_of(j);
     const int64_t all = lane_value(wave_prefix(sum), 63) * units;
     // (a division of 64 bits takes microseconds)
-    const int64_t wide64 = all < 1 << 30 ? ((uint32_t)all + (uint32_t)a.workers - 1) / (uint32_t)a.workers : (all + a.workers - 1) / a.workers;
-    PageShare s{-1, 0, 0, 0, 0, uniform((int)min(max(wide64, (int64_t)kPageShare), (int64_t)1 << 28))};
-    auto parts_of = [&](int n) { return (int)((uint32_t)(n + s.wide - 1) / (uint32_t)s.wide); };
-    int parts = 0;   // no more than a.workers / units and one a group
-    for (int j = g0; j < g1; ++j) parts += parts_of(items_of(j));
-    const int upto = wave_prefix(parts);
-    const int64_t from = (int64_t)(upto - parts) * units;
-    const bool here = (int)blockIdx.x >= from && (int)blockIdx.x < from + (int64_t)parts * units;
+    const int64_t average64 = all < 1 << 30 ? ((uint32_t)all + (uint32_t)a.at_once - 1) / (uint32_t)a.at_once : (all + a.at_once - 1) / a.at_once;
+    const int average = uniform((int)min(max(average64, (int64_t)kPageShare), (int64_t)1 << 28));
+    PageShare s{-1, 0, 0, 0, {0, average}};
+    if (average >= kPageMany) {
+        s.cuts.large = average;
+        s.cuts.small = (average + 1) / 2;
+    } else {   // three widths at a time
+        int n0 = 0, n1 = 0, n2 = 0;
+        const int w1 = average + 1 + average / 16, w2 = average + 2 + average / 8;
+        for (int j = g0; j < g1; ++j) {
+            const int n = items_of(j);
+            n0 += (int)((uint32_t)(n + average - 1) / (uint32_t)average);
+            n1 += (int)((uint32_t)(n + w1 - 1) / (uint32_t)w1);
+            n2 += (int)((uint32_t)(n + w2 - 1) / (uint32_t)w2);
+        }
+        auto fits = [&](int n) { return (int64_t)__builtin_amdgcn_readlane(wave_prefix(n), 63) * units <= a.at_once; };
+        if (!fits(n0)) s.cuts.small = fits(n1) ? w1 : fits(n2) ? w2 : average;
+    }
+    // all large parts in a row, then all small ones
+    int large, small, large_upto, small_upto;   // of a lane's groups, a unit of each
+    int64_t all_large;
+    auto count_parts = [&] {
+        large = small = 0;
+        for (int j = g0; j < g1; ++j) {
+            const int n = items_of(j);
+            large += s.cuts.large_of(n);
+            small += s.cuts.small_of(n);
+        }
+        large_upto = wave_prefix(large);
+        small_upto = wave_prefix(small);
+        all_large = (int64_t)__builtin_amdgcn_readlane(large_upto, 63) * units;
+        return all_large + (int64_t)__builtin_amdgcn_readlane(small_upto, 63) * units;
+    };
+    if (count_parts() > gridDim.x) {
+        s.cuts = {0, a.group == 1 ? (average + 1) / 2 : average};
+        count_parts();
+    }
+    const bool is_large = (int)blockIdx.x < all_large;
+    const int64_t from = is_large ? (int64_t)(large_upto - large) * units : all_large + (int64_t)(small_upto - small) * units;
+    int64_t off64 = (int)blockIdx.x - from;
+    const bool here = off64 >= 0 && off64 < (int64_t)(is_large ? large : small) * units;
     const uint64_t whose = __ballot(here);
     if (!whose) return s;
-    int my_j = g0, my_n = 0, my_parts = 0, off = (int)(blockIdx.x - from);
+    int my_j = g0, my_n = 0, off = (int)off64, parts = 0;
     if (here)
         while (true) {
             my_n = items_of(my_j);
-            my_parts = parts_of(my_n);
-            if (off < my_parts * units) break;
-            off -= my_parts * units;
+            parts = is_large ? s.cuts.large_of(my_n) : s.cuts.small_of(my_n);
+            if (off < parts * units) break;
+            off -= parts * units;
             ++my_j;
         }
     const int owner = __ffsll((unsigned long long)whose) - 1;
     s.j = __builtin_amdgcn_readlane(my_j, owner);
     s.count = __builtin_amdgcn_readlane(my_n, owner);
-    s.n = __builtin_amdgcn_readlane(my_parts, owner);
+    parts = __builtin_amdgcn_readlane(parts, owner);
     off = __builtin_amdgcn_readlane(off, owner);
-    s.hb = uniform((int)((uint32_t)off / (uint32_t)s.n));
-    s.k = off - s.hb * s.n;
+    s.hb = uniform((int)((uint32_t)off / (uint32_t)parts));
+    s.k = off - s.hb * parts;
+    if (!is_large) s.k += uniform(s.cuts.large_of(s.count));
     return s;
 }
+
+// Notes for the join: how units are cut, then the first large and the first small part of each unit.
+struct PageNotes {
+    PageCuts cuts;
+    int pad[2];
+    int2 first[1];
+};
 
 template <int HD, typename T, typename C, int QT, bool DEALT>
 __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attention_pages(PageAttentionArgs a)
@@ -692,10 +755,15 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                 page_store<T, 8>(a, w * a.group + r / a.heads, r % a.heads, e % (HD / 8) * 8, zero);
             }
         const PageShare sh = page_share(a, units, n_groups);
-        if (w == 0 && t == 0) *(int32_t*)a.records = sh.wide;
+        PageNotes* notes = (PageNotes*)a.notes;
+        if (w == 0 && t == 0) notes->cuts = sh.cuts;
         if (sh.j < 0) return;
-        if (sh.k == 0 && t == 0) ((int32_t*)a.records)[4 + sh.j * units + sh.hb] = w;
-        piece(sh.j, sh.hb, page_cut(sh.count, sh.k, sh.n), page_cut(sh.count, sh.k + 1, sh.n), sh.n == 1, a.part + (size_t)w * ROWS * (HD + 4));
+        const int large = uniform(sh.cuts.large_of(sh.count)), n = large + uniform(sh.cuts.small_of(sh.count)), unit = sh.j * units + sh.hb;
+        if (sh.k == 0 && large > 0 && t == 0) notes->first[unit].x = w;
+        if (sh.k == large && t == 0) notes->first[unit].y = w;
+        int i0, i1;
+        sh.cuts.part(sh.count, sh.k, &i0, &i1);
+        piece(sh.j, sh.hb, uniform(i0), uniform(i1), n == 1, a.part + (size_t)w * ROWS * (HD + 4));
     }
 }
 
@@ -709,12 +777,19 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
     __shared__ float s_m[GROUPS], s_l[GROUPS];
     __shared__ float4 s_x[GROUPS][LPG];
     const int unit = blockIdx.x, n_kv = a.p.n_kv, G = a.heads / n_kv, units = n_kv * a.row_blocks, j = unit / units, hb = unit % units;
-    const int count = group_items(a, j), wide = a.parts > 0 ? 0 : *(const int32_t*)a.records, first_part = a.parts > 0 ? unit * a.parts : ((const int32_t*)a.records)[4 + unit];
-    const int n = a.parts > 0 ? page_parts(count, a.parts) : (int)((uint32_t)(count + wide - 1) / (uint32_t)wide);
+    const int count = group_items(a, j);
+    const PageNotes* notes = (const PageNotes*)a.notes;
+    int n = page_parts(count, a.parts), large = 0, first_large = 0, first_small = unit * a.parts;
+    if (a.parts == 0) {
+        const PageCuts cuts = notes->cuts;
+        large = cuts.large_of(count);
+        n = large + cuts.small_of(count);
+        first_large = notes->first[unit].x;
+        first_small = notes->first[unit].y;
+    }
     if (n < 2) return;
     const int group = threadIdx.x / LPG, e = threadIdx.x % LPG, first = blockIdx.y * GROUPS;
     const int rb = hb / n_kv, h = hb - rb * n_kv, r0 = rb * ROWS;
-    const float* parts = a.part + (size_t)first_part * ROWS * (HD + 4);
     const int n_rows = min(min(a.group * G - r0, ROWS) - first, GROUPS);
     if (n_rows <= 0) return;
     int sharers = 1;
@@ -738,7 +813,7 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int part = min(k + i * sharers, n - 1);
-                const float* q = parts + ((size_t)part * ROWS + r) * (HD + 4);
+                const float* q = a.part + ((size_t)(part < large ? first_large + part : first_small + part - large) * ROWS + r) * (HD + 4);
                 y[i] = *(const float4*)(q + 4 * e);
                 ml[i] = *(const float2*)(q + HD);
             }
@@ -1011,7 +1086,7 @@ void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s
         typedef decltype(e) C;
         const int units = a.p.n_kv * a.row_blocks, groups = a.n / a.group;
         if (a.parts > 0) k_attention_pages<HD, T, C, QT, false><<<dim3(units, a.parts, groups), 256, 0, s>>>(a);
-        else k_attention_pages<HD, T, C, QT, true><<<a.workers + units * groups, 256, 0, s>>>(a);
+        else k_attention_pages<HD, T, C, QT, true><<<page_grid(a.at_once, units * groups, a.group), 256, 0, s>>>(a);
         if (a.parts != 1) k_page_join<HD, T, QT><<<dim3(units * groups, 16 * QT * HD / 1024), 256, 0, s>>>(a);
     };
     with_types(a.p.hd, token, a.p.dtype, [&](auto dim, auto t, auto e) {

@@ -416,17 +416,14 @@ PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_l
     const long long rows = (long long)group * heads_each;
     p.tiles = rows <= 16 ? 1 : 2;
     p.row_blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-    p.workers = 0;
     p.parts = 1;
+    p.at_once = (p.tiles == 2 ? 2 : hd == 64 ? 4 : 3) * n_cu;
     if (max_length <= kPageWholeSlots) return p;
-    const long long groups = std::max(1, n / group), units = groups * n_kv * p.row_blocks, at_once = (p.tiles == 2 ? 2LL : hd == 64 ? 4LL : 3LL) * n_cu;
+    const long long groups = std::max(1, n / group), units = groups * n_kv * p.row_blocks;
     const long long items = (long long)group * ((max_length + 15LL) / 16);   // of a unit, at most
-    if (groups == 1 || items * units <= at_once * kPageFew) {
-        p.parts = (int)std::max(1LL, std::min(at_once / units, (items + kPageShare - 1) / kPageShare));
-    } else {
-        p.parts = 0;
-        p.workers = (int)at_once * kPageRounds;
-    }
+    p.parts = 0;
+    if (groups == 1 || items * units <= (long long)p.at_once * kPageFew)
+        p.parts = (int)std::max(1LL, std::min(p.at_once / units, (items + kPageShare - 1) / kPageShare));
     return p;
 }
 
@@ -434,9 +431,9 @@ PageSpace page_space(const PagePlan& p, int n, int group, int n_kv, int hd, int 
 {
     auto whole = [](size_t b) { return (b + 15) / 16 * 16; };
     PageSpace s;
-    const size_t units = (size_t)(n / group) * n_kv * p.row_blocks, kept = p.parts == 0 ? p.workers + units : p.parts == 1 ? 0 : units * p.parts;
-    s.records = kept * 16 * p.tiles * (hd + 4) * 4;
-    s.counts = s.records + (p.parts == 0 ? whole((units + 4) * 4) : 0);
+    const size_t units = (size_t)(n / group) * n_kv * p.row_blocks, kept = p.parts == 0 ? (size_t)page_grid(p.at_once, units, group) : p.parts == 1 ? 0 : units * p.parts;
+    s.notes = kept * 16 * p.tiles * (hd + 4) * 4;
+    s.counts = s.notes + (p.parts == 0 ? whole(16 + units * 8) : 0);
     const size_t groups = group > 1 ? n / group : 0;
     s.items = s.counts + whole(groups * 4);
     s.items_stride = (long long)group * stride * (page / 16);

@@ -225,16 +225,18 @@ constexpr int tree_chunks(int len, int chunk, int most)
 }
 
 // Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles.  parts > 0: a unit's items of 16 slots are cut into
-// so many equal parts, of at least kPageShare items, a workgroup each (1: no join); parts == 0: into parts of one size, that there are about `workers` of,
-// found from the rows' lengths, which costs microseconds first, and is worth it where there are more than kPageFew items for a place on the chip.
-constexpr int kPageShare = 8, kPageRounds = 4, kPageWholeSlots = 512, kPageFew = 24;
+// so many equal parts, of at least kPageShare items, a workgroup each (1: no join); parts == 0: the rows' lengths decide (PageCuts), which costs microseconds
+// first, and is worth it where there may be more than kPageFew items for each of the at_once workgroups that the chip holds.
+constexpr int kPageShare = 8, kPageWholeSlots = 512, kPageFew = 24, kPageMany = 64;
 struct PagePlan {
-    int tiles, row_blocks, parts, workers;
+    int tiles, row_blocks, parts, at_once;
 };
+// Workgroups that are enough however the units are cut (a workgroup that gets nothing has found that out first: 2 us for every round of them).
+constexpr long long page_grid(int at_once, long long units, int group) { return (group == 1 ? 2LL : 1LL) * at_once + units; }
 PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_length, int n_cu);
 // Its workspace: where its parts begin and how large it is (bytes, all multiples of 16).
 struct PageSpace {
-    size_t records, counts, items, bytes;   // the parts of workers begin at 0
+    size_t notes, counts, items, bytes;   // the parts begin at 0
     long long items_stride;
 };
 PageSpace page_space(const PagePlan& p, int n, int group, int n_kv, int hd, int page, int stride);
