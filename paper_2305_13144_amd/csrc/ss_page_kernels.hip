@@ -894,6 +894,43 @@ __global__ __launch_bounds__(256) void k_pages_inherit(ForkArgs a)
 
 constexpr int kForkThreads = 1024, kForkPages = 4096;   // pages of a workgroup
 
+// Counts, over all n entries of a list (16-byte aligned), those that f takes: this thread's four of the kForkPages from `first` on, its
+// share of those before `first`, and of all.  Four loads at a time.
+struct Counts {
+    int mine, ahead, every;
+};
+template <typename F>
+__device__ __forceinline__ Counts count_pages(const int32_t* list, int n, int first, F f)
+{
+    Counts c{0, 0, 0};
+    constexpr int AT_ONCE = 4;
+    for (int p0 = 0; p0 < n; p0 += AT_ONCE * kForkPages) {
+        int x[AT_ONCE][4];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int p = p0 + u * kForkPages + 4 * (int)threadIdx.x;
+            if (p + 3 < n) {
+                const int4 v = *(const int4*)(list + p);
+                x[u][0] = v.x, x[u][1] = v.y, x[u][2] = v.z, x[u][3] = v.w;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[u][k] = p + k < n ? list[p + k] : 0;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int at = p0 + u * kForkPages, p = at + 4 * (int)threadIdx.x;
+            int here = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) here += p + k < n && f(x[u][k], p + k);
+            c.every += here;
+            if (at < first) c.ahead += here;
+            if (at == first) c.mine = here;
+        }
+    }
+    return c;
+}
+
 __global__ __launch_bounds__(kForkThreads) void k_pages_hand_out(ForkArgs a)
 {
     extern __shared__ int s_start[];   // [rows + 1] first of each row's pages among those handed out
@@ -911,21 +948,9 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_hand_out(ForkArgs a)
         if (i < rows) s_start[i] = total + s.before;
         total += s.all;
     }
-    int mine = 0, ahead = 0, every = 0;   // free pages of this thread (4 neighbours), before this workgroup, at all
-    for (int p0 = 0; p0 < n; p0 += kForkPages) {
-        int free_here = 0;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int p = p0 + 4 * t + k;
-            free_here += p < n && a.claim[p] == kFree;
-        }
-        if (p0 == first) mine = free_here;
-        if (p0 < first) ahead += free_here;
-        every += free_here;
-    }
-    every = Scan<kForkThreads>(every, s_scan).all;
-    ahead = Scan<kForkThreads>(ahead, s_scan).all;
-    int rank = ahead + Scan<kForkThreads>(mine, s_scan).before;
+    const Counts c = count_pages(a.claim, n, first, [](int x, int) { return x == kFree; });
+    const int every = Scan<kForkThreads>(c.every, s_scan).all, ahead = Scan<kForkThreads>(c.ahead, s_scan).all;
+    int rank = ahead + Scan<kForkThreads>(c.mine, s_scan).before;
     __syncthreads();
     auto give = [&](int rank, int page) {   // the rank-th page that is needed
         int lo = 0, hi = rows - 1;          // the last row whose first is not behind it
@@ -951,6 +976,86 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_hand_out(ForkArgs a)
     if (t == 0) *a.missing = max(total - every, 0);
 }
 
+// The same in one workgroup, with the claims in LDS: where rows and pages are few the three launches are most of the time.
+constexpr int kFewRowsOfTable = 1024, kFewPages = 16384, kFewEntries = 32768;   // of one workgroup
+template <typename A>
+__device__ __forceinline__ int entry_row(int e, const A& t) { return (int)((uint32_t)e / (uint32_t)t.stride); }
+
+__global__ __launch_bounds__(kForkThreads) void k_pages_fork_few(ForkArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) int s_claim[];   // [n_pages, in whole fours of a thread]
+    __shared__ int s_start[kFewRowsOfTable], s_parent[kFewRowsOfTable], s_held[kFewRowsOfTable], s_last[kFewRowsOfTable], s_source[kFewRowsOfTable];
+    __shared__ int s_scan[kForkThreads / 64 + 1];
+    const int rows = a.to.rows, n = a.to.n_pages, t = threadIdx.x, per = (n + 4 * kForkThreads - 1) / (4 * kForkThreads) * 4;
+    int wanted = 0;
+    if (t < rows) {
+        const Fork f(a, t);
+        s_parent[t] = f.parent;
+        s_held[t] = f.held;
+        s_last[t] = f.last;
+        s_source[t] = -1;
+        wanted = f.wanted - f.held;
+        a.to.lengths[t] = f.new_len;
+        a.src[t] = a.dst[t] = -1;
+    }
+    for (int p = t; p < per * kForkThreads; p += kForkThreads) s_claim[p] = p >= n || (a.held && a.held[p]) ? -1 : kFree;
+    __syncthreads();
+    constexpr int AT_ONCE = 4;
+    const int entries = rows * a.to.stride;
+    for (int e0 = t; e0 < entries; e0 += AT_ONCE * kForkThreads) {
+        int row[AT_ONCE], entry[AT_ONCE], page[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            const int e = min(e0 + u * kForkThreads, entries - 1);
+            row[u] = entry_row(e, a.to);
+            entry[u] = e - row[u] * a.to.stride;
+            page[u] = -1;
+            if (entry[u] < s_held[row[u]]) page[u] = a.from.pages[(int64_t)s_parent[row[u]] * a.from.stride + entry[u]];
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+            if (e0 + u * kForkThreads >= entries) break;
+            const bool there = is_page(a.from, page[u]), last = entry[u] == s_last[row[u]];
+            if (there) atomicMin(&s_claim[page[u]], last ? row[u] : -1);
+            if (there && last) s_source[row[u]] = page[u];
+            a.to.pages[e0 + u * kForkThreads] = there ? page[u] : -1;
+        }
+    }
+    __syncthreads();   // which also has the entries written before some of them are written again
+    const bool copies = t < rows && s_source[t] >= 0 && s_claim[s_source[t]] != t;
+    const Scan<kForkThreads> need(t < rows ? wanted + copies : 0, s_scan);
+    if (t < rows) {
+        s_start[t] = need.before;
+        if (!copies) s_source[t] = -1;
+    }
+    const int4* mine = (const int4*)(s_claim + t * per);
+    int free_here = 0;
+    for (int k = 0; k < per / 4; ++k) free_here += (mine[k].x == kFree) + (mine[k].y == kFree) + (mine[k].z == kFree) + (mine[k].w == kFree);
+    const Scan<kForkThreads> free_pages(free_here, s_scan);
+    __syncthreads();
+    auto give = [&](int rank, int page) {   // as in k_pages_hand_out
+        int lo = 0, hi = rows - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (s_start[mid] <= rank) lo = mid;
+            else hi = mid - 1;
+        }
+        const int shared = s_source[lo], k = rank - s_start[lo] - (shared >= 0);
+        a.to.pages[(int64_t)lo * a.to.stride + (k < 0 ? s_last[lo] : s_held[lo] + k)] = page;
+        if (k < 0 && page >= 0) {
+            a.src[lo] = shared;
+            a.dst[lo] = page;
+        }
+    };
+    if (free_here > 0 && free_pages.before < need.all) {
+        int rank = free_pages.before;
+        for (int k = 0; k < per && rank < need.all; ++k)
+            if (s_claim[t * per + k] == kFree) give(rank++, t * per + k);
+    }
+    for (int k = free_pages.all + t; k < need.all; k += kForkThreads) give(k, -1);
+    if (t == 0) *a.missing = max(need.all - free_pages.all, 0);
+}
+
 // ------------------------------------------------------------------------------------------ compact
 __global__ __launch_bounds__(256) void k_pages_unused(int32_t* __restrict__ used, const uint8_t* __restrict__ held, int n)
 {
@@ -972,23 +1077,12 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_rank(CompactArgs a)
 {
     __shared__ int s_scan[kForkThreads / 64 + 1];
     const int n = a.from.n_pages, t = threadIdx.x, first = blockIdx.x * kForkPages;
-    int mine = 0, ahead = 0, every = 0, below = 0;
-    for (int p0 = 0; p0 < n; p0 += kForkPages) {
-        int here = 0;
-        for (int k = 0; k < 4; ++k) {
-            const int p = p0 + 4 * t + k;
-            here += p < n && a.used[p];
-        }
-        if (p0 == first) mine = here;
-        if (p0 < first) ahead += here;
-        every += here;
-    }
-    every = Scan<kForkThreads>(every, s_scan).all;
-    ahead = Scan<kForkThreads>(ahead, s_scan).all;
-    for (int p = t; p < every; p += kForkThreads) below += a.used[p] != 0;
-    below = Scan<kForkThreads>(below, s_scan).all;      // pages in use that keep their numbers
+    const Counts c = count_pages(a.used, n, first, [](int x, int) { return x != 0; });
+    const int every = Scan<kForkThreads>(c.every, s_scan).all, ahead = Scan<kForkThreads>(c.ahead, s_scan).all;
+    // pages in use that keep their numbers
+    const int below = Scan<kForkThreads>(count_pages(a.used, every, 0, [](int x, int) { return x != 0; }).every, s_scan).all;
     const int moves = every - below;
-    int used_before = ahead + Scan<kForkThreads>(mine, s_scan).before;
+    int used_before = ahead + Scan<kForkThreads>(c.mine, s_scan).before;
     for (int k = 0; k < 4; ++k) {
         const int p = first + 4 * t + k;
         if (p >= n) break;
@@ -1031,8 +1125,89 @@ __global__ __launch_bounds__(256) void k_pages_renumber(CompactArgs a)
     if (threadIdx.x == 0) a.to.lengths[i] = len;
 }
 
+// The same in one workgroup, as k_pages_fork_few.
+__global__ __launch_bounds__(kForkThreads) void k_pages_compact_few(CompactArgs a)
+{
+    extern __shared__ __attribute__((aligned(16))) int s_place[];   // [n_pages, in whole fours of a thread]: in use or not, then the new number
+    __shared__ int s_hole[kFewPages / 2], s_len[kFewRowsOfTable], s_scan[kForkThreads / 64 + 1];
+    const int rows = a.from.rows, n = a.from.n_pages, t = threadIdx.x, per = (n + 4 * kForkThreads - 1) / (4 * kForkThreads) * 4;
+    if (t < rows) {
+        s_len[t] = row_length(a.from, t);
+        a.to.lengths[t] = s_len[t];
+    }
+    for (int p = t; p < per * kForkThreads; p += kForkThreads) s_place[p] = p < n && a.held && a.held[p];
+    __syncthreads();
+    constexpr int AT_ONCE = 4;
+    const int entries = rows * a.from.stride;
+    auto page_at = [&](int e) {
+        const int row = entry_row(e, a.from);
+        if ((e - row * a.from.stride) * a.from.page >= s_len[row]) return -1;
+        const int p = a.from.pages[e];
+        return is_page(a.from, p) ? p : -1;
+    };
+    auto every = [&](auto f) {   // f(entry, page), some loads at a time
+        for (int e0 = t; e0 < entries; e0 += AT_ONCE * kForkThreads) {
+            int page[AT_ONCE];
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) page[u] = page_at(min(e0 + u * kForkThreads, entries - 1));
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (e0 + u * kForkThreads < entries) f(e0 + u * kForkThreads, page[u]);
+        }
+    };
+    every([&](int, int p) {
+        if (p >= 0) s_place[p] = 1;
+    });
+    __syncthreads();
+    const int first = t * per;
+    int used_here = 0;
+    for (int k = 0; k < per; k += 4) {
+        const int4 x = *(const int4*)(s_place + first + k);
+        used_here += (x.x + x.y) + (x.z + x.w);
+    }
+    const Scan<kForkThreads> used(used_here, s_scan);
+    int below_here = 0;   // pages in use that keep their numbers
+    for (int k = 0; k < per && first + k < used.all; ++k) below_here += s_place[first + k];
+    const Scan<kForkThreads> below(below_here, s_scan);
+    const int moves = used.all - below.all;
+    int before = used.before;
+    for (int k = 0; k < per && first + k < used.all; ++k) {
+        const int p = first + k;
+        if (s_place[p]) ++before;
+        else {
+            s_hole[p - before] = p;
+            a.dst[p - before] = p;
+        }
+    }
+    __syncthreads();
+    before = used.before;
+    for (int k = 0; k < per && first + k < n; ++k) {
+        const int p = first + k;
+        int to = -1;
+        if (s_place[p]) {
+            to = p;
+            if (p >= used.all) {
+                const int rank = before - below.all;
+                to = s_hole[rank];
+                a.src[rank] = p;
+            }
+            ++before;
+        }
+        s_place[p] = to;
+        if (p >= moves && p < n / 2) a.src[p] = a.dst[p] = -1;
+    }
+    if (t == 0) {
+        a.counts[0] = used.all;
+        a.counts[1] = moves;
+    }
+    __syncthreads();
+    every([&](int e, int p) { a.to.pages[e] = p >= 0 ? s_place[p] : -1; });
+    if (a.place)
+        for (int p = t; p < n; p += kForkThreads) a.place[p] = s_place[p];
+}
+
 // ------------------------------------------------------------------------------------------ copies
-constexpr int kCopyLayers = 32;   // of a launch
+constexpr int kCopyLayers = 32, kCopyPairs = 2048;   // of a launch
 struct CopyArgs {
     void* p[kCopyLayers][2];
     float* scale[kCopyLayers][2];
@@ -1041,17 +1216,29 @@ struct CopyArgs {
     int64_t bytes, scale_bytes;   // of a page
 };
 
+// A workgroup takes a piece of kCopyPiece bytes of a page's keys or values (the first one the scales too) in one layer, of every gridDim.x-th pair.  All
+// loads of a piece are issued before its first store.  Bound by the bytes: rows that get copies of the same page are neighbours, so its second reader
+// finds it in a cache, and what is written goes past them (512 rows and 24 layers 67 us, 1.7 GB of a compaction 325; reads past the caches too 77, 320; written
+// into them 70, 349).
+constexpr int kCopyAtOnce = 4, kCopyPiece = kCopyAtOnce * 256 * 16;
 __global__ __launch_bounds__(256) void k_pages_copy(CopyArgs a)
 {
     const int layer = blockIdx.y >> 1, which = blockIdx.y & 1;
     const int n = a.count ? min(a.n, *a.count) : a.n;
+    const int64_t k0 = (int64_t)blockIdx.z * kCopyPiece + threadIdx.x * 16;
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
         const int s = a.src[i], d = a.dst[i];
         if (s < 0 || s >= a.n_pages || d < 0 || d >= a.n_pages || s == d) continue;
         const char* from = (const char*)a.p[layer][which] + s * a.bytes;
         char* to = (char*)a.p[layer][which] + d * a.bytes;
-        for (int64_t k = threadIdx.x * 16; k < a.bytes; k += 256 * 16) *(u32x4*)(to + k) = *(const u32x4*)(from + k);
-        if (!a.scale_bytes) continue;
+        u32x4 x[kCopyAtOnce];
+#pragma unroll
+        for (int u = 0; u < kCopyAtOnce; ++u)
+            if (k0 + u * 4096 < a.bytes) x[u] = *(const u32x4*)(from + k0 + u * 4096);
+#pragma unroll
+        for (int u = 0; u < kCopyAtOnce; ++u)
+            if (k0 + u * 4096 < a.bytes) __builtin_nontemporal_store(x[u], (u32x4*)(to + k0 + u * 4096));
+        if (!a.scale_bytes || blockIdx.z > 0) continue;
         from = (const char*)a.scale[layer][which] + s * a.scale_bytes;
         to = (char*)a.scale[layer][which] + d * a.scale_bytes;
         for (int64_t k = threadIdx.x * 16; k < a.scale_bytes; k += 256 * 16) *(u32x4*)(to + k) = *(const u32x4*)(from + k);
@@ -1099,9 +1286,16 @@ void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s
     });
 }
 
+// Whether one workgroup does it: what its 1024 threads take one after another costs more than two or three launches from some number of pages or entries on.
+static bool pages_few(int n_pages, int rows, int stride) { return rows <= kFewRowsOfTable && n_pages <= kFewPages && (int64_t)rows * stride <= kFewEntries; }
+
 void launch_pages_fork(const ForkArgs& a, hipStream_t s)
 {
     const int n = a.to.n_pages;
+    if (pages_few(n, a.to.rows, a.to.stride)) {
+        k_pages_fork_few<<<1, kForkThreads, (size_t)(n + 4 * kForkThreads - 1) / (4 * kForkThreads) * (16 * kForkThreads), s>>>(a);
+        return;
+    }
     k_pages_claims<<<(n + 255) / 256, 256, 0, s>>>(a.claim, a.held, n);
     k_pages_inherit<<<a.to.rows, 256, 0, s>>>(a);
     k_pages_hand_out<<<(n + kForkPages - 1) / kForkPages, kForkThreads, (size_t)(a.to.rows + 1) * 4, s>>>(a);
@@ -1110,6 +1304,10 @@ void launch_pages_fork(const ForkArgs& a, hipStream_t s)
 void launch_pages_compact(const CompactArgs& a, hipStream_t s)
 {
     const int n = a.from.n_pages;
+    if (pages_few(n, a.from.rows, a.from.stride)) {
+        k_pages_compact_few<<<1, kForkThreads, (size_t)(n + 4 * kForkThreads - 1) / (4 * kForkThreads) * (16 * kForkThreads), s>>>(a);
+        return;
+    }
     k_pages_unused<<<(n + 255) / 256, 256, 0, s>>>(a.used, a.held, n);
     if (a.from.rows > 0) k_pages_mark<<<a.from.rows, 256, 0, s>>>(a);
     k_pages_rank<<<(n + kForkPages - 1) / kForkPages, kForkThreads, 0, s>>>(a);
@@ -1136,7 +1334,7 @@ void launch_pages_copy(const PagesView* layers, int n_layers, const int32_t* src
         a.count = count;
         a.n = n;
         a.n_pages = p.n_pages;
-        k_pages_copy<<<dim3(n < 2048 ? n : 2048, 2 * here), 256, 0, s>>>(a);
+        k_pages_copy<<<dim3(n < kCopyPairs ? n : kCopyPairs, 2 * here, (unsigned)((a.bytes + kCopyPiece - 1) / kCopyPiece)), 256, 0, s>>>(a);
     }
 }
 

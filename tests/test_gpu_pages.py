@@ -385,7 +385,7 @@ def test_what_a_fork_does():
     check_fork([[1, 1]], [20], 16, 5, 3, [0])                                      # the same page twice
 
 
-@pytest.mark.parametrize("n_pages,n", [(40000, 700), (5000, 3000), (4096, 1), (4097, 1025), (100003, 50)])
+@pytest.mark.parametrize("n_pages,n", [(40000, 700), (5000, 3000), (4096, 1), (4097, 1025), (100003, 50), (16384, 1024), (16385, 1000), (16383, 900)])
 def test_large_forks(n_pages, n):
     r = np.random.default_rng(n)
     table, lengths = random_table(r, 200, 20, 16, n_pages)
@@ -436,6 +436,9 @@ def test_dense_empty_and_large_pools():
     r = np.random.default_rng(1)
     check_compact(*random_table(r, 300, 60, 16, 50001), 16, 50001)
     check_compact(*random_table(r, 30, 60, 16, 4096), 16, 4096)
+    for n in (16383, 16384, 16385):
+        check_compact(*random_table(r, 500, 60, 16, n), 16, n)
+        check_compact(*random_table(r, 700, 20, 16, n), 16, n, in_place=True)
 
 
 # ------------------------------------------------------------------------------------------------ copies
