@@ -271,33 +271,6 @@ __device__ __forceinline__ I wave_prefix(I x)
     return x;
 }
 
-// Parts of a unit of `count` items, and where the k-th of n begins.
-__device__ __forceinline__ int page_parts(int count, int most) { return max(min(most, (count + kPageShare - 1) / kPageShare), 1); }
-__device__ __forceinline__ int page_cut(int count, int k, int n) { return (int)((uint32_t)count / (uint32_t)n) * k + (int)((uint32_t)count % (uint32_t)n * (uint32_t)k / (uint32_t)n); }
-
-// How units are cut where the groups' counts decide, the same for all.  Of many items for each of the `at_once` workgroups that the chip holds: large parts
-// of what falls to one of them, as many as fit into the unit, and what is left in one part or two.  All large parts come first, and the small ones
-// fill in as workgroups end, which those of one size do at unlike times (54 to 97 us).  (Equal parts, 64 rows to 8000 slots: half of what falls to
-// one 107 us, a quarter 110; large ones of three quarters, small ones of a fifth 108.)
-// Of few items: one round of equal parts where a width not much above the average allows it, since a part costs microseconds before its first
-// item.  Where more parts would come of it than there are workgroups: equal ones.
-struct PageCuts {
-    int large, small;   // items
-    __device__ __forceinline__ int large_of(int n) const { return large > 0 ? (int)((uint32_t)n / (uint32_t)large) : 0; }
-    __device__ __forceinline__ int small_of(int n) const { return (int)((uint32_t)(n - large_of(n) * large + small - 1) / (uint32_t)small); }
-    // items of the k-th part of n, large ones first: from the first to the last's end
-    __device__ __forceinline__ void part(int n, int k, int* i0, int* i1) const
-    {
-        const int l = large_of(n);
-        *i0 = k * large;
-        *i1 = *i0 + large;
-        if (k < l) return;
-        const int rest = n - l * large, parts = small_of(n);
-        *i0 = l * large + page_cut(rest, k - l, parts);
-        *i1 = l * large + page_cut(rest, k - l + 1, parts);
-    }
-};
-
 // What a workgroup gets: the k-th part of unit hb of group j (j < 0: nothing).  Every wave finds its place by itself, a lane a group (or some), so
 // that there is nothing to wait for.
 struct PageShare {
@@ -317,19 +290,18 @@ __device__ __forceinline__ PageShare page_share(const PageAttentionArgs& a, int 
     const int average = uniform((int)min(max(average64, (int64_t)kPageShare), (int64_t)1 << 28));
     PageShare s{-1, 0, 0, 0, {0, average}};
     if (average >= kPageMany) {
-        s.cuts.large = average;
-        s.cuts.small = (average + 1) / 2;
-    } else {   // three widths at a time
-        int n0 = 0, n1 = 0, n2 = 0;
-        const int w1 = average + 1 + average / 16, w2 = average + 2 + average / 8;
+        s.cuts = page_large_cuts(average);
+    } else {   // three widths at a time; with the widest there is a place for every part, as a unit has one that is not whole
+        const int all_units = n_groups * units, places = all_units < a.at_once / 4 * 3 ? a.at_once - all_units : a.at_once;
+        const int w2 = uniform((int)(((uint32_t)all + (uint32_t)places - 1) / (uint32_t)places)), w1 = (average + w2) / 2;   // all < 64 * at_once
+        int n0 = 0, n1 = 0;
         for (int j = g0; j < g1; ++j) {
             const int n = items_of(j);
             n0 += (int)((uint32_t)(n + average - 1) / (uint32_t)average);
             n1 += (int)((uint32_t)(n + w1 - 1) / (uint32_t)w1);
-            n2 += (int)((uint32_t)(n + w2 - 1) / (uint32_t)w2);
         }
         auto fits = [&](int n) { return (int64_t)__builtin_amdgcn_readlane(wave_prefix(n), 63) * units <= a.at_once; };
-        if (!fits(n0)) s.cuts.small = fits(n1) ? w1 : fits(n2) ? w2 : average;
+        if (!fits(n0)) s.cuts.small = fits(n1) ? w1 : max(w2, average);
     }
     // all large parts in a row, then all small ones
     int large, small, large_upto, small_upto;   // of a lane's groups, a unit of each
@@ -347,7 +319,7 @@ __device__ __forceinline__ PageShare page_share(const PageAttentionArgs& a, int 
         return all_large + (int64_t)__builtin_amdgcn_readlane(small_upto, 63) * units;
     };
     if (count_parts() > gridDim.x) {
-        s.cuts = {0, a.group == 1 ? (average + 1) / 2 : average};
+        s.cuts = page_least_cuts(average, a.group);
         count_parts();
     }
     const bool is_large = (int)blockIdx.x < all_large;
@@ -977,7 +949,7 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_hand_out(ForkArgs a)
 }
 
 // The same in one workgroup, with the claims in LDS: where rows and pages are few the three launches are most of the time.
-constexpr int kFewRowsOfTable = 1024, kFewPages = 16384, kFewEntries = 32768;   // of one workgroup
+constexpr int kFewRowsOfTable = 1024, kFewPages = 16384;   // of one workgroup
 template <typename A>
 __device__ __forceinline__ int entry_row(int e, const A& t) { return (int)((uint32_t)e / (uint32_t)t.stride); }
 
@@ -1129,7 +1101,7 @@ __global__ __launch_bounds__(256) void k_pages_renumber(CompactArgs a)
 __global__ __launch_bounds__(kForkThreads) void k_pages_compact_few(CompactArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) int s_place[];   // [n_pages, in whole fours of a thread]: in use or not, then the new number
-    __shared__ int s_hole[kFewPages / 2], s_len[kFewRowsOfTable], s_scan[kForkThreads / 64 + 1];
+    __shared__ int s_hole[kFewPages / 4], s_len[kFewRowsOfTable], s_scan[kForkThreads / 64 + 1];
     const int rows = a.from.rows, n = a.from.n_pages, t = threadIdx.x, per = (n + 4 * kForkThreads - 1) / (4 * kForkThreads) * 4;
     if (t < rows) {
         s_len[t] = row_length(a.from, t);
@@ -1286,13 +1258,19 @@ void launch_attention_pages(const PageAttentionArgs& a, int token, hipStream_t s
     });
 }
 
-// Whether one workgroup does it: what its 1024 threads take one after another costs more than two or three launches from some number of pages or entries on.
-static bool pages_few(int n_pages, int rows, int stride) { return rows <= kFewRowsOfTable && n_pages <= kFewPages && (int64_t)rows * stride <= kFewEntries; }
+// Whether one workgroup does it: what its 1024 threads take one after another costs more than two or three launches from some number of entries on.  Three
+// launches / one (us, with a copy of 5 behind them, graphs): forks of 32 rows of 110 entries 16.7 / 10.0, 20 of 950 15.3 / 11.4, 512 of 50 19.7 / 17.0, 256 of 133
+// 17.8 / 22.8, 1024 of 50 22.4 / 27.9.  Compactions, which go through the entries twice, 24 rows of 60 15.2 / 9.7, 64 of 150 18.3 / 16.2, 200 of 65 19.3 /
+// 19.5, 20 of 950 and 12000 pages 25.4 / 33.7.
+static bool pages_few(int n_pages, int rows, int stride, int most_pages, int most_entries)
+{
+    return rows <= kFewRowsOfTable && n_pages <= most_pages && (int64_t)rows * stride <= most_entries;
+}
 
 void launch_pages_fork(const ForkArgs& a, hipStream_t s)
 {
     const int n = a.to.n_pages;
-    if (pages_few(n, a.to.rows, a.to.stride)) {
+    if (pages_few(n, a.to.rows, a.to.stride, kFewPages, 28000)) {
         k_pages_fork_few<<<1, kForkThreads, (size_t)(n + 4 * kForkThreads - 1) / (4 * kForkThreads) * (16 * kForkThreads), s>>>(a);
         return;
     }
@@ -1304,7 +1282,7 @@ void launch_pages_fork(const ForkArgs& a, hipStream_t s)
 void launch_pages_compact(const CompactArgs& a, hipStream_t s)
 {
     const int n = a.from.n_pages;
-    if (pages_few(n, a.from.rows, a.from.stride)) {
+    if (pages_few(n, a.from.rows, a.from.stride, kFewPages / 2, 12000)) {
         k_pages_compact_few<<<1, kForkThreads, (size_t)(n + 4 * kForkThreads - 1) / (4 * kForkThreads) * (16 * kForkThreads), s>>>(a);
         return;
     }

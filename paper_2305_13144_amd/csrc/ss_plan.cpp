@@ -416,14 +416,13 @@ PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_l
     const long long rows = (long long)group * heads_each;
     p.tiles = rows <= 16 ? 1 : 2;
     p.row_blocks = (int)((rows + 16 * p.tiles - 1) / (16 * p.tiles));
-    p.parts = 1;
     p.at_once = (p.tiles == 2 ? 2 : hd == 64 ? 4 : 3) * n_cu;
-    if (max_length <= kPageWholeSlots) return p;
     const long long groups = std::max(1, n / group), units = groups * n_kv * p.row_blocks;
-    const long long items = (long long)group * ((max_length + 15LL) / 16);   // of a unit, at most
+    const long long items = (max_length + 15LL) / 16;   // of a unit's longest row: rows of a group may share all they have
+    p.parts = 1;
+    if (items <= kPageWhole || (2 * units >= p.at_once && items <= std::max(1LL, units / p.at_once) * kPageWholeOfMany)) return p;
     p.parts = 0;
-    if (groups == 1 || items * units <= (long long)p.at_once * kPageFew)
-        p.parts = (int)std::max(1LL, std::min(p.at_once / units, (items + kPageShare - 1) / kPageShare));
+    if (groups == 1 || items * units <= (long long)p.at_once * kPageFew) p.parts = (int)std::max(1LL, std::min(p.at_once / units, items * group / kPageShare));
     return p;
 }
 

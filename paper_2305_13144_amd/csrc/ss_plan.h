@@ -224,14 +224,45 @@ constexpr int tree_chunks(int len, int chunk, int most)
     return len <= chunk ? 1 : len > (most - 1) * (long long)chunk ? most : (len + chunk - 1) / chunk;
 }
 
-// Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles.  parts > 0: a unit's items of 16 slots are cut into
-// so many equal parts, of at least kPageShare items, a workgroup each (1: no join); parts == 0: the rows' lengths decide (PageCuts), which costs microseconds
-// first, and is worth it where there may be more than kPageFew items for each of the at_once workgroups that the chip holds.
-constexpr int kPageShare = 8, kPageWholeSlots = 512, kPageFew = 24, kPageMany = 64;
+// Attention over pages (k_attention_pages): query rows of a unit go to workgroups in blocks of 16 * tiles.  parts == 1: a workgroup a unit, no join; parts > 1:
+// a unit's items of 16 slots are cut into so many equal parts, of at least kPageShare items, a workgroup each; parts == 0: the rows' lengths decide (PageCuts),
+// which costs microseconds first.  Measured (32 heads of 128 in 8 bits, rows up to the length named, most much shorter; us, graphs):
+//   a workgroup a unit / parts     1 row of 450 slots, 8 heads of keys 10.1 / 9.5, 32 13.5 / 11.1; 16 rows 13.1 / 11.9; of 250 slots the same
+//   a workgroup a unit / PageCuts  512 units, 850 slots 24.3 / 28.3, 1550 34.1 / 31.8 and 31.9 / 39.5, 8000 150 / 100; 2048 units, 450 slots 39 / 51, 1550 87 / 97
+//   parts / PageCuts               4 rows of 4000 slots and 8 heads of keys 15.0 / 17.7, 32 25.8 / 27.0; 8 rows of 4000 and 32 heads of keys 43 / 36, 16 of 8000 159 / 115;
+//                                  8 beams of 2 prompts of 1600 slots 23.3 / 24.3, of 16 prompts of 4000 51 / 48
+constexpr int kPageShare = 8, kPageWhole = 16, kPageWholeOfMany = 100, kPageFew = 48, kPageMany = 64;
 struct PagePlan {
     int tiles, row_blocks, parts, at_once;
 };
-// Workgroups that are enough however the units are cut (a workgroup that gets nothing has found that out first: 2 us for every round of them).
+// Equal parts of a unit of `count` items, of at least kPageShare: how many, at most `most`, and where the k-th of n begins.
+constexpr int page_parts(int count, int most)
+{
+    const int n = count / kPageShare;
+    return n < 1 || most < 1 ? 1 : n < most ? n : most;
+}
+constexpr int page_cut(int count, int k, int n) { return (int)((uint32_t)count / (uint32_t)n) * k + (int)((uint32_t)count % (uint32_t)n * (uint32_t)k / (uint32_t)n); }
+// How units are cut where the groups' counts decide, the same for all.  Of many items for each of the `at_once` workgroups that the chip holds: large parts
+// of what falls to one of them, as many as fit into the unit, and what is left in one part or two.  All large parts come first, and the small ones
+// fill in as workgroups end, which those of one size do at unlike times (54 to 97 us).  (Equal parts, 64 rows to 8000 slots: half of what falls to
+// one 107 us, a quarter 110; large ones of three quarters, small ones of a fifth 108.)
+// Of few items: one round of equal parts where a width not much above the average allows it, since a part costs microseconds before its first
+// item.  Where more parts would come of it than there are workgroups: equal ones.
+struct PageCuts {
+    int large, small;   // items
+    constexpr int large_of(int n) const { return large > 0 ? (int)((uint32_t)n / (uint32_t)large) : 0; }
+    constexpr int small_of(int n) const { return (int)(((uint32_t)(n - large_of(n) * large) + (uint32_t)small - 1) / (uint32_t)small); }
+    // items of the k-th part of n, large ones first: from the first to the last's end
+    constexpr void part(int n, int k, int* i0, int* i1) const
+    {
+        const int l = large_of(n), rest = n - l * large, parts = small_of(n);
+        *i0 = k < l ? k * large : l * large + page_cut(rest, k - l, parts);
+        *i1 = k < l ? *i0 + large : l * large + page_cut(rest, k - l + 1, parts);
+    }
+};
+constexpr PageCuts page_large_cuts(int average) { return {average, (average + 1) / 2}; }
+constexpr PageCuts page_least_cuts(int average, int group) { return {0, group == 1 ? (average + 1) / 2 : average}; }
+// Workgroups that are enough for page_least_cuts (one that gets nothing has found that out first: 2 us for every round of them).
 constexpr long long page_grid(int at_once, long long units, int group) { return (group == 1 ? 2LL : 1LL) * at_once + units; }
 PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_length, int n_cu);
 // Its workspace: where its parts begin and how large it is (bytes, all multiples of 16).

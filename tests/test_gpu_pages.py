@@ -8,7 +8,7 @@ import pytest
 import torch
 
 from paper_2305_13144_amd import binding as ss
-from test_gpu_operators import BF16, F16, I8, assert_attention, codes_of, gen, i32, randn
+from test_gpu_operators import BF16, F16, I8, assert_attention, codes_of, gen, half_step, i32, randn
 
 pytestmark = pytest.mark.gpu
 
@@ -214,6 +214,35 @@ def test_entries_that_are_no_page_are_not_seen(group, dtype, held):
     assert not ss.ss_attention_pages(q, pages, table_of([[-1, -1], [5], [], [-7]], [32, 16, 0, -9], 2, 16, 3), 32, group).any()
 
 
+@pytest.mark.parametrize("dtype,held", TYPES)
+@pytest.mark.parametrize("n,kv,each,dim,top,group", [(150, 16, 1, 64, 9000, 1), (60, 8, 4, 128, 16000, 1), (40, 12, 20, 64, 12000, 1), (64, 16, 2, 64, 9000, 4)])
+def test_many_long_rows_of_unlike_length(dtype, held, n, kv, each, dim, top, group):
+    """So much that units are cut into large parts and small ones.  Rows take their pages from a small pool, which rows of a table may share."""
+    r = np.random.default_rng(n)
+    page, n_pages = 64, 300
+    pages, (k, v) = pool_of(n, n_pages, page, kv, dim, held)
+    lengths = [int(top * x ** 2) for x in r.random(n)]
+    lengths[3], lengths[7], lengths[n - 1] = top, 0, 1
+    stride = -(-top // page)
+    table = r.integers(0, n_pages, (n, stride)).astype(np.int32)
+    if group > 1:
+        for i in range(n):
+            if i % group:
+                table[i, :stride // 2] = table[i - 1, :stride // 2]
+    q = randn(gen(1), n, kv * each, dim, dtype=dtype)
+    tb = ss.PageTable(torch.tensor(table, device="cuda"), i32(lengths), page, n_pages)
+    got = ss.ss_attention_pages(q, pages, tb, top, group)
+    assert torch.equal(got, ss.ss_attention_pages(q, pages, tb, top, group)) and not got[7].any()
+    for i in [i for i in (1, 3, n // 2, n - 1) if lengths[i]]:
+        m = torch.tensor(table[i], device="cuda").long()
+        kk, vv = (x[m].permute(1, 0, 2, 3).reshape(kv, -1, dim)[:, :lengths[i]] for x in (k, v))
+        for h in (0, kv - 1):
+            assert_attention(got[i, h * each:(h + 1) * each], q[i, h * each:(h + 1) * each], kk[h], vv[h],
+                             torch.ones(each, lengths[i], dtype=torch.bool, device="cuda"), dim ** -0.5, F16 if held == I8 else held)
+    few = ss.ss_attention_pages(q, pages, tb, 1, group)          # a workgroup a unit: other sums, the same results but for roundings
+    assert ((few.double() - got.double()).abs() <= 4 * half_step(dtype) * (got.double().abs() + v.abs().max() * 0.1)).all()
+
+
 def test_rows_chosen_by_a_list_and_results_with_strides():
     check_attention(11, [100, 37, 250, 1], 32, 2, 2, 128, F16, I8, pick=[2, 0, -1, 2, 4, 3, 2**31 - 1], out="wide")
     check_attention(12, [100, 37, 250, 1], 32, 2, 2, 64, BF16, BF16, group=2, pick=[2, 0, 1, 3, -5, 2], out="wide")
@@ -385,7 +414,7 @@ def test_what_a_fork_does():
     check_fork([[1, 1]], [20], 16, 5, 3, [0])                                      # the same page twice
 
 
-@pytest.mark.parametrize("n_pages,n", [(40000, 700), (5000, 3000), (4096, 1), (4097, 1025), (100003, 50), (16384, 1024), (16385, 1000), (16383, 900)])
+@pytest.mark.parametrize("n_pages,n", [(40000, 700), (5000, 3000), (4096, 1), (4097, 1025), (100003, 50), (16384, 1024), (16385, 1000), (16383, 900), (16384, 1000)])
 def test_large_forks(n_pages, n):
     r = np.random.default_rng(n)
     table, lengths = random_table(r, 200, 20, 16, n_pages)
@@ -436,9 +465,9 @@ def test_dense_empty_and_large_pools():
     r = np.random.default_rng(1)
     check_compact(*random_table(r, 300, 60, 16, 50001), 16, 50001)
     check_compact(*random_table(r, 30, 60, 16, 4096), 16, 4096)
-    for n in (16383, 16384, 16385):
-        check_compact(*random_table(r, 500, 60, 16, n), 16, n)
-        check_compact(*random_table(r, 700, 20, 16, n), 16, n, in_place=True)
+    for n in (8191, 8192, 8193, 16384):
+        check_compact(*random_table(r, 200, 60, 16, n), 16, n)
+        check_compact(*random_table(r, 500, 20, 16, n), 16, n, in_place=True)
 
 
 # ------------------------------------------------------------------------------------------------ copies
