@@ -853,7 +853,8 @@ def ss_pages_copy(layers: Sequence[Pages], src, dst, count=None, stream: Optiona
     n, i32 = src.numel(), t.int32
     structs = (ss_pages * len(layers))(*[x.struct for x in layers])
     _check(_lib.ss_pages_copy(structs, len(layers), _table(src, "src", index, n, i32), _table(dst, "dst", index, n, i32), _count(n, "the number of pairs"),
-                              _table(count, "count", index, 1, i32), _on(stream, index, src, dst, count, *(y for x in layers for y in x.tensors))))
+                              _table(count, "count", index, 1, i32),
+                              _stream(index) if stream is None else _on(stream, index, src, dst, count, *(y for x in layers for y in x.tensors))))
 
 
 class Beams(NamedTuple):

@@ -671,22 +671,24 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
         __syncthreads();
         // wave i takes elements ET * (4g + i) .. of every row: ET neighbours per lane
         const int e0 = ET * (4 * g + wave);
+        float x[QT][ET];
 #pragma unroll
-        for (int u = 0; u < QT; ++u) {
-            const int r = u * 16 + ql, b = (r0 + r) / G;
-            float x[ET];
+        for (int u = 0; u < QT; ++u)
 #pragma unroll
             for (int e = 0; e < ET; ++e) {
-                x[e] = 0.f;
+                x[u][e] = 0.f;
 #pragma unroll
-                for (int w = 0; w < NW; ++w) x[e] += s_o[w][u][wave][lane][e];
+                for (int w = 0; w < NW; ++w) x[u][e] += s_o[w][u][wave][lane][e];
             }
-            if (r >= n_rows) continue;
-            if (careful) {   // rare: infinite or NaN values, or slots that hold them and are not seen: these sums slot by slot, relative to the same maximum
+        if (careful) {   // rare: infinite or NaN values, or slots that hold them and are not seen: these sums slot by slot, relative to the same maximum
+            const float flip = a.scale < 0.f ? -1.f : 1.f;
 #pragma unroll
-                for (int e = 0; e < ET; ++e) x[e] = 0.f;
-                const float flip = a.scale < 0.f ? -1.f : 1.f;
-                const T* qp = (const T*)a.q.p + (int64_t)(j * a.group + b) * a.q.row + (int64_t)(h * G + r0 + r - b * G) * a.q.head;
+            for (int u = 0; u < QT; ++u) {
+#pragma unroll
+                for (int e = 0; e < ET; ++e) x[u][e] = 0.f;
+                const int r = r0 + u * 16 + ql;
+                if (u * 16 + ql >= n_rows) continue;
+                const T* qp = (const T*)a.q.p + (int64_t)(j * a.group + bit[u]) * a.q.row + (int64_t)(h * G + r - bit[u] * G) * a.q.head;
                 for (int i = i0; i < i1; ++i) {
                     const PageItem one = group_item(a, j, row0, len0, i);
                     const int seen = one.mask >> bit[u] & 1 ? min(len[u] - one.p0, 16) : 0;
@@ -696,20 +698,26 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                         for (int e = 0; e < HD; ++e) score = fmaf((float)qp[e] * flip, (float)((const C*)K)[at + e], score);
                         const float p = __builtin_amdgcn_exp2f((score - m_all[u]) * sc[u]);
 #pragma unroll
-                        for (int e = 0; e < ET; ++e) x[e] = fmaf(p, (float)((const C*)V)[at + e0 + e], x[e]);
+                        for (int e = 0; e < ET; ++e) x[u][e] = fmaf(p, (float)((const C*)V)[at + e0 + e], x[u][e]);
                     }
                 }
             }
+            __syncthreads();   // the results may take the queries' place
+        }
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            const int r = u * 16 + ql;
+            if (r >= n_rows) continue;
             if (!whole) {
                 float* to = part + (size_t)r * (HD + 4);
 #pragma unroll
-                for (int e = 0; e < ET; e += 4) *(float4*)(to + e0 + e) = make_float4(x[e], x[e + 1], x[e + 2], x[e + 3]);
+                for (int e = 0; e < ET; e += 4) *(float4*)(to + e0 + e) = make_float4(x[u][e], x[u][e + 1], x[u][e + 2], x[u][e + 3]);
                 if (wave == 0 && g == 0) *(float2*)(to + HD) = make_float2(part_top(m_all[u] * sc[u]), l_all[u]);
             } else {
                 const float inv = l_all[u] != 0.f ? 1.f / l_all[u] : 0.f;   // a row that sees nothing gets zeros
 #pragma unroll
-                for (int e = 0; e < ET; ++e) x[e] *= inv;
-                page_store<T, ET>(a, j * a.group + b, h * G + r0 + r - b * G, e0, x);
+                for (int e = 0; e < ET; ++e) x[u][e] *= inv;
+                page_store<T, ET>(a, j * a.group + bit[u], h * G + r0 + r - bit[u] * G, e0, x[u]);
             }
         }
     };
@@ -1275,7 +1283,7 @@ void launch_pages_fork(const ForkArgs& a, hipStream_t s)
         return;
     }
     k_pages_claims<<<(n + 255) / 256, 256, 0, s>>>(a.claim, a.held, n);
-    k_pages_inherit<<<a.to.rows, 256, 0, s>>>(a);
+    if (a.to.rows > 0) k_pages_inherit<<<a.to.rows, 256, 0, s>>>(a);
     k_pages_hand_out<<<(n + kForkPages - 1) / kForkPages, kForkThreads, (size_t)(a.to.rows + 1) * 4, s>>>(a);
 }
 
@@ -1289,7 +1297,7 @@ void launch_pages_compact(const CompactArgs& a, hipStream_t s)
     k_pages_unused<<<(n + 255) / 256, 256, 0, s>>>(a.used, a.held, n);
     if (a.from.rows > 0) k_pages_mark<<<a.from.rows, 256, 0, s>>>(a);
     k_pages_rank<<<(n + kForkPages - 1) / kForkPages, kForkThreads, 0, s>>>(a);
-    k_pages_renumber<<<a.from.rows + (a.place ? (n + 255) / 256 : 0), 256, 0, s>>>(a);
+    if (const int blocks = a.from.rows + (a.place ? (n + 255) / 256 : 0)) k_pages_renumber<<<blocks, 256, 0, s>>>(a);
 }
 
 void launch_pages_copy(const PagesView* layers, int n_layers, const int32_t* src, const int32_t* dst, int n, const int32_t* count, hipStream_t s)

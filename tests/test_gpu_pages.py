@@ -284,6 +284,26 @@ def test_values_that_are_not_finite_reach_those_who_see_them(group, held):
     assert ok.all()
 
 
+@pytest.mark.parametrize("dtype,held", TYPES)
+@pytest.mark.parametrize("group,spoil", [(1, False), (4, False), (1, True), (4, True)])
+def test_results_in_the_place_of_the_queries(group, spoil, dtype, held):
+    """... also where a value that is not finite has sums formed again, from the queries."""
+    r = np.random.default_rng(3)
+    lengths = [700, 33, 120, 650, 5, 0, 16, 300]
+    rows, n_pages, stride = random_rows(r, lengths, 16, group, 0.7)
+    pages, _ = pool_of(3, n_pages, 16, 2, 128, held)
+    if spoil and held != I8:
+        for i, n in enumerate(lengths):
+            if n:
+                pages.v.view(n_pages, 2, 16, 128)[rows[i][0], :, 3, 7] = math.inf
+    table = table_of(rows, lengths, stride, 16, n_pages)
+    q = randn(gen(1), 8, 10, 128, dtype=dtype)
+    for most in (700, 1):
+        want, place = ss.ss_attention_pages(q, pages, table, most, group), q.clone()
+        assert ss.ss_attention_pages(place, pages, table, most, group, out=place) is place
+        assert torch.equal(place, want) or (spoil and torch.equal(place.nan_to_num(), want.nan_to_num()))
+
+
 @pytest.mark.parametrize("held", [F16, I8])
 def test_pages_beyond_32_bits(held):
     """A pool of more than 2^32 bytes of keys; the rows' pages are its last ones."""
@@ -419,6 +439,25 @@ def test_large_forks(n_pages, n):
     r = np.random.default_rng(n)
     table, lengths = random_table(r, 200, 20, 16, n_pages)
     check_fork(table, lengths, 16, n_pages, 24, [int(x) for x in r.integers(-1, 200, n)], [int(x) for x in r.integers(0, 60, n)])
+
+
+@pytest.mark.parametrize("n_pages", [5, 20000])
+def test_tables_of_nothing(n_pages):
+    for rows, stride in ((0, 3), (3, 0), (0, 0)):
+        a, b = (ss.PageTable.allocate(rows, stride, 16, n_pages) for _ in range(2))
+        src, dst, missing = ss.ss_pages_fork(a, b)
+        assert missing.item() == 0 and src.tolist() == dst.tolist() == [-1] * rows and b.lengths.tolist() == [0] * rows
+        _, _, place, counts = ss.ss_pages_compact(a, b)
+        assert counts.tolist() == [0, 0] and (place == -1).all()
+        pages = ss.Pages.allocate(n_pages, 16, 1, 64, F16)
+        q = randn(gen(1), rows, 2, 64, dtype=F16)
+        assert not ss.ss_attention_pages(q, pages, a, 100).any()
+        k = torch.ones(rows, 1, 64, dtype=F16, device="cuda")
+        ss.ss_pages_write(pages, a, k, k)
+        assert not pages.k.any()
+        one = ss.PageTable.allocate(1, 2, 16, n_pages)
+        ss.ss_pages_fork(a, one, i32([0]), i32([20]))
+        assert one.pages.tolist() == [[0, 1]] and one.lengths.tolist() == [20]
 
 
 def test_the_largest_number_of_rows():
