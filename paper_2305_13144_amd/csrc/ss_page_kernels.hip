@@ -14,7 +14,8 @@ __device__ __forceinline__ int pages_of(int length, int page) { return (length +
 
 // ------------------------------------------------------------------------------------------ write and read
 // As k_cache_write: a vector of HD elements is HD / 8 neighbouring lanes', 16 bytes each; a workgroup takes 16 tokens through kPagePasses passes
-// over 128 / HD heads, keys and values in different workgroups.
+// over 128 / HD heads, keys and values in different workgroups.  Bound by the bytes (8746 tokens of 32 heads of 128, halves into 8 bits, written and read:
+// 82 us, 4.7 TB/s), a step of few tokens by its chain of loads: row, length and entry come before the slot.
 constexpr int kPagePasses = 4, kPageTokens = 16;
 
 // Of a lane: its token, that token's vector of head 0 in the pool (-1: none), its first head.
@@ -152,6 +153,9 @@ struct Scan {
 // whole in memory, so nothing is clamped; scores of slots that a row does not see are set to -inf.  Values of such slots meet weights of 0: in 8 bits
 // they are finite whatever lies there (the scale is left out), in 16 bits an infinity or NaN shows in the sums, and the piece is done again,
 // slot by slot (k_attention_pages' `careful`).
+// Bound by the cache's bytes (64 rows to 8000 slots, 32 heads on 8, 8 bits: 439 MB in 90 us with the join, 6.5 TB/s while large parts run, 4.9 in all), with few
+// or short rows by a chain of latencies (one row of 3900 slots and 32 heads: 12 us, and 3 of the join).  3 workgroups on a unit (QT == 1, heads of 128): a
+// fourth wave a SIMD spills.
 // Who takes what (page_plan): short rows a workgroup a unit; one long row, or few that are not very long, a workgroup one of `parts` equal parts of a unit; else
 // (DEALT) units are cut by the rows' lengths (PageCuts).  k_page_join adds up the parts of units.
 struct PageItem {
@@ -176,7 +180,8 @@ __device__ __forceinline__ PageItem group_item(const PageAttentionArgs& a, int j
     return {p, p0, 1u, p0 + 16 <= len};
 }
 
-// The items of a group, by position and there by the first row that holds the page.
+// The items of a group, by position and there by the first row that holds the page: a round of as many positions as the threads hold, compared through LDS.
+// 8 rows of 206 entries: 6.4 us, two rounds of latencies; rows in neighbouring lanes that compare by shuffles, twice through to count first: 7.4.
 constexpr int kItemThreads = 1024;
 __global__ __launch_bounds__(kItemThreads) void k_page_items(PageAttentionArgs a)
 {
@@ -817,7 +822,7 @@ __global__ __launch_bounds__(256) void k_page_join(PageAttentionArgs a)
 }
 
 // ------------------------------------------------------------------------------------------ fork
-// Three launches.  Claims: of each page the lowest row of `to` that writes into it, -1 if a row holds it that does not (or somebody else
+// Three launches, or one (k_pages_fork_few).  Claims: of each page the lowest row of `to` that writes into it, -1 if a row holds it that does not (or somebody else
 // does), INT_MAX if none does, as one minimum over all entries.  Then every workgroup knows from the claims which pages are free and how many each
 // row needs, and the workgroup that has the k-th free page finds the row that gets it.
 constexpr int kFree = INT_MAX;
@@ -956,7 +961,8 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_hand_out(ForkArgs a)
     if (t == 0) *a.missing = max(total - every, 0);
 }
 
-// The same in one workgroup, with the claims in LDS: where rows and pages are few the three launches are most of the time.
+// The same in one workgroup, with the claims in LDS: where rows and pages are few the three launches are most of the time.  Bound by the chain parent,
+// length, entries, needs, pages: 6.8 us for 32 rows of 110 entries (three launches 13), 9.8 for 512 of 18.
 constexpr int kFewRowsOfTable = 1024, kFewPages = 16384;   // of one workgroup
 template <typename A>
 __device__ __forceinline__ int entry_row(int e, const A& t) { return (int)((uint32_t)e / (uint32_t)t.stride); }
@@ -1037,6 +1043,9 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_fork_few(ForkArgs a)
 }
 
 // ------------------------------------------------------------------------------------------ compact
+// Four launches, or one (k_pages_compact_few): which pages are in use; how many before each, so that the k-th that has to move and the k-th hole below
+// meet at k; tables and places by that.  The counting reads the whole list in every workgroup (26521 pages 11 us, half a million would take
+// 100: then blocks of it would have to be counted first).
 __global__ __launch_bounds__(256) void k_pages_unused(int32_t* __restrict__ used, const uint8_t* __restrict__ held, int n)
 {
     const int i = blockIdx.x * 256 + threadIdx.x;
