@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
             next[k] = u32x4{0, 0, 0, 0};
             if (first + k < end) load(first + k, next[k]);
         }
-        ref = -3.0e38f;
+        ref = -3.4028235e38f;   // the lowest: a row may hold nothing else
 #pragma unroll
         for (int k = 0; k < kBeamAhead; ++k)
             if (first + k < end) {

@@ -181,6 +181,20 @@ def test_extreme_logits():
     assert got.token.tolist() == [4999, 0]
 
 
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab", [3, 700, 40000])
+def test_logits_that_are_masked_with_the_lowest_number_are_candidates_far_behind(dtype, vocab):
+    low = torch.finfo(dtype).min
+    x = torch.full((4, vocab), low, device="cuda", dtype=dtype)
+    x[1, vocab - 1] = 2.0                                                 # all but one
+    x[2, : vocab // 2] = randn(gen(1), vocab // 2).to(dtype)              # half of them
+    x[3, ::2] = -math.inf                                                 # the others are no candidates at all
+    got = check(x, torch.tensor([[-1.0], [-2.0], [-3.0], [-4.0]], device="cuda"), 2)
+    for row, n in ((0, vocab), (3, vocab // 2)):                          # whole rows of the lowest number: all alike
+        assert got.totals[row, 0].isfinite() and abs(got.totals[row, 0].item() + (1.0, 2.0, 3.0, 4.0)[row] + math.log(n)) <= 2.0 ** -18 + 2.0 ** -24 * 20
+    assert got.token.view(4, 2)[0].tolist() == [0, 1] and got.totals[1, 0] == -2.0 and got.token.view(4, 2)[1].tolist() == [vocab - 1, 0]
+
+
 def test_ended_beams_stay_with_their_sum():
     x = torch.zeros(4, 100, device="cuda")
     totals = torch.tensor([[-1.0, -0.5, -9.0, -9.0]], device="cuda")
