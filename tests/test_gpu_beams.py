@@ -218,6 +218,19 @@ def test_histories_without_room_and_of_another_width():
             check(x, totals, n, lengths, ended, 3, 0.0, history, out=out)
 
 
+def test_the_largest_number_of_rows():
+    x = randn(gen(1), 65535, 37)
+    totals = -torch.rand(65535, 1, device="cuda", generator=gen(2))
+    got = ss.ss_beam_select(x, totals, 2)
+    best = torch.sort(x, dim=1, descending=True, stable=True)
+    assert torch.equal(got.token.view(-1, 2), best.indices[:, :2].int()) and torch.equal(got.parent.view(-1, 2), i32(list(range(65535)))[:, None].expand(-1, 2))
+    want = totals.double() + torch.log_softmax(x.double(), 1).gather(1, best.indices[:, :2])
+    assert ((got.totals.double() - want).abs() <= 2.0 ** -18 + 2.0 ** -23 * want.abs()).all()
+    got = ss.ss_beam_select(x[:65472], totals.view(-1)[:65472].view(1023, 64), 64)
+    want = (totals.view(-1)[:65472, None].double() + torch.log_softmax(x[:65472].double(), 1)).view(1023, -1).sort(1, descending=True).values[:, :64]
+    assert ((got.totals.double() - want).abs() <= 2.0 ** -18 + 2.0 ** -23 * want.abs()).all()
+
+
 def test_new_rows_of_a_search_begin_from_one_beam():
     x = randn(gen(2), 3, 4000)
     got = check(x, torch.zeros(3, 1, device="cuda"), 5)

@@ -243,6 +243,25 @@ def test_many_long_rows_of_unlike_length(dtype, held, n, kv, each, dim, top, gro
     assert ((few.double() - got.double()).abs() <= 4 * half_step(dtype) * (got.double().abs() + v.abs().max() * 0.1)).all()
 
 
+@pytest.mark.parametrize("group", [1, 5])
+@pytest.mark.parametrize("most", [16, 5000])
+def test_the_largest_number_of_queries(group, most):
+    """65535 rows of one page each; with a longest length that is far too large units are cut by the rows' lengths all the same."""
+    n, n_pages = 65535, 50
+    pages, (k, v) = pool_of(1, n_pages, 16, 1, 64, F16)
+    at = torch.randint(0, n_pages, (n, 1), device="cuda", generator=gen(2)).int()
+    lengths = torch.randint(0, 17, (n,), device="cuda", generator=gen(3)).int()
+    q = randn(gen(4), n, 1, 64, dtype=F16)
+    got = ss.ss_attention_pages(q, pages, ss.PageTable(at, lengths, 16, n_pages), most, group)
+    kk, vv = k[at[:, 0].long(), 0], v[at[:, 0].long(), 0]                      # [n, 16, 64]
+    score = (kk * q[:, 0, None, :].double()).sum(-1) * 0.125
+    score = score.masked_fill(torch.arange(16, device="cuda") >= lengths[:, None], -math.inf)
+    w = torch.softmax(score, -1).nan_to_num(0.0)
+    want, A = (w[..., None] * vv).sum(1), (w[..., None] * vv.abs()).sum(1)
+    tol = half_step(F16) * want.abs() + (half_step(F16) + 2.0 ** -13) * A + 16 * 2.0 ** -23 * v.abs().max()   # as assert_attention; the scores' part is below 2^-14
+    assert ((got[:, 0].double() - want).abs() <= tol).all()
+
+
 def test_rows_chosen_by_a_list_and_results_with_strides():
     check_attention(11, [100, 37, 250, 1], 32, 2, 2, 128, F16, I8, pick=[2, 0, -1, 2, 4, 3, 2**31 - 1], out="wide")
     check_attention(12, [100, 37, 250, 1], 32, 2, 2, 64, BF16, BF16, group=2, pick=[2, 0, 1, 3, -5, 2], out="wide")
