@@ -3,6 +3,8 @@ from __future__ import annotations
 
 import os
 import subprocess
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -12,14 +14,25 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared", "-pth
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 
 
-def build(verbose: bool = False) -> str:
-    cmd = ["hipcc", *FLAGS, *[os.path.join(CSRC, s) for s in SOURCES], "-o", LIB]
+def _run(cmd) -> str:
     r = subprocess.run(cmd, capture_output=True, text=True)
     noise = "is not a recognized feature for this target"
     err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
     if r.returncode != 0:
         raise RuntimeError("hipcc failed:\n" + err)
-    if verbose and err.strip():
+    return err
+
+
+def build(verbose: bool = False) -> str:
+    """Every source by itself, some at a time, then the library."""
+    with tempfile.TemporaryDirectory() as tmp:
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        flags = [f for f in FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(max_workers=4) as pool:
+            said = list(pool.map(lambda p: _run(["hipcc", *flags, "-c", os.path.join(CSRC, p[0]), "-o", p[1]]), zip(SOURCES, objects)))
+        said.append(_run(["hipcc", "--offload-arch=gfx950", "-shared", "-pthread", *objects, "-o", LIB]))
+    err = "\n".join(e for e in said if e.strip())
+    if verbose and err:
         print(err)
     return LIB
 
