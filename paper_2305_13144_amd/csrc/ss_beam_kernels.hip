@@ -326,18 +326,20 @@ __device__ __forceinline__ int beam_length(int length, bool more) { return min(m
 
 // Up to kBeamRanked candidates find their places by counting those before them, once each wave has left out what is not among its best; more (then a row is one slice) are taken one by one, a lane of
 // the first wave holding the best of its beam that is left.  Bound by a chain of latencies (a launch's start, two loads behind each other, fp64 exp,
-// log and pow of a lane per beam): all that does not depend on other loads is requested at the start.
-__global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
+// log and pow of a lane per beam): all that does not depend on other loads is requested at the start.  512 threads, two candidates each, against 256 of four: 6.2 for 6.9 us
+// (4 beams, 32000 logits), 7.6 for 8.9 (32 x 8), 7.2 for 9.4 (96 x 8, 100003 logits).
+constexpr int kPickThreads = 512;
+__global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a)
 {
     struct Ranked {
         double rank;
         uint64_t key;   // beam and token: of equal ranks the lower one is first
     };
     constexpr uint64_t kNone = ~0ull;
-    constexpr int PER = kBeamRanked / 256;
+    constexpr int NT = kPickThreads, NW = NT / 64, PER = kBeamRanked / NT;
     __shared__ Ranked s_c[kBeamRanked];
     __shared__ double s_top[kBeamMax], s_log[kBeamMax], s_total[kBeamMax], s_power[kBeamMax];
-    __shared__ int s_over[kBeamMax], s_row[kBeamMax], s_token[kBeamMax], s_len[kBeamMax], s_kept[4];
+    __shared__ int s_over[kBeamMax], s_row[kBeamMax], s_token[kBeamMax], s_len[kBeamMax], s_kept[NW];
     const int g = blockIdx.x, t = threadIdx.x, per = beam_part_floats(a.keep), lists = a.slices * a.keep, n = a.beams * lists, sums = a.beams * a.slices;
     const float* part = a.part + (int64_t)g * a.beams * a.slices * per;
     const bool ranked = n <= kBeamRanked;
@@ -347,7 +349,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
     int token_of[PER];
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int c = t + 256 * k;
+        const int c = t + NT * k;
         if (c < sums) {
             ref[k] = part[c * per];
             sum_of[k] = *(const double*)(part + c * per + 2);
@@ -369,14 +371,14 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
     if (t < a.keep) s_row[t] = s_token[t] = -1;
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int c = t + 256 * k;
+        const int c = t + NT * k;
         if (c < sums) s_c[c].rank = ref[k];
     }
     __syncthreads();
     double share[PER];   // a slice's sum, relative to its row's largest reference
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int c = t + 256 * k;
+        const int c = t + NT * k;
         if (c >= sums) break;
         const int beam = c / a.slices;
         if (s_over[beam]) continue;
@@ -388,7 +390,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < PER; ++k) {
-        const int c = t + 256 * k;
+        const int c = t + NT * k;
         if (c < sums) s_c[c].rank = share[k];
     }
     __syncthreads();
@@ -433,7 +435,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
         uint32_t as_float[PER];
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            const int c = t + 256 * k;
+            const int c = t + NT * k;
             mine[k] = {-__builtin_inf(), kNone};
             if (c < n) mine[k].rank = candidate(c / lists, c % lists, cand[k], token_of[k], &sum[k], &mine[k].key);
             as_float[k] = ordered((float)mine[k].rank);
@@ -443,13 +445,13 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
             int there = 0;
 #pragma unroll
             for (int k = 0; k < PER; ++k)
-                if (256 * k < n) there += __popcll(__ballot(as_float[k] >= (least | 1u << b)));
+                if (NT * k < n) there += __popcll(__ballot(as_float[k] >= (least | 1u << b)));
             if (there >= a.keep) least |= 1u << b;
         }
         int kept = 0;
 #pragma unroll
         for (int k = 0; k < PER; ++k) {
-            if (256 * k >= n) break;
+            if (NT * k >= n) break;
             const bool stays = mine[k].key != kNone && as_float[k] >= least;
             const uint64_t all = __ballot(stays);
             if (stays) s_c[(t >> 6) * (64 * PER) + kept + __popcll(all & ((1ull << (t & 63)) - 1))] = mine[k];
@@ -459,13 +461,16 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
         if ((t & 63) == 0) s_kept[t >> 6] = kept;
         __syncthreads();
         int before[PER] = {};
-        for (int w = 0; w < 4; ++w)
-            for (int o = 0; o < s_kept[w]; ++o) {
+        for (int w = 0; w < NW; ++w) {
+            const int there = s_kept[w];
+#pragma unroll 4
+            for (int o = 0; o < there; ++o) {
                 const Ranked x = s_c[w * (64 * PER) + o];
 #pragma unroll
                 for (int k = 0; k < PER; ++k)
-                    if (256 * k < n) before[k] += x.rank > mine[k].rank || (x.rank == mine[k].rank && x.key < mine[k].key);
+                    if (NT * k < n) before[k] += (x.rank > mine[k].rank) | ((x.rank == mine[k].rank) & (x.key < mine[k].key));
             }
+        }
 #pragma unroll
         for (int k = 0; k < PER; ++k)
             if (mine[k].key != kNone && before[k] < a.keep) take(before[k], mine[k].key, sum[k]);
@@ -510,9 +515,9 @@ __global__ __launch_bounds__(256) void k_beam_pick(BeamArgs a)
         if (a.next_ended) a.next_ended[at] = 1;
     }
     if (!a.next_history) return;
-    constexpr int AT_ONCE = 8;   // a wave takes a history, so many loads at a time
+    constexpr int AT_ONCE = 16;   // a wave takes a history, so many loads at a time
     const int width = a.next_history_stride;
-    for (int k = t >> 6; k < a.keep; k += 4) {
+    for (int k = t >> 6; k < a.keep; k += NW) {
         const int row = s_row[k], len = row < 0 ? 0 : max(s_len[row - g * a.beams], 0), token = s_token[k], kept = min(len, a.history_stride);
         const int32_t* from = a.history + (int64_t)max(row, 0) * a.history_stride;
         int32_t* to = a.next_history + ((int64_t)g * a.keep + k) * width;
@@ -537,7 +542,7 @@ void launch_beam_select(const BeamArgs& a, int dtype, hipStream_t s)
     if (dtype == kF32) k_beam_rows<float><<<grid, 256, 0, s>>>(a);
     else if (dtype == kF16) k_beam_rows<_Float16><<<grid, 256, 0, s>>>(a);
     else k_beam_rows<__bf16><<<grid, 256, 0, s>>>(a);
-    k_beam_pick<<<a.n_groups, 256, 0, s>>>(a);
+    k_beam_pick<<<a.n_groups, kPickThreads, 0, s>>>(a);
 }
 
 }  // namespace ss
