@@ -53,10 +53,10 @@ __device__ __forceinline__ double wave_sum(double x)
     return x;
 }
 
-// A number's bits, ordered as the numbers.
+// A number's bits, ordered as the numbers; -0, which is equal to +0, becomes it.
 __device__ __forceinline__ uint32_t ordered(float x)
 {
-    const uint32_t u = __float_as_uint(x);
+    const uint32_t u = __float_as_uint(x + 0.f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 

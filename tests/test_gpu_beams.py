@@ -152,6 +152,26 @@ def test_equal_candidates_in_order_of_their_numbers():
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("keep", [1, 4, 64])
+def test_zeros_of_either_sign_are_equal(dtype, keep):
+    """More of them in a wave than its list holds, and than are taken."""
+    x = torch.zeros(16, 20000, device="cuda", dtype=dtype)
+    x[:, ::2] = -0.0
+    assert check(x[:1], torch.zeros(1, 1, device="cuda"), keep, exact=True).token.tolist() == list(range(keep))
+    check(x, torch.zeros(1, 16, device="cuda"), keep, exact=True)
+    # half of them multiplied by a mask of 0
+    x = -randn(gen(keep), 2, 30000).abs().to(dtype) * (torch.rand(2, 30000, device="cuda", generator=gen(1)) < 0.5)
+    check(x, torch.full((1, 2), -3.0, device="cuda"), keep, exact=True)
+
+
+def test_ended_beams_with_sums_of_either_zero_are_equal():
+    x = torch.zeros(4, 100, device="cuda")
+    for keep in (1, 2, 3):
+        got = check(x, torch.tensor([[-0.0, 0.0, 0.0, -0.0]], device="cuda"), keep, ended=u8([1] * 4), end_id=7, exact=True)
+        assert got.parent.tolist() == list(range(keep))
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_logits_that_are_not_finite_are_no_candidates(dtype):
     x = (randn(gen(1), 8, 9000) * 2).to(dtype)
     x[0] = -math.inf
