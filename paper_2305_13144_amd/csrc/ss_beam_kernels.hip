@@ -216,7 +216,7 @@ __global__ __launch_bounds__(256) void k_beam_rows(BeamArgs a)
                 float v[N];
                 open(now[k], v);
                 const float top = largest(v);
-                if (__any(top > ref + 80.f)) {
+                if (__any(top - ref > 80.f)) {   // (ref + 80 may round to where exp overflows)
                     const float moved = wave_max(top);
                     sum *= exp2((double)(ref - moved) * (double)kLog2e);
                     ref = moved;

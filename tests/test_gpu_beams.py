@@ -201,6 +201,19 @@ def test_extreme_logits():
     assert got.token.tolist() == [4999, 0]
 
 
+@pytest.mark.parametrize("power", range(22, 32))
+def test_logits_so_large_that_few_numbers_lie_between_them(power):
+    """The largest logits of rows behind a wave's first steps, one to eight units above the rest."""
+    unit = 2.0 ** (power - 23)
+    x = torch.full((16, 20000), 2.0 ** power, device="cuda")
+    for b in range(16):
+        x[b] += unit * (b % 2)
+        x[b, 19000 + b] += unit * (1 + b // 2)
+    x[8:] = -x[8:].flip(1)
+    x[8:, 19999] = -2.0 ** power + unit * 4
+    check(x, torch.linspace(-0.5, -8.0, 16, device="cuda")[None], 64)
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("vocab", [3, 700, 40000])
 def test_logits_that_are_masked_with_the_lowest_number_are_candidates_far_behind(dtype, vocab):
