@@ -1,4 +1,5 @@
 // Kernels of beam search: of all continuations of a group's beams the best ones.
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -366,7 +367,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a)
         s_over[t] = over;
         s_len[t] = len;
         s_total[t] = a.totals[row];
-        s_power[t] = a.power != 0.f ? pow((double)max(beam_length(len, !over), 1), (double)a.power) : 1.0;
+        // (not 0 where a power is below all numbers: a sum of 0 has the rank 0 there too)
+        s_power[t] = a.power != 0.f ? fmax(pow((double)max(beam_length(len, !over), 1), (double)a.power), DBL_MIN) : 1.0;
     }
     if (t < a.keep) s_row[t] = s_token[t] = -1;
 #pragma unroll

@@ -239,6 +239,16 @@ def test_ended_beams_stay_with_their_sum():
     assert got.parent.tolist() == [1, 0, 2, 3, -1, -1]
 
 
+def test_a_power_below_all_numbers_leaves_sums_of_zero_first():
+    """10^-400 is 0 in float64, and 0 / 0 no rank."""
+    x = torch.full((3, 5), -math.inf, device="cuda")
+    x[0, 1] = x[1, 2] = x[2, 3] = 1.0
+    totals = torch.tensor([[0.0, -1.0, 0.0]], device="cuda")
+    got = ss.ss_beam_select(x, totals, 4, i32([9, 9, 9]), length_power=-400.0)
+    assert got.parent.tolist() == [0, 2, 1, -1] and got.token.tolist() == [1, 3, 2, -1]
+    assert got.totals.tolist() == [[0.0, 0.0, -1.0, -math.inf]]
+
+
 def test_histories_without_room_and_of_another_width():
     x = randn(gen(1), 4, 50)
     totals, lengths, ended, history = state(3, 1, 4, 6)
