@@ -151,8 +151,9 @@ struct Scan {
 // The mathematics of a step of two items is that of k_attention_tree (ss_cache_kernels.h): S^T = K Q^T, an online softmax in powers of two whose weights
 // are the operand of O^T += V^T P^T as they lie, nothing staged in LDS; what differs is where slots lie and who sees them.  An item is always
 // whole in memory, so nothing is clamped; scores of slots that a row does not see are set to -inf.  Values of such slots meet weights of 0: in 8 bits
-// they are finite whatever lies there (the scale is left out), in 16 bits an infinity or NaN shows in the sums, and the piece is done again,
-// slot by slot (k_attention_pages' `careful`).
+// they are finite whatever lies there (the scale is left out); in 16 bits an infinity or NaN shows in a wave's sums, and the wave goes through its items again with
+// such values counting as 0 in steps that not every row sees in all slots (16 x 8 beams with NaN wherever no row looks 66 us, with numbers 48).  Those that some
+// row sees are added to its sums at the end, so a row's bits do not depend on what it does not see.
 // Bound by the cache's bytes (64 rows to 8000 slots, 32 heads on 8, 8 bits: 439 MB in 90 us with the join, 6.5 TB/s while large parts run, 4.9 in all), with few
 // or short rows by a chain of latencies (one row of 3900 slots and 32 heads: 12 us, and 3 of the join).  3 workgroups on a unit (QT == 1, heads of 128): a
 // fourth wave a SIMD spills.
@@ -274,6 +275,15 @@ __device__ __forceinline__ I wave_prefix(I x)
     x += from_before<0x142, 0xa>(x);
     x += from_before<0x143, 0xc>(x);
     return x;
+}
+
+// The largest number of a row of 16 lanes, in all of them.
+__device__ __forceinline__ int row_max(int x)
+{
+    x = max(x, __builtin_amdgcn_mov_dpp(x, kDppXor1, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_mov_dpp(x, kDppXor2, 0xf, 0xf, false));
+    x = max(x, __builtin_amdgcn_mov_dpp(x, kDppHalfMirror, 0xf, 0xf, false));
+    return max(x, __builtin_amdgcn_mov_dpp(x, kDppMirror, 0xf, 0xf, false));
 }
 
 // What a workgroup gets: the k-th part of unit hb of group j (j < 0: nothing).  Every wave finds its place by itself, a lane a group (or some), so
@@ -439,44 +449,10 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
             bit[u] = b;
             len[u] = a.group == 1 ? len0 : attended_length(a, attended_row(a, j * a.group + b));
         }
-        if constexpr (std::is_same<M, T>::value) {
-            const uint32_t flip = !I8 && a.scale < 0.f ? 0x80008000u : 0u;
-#pragma unroll
-            for (int u = 0; u < QT; ++u) {
-                sc[u] = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
-#pragma unroll
-                for (int i = 0; i < KS; ++i) qf[u][i] = __builtin_bit_cast(m8, qreg[u][i] ^ u32x4{flip, flip, flip, flip});
-            }
-        } else {   // bf16 queries, half arithmetic: the largest magnitude of each row becomes 2^14 to 2^15
-#pragma unroll
-            for (int u = 0; u < QT; ++u) {
-                float top = 0.f, x[8];
-#pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    to_floats<T>(qreg[u][i], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
-                }
-                top = across<32>(across<16>(top, Max()), Max());
-                const float down = half_power(top, &sc[u]);
-#pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    to_floats<T>(qreg[u][i], x);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) qf[u][i][e] = (_Float16)(x[e] * down);
-                }
-            }
-        }
         f32x4 o[QT][ET];
         float m_run[QT], l_run[QT];
         WeightUnit unit[QT];
-#pragma unroll
-        for (int u = 0; u < QT; ++u) {
-#pragma unroll
-            for (int e = 0; e < ET; ++e) o[u][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
-            m_run[u] = kLowest;
-            l_run[u] = 0.f;
-        }
+        bool odd = false;
         // A wave takes every fourth step of two items; its lanes hold those of its next 32 steps.
         const int n_items = i1 - i0, steps = (n_items + 1) >> 1;
         PageItem held;
@@ -501,13 +477,52 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
             }
             ++turn;
         };
-        if (wave < steps) {
-            place(wave);
-            load_keys(at);
-            load_values(at);
-        }
-        for (int step = wave; step < steps; step += NW) {
-            {
+#pragma unroll
+        for (int pass = 0; pass < (I8 ? 1 : 2); ++pass) {
+            const bool again = pass > 0;   // (nothing is requested ahead then: there are no registers for it)
+            turn = 0;
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+#pragma unroll
+                for (int e = 0; e < ET; ++e) o[u][e] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                m_run[u] = kLowest;
+                l_run[u] = 0.f;
+            }
+            if (wave < steps) {
+                place(wave);
+                load_keys(at);
+                load_values(at);
+            }
+            // made into operands here, behind the first requests: sooner, those would wait for the queries (one row of 3900 slots in 16 bits 17.0 us, 17.3)
+            if constexpr (std::is_same<M, T>::value) {
+                const uint32_t flip = !I8 && a.scale < 0.f ? 0x80008000u : 0u;
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    sc[u] = I8 ? 1.f : fmaxf(fabsf(log2_scale), 1e-37f);
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) qf[u][i] = __builtin_bit_cast(m8, qreg[u][i] ^ u32x4{flip, flip, flip, flip});
+                }
+            } else {   // bf16 queries, half arithmetic: the largest magnitude of each row becomes 2^14 to 2^15
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    float top = 0.f, x[8];
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        to_floats<T>(qreg[u][i], x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(x[e]));
+                    }
+                    top = across<32>(across<16>(top, Max()), Max());
+                    const float down = half_power(top, &sc[u]);
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        to_floats<T>(qreg[u][i], x);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) qf[u][i][e] = (_Float16)(x[e] * down);
+                    }
+                }
+            }
+            for (int step = wave; step < steps; step += NW) {
                 const bool more = step + NW < steps;
                 const int it_p0[2] = {p0[0], p0[1]}, all = full;
                 const unsigned it_mask[2] = {mask[0], mask[1]};
@@ -540,7 +555,7 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                     for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) kq[kt][i] = ks[kt][i] * log2_scale;
-                if (more) load_keys(at);
+                if (!again && more) load_keys(at);
                 m8 pb[QT], rest[QT];
 #pragma unroll
                 for (int u = 0; u < QT; ++u) {
@@ -614,6 +629,26 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                         for (int i = 0; i < 4; ++i) l_run[u] = add_pair<M>(__builtin_bit_cast(u32x4, pb[u])[i], l_run[u]);
                     }
                 }
+                if constexpr (!I8)
+                    if (again && !all) {
+                        constexpr uint32_t INF = std::is_same<M, _Float16>::value ? 0x7c00u : 0x7f80u;
+#pragma unroll
+                        for (int kt = 0; kt < 2; ++kt) {
+                            int seen = 0;   // of this lane's four slots, by any row
+#pragma unroll
+                            for (int u = 0; u < QT; ++u)
+                                if (it_mask[kt] >> bit[u] & 1) seen = max(seen, len[u] - it_p0[kt] - 4 * g);
+                            seen = row_max(seen);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                for (int w = 0; w < VW; ++w) {
+                                    const uint32_t x = vreg[4 * kt + i][w], lo = (x & INF) == INF ? 0xffffu : 0u, up = (x >> 16 & INF) == INF ? 0xffff0000u : 0u;
+                                    odd = odd || (i < seen && (lo | up));
+                                    vreg[4 * kt + i][w] = x & ~(lo | up);
+                                }
+                        }
+                    }
 #pragma unroll
                 for (int e = 0; e < ET; ++e) {
                     u32x4 w;
@@ -629,21 +664,24 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                         if constexpr (PAIRS) o[u][e] = Half<M>::mma(vf, rest[u], o[u][e]);
                     }
                 }
-                if (more) load_values(at);
+                if (more) {
+                    if (again) load_keys(at);
+                    load_values(at);
+                }
             }
+            bool finite = true;
+            if constexpr (!I8)
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int e = 0; e < ET; ++e)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) finite = finite && fabsf(o[u][e][i]) <= 3.4e38f;
+            if (__builtin_expect(__all(finite), 1)) break;
         }
 
         // the waves' sums together: each brings its own to the common maximum
-        bool odd = false;
-        if constexpr (!I8) {
-#pragma unroll
-            for (int u = 0; u < QT; ++u)
-#pragma unroll
-                for (int e = 0; e < ET; ++e)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) odd = odd || !(fabsf(o[u][e][i]) <= 3.4e38f);
-            odd = __any(odd);
-        }
+        odd = __any(odd);
         if (lane == 0) s_odd[wave] = odd;
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
@@ -672,7 +710,6 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                     *(float4*)&s_o[wave][u][i][lane][e] = x;
                 }
         }
-        const bool careful = !I8 && (s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3]);
         __syncthreads();
         // wave i takes elements ET * (4g + i) .. of every row: ET neighbours per lane
         const int e0 = ET * (4 * g + wave);
@@ -685,30 +722,24 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
 #pragma unroll
                 for (int w = 0; w < NW; ++w) x[u][e] += s_o[w][u][wave][lane][e];
             }
-        if (careful) {   // rare: infinite or NaN values, or slots that hold them and are not seen: these sums slot by slot, relative to the same maximum
-            const float flip = a.scale < 0.f ? -1.f : 1.f;
+        if constexpr (!I8)
+            if (__builtin_expect(s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3], 0))   // the values that counted as 0, to the rows that see them
+                for (int i = i0; i < i1; i += 2) {
+                    PageItem two[2] = {group_item(a, j, row0, len0, i), PageItem{0, 0, 0u, 0}};
+                    if (i + 1 < i1) two[1] = group_item(a, j, row0, len0, i + 1);
+                    if (two[0].full & two[1].full) continue;
+                    for (const PageItem& one : two)
 #pragma unroll
-            for (int u = 0; u < QT; ++u) {
+                        for (int u = 0; u < QT; ++u) {
+                            const int seen = one.mask >> bit[u] & 1 ? min(len[u] - one.p0, 16) : 0;
+                            for (int slot = 0; slot < seen; ++slot) {
+                                const C* v = (const C*)V + (slot_of(one.page, one.p0) + slot) * HD + e0;
 #pragma unroll
-                for (int e = 0; e < ET; ++e) x[u][e] = 0.f;
-                const int r = r0 + u * 16 + ql;
-                if (u * 16 + ql >= n_rows) continue;
-                const T* qp = (const T*)a.q.p + (int64_t)(j * a.group + bit[u]) * a.q.row + (int64_t)(h * G + r - bit[u] * G) * a.q.head;
-                for (int i = i0; i < i1; ++i) {
-                    const PageItem one = group_item(a, j, row0, len0, i);
-                    const int seen = one.mask >> bit[u] & 1 ? min(len[u] - one.p0, 16) : 0;
-                    for (int slot = 0; slot < seen; ++slot) {
-                        const int64_t at = (slot_of(one.page, one.p0) + slot) * HD;
-                        float score = 0.f;
-                        for (int e = 0; e < HD; ++e) score = fmaf((float)qp[e] * flip, (float)((const C*)K)[at + e], score);
-                        const float p = __builtin_amdgcn_exp2f((score - m_all[u]) * sc[u]);
-#pragma unroll
-                        for (int e = 0; e < ET; ++e) x[u][e] = fmaf(p, (float)((const C*)V)[at + e0 + e], x[u][e]);
-                    }
+                                for (int e = 0; e < ET; ++e)
+                                    if (!(fabsf((float)v[e]) <= 3.4e38f)) x[u][e] += (float)v[e];
+                            }
+                        }
                 }
-            }
-            __syncthreads();   // the results may take the queries' place
-        }
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             const int r = u * 16 + ql;

@@ -303,6 +303,60 @@ def test_values_that_are_not_finite_reach_those_who_see_them(group, held):
     assert ok.all()
 
 
+@pytest.mark.parametrize("held", [F16, BF16])
+@pytest.mark.parametrize("group,each,dim", [(1, 1, 64), (1, 4, 128), (4, 4, 128), (8, 8, 64)])
+@pytest.mark.parametrize("most", [1, 700, 9000])
+def test_what_no_row_sees_changes_no_bit(held, group, each, dim, most):
+    """Ends of last pages, pages of nobody, and page 0, which stands in for entries that are no page."""
+    r = np.random.default_rng(group)
+    lengths = [700, 33, 120, 650, 5, 0, 16, 300] * 2
+    rows, n_pages, stride = random_rows(r, lengths, 16, group, 0.7)
+    rows = [[p + 1 for p in m] for m in rows]
+    rows[2][1] = rows[3][7] = rows[3][8] = -1
+    n_pages += 1
+    pages, _ = pool_of(3, n_pages, 16, 2, dim, held)
+    unseen = torch.ones(n_pages, 16, dtype=torch.bool)
+    for m, n in zip(rows, lengths):
+        for e, p in enumerate(m):
+            if p > 0:
+                unseen[p, :max(min(16, n - e * 16), 0)] = False
+    assert unseen[0].all()
+    bad = unseen.cuda()[:, None, :].expand(n_pages, 2, 16)
+    table = table_of(rows, lengths, stride, 16, n_pages)
+    q = randn(gen(1), 16, 2 * each, dim, dtype=held)
+    want = ss.ss_attention_pages(q, pages, table, most, group)
+    for x in (math.nan, math.inf, 1e4):
+        for t in (pages.k, pages.v):
+            t.view(n_pages, 2, 16, dim)[bad] = x
+        assert torch.equal(ss.ss_attention_pages(q, pages, table, most, group), want)
+
+
+@pytest.mark.parametrize("held", [F16, BF16])
+@pytest.mark.parametrize("each,dim", [(1, 64), (4, 128)])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_what_another_row_sees_changes_no_bit(held, each, dim, bad):
+    pages, _ = pool_of(5, 12, 16, 1, dim, held)
+    table = table_of([[0, 1, 2, 3], [0, 1, 4, 3], [0, 1, 2, 5], [0, 1, 4, 6]], [60, 49, 50, 51], 4, 16, 12)
+    q = randn(gen(3), 4, each, dim, dtype=held)
+    want = ss.ss_attention_pages(q, pages, table, 60, 4)
+    pages.v.view(12, 16, dim)[3, 5, 9] = bad                               # page 3 is row 0's to slot 11, row 1's to slot 0
+    pages.v.view(12, 16, dim)[6, 1, 3] = bad                               # row 3's
+    got = ss.ss_attention_pages(q, pages, table, 60, 4)
+    assert torch.equal(got[1], want[1]) and torch.equal(got[2], want[2])
+    for i, e in ((0, 9), (3, 3)):
+        assert (got[i, :, e].isnan() if math.isnan(bad) else got[i, :, e].float() >= 65504).all()      # half saturates
+        other = torch.arange(dim, device="cuda") != e
+        assert torch.equal(got[i][:, other], want[i][:, other])
+
+
+@pytest.mark.parametrize("dtype,held", TYPES)
+@pytest.mark.parametrize("page,kv,each,dim,group", [(16, 2, 3, 64, 1), (64, 4, 1, 128, 1), (16, 2, 4, 128, 4), (32, 1, 8, 64, 8), (256, 3, 7, 128, 2)])
+def test_rows_over_pools_without_anything_spoiled(dtype, held, page, kv, each, dim, group):
+    """The tests above have NaN wherever no row looks, with which sums are formed again; here none are."""
+    lengths = [1, 0, 15, 16, 17, 33, page - 1, page, page + 1, 2 * page, 700, 129, 650, 300, 31, 5]
+    check_attention(page + dim, lengths, page, kv, each, dim, dtype, held, group, 0.7, spoil=False)
+
+
 @pytest.mark.parametrize("dtype,held", TYPES)
 @pytest.mark.parametrize("group,spoil", [(1, False), (4, False), (1, True), (4, True)])
 def test_results_in_the_place_of_the_queries(group, spoil, dtype, held):
