@@ -51,15 +51,18 @@ __device__ __forceinline__ u32x4 from_floats(const float (&f)[8])
 
 // What a weight's exponent s * sc takes off, of the maximum m that the weights are relative to.  Its rounding, up to 2^-24 of it, is a
 // factor common to all of a row's slots, but where it is large no factor that a weight can hold (from 2^28 on half's range is left, from 2^31
-// on the exponential's): there the differences are formed first.  A branch of the wave that ordinary scores never take.
-template <typename V, int N>
+// on the exponential's): there the differences are formed first.  A branch of the wave that ordinary scores never take.  EACH: by a row's own maximum,
+// else for all rows of the wave if one needs it.
+template <bool EACH = false, typename V, int N>
 __device__ __forceinline__ float exponent_top(float m, float sc, V (&s)[N])
 {
     float top = fmaxf(m * sc, kLowest);
-    if (__any(fabsf(top) > 0x1p22f)) {
+    const bool large = fabsf(top) > 0x1p22f;
+    if (__any(large)) {
+        const float off = EACH && !large ? 0.f : m;
 #pragma unroll
-        for (int i = 0; i < N; ++i) s[i] -= m;
-        top = 0.f;
+        for (int i = 0; i < N; ++i) s[i] -= off;
+        top = EACH && !large ? top : 0.f;
     }
     return top;
 }

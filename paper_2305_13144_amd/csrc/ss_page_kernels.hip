@@ -583,11 +583,11 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
 #pragma unroll
                         for (int i = 0; i < 4; ++i) mt = fmaxf(mt, s[u][kt][i]);
                     mt = across<32>(across<16>(mt, Max()), Max());
-                    // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1
+                    // the weights are relative to a maximum that is followed in steps of 2^8: half holds 2^8 as well as 1; each row's by itself, as all that follows
                     float alpha = 1.f;
-                    const bool moves = __any((mt - m_run[u]) * sc[u] > 8.f);
-                    if (moves) {
-                        const float m_new = fmaxf(m_run[u], mt);
+                    const bool moves = (mt - m_run[u]) * sc[u] > 8.f, any_moves = __any(moves);
+                    if (any_moves) {
+                        const float m_new = moves ? mt : m_run[u];
                         alpha = __builtin_amdgcn_exp2f((m_run[u] - m_new) * sc[u]);
                         m_run[u] = m_new;
                         l_run[u] *= alpha;
@@ -595,7 +595,7 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
 #pragma unroll
                             for (int e = 0; e < ET; ++e) o[u][e] *= alpha;
                     }
-                    const float m_sc = I8 ? fmaxf(m_run[u] * sc[u], kLowest) : exponent_top(m_run[u], sc[u], s[u]);   // 8 bits: sc is a power of two
+                    const float m_sc = I8 ? fmaxf(m_run[u] * sc[u], kLowest) : exponent_top<true>(m_run[u], sc[u], s[u]);   // 8 bits: sc is a power of two
                     float top = 0.f;
 #pragma unroll
                     for (int kt = 0; kt < 2; ++kt)
@@ -611,8 +611,10 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
                             }
                         }
                     if constexpr (I8) {
-                        if (moves || __any(top > unit[u].largest())) {
-                            const float f = unit[u].follow(alpha, across<32>(across<16>(top, Max()), Max()));
+                        if (any_moves || __any(top > unit[u].largest())) {
+                            top = across<32>(across<16>(top, Max()), Max());
+                            float f = 1.f;
+                            if (moves || top > unit[u].largest()) f = unit[u].follow(alpha, top);
 #pragma unroll
                             for (int e = 0; e < ET; ++e) o[u][e] *= f;
                         }

@@ -350,6 +350,38 @@ def test_what_another_row_sees_changes_no_bit(held, each, dim, bad):
 
 
 @pytest.mark.parametrize("dtype,held", TYPES)
+@pytest.mark.parametrize("group,each,dim", [(1, 8, 64), (4, 1, 128), (4, 8, 64), (8, 4, 128)])
+@pytest.mark.parametrize("times", [4.0, 300.0, 1e-3])
+def test_other_rows_queries_and_keys_change_no_bit(dtype, held, group, each, dim, times):
+    """Large scores of one head of a row, and of one row's own pages, move maxima and units of their own only."""
+    r = np.random.default_rng(7)
+    lengths = [330, 300, 320, 310, 325, 305, 315, 295]
+    rows, n_pages, stride = random_rows(r, lengths, 16, group, 0.5)
+    pages, _ = pool_of(3, n_pages, 16, 2, dim, held)
+    table = table_of(rows, lengths, stride, 16, n_pages)
+    q = randn(gen(1), 8, 2 * each, dim, dtype=dtype)
+    calls = [lambda x, most=most: ss.ss_attention_pages(x, pages, table, most, group) for most in (1, 330)]
+    want = [f(q) for f in calls]
+    loud = q.clone()
+    loud[2, 0] *= times
+    others = torch.ones(8, 2 * each, dtype=torch.bool, device="cuda")
+    others[2, 0] = False
+    for f, w in zip(calls, want):
+        assert torch.equal(f(loud)[others], w[others])
+    if group > 1:                                                          # pages that only row 2 holds
+        mine = [p for p in rows[2] if not any(p in m for i, m in enumerate(rows) if i != 2)]
+        assert mine
+        if held == I8:
+            pages.k_scale.view(n_pages, -1)[mine] *= times
+            pages.v_scale.view(n_pages, -1)[mine] *= times
+        else:
+            pages.k.view(n_pages, -1)[mine] *= times
+        others = torch.arange(8, device="cuda") != 2
+        for f, w in zip(calls, want):
+            assert torch.equal(f(q)[others], w[others])
+
+
+@pytest.mark.parametrize("dtype,held", TYPES)
 @pytest.mark.parametrize("page,kv,each,dim,group", [(16, 2, 3, 64, 1), (64, 4, 1, 128, 1), (16, 2, 4, 128, 4), (32, 1, 8, 64, 8), (256, 3, 7, 128, 2)])
 def test_rows_over_pools_without_anything_spoiled(dtype, held, page, kv, each, dim, group):
     """The tests above have NaN wherever no row looks, with which sums are formed again; here none are."""
