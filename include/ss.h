@@ -644,7 +644,8 @@ typedef struct {
  *   parent       device, int32[n_groups * keep]: the row that the candidate continues, as ss_pages_fork takes it
  *   token        device, int32[n_groups * keep]
  * A group with fewer candidates has none in its last places: parent and token -1, sum -inf, length 0, ended.
- * 1 <= beams, keep <= SS_BEAM_MAX.  Ranks and sums are formed in float64 (log sum exp to about 2^-23), sums rounded to float32 once per step.
+ * 1 <= beams, keep <= SS_BEAM_MAX.  Ranks and sums are formed in float64, of exponentials in float32: log sum exp to 2^-18 (to
+ * (5 + 2.25 d) 2^-24, d the distance of the largest logit from their mean by probability), sums rounded to float32 once per step.
  *   workspace    device, 16-byte aligned, ss_beam_select_workspace bytes; contents do not matter
  */
 int ss_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep,

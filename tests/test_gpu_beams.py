@@ -215,6 +215,34 @@ def test_logits_so_large_that_few_numbers_lie_between_them(power):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("kind", ["late", "early", "ascending", "descending"])
+def test_how_near_the_sum_of_exponentials_is(dtype, kind):
+    """Rows of zeros with a peak behind a wave's first steps or in them, and rows in order.  An exponential is off by 2^-23 of itself, and three additions of those
+    of 16 bytes by 2^-24 each: 5 * 2^-24 of the sum.  The argument, x log2 e with x = logit - largest so far, is a rounded difference times a rounded constant
+    (2^-26.2 of it), rounded: |x| (2 + 2^-2.2) 2^-24, which counts by the term's share of the sum.  What is in float64 adds nothing that counts; a sum is
+    rounded to float32, 2^-24 of it.  No log probability is above 0."""
+    if kind in ("late", "early"):
+        tops = [0.25, 0.75, 0.875, 1.0, 1.5, 3.0, 5.0, 7.5, 10.0, 14.0, 20.875, 30.0, 40.0, 60.0, 79.0, 79.5]
+        x = torch.zeros(16, 32000, device="cuda", dtype=dtype)
+        for b, top in enumerate(tops):
+            x[b, 31000 - 7 * b if kind == "late" else 7 * b] = top
+    else:
+        x = (torch.arange(32000, device="cuda") * torch.logspace(-6, -2, 16, device="cuda")[:, None]).to(dtype)
+        x = x if kind == "ascending" else x.flip(1).contiguous()
+    got = ss.ss_beam_select(x, torch.zeros(1, 16, device="cuda"), 64)
+    logp = torch.log_softmax(x.double(), 1)
+    off = (logp.exp() * (x.double().amax(1, keepdim=True) - x.double())).sum(1)
+    parent = got.parent.long()
+    want = logp[parent, got.token.long()]
+    assert (parent >= 0).all() and (got.totals <= 0).all()
+    assert ((got.totals[0].double() - want).abs() <= 2.0 ** -24 * (5 + 2.25 * off[parent]) + 2.0 ** -24 * want.abs()).all()
+    alone = ss.ss_beam_select(x, torch.zeros(16, 1, device="cuda"), 1)                 # each row's largest, its parts in several workgroups
+    want = logp.amax(1)
+    assert (alone.totals <= 0).all()
+    assert ((alone.totals[:, 0].double() - want).abs() <= 2.0 ** -24 * (5 + 2.25 * off) + 2.0 ** -24 * want.abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("vocab", [3, 700, 40000])
 def test_logits_that_are_masked_with_the_lowest_number_are_candidates_far_behind(dtype, vocab):
     low = torch.finfo(dtype).min
