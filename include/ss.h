@@ -521,7 +521,7 @@ int ss_attention_packed(const ss_rows* q, const ss_rows* k, const ss_rows* v, co
 typedef struct {
     void *k, *v;              /* device, 16-byte aligned, n_pages * n_kv_heads * page_slots * head_dim elements */
     float *k_scale, *v_scale; /* device, 16-byte aligned, n_pages * n_kv_heads * page_slots, SS_I8 only         */
-    int32_t n_pages;
+    int32_t n_pages;          /* 1 to SS_PAGES_MAX        */
     int32_t page_slots;       /* 16, 32, 64, 128 or 256 */
     int32_t n_kv_heads, head_dim; /* head_dim 64 or 128 */
     int32_t dtype;            /* SS_F16, SS_BF16, SS_I8 */
@@ -540,6 +540,7 @@ typedef struct {
     int32_t page_slots, n_pages; /* of the pools */
 } ss_page_table;
 
+#define SS_PAGES_MAX (1 << 27) /* pages of a pool: no memory holds more */
 #define SS_PAGES_MAX_ROWS 8192 /* of a table that forks or is made dense */
 
 /*

@@ -22,7 +22,7 @@ SS_OPT_IN_FLIGHT, SS_IN_FLIGHT_MAX, SS_IN_FLIGHT_DEFAULT = 2, 4, 4
 SS_OPT_WEIGHT_COPIES, SS_OPT_CACHE_BITS = 3, 4
 SS_BF16, SS_F32, SS_F16, SS_I8 = 0, 1, 2, 3
 SS_TREE_MAX_NODES = 1024
-SS_PAGES_MAX_ROWS, SS_PAGES_MAX_GROUP, SS_BEAM_MAX = 8192, 32, 64
+SS_PAGES_MAX, SS_PAGES_MAX_ROWS, SS_PAGES_MAX_GROUP, SS_BEAM_MAX = 1 << 27, 8192, 32, 64
 FLAG_BITS = dict(SORT=SS_SORT, BIN=SS_BIN, FCR=SS_FCR, VBS=SS_VBS, COMPACT=SS_COMPACT)
 
 EXPORTS = ["ss_last_error", "ss_set_verbose", "ss_set_gemm_mode", "ss_schedule", "ss_schedule_failures", "ss_plan_free", "ss_weights_create",

@@ -135,7 +135,7 @@ int check_pages(const ss_pages* p)
     if (p->head_dim != 64 && p->head_dim != 128) return fail(SS_EINVAL, "pages: head_dim must be 64 or 128");
     if (!is_half(p->dtype) && p->dtype != SS_I8) return fail(SS_EINVAL, "pages: dtype must be SS_F16, SS_BF16 or SS_I8");
     if (p->n_kv_heads < 1 || p->n_kv_heads > 65535) return fail(SS_EINVAL, "pages: 1 to 65535 heads");
-    if (p->n_pages < 1) return fail(SS_EINVAL, "pages: there must be a page");
+    if (p->n_pages < 1 || p->n_pages > SS_PAGES_MAX) return fail(SS_EINVAL, "pages: there must be a page, and at most %d pages", SS_PAGES_MAX);
     if (!is_page_size(p->page_slots)) return fail(SS_EINVAL, "pages: page_slots must be 16, 32, 64, 128 or 256");
     if (!p->k || !p->v) return fail(SS_EINVAL, "pages: k or v is NULL");
     if (!aligned(p->k) || !aligned(p->v)) return fail(SS_EINVAL, "pages: k and v must be 16-byte aligned");
@@ -148,7 +148,7 @@ int check_table(const ss_page_table* t, const char* name)
 {
     if (!t) return fail(SS_EINVAL, "%s is NULL", name);
     if (t->n_rows < 0 || t->stride < 0) return fail(SS_EINVAL, "%s: negative number of rows or entries", name);
-    if (t->n_pages < 1) return fail(SS_EINVAL, "%s: there must be a page", name);
+    if (t->n_pages < 1 || t->n_pages > SS_PAGES_MAX) return fail(SS_EINVAL, "%s: there must be a page, and at most %d pages", name, SS_PAGES_MAX);
     if (!is_page_size(t->page_slots)) return fail(SS_EINVAL, "%s: page_slots must be 16, 32, 64, 128 or 256", name);
     if ((int64_t)t->stride * t->page_slots > INT_MAX - 1024) return fail(SS_EINVAL, "%s: rows of more than 2^31 positions", name);
     if ((int64_t)t->n_rows * t->stride > INT_MAX) return fail(SS_EINVAL, "%s: more than 2^31 entries", name);
@@ -434,7 +434,7 @@ extern "C" int ss_pages_workspace(int32_t n_pages, size_t* bytes)
 {
     ss::clear_error();
     if (!bytes) return fail(SS_EINVAL, "bytes is NULL");
-    if (n_pages < 1) return fail(SS_EINVAL, "there must be a page");
+    if (n_pages < 1 || n_pages > SS_PAGES_MAX) return fail(SS_EINVAL, "there must be a page, and at most %d pages", SS_PAGES_MAX);
     *bytes = pages_workspace(n_pages);
     return SS_OK;
 }

@@ -175,6 +175,20 @@ def test_forks_and_compactions_that_do_not_fit_are_refused(lib):
     refused(lib.ss_pages_workspace(5, None), "NULL")
 
 
+@pytest.mark.parametrize("n", [ss.SS_PAGES_MAX + 1, 2**31 - 1])
+def test_more_pages_than_any_pool_has_are_refused(lib, n):
+    """Where pages are counted, sums of their numbers and of a step of 4 x 4096 are 32 bits."""
+    a, b, p = table(n_pages=n), table(pages=Q, lengths=Q, n_pages=n), pages(n_pages=n)
+    for call in (fork, compact):
+        refused(call(lib, a=a, b=b, nbytes=1 << 40), "at most")
+    for call in (write, read, attend):
+        refused(call(lib, p=p, t=a), "at most")
+    refused(copy(lib, layers=(p,)), "at most")
+    need = C.c_size_t(0)
+    refused(lib.ss_pages_workspace(n, need), "at most")
+    assert lib.ss_pages_workspace(ss.SS_PAGES_MAX, need) == ss.SS_OK and need.value == 8 * ss.SS_PAGES_MAX
+
+
 def test_copies_that_do_not_fit_are_refused(lib):
     for other in (pages(n_pages=11), pages(page_slots=32), pages(n_kv_heads=1), pages(head_dim=128), pages(dtype=ss.SS_F16)):
         refused(copy(lib, layers=(pages(), other)), "layer 1")
