@@ -564,8 +564,8 @@ int ss_pages_read(const ss_pages* pages, const ss_page_table* table, const int32
  *   rows        device, int32[n], nullable: the table's row of the j-th query; NULL = row j.  A row that does not exist gets zeros
  *   max_length  the largest length (host; it only chooses how the work is shared out: a longer row is attended all the same)
  *   group       n is a multiple of it: queries j * group .. j * group + group - 1 are looked at together, and where their rows hold the same
- *               page in the same entry (the beams of a prompt do) it is read once for all of them.  1 to SS_PAGES_MAX_GROUP.  It changes the time, and
- *               results by roundings, nothing else
+ *               page in the same entry (the beams of a prompt do) it is read once for all of them.  1 to SS_PAGES_MAX_GROUP, and group * stride * page_slots
+ *               below 2^35.  It changes the time, and results by roundings, nothing else
  *   workspace   device, 16-byte aligned, at least the bytes that ss_attention_pages_workspace gives for the same counts and stride on the
  *               same device (0: may be NULL); its contents need not be kept and do not matter
  */

@@ -200,7 +200,7 @@ int check_workspace(const void* workspace, size_t given, size_t need)
 ss::PagesView view(const ss_pages* p) { return {p->k, p->v, p->k_scale, p->v_scale, p->n_pages, p->page_slots, p->n_kv_heads, p->head_dim, p->dtype}; }
 ss::TableView view(const ss_page_table* t) { return {t->pages, t->lengths, t->n_rows, t->stride, t->page_slots, t->n_pages}; }
 
-int check_page_attention(int32_t n_heads, int32_t n_kv_heads, int32_t n, int32_t max_length, int32_t group)
+int check_page_attention(int32_t n_heads, int32_t n_kv_heads, int32_t page_slots, int32_t stride, int32_t n, int32_t max_length, int32_t group)
 {
     if (n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads) return fail(SS_EINVAL, "n_heads must be a multiple of the key/value heads");
     if (n_heads > 65535) return fail(SS_EINVAL, "more than 65535 heads");
@@ -208,6 +208,7 @@ int check_page_attention(int32_t n_heads, int32_t n_kv_heads, int32_t n, int32_t
     if (n > 65535) return fail(SS_EINVAL, "more than 65535 rows");
     if (group < 1 || group > SS_PAGES_MAX_GROUP) return fail(SS_EINVAL, "group must be 1 to %d", SS_PAGES_MAX_GROUP);
     if (n % group) return fail(SS_EINVAL, "%d rows are no whole groups of %d", n, group);
+    if ((int64_t)group * stride * page_slots / 16 > INT_MAX) return fail(SS_EINVAL, "the rows of a group have more than 2^31 pieces of 16 positions");
     if ((int64_t)n / group * n_kv_heads * (((int64_t)group * (n_heads / n_kv_heads) + 15) / 16) > 1 << 22) return fail(SS_EINVAL, "too many rows and heads");
     return SS_OK;
 }
@@ -384,7 +385,7 @@ extern "C" int ss_attention_pages_workspace(int32_t n_heads, int32_t n_kv_heads,
     if (head_dim != 64 && head_dim != 128) return fail(SS_EINVAL, "head_dim must be 64 or 128");
     if (!is_page_size(page_slots)) return fail(SS_EINVAL, "page_slots must be 16, 32, 64, 128 or 256");
     if (stride < 0 || (int64_t)stride * page_slots > INT_MAX - 1024) return fail(SS_EINVAL, "rows of negative length or of more than 2^31 positions");
-    if (int rc = check_page_attention(n_heads, n_kv_heads, n, max_length, group)) return rc;
+    if (int rc = check_page_attention(n_heads, n_kv_heads, page_slots, stride, n, max_length, group)) return rc;
     *bytes = ss::page_space(plan_of_pages(n_heads, n_kv_heads, head_dim, n, max_length, group), n, group, n_kv_heads, head_dim, page_slots, stride).bytes;
     return SS_OK;
 }
@@ -397,7 +398,7 @@ extern "C" int ss_attention_pages(const ss_pages* pages, const ss_page_table* ta
     if (int rc = check_pages_and_table(pages, table)) return rc;
     if (int rc = check_rows(q, "q")) return rc;
     if (int rc = check_rows(out, "out")) return rc;
-    if (int rc = check_page_attention(n_heads, pages->n_kv_heads, n, max_length, group)) return rc;
+    if (int rc = check_page_attention(n_heads, pages->n_kv_heads, table->page_slots, table->stride, n, max_length, group)) return rc;
     if (q->dtype != out->dtype) return fail(SS_EINVAL, "q and out differ in type");
     if (pages->dtype != SS_I8 && pages->dtype != q->dtype) return fail(SS_EINVAL, "pages of 16 bits and q must have the same type");
     if (q->rows < n || out->rows < n) return fail(SS_EINVAL, "q or out has fewer than %d rows", n);

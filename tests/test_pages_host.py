@@ -189,6 +189,17 @@ def test_more_pages_than_any_pool_has_are_refused(lib, n):
     assert lib.ss_pages_workspace(ss.SS_PAGES_MAX, need) == ss.SS_OK and need.value == 8 * ss.SS_PAGES_MAX
 
 
+def test_groups_whose_pieces_pass_32_bits_are_refused(lib):
+    """A group's list of pieces of 16 positions is counted in 32 bits; its rows may have nothing in common."""
+    need = C.c_size_t(0)
+    for page, stride in ((16, 2**26), (256, 2**22)):                   # 2^30 positions a row, 32 rows: 2^31 pieces
+        refused(lib.ss_attention_pages_workspace(4, 2, 64, page, stride, 32, 64, 32, need), "pieces")
+        refused(attend(lib, p=pages(page_slots=page), t=table(page_slots=page, stride=stride, n_rows=1), rows=P, q=rows(rows=32), out=rows(rows=32), n=32, group=32),
+                "pieces")
+        assert lib.ss_attention_pages_workspace(4, 2, 64, page, stride - 1, 32, 64, 32, need) == ss.SS_OK
+        assert lib.ss_attention_pages_workspace(4, 2, 64, page, stride, 32, 64, 1, need) == ss.SS_OK
+
+
 def test_copies_that_do_not_fit_are_refused(lib):
     for other in (pages(n_pages=11), pages(page_slots=32), pages(n_kv_heads=1), pages(head_dim=128), pages(dtype=ss.SS_F16)):
         refused(copy(lib, layers=(pages(), other)), "layer 1")
