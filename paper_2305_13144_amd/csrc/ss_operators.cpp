@@ -187,6 +187,29 @@ int check_two_tables(const ss_page_table* from, const ss_page_table* to)
     return SS_OK;
 }
 
+// Whether a part of one table is in the other; `in_place`: other than the same part in the same place.
+bool tables_meet(const ss_page_table* a, const ss_page_table* b, bool in_place)
+{
+    struct Part {
+        const void* p;
+        size_t bytes;
+    };
+    auto parts = [](const ss_page_table* t, Part (&of)[2]) {
+        of[0] = {t->pages, (size_t)t->n_rows * t->stride * 4};
+        of[1] = {t->lengths, (size_t)t->n_rows * 4};
+    };
+    Part x[2], y[2];
+    parts(a, x);
+    parts(b, y);
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2; ++j) {
+            const uintptr_t p = (uintptr_t)x[i].p, q = (uintptr_t)y[j].p;
+            if (x[i].bytes == 0 || y[j].bytes == 0 || p >= q + y[j].bytes || q >= p + x[i].bytes) continue;
+            if (!in_place || i != j || p != q) return true;
+        }
+    return false;
+}
+
 size_t pages_workspace(int32_t n_pages) { return (size_t)n_pages * 8; }
 
 int check_workspace(const void* workspace, size_t given, size_t need)
@@ -447,8 +470,7 @@ extern "C" int ss_pages_fork(const ss_page_table* from, const ss_page_table* to,
     ss::clear_error();
     if (int rc = check_two_tables(from, to)) return rc;
     if ((to->n_rows > 0 && (!src || !dst)) || !missing) return fail(SS_EINVAL, "src, dst or missing is NULL");
-    if (from->n_rows > 0 && to->n_rows > 0 && ((from->stride > 0 && from->pages == to->pages) || from->lengths == to->lengths))
-        return fail(SS_EINVAL, "to must not be from: rows change places");
+    if (tables_meet(from, to, false)) return fail(SS_EINVAL, "to must not be from, or share memory with it: rows change places");
     if (int rc = check_workspace(workspace, workspace_bytes, pages_workspace(to->n_pages))) return rc;
     ss::ForkArgs a{view(from), view(to), parent, grow, held, src, dst, missing, (int32_t*)workspace};
     return launch([&] { ss::launch_pages_fork(a, (hipStream_t)hip_stream); });
@@ -460,6 +482,7 @@ extern "C" int ss_pages_compact(const ss_page_table* from, const ss_page_table* 
     ss::clear_error();
     if (int rc = check_two_tables(from, to)) return rc;
     if (from->n_rows != to->n_rows || from->stride != to->stride) return fail(SS_EINVAL, "from and to differ in rows or stride");
+    if (tables_meet(from, to, true)) return fail(SS_EINVAL, "to must be from itself, or share no memory with it");
     if ((from->n_pages > 1 && (!src || !dst)) || !counts) return fail(SS_EINVAL, "src, dst or counts is NULL");
     if (int rc = check_workspace(workspace, workspace_bytes, pages_workspace(from->n_pages))) return rc;
     ss::CompactArgs a{view(from), view(to), held, src, dst, place, counts, (int32_t*)workspace, (int32_t*)workspace + from->n_pages};

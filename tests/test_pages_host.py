@@ -200,6 +200,17 @@ def test_groups_whose_pieces_pass_32_bits_are_refused(lib):
         assert lib.ss_attention_pages_workspace(4, 2, 64, page, stride, 32, 64, 1, need) == ss.SS_OK
 
 
+def test_tables_that_lie_in_each_other_are_refused(lib):
+    """Tables of 8 rows of 4 entries, 128 bytes, and 8 lengths, 32: what is written where the other table is read could lead out of it."""
+    for call, word in ((fork, "share memory"), (compact, "share no memory")):
+        for at in (P - 124, P - 4, P + 4, P + 124):
+            refused(call(lib, b=table(pages=at, lengths=Q)), word)
+        for at in (P - 28, P + 4, P + 124):                            # its lengths among the other's entries
+            refused(call(lib, a=table(lengths=Q), b=table(pages=2 * Q, lengths=at)), word)
+            refused(call(lib, a=table(pages=2 * Q, lengths=at), b=table(lengths=Q)), word)
+        refused(call(lib, a=table(pages=2 * Q), b=table(pages=3 * Q, lengths=P + 28)), word)
+
+
 def test_copies_that_do_not_fit_are_refused(lib):
     for other in (pages(n_pages=11), pages(page_slots=32), pages(n_kv_heads=1), pages(head_dim=128), pages(dtype=ss.SS_F16)):
         refused(copy(lib, layers=(pages(), other)), "layer 1")
