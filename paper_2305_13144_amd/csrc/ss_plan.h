@@ -247,7 +247,7 @@ constexpr int page_cut(int count, int k, int n) { return (int)((uint32_t)count /
 // fill in as workgroups end, which those of one size do at unlike times (54 to 97 us).  (Equal parts, 64 rows to 8000 slots: half of what falls to
 // one 107 us, a quarter 110; large ones of three quarters, small ones of a fifth 108.)
 // Of few items: one round of equal parts where a width not much above the average allows it, since a part costs microseconds before its first
-// item.  Where more parts would come of it than there are workgroups: equal ones.
+// item.  Where more parts would come of it than there are workgroups, which single rows' cuts never do: equal ones.
 struct PageCuts {
     int large, small;   // items
     constexpr int large_of(int n) const { return large > 0 ? (int)((uint32_t)n / (uint32_t)large) : 0; }
@@ -261,8 +261,9 @@ struct PageCuts {
     }
 };
 constexpr PageCuts page_large_cuts(int average) { return {average, (average + 1) / 2}; }
-constexpr PageCuts page_least_cuts(int average, int group) { return {0, group == 1 ? (average + 1) / 2 : average}; }
-// Workgroups that are enough for page_least_cuts (one that gets nothing has found that out first: 2 us for every round of them).
+constexpr PageCuts page_least_cuts(int average, int /* rows of a group */) { return {0, average}; }
+// Workgroups that are enough for page_least_cuts, and for single rows' page_large_cuts: at most 2 n / average + 1 parts of n items (one that gets nothing has found
+// that out first: 2 us for every round of them).
 constexpr long long page_grid(int at_once, long long units, int group) { return (group == 1 ? 2LL : 1LL) * at_once + units; }
 PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_length, int n_cu);
 // Its workspace: where its parts begin and how large it is (bytes, all multiples of 16).

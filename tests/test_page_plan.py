@@ -91,6 +91,57 @@ int main()
 """
 
 
+SINGLE = r"""
+#include "ss_plan.h"
+#include <algorithm>
+#include <cstdio>
+#include <random>
+#include <vector>
+#define CHECK(x) do { if (!(x)) { std::printf("line %d: %s\n", __LINE__, #x); return 1; } } while (0)
+using namespace ss;
+static long long parts_of(const PageCuts& c, const std::vector<int>& count, int units)
+{
+    long long parts = 0;
+    for (int n : count) parts += (long long)(c.large_of(n) + c.small_of(n)) * units;
+    return parts;
+}
+int main()
+{
+    std::mt19937 r(11);
+    long tried = 0;
+    for (int round = 0; round < 200000; ++round) {
+        const int groups = 1 + r() % (round % 10 ? 100 : 5000), units = 1 + r() % 40, at_once = r() % 2 ? 768 : 512;
+        const long long top = r() % 2 ? 6000 : 1 << (4 + r() % 23);
+        std::vector<int> count(groups);
+        long long all = 0;
+        for (int& c : count) all += c = r() % 4 == 0 ? 0 : r() % 3 ? (int)(r() % top) : (int)top;
+        auto average_of = [&](long long n) { return std::max((n * units + at_once - 1) / at_once, (long long)kPageShare); };
+        if (r() % 5 == 0 && average_of(all) < 1 << 20) {   // as many items as make half a part and one more: two small parts of what is left, everywhere
+            const int some = (int)average_of(all);
+            all = 0;
+            for (int& c : count) all += c = some * (int)(r() % 3) + some / 2 + 1;
+        }
+        if (all == 0 || average_of(all) > 1 << 28) continue;
+        const int a = (int)average_of(all);
+        const long long grid = page_grid(at_once, (long long)groups * units, 1);
+        CHECK(parts_of(page_large_cuts(a), count, units) <= grid);
+        CHECK(parts_of(page_least_cuts(a, 1), count, units) <= page_grid(at_once, (long long)groups * units, 2));
+        ++tried;
+    }
+    std::printf("ok %ld\n", tried);
+}
+"""
+
+
+def test_a_grid_has_room_for_every_part_of_single_rows(tmp_path):
+    """... with the cuts that are tried first: others are never needed there."""
+    src, exe = tmp_path / "single.cpp", tmp_path / "single"
+    src.write_text(SINGLE)
+    subprocess.run(["g++", "-std=c++17", "-O2", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-I", CSRC, str(src), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert out.returncode == 0 and out.stdout.startswith("ok"), out.stdout + out.stderr
+
+
 def test_every_item_is_in_one_part(tmp_path):
     src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
     src.write_text(PROGRAM)
