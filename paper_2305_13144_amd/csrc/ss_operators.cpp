@@ -236,9 +236,10 @@ int check_page_attention(int32_t n_heads, int32_t n_kv_heads, int32_t page_slots
     return SS_OK;
 }
 
-ss::PagePlan plan_of_pages(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t n, int32_t max_length, int32_t group)
+// No row is longer than its entries, whatever a caller allows for.
+ss::PagePlan plan_of_pages(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t page_slots, int32_t stride, int32_t n, int32_t max_length, int32_t group)
 {
-    return ss::page_plan(n, group, n_kv_heads, n_heads / n_kv_heads, head_dim, max_length, compute_units());
+    return ss::page_plan(n, group, n_kv_heads, n_heads / n_kv_heads, head_dim, (int)std::min<int64_t>(max_length, (int64_t)stride * page_slots), compute_units());
 }
 
 int check_beams(int32_t n_groups, int32_t beams, int32_t vocab, int32_t keep)
@@ -409,7 +410,7 @@ extern "C" int ss_attention_pages_workspace(int32_t n_heads, int32_t n_kv_heads,
     if (!is_page_size(page_slots)) return fail(SS_EINVAL, "page_slots must be 16, 32, 64, 128 or 256");
     if (stride < 0 || (int64_t)stride * page_slots > INT_MAX - 1024) return fail(SS_EINVAL, "rows of negative length or of more than 2^31 positions");
     if (int rc = check_page_attention(n_heads, n_kv_heads, page_slots, stride, n, max_length, group)) return rc;
-    *bytes = ss::page_space(plan_of_pages(n_heads, n_kv_heads, head_dim, n, max_length, group), n, group, n_kv_heads, head_dim, page_slots, stride).bytes;
+    *bytes = ss::page_space(plan_of_pages(n_heads, n_kv_heads, head_dim, page_slots, stride, n, max_length, group), n, group, n_kv_heads, head_dim, page_slots, stride).bytes;
     return SS_OK;
 }
 
@@ -429,7 +430,7 @@ extern "C" int ss_attention_pages(const ss_pages* pages, const ss_page_table* ta
     if (int rc = check_apart(out, "out", n_heads, pages->head_dim)) return rc;
     if (!rows && n > table->n_rows) return fail(SS_EINVAL, "the table has fewer than %d rows", n);
     if (n == 0) return SS_OK;
-    const ss::PagePlan p = plan_of_pages(n_heads, pages->n_kv_heads, pages->head_dim, n, max_length, group);
+    const ss::PagePlan p = plan_of_pages(n_heads, pages->n_kv_heads, pages->head_dim, table->page_slots, table->stride, n, max_length, group);
     const ss::PageSpace space = ss::page_space(p, n, group, pages->n_kv_heads, pages->head_dim, table->page_slots, table->stride);
     if (int rc = check_workspace(workspace, workspace_bytes, space.bytes)) return rc;
     ss::PageAttentionArgs a{};

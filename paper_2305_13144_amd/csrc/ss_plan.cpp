@@ -420,7 +420,8 @@ PagePlan page_plan(int n, int group, int n_kv, int heads_each, int hd, int max_l
     const long long groups = std::max(1, n / group), units = groups * n_kv * p.row_blocks;
     const long long items = (max_length + 15LL) / 16;   // of a unit's longest row: rows of a group may share all they have
     p.parts = 1;
-    if (items <= kPageWhole || (2 * units >= p.at_once && items <= std::max(1LL, units / p.at_once) * kPageWholeOfMany)) return p;
+    const long long rounds = units / p.at_once, turns = (groups + 63) / 64;
+    if (items <= kPageWhole || (2 * units >= p.at_once && items <= std::max(std::max(1LL, rounds) * kPageWholeOfMany, (rounds + 2) * turns * kPageTurn))) return p;
     p.parts = 0;
     if (groups == 1 || items * units <= (long long)p.at_once * kPageFew) p.parts = (int)std::max(1LL, std::min(p.at_once / units, items * group / kPageShare));
     return p;

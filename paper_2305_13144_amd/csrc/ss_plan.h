@@ -229,9 +229,11 @@ constexpr int tree_chunks(int len, int chunk, int most)
 // which costs microseconds first.  Measured (32 heads of 128 in 8 bits, rows up to the length named, most much shorter; us, graphs):
 //   a workgroup a unit / parts     1 row of 450 slots, 8 heads of keys 10.1 / 9.5, 32 13.5 / 11.1; 16 rows 13.1 / 11.9; of 250 slots the same
 //   a workgroup a unit / PageCuts  512 units, 850 slots 24.3 / 28.3, 1550 34.1 / 31.8 and 31.9 / 39.5, 8000 150 / 100; 2048 units, 450 slots 39 / 51, 1550 87 / 97
+//                                  many groups, of whose counts every workgroup takes 64 at a turn of some 0.9 us, two items' time: rows to 2500 slots, as if they were
+//                                  far longer, 512 x 8 heads 223 / 320, 1024 x 8 433 / 660, 4096 x 8 1684 / 4174, 16384 x 1 of 40 slots 98 / 6539
 //   parts / PageCuts               4 rows of 4000 slots and 8 heads of keys 15.0 / 17.7, 32 25.8 / 27.0; 8 rows of 4000 and 32 heads of keys 43 / 36, 16 of 8000 159 / 115;
 //                                  8 beams of 2 prompts of 1600 slots 23.3 / 24.3, of 16 prompts of 4000 51 / 48
-constexpr int kPageShare = 8, kPageWhole = 16, kPageWholeOfMany = 100, kPageFew = 48, kPageMany = 64;
+constexpr int kPageShare = 8, kPageWhole = 16, kPageWholeOfMany = 100, kPageTurn = 2, kPageFew = 48, kPageMany = 64;
 struct PagePlan {
     int tiles, row_blocks, parts, at_once;
 };

@@ -262,6 +262,36 @@ def test_the_largest_number_of_queries(group, most):
     assert ((got[:, 0].double() - want).abs() <= tol).all()
 
 
+@pytest.mark.parametrize("group,n", [(1, 4096), (5, 4095)])
+@pytest.mark.parametrize("dtype,held", [(F16, F16), (BF16, I8)])
+def test_thousands_of_queries_cut_by_their_rows_lengths(group, n, dtype, held):
+    """A lane of a workgroup that looks for its part has many groups here.  The queries share 40 rows, and some have none."""
+    r = np.random.default_rng(n)
+    page, stride, n_pages, dim = 16, 800, 2000, 64
+    pages, (k, v) = pool_of(1, n_pages, page, 1, dim, held)
+    lengths = [int(stride * page * x ** 3) for x in r.random(40)]
+    lengths[5], lengths[6], lengths[7] = stride * page, 0, 1
+    table = r.integers(0, n_pages, (40, stride)).astype(np.int32)
+    tb = ss.PageTable(torch.tensor(table, device="cuda"), i32(lengths), page, n_pages)
+    pick = r.integers(-1, 41, n)
+    pick[::7] = 7
+    pick[100:103] = 5
+    q = randn(gen(4), n, 1, dim, dtype=dtype)
+    most = stride * page
+    dealt, whole = (ss.ss_attention_pages_workspace(1, 1, dim, page, stride, n, m, group) for m in (most, 16))
+    assert dealt >= whole + n // group * 8 + 1024 * 16 * (dim + 4) * 4      # parts, and notes of where those of each unit lie
+    got = ss.ss_attention_pages(q, pages, tb, most, group, rows=i32(pick.tolist()))
+    for i in range(-1, 41):
+        at = torch.tensor(np.nonzero(pick == i)[0], device="cuda")
+        if not 0 <= i < 40 or lengths[i] == 0:
+            assert not got[at].any()
+            continue
+        m = torch.tensor(table[i], device="cuda").long()
+        kk, vv = (x[m, 0].reshape(-1, dim)[:lengths[i]] for x in (k, v))
+        for a in at.split(512):
+            assert_attention(got[a, 0], q[a, 0], kk, vv, torch.ones(len(a), lengths[i], dtype=torch.bool, device="cuda"), dim ** -0.5, F16 if held == I8 else held)
+
+
 def test_rows_chosen_by_a_list_and_results_with_strides():
     check_attention(11, [100, 37, 250, 1], 32, 2, 2, 128, F16, I8, pick=[2, 0, -1, 2, 4, 3, 2**31 - 1], out="wide")
     check_attention(12, [100, 37, 250, 1], 32, 2, 2, 64, BF16, BF16, group=2, pick=[2, 0, 1, 3, -5, 2], out="wide")
@@ -305,7 +335,7 @@ def test_values_that_are_not_finite_reach_those_who_see_them(group, held):
 
 @pytest.mark.parametrize("held", [F16, BF16])
 @pytest.mark.parametrize("group,each,dim", [(1, 1, 64), (1, 4, 128), (4, 4, 128), (8, 8, 64)])
-@pytest.mark.parametrize("most", [1, 700, 9000])
+@pytest.mark.parametrize("most", [1, 700, 2**20])
 def test_what_no_row_sees_changes_no_bit(held, group, each, dim, most):
     """Ends of last pages, pages of nobody, and page 0, which stands in for entries that are no page."""
     r = np.random.default_rng(group)
@@ -314,6 +344,7 @@ def test_what_no_row_sees_changes_no_bit(held, group, each, dim, most):
     rows = [[p + 1 for p in m] for m in rows]
     rows[2][1] = rows[3][7] = rows[3][8] = -1
     n_pages += 1
+    stride = max(stride, most // 16)                                       # with room for rows so long
     pages, _ = pool_of(3, n_pages, 16, 2, dim, held)
     unseen = torch.ones(n_pages, 16, dtype=torch.bool)
     for m, n in zip(rows, lengths):
@@ -356,11 +387,11 @@ def test_other_rows_queries_and_keys_change_no_bit(dtype, held, group, each, dim
     """Large scores of one head of a row, and of one row's own pages, move maxima and units of their own only."""
     r = np.random.default_rng(7)
     lengths = [330, 300, 320, 310, 325, 305, 315, 295]
-    rows, n_pages, stride = random_rows(r, lengths, 16, group, 0.5)
+    rows, n_pages, _ = random_rows(r, lengths, 16, group, 0.5)
     pages, _ = pool_of(3, n_pages, 16, 2, dim, held)
-    table = table_of(rows, lengths, stride, 16, n_pages)
+    table = table_of(rows, lengths, 2**16, 16, n_pages)
     q = randn(gen(1), 8, 2 * each, dim, dtype=dtype)
-    calls = [lambda x, most=most: ss.ss_attention_pages(x, pages, table, most, group) for most in (1, 330)]
+    calls = [lambda x, most=most: ss.ss_attention_pages(x, pages, table, most, group) for most in (1, 330, 2**20)]
     want = [f(q) for f in calls]
     loud = q.clone()
     loud[2, 0] *= times

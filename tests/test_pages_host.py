@@ -152,6 +152,15 @@ def test_a_workspace_of_the_attention_that_is_too_small_is_refused_with_its_size
     refused(attend(lib, t=t, most=64000, group=4, work=P + 4, nbytes=need.value), "aligned")
 
 
+def test_a_longest_length_beyond_the_entries_shares_out_as_the_entries_do(lib):
+    """No row is longer than its entries: what a caller allows beyond that takes no workspace (and no time)."""
+    a, b = C.c_size_t(0), C.c_size_t(0)
+    for stride, n, group in ((4, 65535, 1), (60, 16384, 8), (800, 40, 1), (3000, 16, 4), (0, 5, 5)):
+        assert lib.ss_attention_pages_workspace(4, 1, 128, 64, stride, n, 64 * stride, group, a) == ss.SS_OK
+        assert lib.ss_attention_pages_workspace(4, 1, 128, 64, stride, n, 2**31 - 1, group, b) == ss.SS_OK
+        assert a.value == b.value
+
+
 def test_forks_and_compactions_that_do_not_fit_are_refused(lib):
     for call in (fork, compact):
         for other in (table(pages=Q, lengths=Q, page_slots=32), table(pages=Q, lengths=Q, n_pages=9)):
