@@ -154,6 +154,9 @@ struct Scan {
 // they are finite whatever lies there (the scale is left out); in 16 bits an infinity or NaN shows in a wave's sums, and the wave goes through its items again with
 // such values counting as 0 in steps that not every row sees in all slots (16 x 8 beams with NaN wherever no row looks 66 us, with numbers 48).  Those that some
 // row sees are added to its sums at the end, so a row's bits do not depend on what it does not see.
+// What is rounded: the weights, to the operand's type.  In 16 bits their sum is of the rounded ones (half 0.00024 of a call, 0.00021 of it the result's own rounding; bf16
+// 0.0019 and 0.0016; sums of two would take registers that there are not).  Over 8 bits with results in half they are sums of two halves: 0.00021 instead of
+// 0.00029, for a second product beside each (16 x 8 beams 38.0 us, 35.6).
 // Bound by the cache's bytes (64 rows to 8000 slots, 32 heads on 8, 8 bits: 439 MB in 90 us with the join, 6.5 TB/s while large parts run, 4.9 in all), with few
 // or short rows by a chain of latencies (one row of 3900 slots and 32 heads: 12 us, and 3 of the join).  3 workgroups on a unit (QT == 1, heads of 128): a
 // fourth wave a SIMD spills.
@@ -380,7 +383,7 @@ __global__ __launch_bounds__(256, QT == 1 ? HD == 64 ? 4 : 3 : 2) void k_attenti
     constexpr int ROW = HD * sizeof(C);      // bytes of a vector
     constexpr int KL = ROW / 64;             // 16-byte loads per 16 slots and lane
     constexpr int VW = ET * sizeof(C) / 4;   // words per slot and lane: ET elements
-    constexpr bool PAIRS = I8 && std::is_same<T, _Float16>::value && QT == 1;   // weights as sums of two halves
+    constexpr bool PAIRS = I8 && std::is_same<T, _Float16>::value;   // weights as sums of two halves: bf16 results round off more than one leaves
     __shared__ float s_m[NW][ROWS], s_l[NW][ROWS];
     __shared__ int s_odd[NW];
     __shared__ __attribute__((aligned(16))) float s_o[NW][QT][4][64][ET];

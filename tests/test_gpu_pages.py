@@ -205,6 +205,31 @@ def test_one_long_row_and_many_short_ones(dtype, held):
     check_attention(5, [17] * 300, 16, 1, 1, 64, dtype, held)
 
 
+@pytest.mark.parametrize("rows,group,each,dim,length", [(1, 1, 16, 128, 3900), (4, 4, 8, 128, 300), (32, 32, 1, 64, 700), (8, 8, 4, 64, 60), (2, 1, 40, 128, 129)])
+@pytest.mark.parametrize("lowest", [0, 3, 20])
+def test_half_results_over_8_bits_have_one_rounding(rows, group, each, dim, length, lowest):
+    """However many rows a unit has: weights are pairs of halves, off by 2^-22 of themselves (2^-11 of what the first leaves, 2^-11), or where they are
+    subnormal by 2^-25 R with 2^6 R at most the largest product, times codes up to 127.  Scores are whole numbers of powers of two from 0 to
+    -20, exact but for scale log2(e), which is 1 within 2^-23: 20 2^-23 ln 2 of a weight, 2^-18 with the exponential and the sums."""
+    r = np.random.default_rng(rows)
+    lists, n_pages, stride = random_rows(r, [length] * rows, 16, group, 0.8)
+    pages, (_, v) = pool_of(126, n_pages, 16, 1, dim, I8)
+    pages.k.zero_()
+    keys = pages.k.view(n_pages, 16, dim)
+    keys[:, :, 0] = -torch.randint(0, lowest + 1, (n_pages, 16), device="cuda", generator=gen(127)).to(I8)
+    pages.k_scale.fill_(1)
+    q = torch.zeros(rows, each, dim, dtype=F16, device="cuda")
+    q[..., 0] = 1
+    got = ss.ss_attention_pages(q, pages, table_of(lists, [length] * rows, stride, 16, n_pages), length, group, scale=math.log(2))
+    for i, m in enumerate(lists):
+        p = torch.exp2(keys[m, :, 0].double()).reshape(-1)[:length]
+        vv, unit = v[m, 0].reshape(-1, dim)[:length], pages.v_scale.view(n_pages, 16)[m].double().reshape(-1)[:length]
+        w = p / p.sum()
+        ref, A = w @ vv, w @ vv.abs()
+        tol = half_step(F16) * ref.abs() + (2.0 ** -22 + 2.0 ** -18) * A + length * 2.0 ** -31 * 127 * (w * unit).max()
+        assert ((got[i].double() - ref).abs() <= tol).all()
+
+
 @pytest.mark.parametrize("group", [1, 4])
 @pytest.mark.parametrize("dtype,held", TYPES)
 def test_entries_that_are_no_page_are_not_seen(group, dtype, held):
