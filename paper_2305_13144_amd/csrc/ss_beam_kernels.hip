@@ -370,8 +370,8 @@ __global__ __launch_bounds__(kPickThreads) void k_beam_pick(BeamArgs a)
         s_over[t] = over;
         s_len[t] = len;
         s_total[t] = a.totals[row];
-        // (not 0 where a power is below all numbers: a sum of 0 has the rank 0 there too)
-        s_power[t] = a.power != 0.f ? fmax(pow((double)max(beam_length(len, !over), 1), (double)a.power), DBL_MIN) : 1.0;
+        const double scale = a.power != 0.f ? pow((double)max(beam_length(len, !over), 1), (double)a.power) : 1.0;
+        s_power[t] = scale > 0 ? scale : DBL_MIN;   // where a power is below all numbers a sum of 0 still has the rank 0
     }
     if (t < a.keep) s_row[t] = s_token[t] = -1;
 #pragma unroll
