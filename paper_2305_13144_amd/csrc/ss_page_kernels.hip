@@ -157,7 +157,7 @@ struct Scan {
 // What is rounded: the weights, to the operand's type.  In 16 bits their sum is of the rounded ones (half 0.00024 of a call, 0.00021 of it the result's own rounding; bf16
 // 0.0019 and 0.0016; sums of two would take registers that there are not).  Over 8 bits with results in half they are sums of two halves: 0.00021 instead of
 // 0.00029, for a second product beside each (16 x 8 beams 38.0 us, 35.6).
-// Bound by the cache's bytes (64 rows to 8000 slots, 32 heads on 8, 8 bits: 439 MB in 90 us with the join, 6.5 TB/s while large parts run, 4.9 in all), with few
+// Bound by the cache's bytes (64 rows to 8000 slots, 32 heads on 8, 8 bits: 439 MB in 88 us with the join, 6.5 TB/s while large parts run, 5.0 in all), with few
 // or short rows by a chain of latencies (one row of 3900 slots and 32 heads: 12 us, and 3 of the join).  3 workgroups on a unit (QT == 1, heads of 128): a
 // fourth wave a SIMD spills.
 // Who takes what (page_plan): short rows a workgroup a unit; one long row, or few that are not very long, a workgroup one of `parts` equal parts of a unit; else
