@@ -636,7 +636,8 @@ typedef struct {
  * logit, and length + 1;
  * of a beam that has ended only itself, with its sum and length, as (b, end_id) (end_id -1: as (b, 0), and its token is -1).  Their rank is
  * sum / length^length_power (a length of 0 counts as 1).  Of a group's candidates the `keep` with the largest rank are taken in that order, of equal ones first that with the
- * lower b * vocab + v.  (Of one beam, unlike logits whose sums float64 cannot tell apart, as below a sum near -1e9, may change places.)  Logits that are infinite or NaN are no candidates and have no part in the sum.
+ * lower b * vocab + v.  (Unlike logits of one beam whose sums float64 cannot tell apart, as below a sum near -1e9, may change places.)
+ * Logits that are infinite or NaN are no candidates and have no part in the sum.
  *   logits       device, [n_groups * beams][vocab] of SS_F32, SS_F16 or SS_BF16, aligned as its elements are; rows `row_stride` elements apart.
  *                Rows of beams that have ended are not read
  *   now          the beams' state; next: that of the taken candidates (n_groups * keep rows), shares no memory with `now`.  next->ended: the

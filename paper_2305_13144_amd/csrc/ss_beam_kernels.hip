@@ -124,7 +124,7 @@ struct Shortlist {
 // A wave goes through its part of a row in order, 64 x 16 bytes a step, kBeamAhead steps requested at a time.
 //   sum         of exp(x - ref): ref is the largest logit so far (first of kBeamAhead steps).  It moves a few times in a row without an order, at each step of one
 //               that ascends (768 rows of 100003 fp32 logits 219 us, 204 where it moved from 80 above it on, which cost the largest terms 2^-18 by
-//               their exponents' rounding).  Exponents are off by 2.3 * 2^-24 of themselves, which is 2.3 * 2^-24 (max - mean logit) of the sum, the mean by
+//               their exponents' rounding).  Exponents are off by 2.25 * 2^-24 of themselves, which is 2.25 * 2^-24 (max - mean logit) of the sum, the mean by
 //               the probabilities; no row's is further than log(vocab) from the maximum.  Exponentials are off by 2^-23; those of 16 bytes are added
 //               in fp32, and their sums in fp64, as thousands of terms follow each other: 5 * 2^-24 more.  The largest logit's is 1, the log of the sum not below 0
 //   candidates  a lane keeps the largest of its 16 bytes' largest logits, with its step, and the second largest: 4 instructions a step, whatever
